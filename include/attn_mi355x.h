@@ -223,6 +223,98 @@ attn_status attn_blockmask_validate(int32_t block, int32_t nblk, int32_t n, int3
 attn_status attn_mfma_ceiling(int32_t iters, int32_t operands, float *clock_ghz, double *flops,
                               void *stream);
 
+/*
+ * Attention with a sliding window and shared keys, forward and backward.  As attn_fwd and attn_bwd, causal, with
+ *   - heads query heads that share kv_heads key heads: query head h reads key head h / (heads / kv_heads), and dK, dV of a key
+ *     head are the sums over its query heads;
+ *   - a window: a pair (i, j) is visible iff j <= i and (window == 0 or i - j < window or j < sinks), i.e. a query sees itself, the
+ *     window - 1 keys in front of it and the first `sinks` keys of the sequence; window == 0 is plain causal attention;
+ *   - sequences of different lengths: with `lens` (DEVICE int32 [batch], may be NULL: n each) rows of sequence b from lens[b] on are
+ *     padding: keys there are visible to nobody and never read into a sum, queries there get O = 0, LSE = -inf and gradients 0.
+ *     (Values below 0 or above n count as 0 and n.)
+ * Q, O, dO, dQ are [batch, heads, n, d] with the q_ strides, K, V, dK, dV [batch, kv_heads, n, d] with the kv_ strides (in
+ * elements, d axis 1); LSE is contiguous [batch, heads, n].  Outputs are overwritten and overlap nothing else; a stride of
+ * an axis with more than one entry is at least d.
+ * Supported: 1 <= d <= 256; ATTN_F32; ATTN_BF16 with d, strides and pointers as for attn_fwd.  ATTN_BF16 with d in {64, 128, 256} runs
+ * bf16-MFMA kernels with fp32 accumulation, everything else fp32 arithmetic on the matrix cores.  The same call gives the same bits.
+ * A NaN or an infinity in a row inside a sequence may reach every query whose tile of keys it lies in, also those that do not see it.
+ * The work goes with the number of visible pairs: tiles that no query of a block sees are neither read nor computed.
+ */
+typedef struct {
+    int32_t batch, heads, kv_heads, n, d;
+    float scale;
+    int32_t window, sinks; /* 0: no window; sinks count only under a window */
+    int32_t dtype;         /* attn_dtype */
+    int32_t reserved;      /* 0 */
+    int64_t q_stride_b, q_stride_h, q_stride_n;
+    int64_t kv_stride_b, kv_stride_h, kv_stride_n;
+} attn_win_desc;
+
+/* Device scratch of attn_win_bwd (row sums v, and sums of the sink keys); attn_win_fwd needs none.  0 if desc is invalid. */
+size_t attn_win_workspace_bytes(const attn_win_desc *desc);
+attn_status attn_win_fwd(const attn_win_desc *desc, const int32_t *lens, const void *Q, const void *K, const void *V,
+                         void *O, float *LSE, void *stream);
+attn_status attn_win_bwd(const attn_win_desc *desc, const int32_t *lens, const void *Q, const void *K, const void *V,
+                         const void *O, const void *dO, const float *LSE, void *dQ, void *dK, void *dV,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Paged cache of keys and values, and the attention of new tokens over it (serving: one token per sequence, a chunk, or a batch of
+ * both).  A page holds page_size consecutive tokens of one sequence for all key heads; table[b][x] (DEVICE int32, rows
+ * table_stride apart) is the page of tokens x * page_size .. of sequence b.  lens[b] counts the tokens of sequence b in the cache,
+ * the new ones included: these are its last, and have rows q_ptr[b] .. q_ptr[b + 1] - 1 of Q, O, K, V (q_ptr: DEVICE int32
+ * [batch + 1], ascending; NULL: max_q rows each, row b * max_q first).  The order of a step is attn_cache_write, then
+ * attn_paged_fwd with the same desc.
+ *   pages   K, V [num_pages] x [kv_heads] x [page_size] x [d] with page_stride_p, _h, _n (elements, d axis 1; any order)
+ *   ATTN_CACHE_PLAIN  pages hold values of `dtype`
+ *   ATTN_CACHE_FP8    pages hold e4m3 codes, K_exp and V_exp ([num_pages, kv_heads, page_size] bytes, contiguous) an exponent byte e
+ *                     per row: a code c stands for c 2^(e - 127), where 2^(e - 127) is the smallest power of two that brings the row's
+ *                     largest magnitude to 448 or less (at least 2^-126; 1 for a row of zeros).  Codes are rounded to nearest, ties
+ *                     to even; NaN and infinities become NaN and do not count for the largest magnitude.
+ * Query t of a sequence is at position i = lens[b] - (its new tokens) + t and sees key j iff j <= i and (window == 0 or
+ * i - j < window or j < sinks).  A query in front of position 0 sees nothing: O = 0, LSE = -inf.
+ * max_q and max_len bound the new tokens and the lengths (they size the launches; what lies beyond them is not worked on; max_len <=
+ * max_pages * page_size).  Pages that no query sees are not read, and their entries of the table are not used for an access; an
+ * entry outside 0 .. num_pages - 1 where a query sees tokens makes the result meaningless, but no access leaves the cache:
+ * attn_cache_write skips such tokens, attn_cache_read gives zeros for them.  Rows beyond the sequences' own are not written.
+ * Supported: page_size a power of two from 8 to 4096, 1 <= d <= 256, d % 8 == 0 for ATTN_BF16 and ATTN_CACHE_FP8, batch <= 65535; with
+ * ATTN_BF16 strides are multiples of 8 and pointers 16-byte aligned, strides of quantised pages are multiples of 8 (of 16 for d a multiple
+ * of 64).  ATTN_BF16 with d in {64, 128, 256} runs bf16-MFMA kernels, everything else fp32 arithmetic.
+ */
+typedef enum { ATTN_CACHE_PLAIN = 0, ATTN_CACHE_FP8 = 1 } attn_cache_kind;
+
+typedef struct {
+    int32_t batch, heads, kv_heads, d;
+    int32_t total_q;            /* rows of Q, O, K, V */
+    int32_t max_q, max_len;     /* most new tokens, most tokens of a sequence */
+    int32_t page_size, num_pages, max_pages; /* max_pages: entries of a row of the table */
+    float scale;
+    int32_t window, sinks;
+    int32_t dtype;              /* attn_dtype of Q, O, K, V */
+    int32_t kind;               /* attn_cache_kind */
+    int32_t reserved;           /* 0 */
+    int64_t q_stride_n, q_stride_h;   /* Q, O [total_q, heads, d] */
+    int64_t kv_stride_n, kv_stride_h; /* K, V [total_q, kv_heads, d] */
+    int64_t page_stride_p, page_stride_h, page_stride_n;
+    int64_t table_stride;
+} attn_paged_desc;
+
+typedef struct { /* DEVICE memory, caller owned */
+    void *K, *V;
+    uint8_t *K_exp, *V_exp;         /* ATTN_CACHE_FP8, else NULL */
+    const int32_t *table, *lens, *q_ptr;
+} attn_cache;
+
+/* The new tokens' K and V into the pages; their places are overwritten, nothing else is. */
+attn_status attn_cache_write(const attn_paged_desc *desc, const attn_cache *cache, const void *K, const void *V, void *stream);
+/* The last tokens of every sequence (as many as q_ptr says) out of the pages into K and V, in order and dequantised. */
+attn_status attn_cache_read(const attn_paged_desc *desc, const attn_cache *cache, void *K, void *V, void *stream);
+/* Device scratch of attn_paged_fwd: sums of the parts into which a long cache is split when there are few rows.  0 if desc is invalid. */
+size_t attn_paged_workspace_bytes(const attn_paged_desc *desc);
+/* O [total_q, heads, d] and LSE, contiguous [total_q, heads] float, of the new tokens. */
+attn_status attn_paged_fwd(const attn_paged_desc *desc, const attn_cache *cache, const void *Q, void *O, float *LSE,
+                           void *workspace, size_t workspace_bytes, void *stream);
+
 /* Static description of a status code. */
 const char *attn_status_str(attn_status s);
 

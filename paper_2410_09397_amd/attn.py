@@ -15,12 +15,14 @@ LIB_PATH = os.path.join(_HERE, "libattn_mi355x.so")
 
 ATTN_OK, ATTN_ERR_INVALID_ARG, ATTN_ERR_UNSUPPORTED, ATTN_ERR_WORKSPACE, ATTN_ERR_DEVICE = range(5)
 ATTN_F32, ATTN_BF16 = 0, 1
+ATTN_CACHE_PLAIN, ATTN_CACHE_FP8 = 0, 1
 (ATTN_BWD_AUTO, ATTN_BWD_TWO_KERNEL, ATTN_BWD_ONEPASS_K64, ATTN_BWD_ONEPASS_K128, ATTN_BWD_PART_DQ,
  ATTN_BWD_PART_DKDV, ATTN_BWD_FOUR_PHASE, ATTN_BWD_SPLIT_D) = range(8)
 
 EXPORTS = ("attn_workspace_bytes", "attn_fwd", "attn_bwd", "attn_bwd_noalloc", "attn_bwd_blocksparse",
            "attn_wgrad_workspace_bytes", "attn_bwd_wgrad", "attn_blockmask_validate", "attn_mfma_ceiling",
-           "attn_status_str")
+           "attn_win_workspace_bytes", "attn_win_fwd", "attn_win_bwd", "attn_cache_write", "attn_cache_read",
+           "attn_paged_workspace_bytes", "attn_paged_fwd", "attn_status_str")
 
 
 class attn_desc(ctypes.Structure):
@@ -34,6 +36,24 @@ class attn_blockmask(ctypes.Structure):
     _fields_ = [("block", ctypes.c_int32), ("nblk", ctypes.c_int32),
                 ("row_ptr", ctypes.c_void_p), ("col_idx", ctypes.c_void_p),
                 ("col_ptr", ctypes.c_void_p), ("row_idx", ctypes.c_void_p), ("nmasks", ctypes.c_int32)]
+
+
+class attn_win_desc(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in ("batch", "heads", "kv_heads", "n", "d")] + [("scale", ctypes.c_float)] + \
+               [(f, ctypes.c_int32) for f in ("window", "sinks", "dtype", "reserved")] + \
+               [(f, ctypes.c_int64) for f in ("q_stride_b", "q_stride_h", "q_stride_n", "kv_stride_b", "kv_stride_h", "kv_stride_n")]
+
+
+class attn_paged_desc(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in ("batch", "heads", "kv_heads", "d", "total_q", "max_q", "max_len", "page_size", "num_pages",
+                                              "max_pages")] + [("scale", ctypes.c_float)] + \
+               [(f, ctypes.c_int32) for f in ("window", "sinks", "dtype", "kind", "reserved")] + \
+               [(f, ctypes.c_int64) for f in ("q_stride_n", "q_stride_h", "kv_stride_n", "kv_stride_h", "page_stride_p", "page_stride_h",
+                                              "page_stride_n", "table_stride")]
+
+
+class attn_cache(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in ("K", "V", "K_exp", "V_exp", "table", "lens", "q_ptr")]
 
 
 class AttnError(RuntimeError):
@@ -72,6 +92,16 @@ def lib():
         L.attn_blockmask_validate.argtypes = [ctypes.c_int32] * 4 + [i32p] * 4
         L.attn_mfma_ceiling.restype = ctypes.c_int
         L.attn_mfma_ceiling.argtypes = [ctypes.c_int32, ctypes.c_int32, vp, ctypes.POINTER(ctypes.c_double), vp]
+        wp, pp, cp = ctypes.POINTER(attn_win_desc), ctypes.POINTER(attn_paged_desc), ctypes.POINTER(attn_cache)
+        L.attn_win_workspace_bytes.restype = L.attn_paged_workspace_bytes.restype = ctypes.c_size_t
+        L.attn_win_workspace_bytes.argtypes = [wp]
+        L.attn_paged_workspace_bytes.argtypes = [pp]
+        L.attn_win_fwd.restype = L.attn_win_bwd.restype = ctypes.c_int
+        L.attn_win_fwd.argtypes = [wp] + [vp] * 7
+        L.attn_win_bwd.argtypes = [wp] + [vp] * 11 + [ctypes.c_size_t, vp]
+        L.attn_cache_write.restype = L.attn_cache_read.restype = L.attn_paged_fwd.restype = ctypes.c_int
+        L.attn_cache_write.argtypes = L.attn_cache_read.argtypes = [pp, cp, vp, vp, vp]
+        L.attn_paged_fwd.argtypes = [pp, cp, vp, vp, vp, vp, ctypes.c_size_t, vp]
         L.attn_status_str.restype = ctypes.c_char_p
         L.attn_status_str.argtypes = [ctypes.c_int]
         _lib = L
@@ -293,3 +323,185 @@ def attn_mfma_ceiling(iters, operands=0, stream=None):
     if st != ATTN_OK:
         raise AttnError(st, "attn_mfma_ceiling")
     return clock, flops.value
+
+
+# ------------------------------------------------------------------------- windowed attention with shared heads
+def _dtype(x):
+    import torch
+    if x.dtype is torch.bfloat16:
+        return ATTN_BF16
+    if x.dtype is torch.float32:
+        return ATTN_F32
+    raise ValueError("expected a bfloat16 or float32 tensor, got %s" % x.dtype)
+
+
+def _int32(name, t, shape, device):
+    """Device address of an int32 tensor that the kernels index."""
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
+        raise ValueError("%s must be a contiguous int32 tensor of shape %s on the device of the other tensors" % (name, shape))
+    return t.data_ptr()
+
+
+def _scratch(nbytes, device, stream):
+    """A workspace allocated on the stream that the kernels will run on (see _workspace)."""
+    import torch
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _win_desc(Q, K, scale, window, sinks):
+    if Q.dim() != 4 or K.dim() != 4 or Q.stride(3) != 1 or K.stride(3) != 1:
+        raise ValueError("expected [batch, heads, n, d] tensors with unit stride along d")
+    b, h, n, d = Q.shape
+    if (K.shape[0], K.shape[2], K.shape[3]) != (b, n, d) or K.dtype != Q.dtype or K.device != Q.device:
+        raise ValueError("Q and K must share batch, n, d, dtype and device")
+    return attn_win_desc(b, h, K.shape[1], n, d, float(scale), int(window), int(sinks), _dtype(Q), 0, *Q.stride()[:3], *K.stride()[:3])
+
+
+def attn_win_workspace_bytes(desc):
+    return lib().attn_win_workspace_bytes(ctypes.byref(desc))
+
+
+def attn_win_fwd(Q, K, V, scale, window=0, sinks=0, lens=None, stream=None, out=None):
+    """O, LSE of causal attention in which a query sees itself, the window - 1 keys in front of it (window = 0: all of them) and the
+    first `sinks` keys.  Q: [batch, heads, n, d]; K, V: [batch, kv_heads, n, d], heads a multiple of kv_heads; lens: the
+    sequences' lengths (int32 [batch]), rows from there on are padding."""
+    import torch
+    _same_layout(K, V)
+    desc = _win_desc(Q, K, scale, window, sinks)
+    if out is None:
+        out = torch.empty_like(Q), torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device)
+    O, LSE = out
+    _same_layout(Q, O)
+    _check_lse(LSE, Q)
+    st = lib().attn_win_fwd(ctypes.byref(desc), _int32("lens", lens, (Q.shape[0],), Q.device), Q.data_ptr(), K.data_ptr(), V.data_ptr(),
+                            O.data_ptr(), LSE.data_ptr(), _stream(stream))
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_win_fwd")
+    return O, LSE
+
+
+def _check_lse(LSE, Q):
+    import torch
+    if LSE.dtype != torch.float32 or not LSE.is_contiguous() or LSE.shape != Q.shape[:-1] or LSE.device != Q.device:
+        raise ValueError("LSE must be a contiguous float32 tensor of the queries' shape without d")
+
+
+def attn_win_bwd(Q, K, V, O, dO, LSE, scale, window=0, sinks=0, lens=None, stream=None, out=None, workspace=None):
+    """dQ, dK, dV of attn_win_fwd from its O and LSE; dK and dV are sums over the query heads that share a key head."""
+    import torch
+    _same_layout(K, V)
+    desc = _win_desc(Q, K, scale, window, sinks)
+    if out is None:
+        out = torch.empty_like(Q), torch.empty_like(K), torch.empty_like(K)
+    dQ, dK, dV = out
+    _same_layout(Q, O, dO, dQ)
+    _same_layout(K, dK, dV)
+    _check_lse(LSE, Q)
+    if workspace is None:
+        workspace = _scratch(max(attn_win_workspace_bytes(desc), 256), Q.device, stream)
+    st = lib().attn_win_bwd(ctypes.byref(desc), _int32("lens", lens, (Q.shape[0],), Q.device), Q.data_ptr(), K.data_ptr(), V.data_ptr(),
+                            O.data_ptr(), dO.data_ptr(), LSE.data_ptr(), dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(),
+                            workspace.data_ptr(), workspace.numel(), _stream(stream))
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_win_bwd")
+    return dQ, dK, dV
+
+
+# ----------------------------------------------------------------------------------------------- the paged cache
+def attn_cache_pages(num_pages, kv_heads, page_size, d, dtype, device="cuda"):
+    """K_pages, V_pages, K_exp, V_exp of an empty cache [num_pages, kv_heads, page_size, d]; dtype torch.float8_e4m3fn: quantised, else the
+    type of the keys and values, and no exponents (None)."""
+    import torch
+    K, V = (torch.zeros(num_pages, kv_heads, page_size, d, dtype=dtype, device=device) for _ in range(2))
+    if dtype is not torch.float8_e4m3fn:
+        return K, V, None, None
+    return K, V, *(torch.full((num_pages, kv_heads, page_size), 127, dtype=torch.uint8, device=device) for _ in range(2))
+
+
+def _paged(name, x, heads_of, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp, scale=1.0, window=0, sinks=0):
+    """The descriptor and the cache structure of a call whose rows are x: [total, heads, d] (heads_of "q": the queries' heads)."""
+    import torch
+    if x.dim() != 3 or x.stride(2) != 1 or K_pages.dim() != 4 or K_pages.stride(3) != 1:
+        raise ValueError("%s: expected rows [total, heads, d] and pages [num_pages, kv_heads, page_size, d] with unit stride along d" % name)
+    _same_layout(K_pages, V_pages)
+    num, kvh, page, d = K_pages.shape
+    total, h, dx = x.shape
+    if dx != d or (heads_of == "kv" and h != kvh) or x.device != K_pages.device:
+        raise ValueError("%s: rows and pages must agree in their heads, d and device" % name)
+    fp8 = K_pages.dtype is torch.float8_e4m3fn
+    if not fp8 and K_pages.dtype != x.dtype:
+        raise ValueError("%s: pages hold the rows' type, or float8_e4m3fn with exponents" % name)
+    for e in (K_exp, V_exp) if fp8 else ():
+        if e is None or e.dtype != torch.uint8 or tuple(e.shape) != (num, kvh, page) or not e.is_contiguous() or e.device != x.device:
+            raise ValueError("%s: quantised pages need contiguous uint8 exponents [num_pages, kv_heads, page_size]" % name)
+    if table.dim() != 2 or table.dtype != torch.int32 or table.stride(1) != 1 or table.device != x.device:
+        raise ValueError("%s: the table must be an int32 tensor [batch, pages] with unit stride along the pages" % name)
+    batch, width = table.shape
+    if q_ptr is None and max_q is None:
+        if batch and total % batch:
+            raise ValueError("%s: without q_ptr every sequence has the same number of rows" % name)
+        max_q = total // batch if batch else 0
+    if max_q is None:
+        raise ValueError("%s: q_ptr needs max_q, the largest number of new tokens of a sequence" % name)
+    sn, sh, _ = x.stride()
+    kind = ATTN_CACHE_FP8 if fp8 else ATTN_CACHE_PLAIN
+    desc = attn_paged_desc(batch, h, kvh, d, total, int(max_q), width * page if max_len is None else int(max_len), page, num, width,
+                           float(scale), int(window), int(sinks), _dtype(x), kind, 0, sn, sh, sn, sh, *K_pages.stride()[:3], table.stride(0))
+    cache = attn_cache(K_pages.data_ptr(), V_pages.data_ptr(), K_exp.data_ptr() if fp8 else None, V_exp.data_ptr() if fp8 else None,
+                       table.data_ptr(), _int32("lens", lens, (batch,), x.device), _int32("q_ptr", q_ptr, (batch + 1,), x.device))
+    return desc, cache
+
+
+def attn_cache_write(K, V, K_pages, V_pages, table, lens, q_ptr=None, max_q=None, K_exp=None, V_exp=None, stream=None):
+    """The new tokens' K and V ([total, kv_heads, d]) into the pages of their sequences, quantised where the pages are float8_e4m3fn.
+    lens (int32 [batch]) counts the new tokens already; rows q_ptr[b] .. q_ptr[b + 1] - 1 belong to sequence b (None: the same number each)."""
+    _same_layout(K, V)
+    desc, cache = _paged("attn_cache_write", K, "kv", K_pages, V_pages, table, lens, q_ptr, max_q, None, K_exp, V_exp)
+    st = lib().attn_cache_write(ctypes.byref(desc), ctypes.byref(cache), K.data_ptr(), V.data_ptr(), _stream(stream))
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_cache_write")
+
+
+def attn_cache_read(K_pages, V_pages, table, lens, dtype, total, q_ptr=None, max_q=None, K_exp=None, V_exp=None, stream=None, out=None):
+    """K, V ([total, kv_heads, d]): the last tokens of every sequence, as many as q_ptr says (None: total / batch each)."""
+    import torch
+    if out is None:
+        shape = (total, K_pages.shape[1], K_pages.shape[3])
+        out = tuple(torch.empty(shape, dtype=dtype, device=K_pages.device) for _ in range(2))
+    K, V = out
+    _same_layout(K, V)
+    desc, cache = _paged("attn_cache_read", K, "kv", K_pages, V_pages, table, lens, q_ptr, max_q, None, K_exp, V_exp)
+    st = lib().attn_cache_read(ctypes.byref(desc), ctypes.byref(cache), K.data_ptr(), V.data_ptr(), _stream(stream))
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_cache_read")
+    return K, V
+
+
+def attn_paged_workspace_bytes(desc):
+    return lib().attn_paged_workspace_bytes(ctypes.byref(desc))
+
+
+def attn_paged_fwd(Q, K_pages, V_pages, table, lens, scale, q_ptr=None, max_q=None, max_len=None, window=0, sinks=0, K_exp=None,
+                   V_exp=None, stream=None, out=None, workspace=None):
+    """O [total, heads, d], LSE [total, heads] of the new tokens Q [total, heads, d] over the paged cache that their keys and values have
+    been written to.  max_len bounds the lengths (None: what the table can hold; a tighter bound gives better launches)."""
+    import torch
+    desc, cache = _paged("attn_paged_fwd", Q, "q", K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp, scale, window, sinks)
+    if out is None:
+        out = torch.empty_like(Q), torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device)
+    O, LSE = out
+    _same_layout(Q, O)
+    _check_lse(LSE, Q)
+    if workspace is None:
+        workspace = _scratch(max(attn_paged_workspace_bytes(desc), 256), Q.device, stream)
+    st = lib().attn_paged_fwd(ctypes.byref(desc), ctypes.byref(cache), Q.data_ptr(), O.data_ptr(), LSE.data_ptr(), workspace.data_ptr(),
+                              workspace.numel(), _stream(stream))
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_paged_fwd")
+    return O, LSE

@@ -1,0 +1,537 @@
+// Windowed attention in 32-bit arithmetic: forward over tensors or pages, backward, for fp32 storage at any d <= 256 and for bf16 (and
+// quantised pages) at the head dimensions that attn_win_fwd.hip and attn_win_bwd.hip do not have.
+//
+// Products are v_mfma_f32_32x32x2_f32.  Operand layout (lane l, h = l / 32): A row l % 32, k = h; B column l % 32, k = h; C as for the
+// bf16 form (column l % 32, register i <-> row 8 (i / 4) + 4 h + i % 4).  The order of k is free as long as both operands have the same:
+//   contraction over d     step (c, e) takes columns 8 c + e (h = 0) and 8 c + 4 + e (h = 1): a lane reads 4 values at a time
+//   contraction over rows  step i takes the rows of accumulator register i, which is then an operand as it stands
+// Every wave works by itself, on 32 rows of queries or keys, and reads its operands straight from memory (the four waves of a
+// workgroup read the same tiles, which L1 holds): no LDS, no barrier, and any layout of the rows.  A step of the second kind has one
+// 4-byte load per lane for 64 cycles of the matrix pipe.
+#include <type_traits>
+
+#include "attn_internal.hpp"
+#include "attn_window.hpp"
+
+namespace attn {
+namespace {
+
+__device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
+
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef __bf16 bf16x4u __attribute__((ext_vector_type(4), aligned(8)));
+
+// columns c .. c + 3 of a row (0 from d on); c is a multiple of 4
+__device__ __forceinline__ f32x4 load4(const float* row, int c, int d) {
+    if (c + 4 <= d) return *reinterpret_cast<const f32x4u*>(row + c);
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+        if (c + e < d) v[e] = row[c + e];
+    return v;
+}
+__device__ __forceinline__ f32x4 load4(const __bf16* row, int c, int d) {  // (d is a multiple of 8)
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (c < d) v = __builtin_convertvector(*reinterpret_cast<const bf16x4u*>(row + c), f32x4);
+    return v;
+}
+__device__ __forceinline__ f32x4 load4(const uint8_t* row, int c, int d) {
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (c < d) {
+        const int u = *reinterpret_cast<const int*>(row + c);
+        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(u, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(u, true);
+        v = f32x4{lo[0], lo[1], hi[0], hi[1]};
+    }
+    return v;
+}
+__device__ __forceinline__ float load1(const float* row, int c, int d) { return c < d ? row[c] : 0.f; }
+__device__ __forceinline__ float load1(const __bf16* row, int c, int d) { return c < d ? (float)row[c] : 0.f; }
+__device__ __forceinline__ float load1(const uint8_t* row, int c, int d) {
+    return c < d ? __builtin_amdgcn_cvt_f32_fp8((int)row[c], 0) : 0.f;
+}
+__device__ __forceinline__ void store4(float* row, int c, int d, f32x4 v) {
+    if (c + 4 <= d) {
+        *reinterpret_cast<f32x4u*>(row + c) = v;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+        if (c + e < d) row[c + e] = v[e];
+}
+__device__ __forceinline__ void store4(__bf16* row, int c, int d, f32x4 v) {
+    if (c < d) *reinterpret_cast<u32x2*>(row + c) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+}
+
+// A resident row as the contraction over d takes it: 4 values of columns 8 c + 4 h .. for every c.  bf16 rows stay packed; fp32 rows of
+// more than 128 columns have no registers to stay in and are read again for every tile.
+template <typename T, int DP, bool kResident = std::is_same_v<T, __bf16> || DP <= 128>
+struct RowOperand {
+    typedef std::conditional_t<std::is_same_v<T, __bf16>, u32x2, f32x4> Chunk;
+    Chunk v[kResident ? DP / 8 : 1];
+    const T* row;
+    int d, h;
+    __device__ __forceinline__ void init(const T* row_, int d_, int h_) {
+        row = row_;
+        d = d_;
+        h = h_;
+        if constexpr (kResident) {
+#pragma unroll
+            for (int c = 0; c < DP / 8; ++c) {
+                const f32x4 x = load4(row, 8 * c + 4 * h, d);
+                if constexpr (std::is_same_v<T, __bf16>) v[c] = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+                else v[c] = x;
+            }
+        }
+    }
+    __device__ __forceinline__ f32x4 get(int c) const {
+        if constexpr (!kResident) return load4(row, 8 * c + 4 * h, d);
+        else if constexpr (std::is_same_v<T, __bf16>) return __builtin_convertvector(__builtin_bit_cast(bf16x4, v[c]), f32x4);
+        else return v[c];
+    }
+};
+
+// The 32 rows of a key tile as a lane sees them: row l % 32 for the contraction over d, every row for the contraction over keys.
+template <typename E>
+struct KeyTile {
+    static constexpr bool kCodes = std::is_same_v<E, uint8_t>;
+    long at;      // element offset of row l % 32 in K and V
+    float sk, sv;  // quantised: what its codes are multiplied with
+    __device__ __forceinline__ void init(const WinParams& p, const WinTiles<32>& tiles, int b, int kvh, int j0, int l32) {
+        const int j = tiles.row(p, j0 + l32);
+        if (p.table) {
+            const PageRow r = win_page_row(p, win_page(p, b, j), kvh, j);
+            at = r.at;
+            if constexpr (kCodes) {
+                sk = exp_value(p.K_exp[r.exp]);
+                sv = exp_value(p.V_exp[r.exp]);
+            }
+        } else {
+            at = (long)b * p.k_b + (long)kvh * p.k_h + (long)j * p.k_n;
+        }
+    }
+    static __device__ __forceinline__ long row_of(long at, int row) {  // of the lane that holds `row`
+        const int lo = __shfl((int)at, row, 64), hi = __shfl((int)(at >> 32), row, 64);
+        return ((long)hi << 32) | (unsigned)lo;
+    }
+};
+
+// s += A B^T over d: rows of `a` (l % 32) are the tile's, rows of b the resident ones
+template <typename E, typename T, int DP, bool R>
+__device__ __forceinline__ void scores(f32x16& s, const E* row, float scale, const RowOperand<T, DP, R>& b, int d, int h) {
+#pragma unroll
+    for (int c = 0; c < DP / 8; ++c) {
+        f32x4 a = load4(row, 8 * c + 4 * h, d);
+        if constexpr (std::is_same_v<E, uint8_t>) a *= scale;
+        const f32x4 q = b.get(c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s = mfma_f32(a[e], q[e], s);
+    }
+}
+
+struct RowPlace {  // of query row r of a (sequence, key head)
+    int t, head;
+};
+__device__ __forceinline__ RowPlace place(const WinParams& p, int kvh, int r) {
+    const int t = (int)((unsigned)r / (unsigned)p.group);
+    return {t, kvh * p.group + r - t * p.group};
+}
+
+// --------------------------------------------------------------------------------------------------------- forward
+template <typename T, typename E, int DP>
+__global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) win_plain_out_kernel(WinParams p, int row_blocks) {
+    constexpr int MT = DP / 32;
+    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int bk = blockIdx.x / row_blocks, b = bk / p.kv_heads, kvh = bk % p.kv_heads;
+    const WinSeq s = win_sequence(p, b);
+    const int rows = s.nq * p.group, r0 = ((blockIdx.x % row_blocks) * 4 + w) * 32;
+    if (r0 >= rows) return;
+    const int r = min(r0 + l32, rows - 1);
+    const RowPlace at = place(p, kvh, r);
+    const int i = s.first + at.t;
+    const int hi = i < s.len ? i : -1, lo = i - p.window + 1;  // this row sees lo .. hi, and the sinks up to hi
+    WinTiles<32> tiles;
+    tiles.init(p, s.len, s.first + place(p, kvh, r0).t, s.first + place(p, kvh, min(r0 + 31, rows - 1)).t);
+    const int it0 = blockIdx.y * p.chunk, it1 = min(tiles.count, it0 + p.chunk);
+
+    RowOperand<T, DP> q;
+    q.init(static_cast<const T*>(p.Q) + s.q_base + (long)at.head * p.q_h + (long)at.t * p.q_n, p.d, h);
+    f32x16 o[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[m][e] = 0.f;
+    float m_run = -__builtin_inff(), l_run = 0.f;  // of scale log2(e) s; this lane's half of the sum
+    const float cs = p.scale * kLog2e;
+    for (int it = it0; it < it1; ++it) {
+        const int j0 = tiles.start(it);
+        KeyTile<E> keys;
+        keys.init(p, tiles, b, kvh, j0, l32);
+        f32x16 st;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) st[e] = 0.f;
+        scores(st, static_cast<const E*>(p.K) + keys.at, keys.sk, q, p.d, h);
+        float mx = -__builtin_inff();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int j = j0 + acc_row(e, h);
+            const bool seen = j <= hi && (j >= lo || j < p.sinks);
+            st[e] = seen ? st[e] * cs : -__builtin_inff();
+            mx = __builtin_elementwise_maximum(mx, st[e]);
+        }
+        mx = __builtin_elementwise_maximum(mx, __shfl_xor(mx, 32, 64));
+        const float m_new = __builtin_elementwise_maximum(m_run, mx), m_use = m_new == -__builtin_inff() ? 0.f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
+        m_run = m_new;
+        l_run *= alpha;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[m][e] *= alpha;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            st[e] = __builtin_amdgcn_exp2f(st[e] - m_use);
+            l_run += st[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int row = acc_row(e, h);
+            const E* v = static_cast<const E*>(p.V) + KeyTile<E>::row_of(keys.at, row);
+            float f = st[e];
+            if constexpr (KeyTile<E>::kCodes) f *= __shfl(keys.sv, row, 64);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) o[m] = mfma_f32(load1(v, 32 * m + l32, p.d), f, o[m]);
+        }
+    }
+    const float l = l_run + __shfl_xor(l_run, 32, 64);
+    if (r0 + l32 >= rows) return;
+    if (p.splits > 1) {
+        const long row = s.lse_base + (long)at.t * p.heads + at.head;
+        float* ml = p.part_ml + (row * p.splits + blockIdx.y) * 2;
+        if (h == 0) {
+            ml[0] = m_run;
+            ml[1] = l;
+        }
+        if (l > 0.f || l != l) {
+            float* dst = p.part_o + (row * p.splits + blockIdx.y) * p.d;
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    store4(dst, 32 * m + 8 * g + 4 * h, p.d, f32x4{o[m][4 * g], o[m][4 * g + 1], o[m][4 * g + 2], o[m][4 * g + 3]});
+        }
+        return;
+    }
+    const bool none = l == 0.f;  // no key: O = 0, LSE = -inf
+    const float inv = none ? 0.f : 1.f / l;
+    T* dst = static_cast<T*>(p.O) + s.q_base + (long)at.head * p.q_h + (long)at.t * p.q_n;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            store4(dst, 32 * m + 8 * g + 4 * h, p.d,
+                   f32x4{o[m][4 * g] * inv, o[m][4 * g + 1] * inv, o[m][4 * g + 2] * inv, o[m][4 * g + 3] * inv});
+    if (h == 0)
+        p.LSE[s.lse_base + (long)at.head * s.lse_h + (long)at.t * s.lse_t] =
+            none ? -__builtin_inff() : (m_run + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// The sums of the parts of a row: O = sum_k 2^(m_k - m) O_k / l, l = sum_k 2^(m_k - m) l_k, in the order of the parts.  One wave per
+// row; every wave reads all maxima (at most 64, one per lane), then the O_k of the parts that saw a key.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) win_join_kernel(WinParams p) {
+    const int lane = threadIdx.x & 63, b = blockIdx.y;
+    const WinSeq s = win_sequence(p, b);
+    const long f = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int t = (int)(f / p.heads), head = (int)(f % p.heads);
+    if (t >= s.nq) return;
+    const long row = s.lse_base + (long)t * p.heads + head;
+    const float* ml = p.part_ml + row * p.splits * 2;
+    const bool mine = lane < p.splits;
+    const float m_k = mine ? ml[2 * lane] : -__builtin_inff(), l_k = mine ? ml[2 * lane + 1] : 0.f;
+    float m = m_k;
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) m = __builtin_elementwise_maximum(m, __shfl_xor(m, x, 64));
+    const float m_use = m == -__builtin_inff() ? 0.f : m;
+    const float f_k = __builtin_amdgcn_exp2f(m_k - m_use);
+    float l = f_k * l_k;
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) l += __shfl_xor(l, x, 64);
+    const bool none = l == 0.f;
+    const float inv = none ? 0.f : 1.f / l;
+    const unsigned long parts = __builtin_amdgcn_ballot_w64(l_k > 0.f || l_k != l_k);
+    const float* src = p.part_o + row * p.splits * p.d;
+    T* dst = static_cast<T*>(p.O) + s.q_base + (long)head * p.q_h + (long)t * p.q_n;
+    const int c = 4 * lane;  // d <= 256
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (unsigned long todo = parts; todo; todo &= todo - 1) {
+        const int k = __builtin_ctzl(todo);
+        const float weight = __shfl(f_k, k, 64);  // (by all lanes)
+        if (c < p.d) sum += load4(src + (long)k * p.d, c, p.d) * weight;
+    }
+    if (c < p.d) store4(dst, c, p.d, sum * inv);
+    if (lane == 0) p.LSE[row] = none ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// -------------------------------------------------------------------------------------------------------- backward
+// delta = rowsum(dO o O) of every query inside its sequence, [batch, heads, n]; eight lanes per row.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) win_rows_kernel(WinParams p) {
+    const long f = ((long)blockIdx.x * kThreads + threadIdx.x) >> 3, rows = (long)p.batch * p.heads * p.n;
+    const int c0 = 4 * (threadIdx.x & 7);
+    float sum = 0.f;
+    if (f < rows) {
+        const int t = (int)(f % p.n), bh = (int)(f / p.n);
+        const long at = (long)(bh / p.heads) * p.q_b + (long)(bh % p.heads) * p.q_h + (long)t * p.q_n;
+        if (!p.lens || t < p.lens[bh / p.heads])
+            for (int c = c0; c < p.d; c += 32) {
+                const f32x4 x = load4(static_cast<const T*>(p.O_in) + at, c, p.d), g = load4(static_cast<const T*>(p.dO) + at, c, p.d);
+                sum += x[0] * g[0] + x[1] * g[1] + x[2] * g[2] + x[3] * g[3];
+            }
+    }
+#pragma unroll
+    for (int x = 1; x < 8; x <<= 1) sum += __shfl_xor(sum, x, 64);
+    if (f < rows && (threadIdx.x & 7) == 0) p.delta[f] = sum;
+}
+
+// dQ: a wave owns 32 query rows; dS^T = P^T o (V dO^T - delta), dQ^T += K^T dS^T.
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) win_plain_dq_kernel(WinParams p, int row_blocks) {
+    constexpr int MT = DP / 32;
+    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int bk = blockIdx.x / row_blocks, b = bk / p.kv_heads, kvh = bk % p.kv_heads;
+    const WinSeq s = win_sequence(p, b);
+    const int rows = s.nq * p.group, r0 = ((blockIdx.x % row_blocks) * 4 + w) * 32;
+    if (r0 >= rows) return;
+    const int r = min(r0 + l32, rows - 1);
+    const RowPlace at = place(p, kvh, r);
+    const int i = s.first + at.t;
+    const int hi = i < s.len ? i : -1, lo = i - p.window + 1;
+    WinTiles<32> tiles;
+    tiles.init(p, s.len, s.first + place(p, kvh, r0).t, s.first + place(p, kvh, min(r0 + 31, rows - 1)).t);
+    const long off = s.q_base + (long)at.head * p.q_h + (long)at.t * p.q_n, stat = s.lse_base + (long)at.head * s.lse_h + at.t;
+    RowOperand<T, DP> q, g;
+    q.init(static_cast<const T*>(p.Q) + off, p.d, h);
+    g.init(static_cast<const T*>(p.dO) + off, p.d, h);
+    const float lse = hi >= 0 ? p.LSE_in[stat] * kLog2e : 0.f, delta = hi >= 0 ? p.delta[stat] : 0.f;
+    f32x16 dq[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dq[m][e] = 0.f;
+    const float cs = p.scale * kLog2e;
+    for (int it = 0; it < tiles.count; ++it) {
+        const int j0 = tiles.start(it);
+        KeyTile<T> keys;
+        keys.init(p, tiles, b, kvh, j0, l32);
+        f32x16 st, dp;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) st[e] = dp[e] = 0.f;
+        scores(st, static_cast<const T*>(p.K) + keys.at, 1.f, q, p.d, h);
+        scores(dp, static_cast<const T*>(p.V) + keys.at, 1.f, g, p.d, h);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int row = acc_row(e, h), j = j0 + row;
+            const bool seen = j <= hi && (j >= lo || j < p.sinks);
+            const float ds = seen ? __builtin_amdgcn_exp2f(fmaf(st[e], cs, -lse)) * (dp[e] - delta) : 0.f;
+            const T* k = static_cast<const T*>(p.K) + KeyTile<T>::row_of(keys.at, row);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) dq[m] = mfma_f32(load1(k, 32 * m + l32, p.d), ds, dq[m]);
+        }
+    }
+    if (r0 + l32 >= rows) return;
+    T* dst = static_cast<T*>(p.dQ) + off;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+            store4(dst, 32 * m + 8 * x + 4 * h, p.d,
+                   f32x4{dq[m][4 * x] * p.scale, dq[m][4 * x + 1] * p.scale, dq[m][4 * x + 2] * p.scale, dq[m][4 * x + 3] * p.scale});
+}
+
+// dK, dV: a workgroup owns 32 keys; its waves take the 32-token tiles of all heads of the group in turn, with scores [query][key], which
+// are the operands of dV^T += dO^T P and dK^T += Q^T dS as they stand.  The waves' sums meet in LDS.  Blocks 0 .. sink_tiles * parts - 1 of a
+// head work on the sink tiles, a share of the tokens each.  d > 192: the columns of the gradients are shared by two workgroups
+// (blockIdx.y), which both form the scores; one would need 600 registers per lane.
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads, 1) win_plain_dkdv_kernel(WinParams p, int key_blocks) {
+    constexpr int MT = DP == 256 ? 4 : DP / 32;
+    extern __shared__ __attribute__((aligned(16))) float meet[];  // [2 MT][4][64] x 16 bytes
+    const int c0 = 32 * MT * blockIdx.y;  // first column of the gradients
+    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int bk = blockIdx.x / key_blocks, b = bk / p.kv_heads, kvh = bk % p.kv_heads;
+    const int blk = blockIdx.x % key_blocks, shared = p.sink_tiles * p.parts;
+    const int part = blk < shared ? blk % p.parts : -1;
+    const int j0 = 32 * (blk < shared ? blk / p.parts : blk - shared + p.sink_tiles);
+    const WinSeq s = win_sequence(p, b);
+    const int j = j0 + l32;
+    const long kv = (long)b * p.k_b + (long)kvh * p.k_h;
+    // tokens i0 .. i1 - 1 see some key of the block
+    int i0 = j0, i1 = s.len;
+    if (j0 >= p.sinks) i1 = (int)min((long)s.len, (long)j0 + 31 + p.window);
+    if (part >= 0) {
+        const int share = ((s.len - j0 + p.parts - 1) / p.parts + 31) & ~31;
+        i0 = min(s.len, j0 + part * share);
+        i1 = min(s.len, i0 + share);
+    }
+    const int t_tiles = j0 < s.len ? (i1 - i0 + 31) / 32 : 0, jobs = max(0, t_tiles) * p.group;
+    const int jr = max(0, min(j, s.len - 1));
+    RowOperand<T, DP, DP <= 128> k, v;
+    k.init(static_cast<const T*>(p.K) + kv + (long)jr * p.k_n, p.d, h);
+    v.init(static_cast<const T*>(p.V) + kv + (long)jr * p.k_n, p.d, h);
+    f32x16 dk[MT], dv[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dk[m][e] = dv[m][e] = 0.f;
+    const float cs = p.scale * kLog2e;
+    for (int job = w; job < jobs; job += 4) {
+        const int head = kvh * p.group + job / t_tiles, t0 = i0 + 32 * (job % t_tiles);
+        const long base = s.q_base + (long)head * p.q_h;
+        const T *Q = static_cast<const T*>(p.Q) + base, *G = static_cast<const T*>(p.dO) + base;
+        const long stat = s.lse_base + (long)head * s.lse_h;
+        const int tr = min(t0 + l32, i1 - 1);
+        f32x16 st, dp;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) st[e] = dp[e] = 0.f;
+        scores(st, Q + (long)tr * p.q_n, 1.f, k, p.d, h);
+        scores(dp, G + (long)tr * p.q_n, 1.f, v, p.d, h);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int i = t0 + acc_row(e, h), ic = min(i, i1 - 1);
+            const bool seen = i < i1 && j <= i && (i - j < p.window || j < p.sinks);
+            const float f = seen ? __builtin_amdgcn_exp2f(fmaf(st[e], cs, -p.LSE_in[stat + ic] * kLog2e)) : 0.f;
+            const float ds = seen ? f * (dp[e] - p.delta[stat + ic]) : 0.f;
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                dv[m] = mfma_f32(load1(G + (long)ic * p.q_n, c0 + 32 * m + l32, p.d), f, dv[m]);
+                dk[m] = mfma_f32(load1(Q + (long)ic * p.q_n, c0 + 32 * m + l32, p.d), ds, dk[m]);
+            }
+        }
+    }
+    auto slot = [&](int m, int x) { return reinterpret_cast<f32x4*>(meet) + (m * 4 + x) * 64 + lane; };
+    for (int from = 1; from < 4; ++from) {
+        if (w == from) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    *slot(m, x) = f32x4{dk[m][4 * x], dk[m][4 * x + 1], dk[m][4 * x + 2], dk[m][4 * x + 3]};
+                    *slot(MT + m, x) = f32x4{dv[m][4 * x], dv[m][4 * x + 1], dv[m][4 * x + 2], dv[m][4 * x + 3]};
+                }
+        }
+        __syncthreads();
+        if (w == 0) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const f32x4 a = *slot(m, x), c = *slot(MT + m, x);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        dk[m][4 * x + e] += a[e];
+                        dv[m][4 * x + e] += c[e];
+                    }
+                }
+        }
+        __syncthreads();
+    }
+    if (w != 0 || j >= p.n) return;
+    if (part >= 0) {
+        float* dst = p.part_kv + (((long)bk * p.sink_tiles + j0 / 32) * p.parts + part) * 2 * 32 * p.d + (long)l32 * p.d;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                store4(dst, c0 + 32 * m + 8 * x + 4 * h, p.d, f32x4{dk[m][4 * x], dk[m][4 * x + 1], dk[m][4 * x + 2], dk[m][4 * x + 3]} * p.scale);
+                store4(dst + 32 * p.d, c0 + 32 * m + 8 * x + 4 * h, p.d, f32x4{dv[m][4 * x], dv[m][4 * x + 1], dv[m][4 * x + 2], dv[m][4 * x + 3]});
+            }
+        return;
+    }
+    const long out = kv + (long)j * p.k_n;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            store4(static_cast<T*>(p.dK) + out, c0 + 32 * m + 8 * x + 4 * h, p.d, f32x4{dk[m][4 * x], dk[m][4 * x + 1], dk[m][4 * x + 2], dk[m][4 * x + 3]} * p.scale);
+            store4(static_cast<T*>(p.dV) + out, c0 + 32 * m + 8 * x + 4 * h, p.d, f32x4{dv[m][4 * x], dv[m][4 * x + 1], dv[m][4 * x + 2], dv[m][4 * x + 3]});
+        }
+}
+
+// dK and dV of the keys in sink tiles: the sum of the parts, in their order.  Eight lanes per row.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) win_sink_kernel(WinParams p, int tile) {
+    const int keys = min(p.sink_tiles * tile, p.n);
+    const long f = ((long)blockIdx.x * kThreads + threadIdx.x) >> 3;
+    if (f >= (long)p.batch * p.kv_heads * keys * 2) return;
+    const int which = (int)(f & 1), j = (int)((f >> 1) % keys), bk = (int)((f >> 1) / keys);
+    const float* src = p.part_kv + (((long)bk * p.sink_tiles + j / tile) * p.parts * 2 + which) * tile * p.d + (long)(j % tile) * p.d;
+    T* dst = static_cast<T*>(which ? p.dV : p.dK) + (long)(bk / p.kv_heads) * p.k_b + (long)(bk % p.kv_heads) * p.k_h + (long)j * p.k_n;
+    for (int c = 4 * (threadIdx.x & 7); c < p.d; c += 32) {
+        f32x4 sum = load4(src, c, p.d);
+        for (int k = 1; k < p.parts; ++k) sum += load4(src + (long)k * 2 * tile * p.d, c, p.d);
+        store4(dst, c, p.d, sum);
+    }
+}
+
+// f(width): head dimensions are taken in widths of 64, 96, 128, 192 and 256
+template <typename F>
+hipError_t with_width(int d, F f) {
+    if (d <= 64) return f(std::integral_constant<int, 64>{});
+    if (d <= 96) return f(std::integral_constant<int, 96>{});
+    if (d <= 128) return f(std::integral_constant<int, 128>{});
+    if (d <= 192) return f(std::integral_constant<int, 192>{});
+    return f(std::integral_constant<int, 256>{});
+}
+
+template <typename T, typename E>
+hipError_t fwd(const WinParams& p, hipStream_t stream) {
+    const int blocks = (int)(((long)p.n * p.group + 127) / 128);
+    return with_width(p.d, [&](auto width) {
+        hipLaunchKernelGGL((win_plain_out_kernel<T, E, decltype(width)::value>), dim3((unsigned)((long)blocks * p.batch * p.kv_heads), (unsigned)p.splits),
+                           dim3(kThreads), 0, stream, p, blocks);
+        return hipGetLastError();
+    });
+}
+
+template <typename T>
+hipError_t bwd(const WinParams& p, hipStream_t stream) {
+    const int blocks = (int)(((long)p.n * p.group + 127) / 128), keys = (p.n + 31) / 32 - p.sink_tiles + p.sink_tiles * p.parts;
+    return with_width(p.d, [&](auto width) {
+        constexpr int DP = decltype(width)::value;
+        hipLaunchKernelGGL((win_plain_dq_kernel<T, DP>), dim3((unsigned)((long)blocks * p.batch * p.kv_heads)), dim3(kThreads), 0, stream, p, blocks);
+        hipLaunchKernelGGL((win_plain_dkdv_kernel<T, DP>), dim3((unsigned)((long)keys * p.batch * p.kv_heads), DP == 256 ? 2 : 1), dim3(kThreads),
+                           (DP == 256 ? 128 : DP) * 256, stream, p, keys);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace
+
+hipError_t launch_win_plain_fwd(bool is_bf16, bool fp8, const WinParams& p, hipStream_t stream) {
+    if (fp8) return is_bf16 ? fwd<__bf16, uint8_t>(p, stream) : fwd<float, uint8_t>(p, stream);
+    return is_bf16 ? fwd<__bf16, __bf16>(p, stream) : fwd<float, float>(p, stream);
+}
+hipError_t launch_win_plain_bwd(bool is_bf16, const WinParams& p, hipStream_t stream) {
+    return is_bf16 ? bwd<__bf16>(p, stream) : bwd<float>(p, stream);
+}
+hipError_t launch_win_join(bool is_bf16, const WinParams& p, hipStream_t stream) {
+    const dim3 grid((unsigned)(((long)p.n * p.heads + 3) / 4), (unsigned)p.batch);
+    if (is_bf16) hipLaunchKernelGGL(win_join_kernel<__bf16>, grid, dim3(kThreads), 0, stream, p);
+    else hipLaunchKernelGGL(win_join_kernel<float>, grid, dim3(kThreads), 0, stream, p);
+    return hipGetLastError();
+}
+hipError_t launch_win_rows(bool is_bf16, const WinParams& p, hipStream_t stream) {
+    const dim3 grid((unsigned)(((long)p.batch * p.heads * p.n * 8 + kThreads - 1) / kThreads));
+    if (is_bf16) hipLaunchKernelGGL(win_rows_kernel<__bf16>, grid, dim3(kThreads), 0, stream, p);
+    else hipLaunchKernelGGL(win_rows_kernel<float>, grid, dim3(kThreads), 0, stream, p);
+    return hipGetLastError();
+}
+hipError_t launch_win_sinks(bool is_bf16, int tile, const WinParams& p, hipStream_t stream) {
+    const long rows = (long)p.batch * p.kv_heads * (p.sink_tiles * tile < p.n ? p.sink_tiles * tile : p.n) * 2;
+    const dim3 grid((unsigned)((rows * 8 + kThreads - 1) / kThreads));
+    if (is_bf16) hipLaunchKernelGGL(win_sink_kernel<__bf16>, grid, dim3(kThreads), 0, stream, p, tile);
+    else hipLaunchKernelGGL(win_sink_kernel<float>, grid, dim3(kThreads), 0, stream, p, tile);
+    return hipGetLastError();
+}
+
+}  // namespace attn

@@ -1,0 +1,122 @@
+// Windowed attention over tensors or over a paged cache: the arguments of its kernels and what they share.
+//
+// A query at position i of its sequence sees key j iff j <= i and (no window, or i - j < window, or j < sinks).  In tensors
+// [batch, heads, n, d] token t has position t and a sequence may be shorter than n; in a paged cache the new tokens of a
+// sequence are its last ones.  The heads of a group share keys and values: the queries of a (sequence, key head) are taken
+// as rows r = t * group + g of one matrix, so that a tile of keys is read once for all of them.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "attn_common.hpp"
+
+namespace attn {
+
+struct WinParams {
+    const void *Q, *K, *V, *dO, *O_in;  // K, V: tensors or pages
+    void *O, *dQ, *dK, *dV;
+    const float* LSE_in;
+    float *LSE, *delta;
+    long q_b, q_h, q_n;     // Q, O, dO, dQ; paged: q_b unused
+    long k_b, k_h, k_n;     // K, V, dK, dV; paged: k_b is the stride of pages
+    const uint8_t *K_exp, *V_exp;  // [page][kv head][token of the page]; nullptr: pages hold values
+    const int32_t *table, *lens, *q_ptr;  // table == nullptr: tensors
+    long table_stride;
+    int batch, heads, kv_heads, group, n, d;  // n: tokens (tensors), largest number of new tokens of a sequence (paged)
+    int page_shift, num_pages, total_q, max_len;
+    float scale;
+    int window, sinks;  // window > 0; no window: larger than any distance, and no sinks
+    // forward: work of a row block shared out over `splits` workgroups of `chunk` tiles each; their sums meet in win_join_kernel
+    int splits, chunk;
+    float *part_o, *part_ml;  // [row][split][d], [row][split][2], row = token row * heads + head
+    // backward: the key tiles that hold sinks are each worked on by `parts` workgroups; their sums meet in win_sink_kernel
+    int sink_tiles, parts;
+    float* part_kv;  // [batch * kv_heads][sink tile][part][dK, dV][keys of a tile][d]
+};
+
+// What a workgroup knows of its sequence.  Everything is uniform; lengths from device memory are brought into the range that the
+// buffers allow, so that no value in them leads outside.
+struct WinSeq {
+    int len, nq, first;  // keys 0 .. len - 1; queries t = 0 .. nq - 1 at positions first + t
+    long q_base, lse_base, lse_h, lse_t;
+};
+__device__ __forceinline__ WinSeq win_sequence(const WinParams& p, int b) {
+    WinSeq s;
+    if (p.table) {
+        const int row0 = p.q_ptr ? min(max(p.q_ptr[b], 0), p.total_q) : b * p.n;
+        const int rows = p.q_ptr ? min(max(p.q_ptr[b + 1] - row0, 0), p.total_q - row0) : p.n;
+        s.len = min(max(p.lens[b], 0), p.max_len);
+        s.first = s.len - rows;
+        s.nq = min(rows, p.n);
+        s.q_base = (long)row0 * p.q_n;
+        s.lse_base = (long)row0 * p.heads;
+        s.lse_h = 1;
+        s.lse_t = p.heads;
+    } else {
+        s.len = p.lens ? min(max(p.lens[b], 0), p.n) : p.n;
+        s.first = 0;
+        s.nq = p.n;
+        s.q_base = (long)b * p.q_b;
+        s.lse_base = (long)b * p.heads * p.n;
+        s.lse_h = p.n;
+        s.lse_t = 1;
+    }
+    return s;
+}
+
+// The key tiles of BC keys that queries at positions i_min .. i_max see some key of: those of the sinks, then those of the windows.
+template <int BC>
+struct WinTiles {
+    int lo, end;    // keys lo .. end - 1, and 0 .. sinks - 1, are seen by some query
+    int ns, first;  // sink tiles; first of the other tiles
+    int count;
+    __device__ __forceinline__ void init(const WinParams& p, int len, int i_min, int i_max) {
+        end = min(i_max, len - 1) + 1;
+        lo = max(0, i_min - p.window + 1);
+        ns = (min(p.sinks, end) + BC - 1) / BC;
+        first = max(lo / BC, ns);
+        count = ns + max(0, (end + BC - 1) / BC - first);
+        if (end <= 0 || i_min >= len) count = 0;
+    }
+    __device__ __forceinline__ int start(int it) const { return (it < ns ? it : it - ns + first) * BC; }
+    // The row that is read for key j of a tile: rows that no query of the block sees (behind the end, before the windows, where pages
+    // may be gone) are replaced by one that some query sees.
+    __device__ __forceinline__ int row(const WinParams& p, int j) const {
+        j = min(j, end - 1);
+        return j < lo && j >= p.sinks ? lo : j;
+    }
+    __device__ __forceinline__ bool whole(const WinParams& p, int j0) const {  // every row of the tile is its own
+        return j0 + BC <= end && (j0 >= lo || j0 + BC <= p.sinks);
+    }
+};
+
+// Element offset of the first value of a key's row in pages, and of its exponent byte.  A page number outside the cache (of a token
+// that a caller declared visible and has no page for) is brought inside it: the result is meaningless, the access is not.
+struct PageRow {
+    long at;
+    long exp;
+};
+__device__ __forceinline__ int win_page(const WinParams& p, int b, int j) {
+    const int page = p.table[(long)b * p.table_stride + (j >> p.page_shift)];
+    return (int)min((unsigned)page, (unsigned)(p.num_pages - 1));
+}
+__device__ __forceinline__ PageRow win_page_row(const WinParams& p, int page, int kvh, int j) {
+    const int slot = j & ((1 << p.page_shift) - 1);
+    return {(long)page * p.k_b + (long)kvh * p.k_h + (long)slot * p.k_n,
+            (((long)page * p.kv_heads + kvh) << p.page_shift) + slot};
+}
+
+// 2^(e - 127) for an exponent byte e of 1 .. 254 (0 and 255, which no row is written with, give 0 and infinity).
+__device__ __forceinline__ float exp_value(uint8_t e) { return __builtin_bit_cast(float, (uint32_t)e << 23); }
+
+// ------------------------------------------------------------------------------------------------------------- host
+// is_bf16: the type of Q, O and of tensors, and of pages that are not quantised (fp8).  The arguments have been checked.
+hipError_t launch_win_plain_fwd(bool is_bf16, bool fp8, const WinParams& p, hipStream_t stream);
+hipError_t launch_win_plain_bwd(bool is_bf16, const WinParams& p, hipStream_t stream);
+hipError_t launch_win_join(bool is_bf16, const WinParams& p, hipStream_t stream);
+hipError_t launch_win_sinks(bool is_bf16, int tile, const WinParams& p, hipStream_t stream);
+hipError_t launch_win_rows(bool is_bf16, const WinParams& p, hipStream_t stream);  // delta
+hipError_t launch_cache_write(bool is_bf16, bool fp8, const WinParams& p, const void* K, const void* V, long s_n, long s_h, hipStream_t stream);
+hipError_t launch_cache_read(bool is_bf16, bool fp8, const WinParams& p, void* K, void* V, long s_n, long s_h, hipStream_t stream);
+
+}  // namespace attn

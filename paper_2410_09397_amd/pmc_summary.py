@@ -43,8 +43,8 @@ def traffic_key(workload, tiling):
     return workload if not tiling else "%s@tiling%d" % (workload, tiling)
 FWD_KERNELS = ("fwd_kernel", "fwd_split_kernel", "fwd_pipe_kernel", "ld_scores_kernel<1", "ld_gemm_kernel<false>", "ld_gemm_wide_kernel<false>",
                "ld_lse_combine", "generic_fwd")
-# launched by neither attn_fwd nor attn_bwd: the weight gradient's own and the measurement aids
-OTHER_KERNELS = ("wgrad_partial", "wgrad_reduce", "proj_kernel", "tile_skeleton_kernel", "mfma_ceiling_kernel")
+# launched by neither attn_fwd nor attn_bwd: the weight gradient's own, windowed attention, the paged cache and the measurement aids
+OTHER_KERNELS = ("wgrad_partial", "wgrad_reduce", "proj_kernel", "tile_skeleton_kernel", "mfma_ceiling_kernel", "win_", "cache_")
 
 
 def _one(pattern):

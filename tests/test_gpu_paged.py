@@ -1,0 +1,369 @@
+"""The paged cache (attn_cache_write, attn_cache_read) and the attention over it (attn_paged_fwd) against their definitions in 64 bits.
+
+Writing and reading back are exact: codes, exponents and values are compared bit for bit.  Attention: max |x - ref| / max |ref| <= 2 % for
+bf16 (P and O are rounded to 8 bits, 2^-9 of a value each, errors of both sides of up to 0.4 %; the quantised keys and values
+are exact in bf16) and 1e-4 for fp32."""
+import math
+
+import pytest
+
+from tests import window_ref
+from tests.helpers import LSE_TOL, TOL
+
+pytestmark = pytest.mark.gpu
+DTYPES = {"f32": "float32", "bf16": "bfloat16"}
+
+
+class Cache:
+    """A cache with sequences of given lengths in it whose pages lie anywhere; what belongs to no token is NaN."""
+
+    def __init__(self, dtype, kind, lens, kvh, d, page, seed=0, layout="phnd", spare=2, width=None):
+        import torch
+        gen = torch.Generator()
+        gen.manual_seed(seed)
+        dt = getattr(torch, DTYPES[dtype])
+        used = [-(-l // page) for l in lens]
+        num = sum(used) + spare
+        self.table = torch.full((len(lens), max([1] + used) if width is None else width), -1, dtype=torch.int32)
+        order = torch.randperm(num, generator=gen).tolist()
+        self.keys, self.values = [], []
+        shape = (num, kvh, page, d) if layout == "phnd" else (num, page, kvh, d)
+        pages = [torch.full(shape, math.nan, dtype=dt) for _ in range(2)]
+        if layout == "pnhd":
+            pages = [x.transpose(1, 2) for x in pages]
+        for b, l in enumerate(lens):
+            mine = [order.pop() for _ in range(used[b])]
+            self.table[b, :used[b]] = torch.tensor(mine, dtype=torch.int32)
+            for which in range(2):
+                x = torch.randn(l, kvh, d, generator=gen)
+                if which == 0:
+                    x = x * torch.exp(0.4 * torch.randn(1, kvh, d, generator=gen))
+                x = x.to(dt)
+                for i, at in enumerate(mine):
+                    rows = x[i * page:(i + 1) * page]
+                    pages[which][at, :, :rows.shape[0]] = rows.transpose(0, 1)
+                (self.keys, self.values)[which].append(x)
+        self.K_exp = self.V_exp = None
+        if kind == "fp8":
+            (k, ke), (v, ve) = (window_ref.quantise(x) for x in pages)
+            if layout == "pnhd":
+                k, v = (x.transpose(1, 2).contiguous().transpose(1, 2) for x in (k, v))
+            pages = [k, v]
+            self.K_exp, self.V_exp = ke.contiguous().cuda(), ve.contiguous().cuda()
+            self.keys, self.values = ([window_ref.values(*window_ref.quantise(x)) for x in xs] for xs in (self.keys, self.values))
+        self.K, self.V = (self._to_gpu(x) for x in pages)
+        self.table = self.table.cuda()
+        self.keys, self.values = ([x.double().cuda() for x in xs] for xs in (self.keys, self.values))
+        self.host_lens = list(lens)
+        self.lens = torch.tensor(lens, dtype=torch.int32, device="cuda")
+
+    @staticmethod
+    def _to_gpu(x):
+        import torch
+        out = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device="cuda")
+        out.view(torch.uint8).copy_(x.view(torch.uint8)) if x.dtype is torch.float8_e4m3fn else out.copy_(x)
+        return out
+
+    def args(self):
+        return (self.K, self.V, self.table, self.lens)
+
+    def exps(self):
+        return dict(K_exp=self.K_exp, V_exp=self.V_exp)
+
+
+def _paged_case(dtype, kind, lens, new, h, kvh, d, page, window=0, sinks=0, layout="phnd", max_len=None, ragged=True, seed=0, width=None):
+    import torch
+    from paper_2410_09397_amd import attn
+    c = Cache(dtype, kind, lens, kvh, d, page, seed=seed, layout=layout, width=width)
+    starts = [0]
+    for q in new:
+        starts.append(starts[-1] + q)
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed + 100)
+    Q = torch.randn(starts[-1], h, d, generator=gen, device="cuda").to(getattr(torch, DTYPES[dtype]))
+    kw = dict(q_ptr=torch.tensor(starts, dtype=torch.int32, device="cuda"), max_q=max([1] + new)) if ragged else {}
+    O, LSE = attn.attn_paged_fwd(Q, *c.args(), d ** -0.5, window=window, sinks=sinks, max_len=max_len, **kw, **c.exps())
+    rO, rL = window_ref.paged_attention(Q, c.keys, c.values, starts, lens, d ** -0.5, window, sinks)
+    none = rL == -math.inf
+    assert torch.equal(LSE == -math.inf, none) and not bool(O[none].any())
+    if bool((~none).any()):
+        err, top = float((O.double() - rO).abs().max()), float(rO.abs().max())
+        lerr = float((LSE.double() - rL)[~none].abs().max())
+        print("O %.3e of %.3e  LSE %.3e" % (err, top, lerr), flush=True)
+        assert err <= TOL[dtype] * top and lerr <= LSE_TOL[dtype] * max(1.0, float(rL[~none].abs().max()))
+    return c, Q, O, LSE
+
+
+CASES = [
+    # dtype, kind, lens, new tokens, heads, kv heads, d, page, window, sinks
+    ("bf16", "plain", [1], [1], 1, 1, 64, 16, 0, 0),
+    ("bf16", "fp8", [5, 1, 0], [1, 1, 0], 4, 2, 128, 16, 0, 0),
+    ("bf16", "plain", [17, 600, 64, 333], [1, 1, 1, 1], 8, 2, 64, 16, 0, 0),
+    ("bf16", "fp8", [17, 600, 64, 333], [1, 1, 1, 1], 32, 4, 128, 32, 0, 0),
+    ("bf16", "plain", [130, 900], [1, 1], 40, 1, 128, 64, 0, 0),       # more heads in a group than a wave has rows
+    ("bf16", "fp8", [5000], [1], 4, 1, 128, 16, 0, 0),
+    ("bf16", "plain", [9000, 30], [1, 1], 5, 5, 64, 128, 0, 0),
+    ("bf16", "plain", [4100, 2000, 100], [1, 1, 1], 8, 2, 128, 16, 100, 4),
+    ("bf16", "fp8", [4100, 2000, 100], [1, 1, 1], 8, 2, 128, 16, 1, 70),
+    ("bf16", "plain", [700], [700], 4, 1, 128, 16, 0, 0),              # a whole prompt
+    ("bf16", "fp8", [700, 431], [300, 431], 6, 2, 64, 16, 0, 0),
+    ("bf16", "plain", [1500, 64, 900, 3], [37, 64, 1, 3], 8, 2, 128, 16, 130, 5),
+    ("bf16", "fp8", [1500, 64, 900, 3], [37, 64, 1, 3], 6, 2, 128, 64, 130, 65),
+    ("bf16", "plain", [300, 200], [1, 150], 4, 2, 256, 16, 0, 0),
+    ("bf16", "fp8", [3000, 200], [1, 1], 4, 2, 256, 8, 50, 3),
+    ("bf16", "fp8", [300, 200], [100, 200], 4, 2, 256, 256, 50, 3),
+    ("bf16", "plain", [400], [90], 15, 3, 96, 16, 60, 3),
+    ("bf16", "fp8", [2000, 50], [1, 7], 4, 2, 72, 16, 0, 0),
+    ("f32", "plain", [1, 40, 2100], [1, 13, 2], 6, 3, 40, 8, 0, 0),
+    ("f32", "plain", [77, 500], [77, 1], 2, 1, 33, 16, 20, 2),
+    ("f32", "fp8", [130, 500], [1, 60], 4, 1, 128, 4096, 0, 0),
+]
+
+
+@pytest.mark.parametrize("dtype,kind,lens,new,h,kvh,d,page,window,sinks", CASES)
+def test_attention_over_pages(dtype, kind, lens, new, h, kvh, d, page, window, sinks):
+    print("case paged", dtype, kind, lens, new, h, kvh, d, page, window, sinks, flush=True)
+    _paged_case(dtype, kind, lens, new, h, kvh, d, page, window, sinks)
+
+
+@pytest.mark.parametrize("kind", ["plain", "fp8"])
+@pytest.mark.parametrize("d", [64, 128, 256, 80])
+def test_pages_of_token_major_layout_and_a_tight_bound_on_the_lengths(kind, d):
+    print("case layout", kind, d, flush=True)
+    _paged_case("bf16", kind, [300, 77, 1000], [1, 1, 1], 4, 2, d, 16, layout="pnhd", max_len=1000)
+    _paged_case("bf16", kind, [300, 77, 1000], [90, 77, 3], 4, 2, d, 16, window=200, sinks=3, layout="pnhd", max_len=1000)
+
+
+def test_rows_in_front_of_the_first_token_see_nothing():
+    """More new rows than the sequence has tokens: the first of them lie in front of position 0."""
+    print("case negative positions", flush=True)
+    _paged_case("bf16", "plain", [3, 0, 70], [9, 4, 100], 4, 2, 128, 16)
+    _paged_case("bf16", "fp8", [1, 0], [2, 2], 4, 2, 64, 16, window=1)
+    _paged_case("f32", "plain", [3, 0], [5, 1], 2, 2, 24, 16)
+
+
+@pytest.mark.parametrize("kind", ["plain", "fp8"])
+@pytest.mark.parametrize("d", [64, 128, 256, 96])
+@pytest.mark.parametrize("new", [1, 50])
+def test_pages_behind_the_window_may_be_gone(kind, d, new):
+    """Their entries are -1 (or anything) and their contents NaN: nothing changes, down to the bits."""
+    import torch
+    from paper_2410_09397_amd import attn
+    print("case pages gone", kind, d, new, flush=True)
+    window, sinks, page, lens = 100, 4, 16, [900, 300, 120]
+    c, Q, O, LSE = _paged_case("bf16", kind, lens, [new] * 3, 4, 2, d, page, window, sinks, ragged=False)
+    for b, l in enumerate(lens):
+        first = max(0, l - new - window + 1) // page  # the oldest page that a window reaches into
+        for x in range(1, first):
+            gone = int(c.table[b, x])
+            c.table[b, x] = [-1, 10 ** 9, -(10 ** 9)][x % 3]
+            for pages, exps in ((c.K, c.K_exp), (c.V, c.V_exp)):
+                if exps is None:
+                    pages[gone] = math.nan
+                else:
+                    pages.view(torch.uint8)[gone] = 0x7f
+                    exps[gone] = 255
+    again = attn.attn_paged_fwd(Q, *c.args(), d ** -0.5, window=window, sinks=sinks, **c.exps())
+    assert torch.equal(again[0], O) and torch.equal(again[1], LSE)
+
+
+def test_rows_of_no_sequence_are_left_alone():
+    import torch
+    from paper_2410_09397_amd import attn
+    print("case gaps in the rows", flush=True)
+    c = Cache("bf16", "plain", [40, 70], 2, 128, 16)
+    Q = torch.randn(10, 4, 128, device="cuda").to(torch.bfloat16)
+    ptr = torch.tensor([2, 3, 9], dtype=torch.int32, device="cuda")  # rows 0, 1 and 9 belong to nobody; max_q cuts the second sequence
+    O, LSE = torch.full_like(Q, 7.0), torch.full((10, 4), 7.0, device="cuda")
+    attn.attn_paged_fwd(Q, *c.args(), 0.1, q_ptr=ptr, max_q=4, out=(O, LSE))
+    want, _ = window_ref.paged_attention(Q, c.keys, c.values, [2, 3, 9], [40, 70], 0.1, 0, 0)
+    assert bool((O[[0, 1, 7, 8, 9]] == 7.0).all()) and bool((LSE[[0, 1, 7, 8, 9]] == 7.0).all())
+    assert float((O[2:7].double() - want[2:7]).abs().max()) <= TOL["bf16"] * float(want.abs().max())
+
+
+@pytest.mark.parametrize("dtype,kind,d,page", [("bf16", "plain", 64, 16), ("bf16", "fp8", 64, 16), ("bf16", "fp8", 128, 64), ("bf16", "plain", 256, 8),
+                                               ("bf16", "fp8", 256, 16), ("bf16", "fp8", 72, 32), ("f32", "plain", 33, 16), ("f32", "fp8", 104, 16)])
+@pytest.mark.parametrize("layout", ["phnd", "pnhd"])
+def test_writing_and_reading_back(dtype, kind, d, page, layout):
+    """Ragged new tokens, first one at any place of a page; what is not written stays; a page that is gone is skipped."""
+    import torch
+    from paper_2410_09397_amd import attn
+    print("case write", dtype, kind, d, page, layout, flush=True)
+    lens, new, kvh = [37, 5, 200, 1, 0], [20, 5, 1, 0, 0], 3
+    c = Cache(dtype, kind, lens, kvh, d, page, layout=layout, seed=3)
+    dt = getattr(torch, DTYPES[dtype])
+    starts = [0, 20, 25, 26, 26, 26]
+    x = [torch.randn(starts[-1], kvh, d).mul(3.0).to(dt) for _ in range(2)]
+    x[0][0] = 0.0
+    x[0][1, 0, 0] = math.inf
+    x[1][2, 1, 1] = math.nan
+    x[1][3] *= 1e-30
+    x[1][4] *= 1e30
+    x[0][5, 0] = 448.0
+    x[0][6, 0], x[0][6, 0, 0] = 0.0, 449.0
+    x[0][7, 0] = -0.0
+    codes = [window_ref.quantise(y) if kind == "fp8" else (y, None) for y in x]
+    want = [c.K.clone(), c.V.clone()]
+    want_exp = [None if e is None else e.clone() for e in (c.K_exp, c.V_exp)]
+    table = c.table.cpu()
+    raw = lambda t: t.view(torch.uint8) if t.dtype is torch.float8_e4m3fn else t
+    c.table[2, 199 // page] = -1  # the page of the third sequence's token
+    for b in range(2):
+        for t in range(new[b]):
+            pos = lens[b] - new[b] + t
+            at, slot = int(table[b, pos // page]), pos % page
+            for which in range(2):
+                raw(want[which])[at, :, slot] = raw(codes[which][0])[starts[b] + t].cuda()
+                if kind == "fp8":
+                    want_exp[which][at, :, slot] = codes[which][1][starts[b] + t].cuda()
+    ptr = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    attn.attn_cache_write(x[0].cuda(), x[1].cuda(), *c.args(), q_ptr=ptr, max_q=20, **c.exps())
+
+    def same(a, b):
+        if a.dtype is torch.float8_e4m3fn:  # (a NaN code has a sign, which means nothing)
+            a, b = a.float(), b.float()
+        return bool(((a == b) & (torch.signbit(a) == torch.signbit(b)) | (torch.isnan(a) & torch.isnan(b))).all())
+    assert same(c.K, want[0]) and same(c.V, want[1])
+    if kind == "fp8":
+        assert torch.equal(c.K_exp, want_exp[0]) and torch.equal(c.V_exp, want_exp[1])
+    got = attn.attn_cache_read(*c.args(), dt, 26, q_ptr=ptr, max_q=20, **c.exps())
+    for which in range(2):
+        y = window_ref.values(*codes[which]).to(dt).cuda()
+        assert same(got[which][:25], y[:25])
+        assert not bool(got[which][25].any())  # no page: zeros
+
+
+def test_without_row_offsets_every_sequence_has_the_same_number_of_tokens():
+    import torch
+    from paper_2410_09397_amd import attn
+    print("case write without offsets", flush=True)
+    c = Cache("bf16", "fp8", [9, 40, 3], 2, 128, 16, seed=6)
+    K, V = (torch.randn(6, 2, 128, device="cuda").to(torch.bfloat16) for _ in range(2))
+    attn.attn_cache_write(K, V, *c.args(), **c.exps())
+    k, v = attn.attn_cache_read(*c.args(), torch.bfloat16, 6, **c.exps())
+    for x, y in ((K, k), (V, v)):
+        assert torch.equal(y, window_ref.values(*window_ref.quantise(x.cpu())).to(torch.bfloat16).cuda())
+
+
+def test_positions_in_front_of_the_first_token_are_neither_written_nor_read():
+    import torch
+    from paper_2410_09397_amd import attn
+    print("case write in front", flush=True)
+    c = Cache("bf16", "plain", [2], 1, 64, 16)
+    before = c.K.clone()
+    K = torch.randn(5, 1, 64, device="cuda").to(torch.bfloat16)
+    attn.attn_cache_write(K, K, *c.args())
+    at = int(c.table[0, 0])
+    assert torch.equal(c.K[at, 0, :2], K[3:, 0])
+    before[at, 0, :2] = K[3:, 0]
+    assert torch.equal(c.K.nan_to_num(9.0), before.nan_to_num(9.0))
+    k, _ = attn.attn_cache_read(*c.args(), torch.bfloat16, 5)
+    assert not bool(k[:3].any()) and torch.equal(k[3:], K[3:])
+
+
+@pytest.mark.parametrize("d,kind", [(128, "plain"), (128, "fp8"), (96, "plain")])
+def test_offsets_beyond_32_bits(d, kind):
+    """A cache of more than 2^32 values whose last pages hold the sequence."""
+    import torch
+    from paper_2410_09397_amd import attn
+    print("case large cache", d, kind, flush=True)
+    kvh, page, n = 8, 64, 300
+    num = (1 << 32) // (kvh * page * d) + 100
+    small = Cache("bf16", kind, [n], kvh, d, page, spare=0)
+    K, V = (torch.empty(num, kvh, page, d, dtype=small.K.dtype, device="cuda") for _ in range(2))
+    exps = {}
+    raw = lambda t: t.view(torch.uint8) if t.dtype is torch.float8_e4m3fn else t
+    used = small.K.shape[0]
+    raw(K)[-used:], raw(V)[-used:] = raw(small.K), raw(small.V)
+    if kind == "fp8":
+        exps = dict(K_exp=torch.empty(num, kvh, page, dtype=torch.uint8, device="cuda"), V_exp=torch.empty(num, kvh, page, dtype=torch.uint8, device="cuda"))
+        exps["K_exp"][-used:], exps["V_exp"][-used:] = small.K_exp, small.V_exp
+    table = small.table + (num - used)
+    for new in (1, 200):
+        Q = torch.randn(new, 16, d, device="cuda").to(torch.bfloat16)
+        far = attn.attn_paged_fwd(Q, K, V, table, small.lens, 0.1, **exps)
+        near = attn.attn_paged_fwd(Q, *small.args(), 0.1, **small.exps())
+        assert torch.equal(far[0], near[0]) and torch.equal(far[1], near[1])
+    x = torch.randn(40, kvh, d, device="cuda").to(torch.bfloat16)
+    attn.attn_cache_write(x, x, K, V, table, small.lens, **exps)
+    attn.attn_cache_write(x, x, *small.args(), **small.exps())
+    assert torch.equal(raw(K)[-used:][raw(K)[-used:] == raw(K)[-used:]], raw(small.K)[raw(small.K) == raw(small.K)])
+    a = attn.attn_cache_read(K, V, table, small.lens, torch.bfloat16, n, **exps)
+    c = attn.attn_cache_read(*small.args(), torch.bfloat16, n, **small.exps())
+    assert torch.equal(a[0], c[0]) and torch.equal(a[1], c[1])
+
+
+@pytest.mark.parametrize("kind,d", [("plain", 128), ("fp8", 128), ("fp8", 64), ("plain", 80)])
+def test_decoding_gives_what_the_windowed_forward_gives(kind, d):
+    """Prompt in pieces, then token by token, written and attended: the rows of attn_win_fwd over the whole sequence (on the values
+    that the cache holds)."""
+    import torch
+    from paper_2410_09397_amd import attn
+    print("case decode against forward", kind, d, flush=True)
+    n, h, kvh, page, window, sinks = 230, 6, 2, 16, 60, 3
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(21)
+    Q, K, V = (torch.randn(1, x, n, d, generator=gen, device="cuda").to(torch.bfloat16) for x in (h, kvh, kvh))
+    Kp, Vp, Ke, Ve = attn.attn_cache_pages(20, kvh, page, d, torch.bfloat16 if kind == "plain" else torch.float8_e4m3fn)
+    table = torch.randperm(20)[None, :15].to(device="cuda", dtype=torch.int32)
+    rows, at = [], 0
+    for step in [100, 77, 1, 1, 40, 1, 1, 1, 8]:
+        lens = torch.tensor([at + step], dtype=torch.int32, device="cuda")
+        new = lambda x: x[0, :, at:at + step].transpose(0, 1).contiguous()
+        attn.attn_cache_write(new(K), new(V), Kp, Vp, table, lens, K_exp=Ke, V_exp=Ve)
+        rows.append(attn.attn_paged_fwd(new(Q), Kp, Vp, table, lens, d ** -0.5, window=window, sinks=sinks, K_exp=Ke, V_exp=Ve))
+        at += step
+    O, LSE = (torch.cat(x) for x in zip(*rows))
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    Kc, Vc = (x.transpose(0, 1)[None].contiguous() for x in attn.attn_cache_read(Kp, Vp, table, lens, torch.bfloat16, n, K_exp=Ke, V_exp=Ve))
+    wO, wL = attn.attn_win_fwd(Q, Kc, Vc, d ** -0.5, window=window, sinks=sinks)
+    assert float((O.transpose(0, 1)[None].double() - wO.double()).abs().max()) <= TOL["bf16"] * float(wO.double().abs().max())
+    assert float((LSE.t()[None] - wL).abs().max()) <= LSE_TOL["bf16"] * float(wL.abs().max())
+
+
+@pytest.mark.parametrize("kind,d", [("plain", 128), ("fp8", 64), ("fp8", 256), ("plain", 48)])
+def test_same_bits_again_on_another_stream_and_in_a_graph(kind, d):
+    """A decoding step as a server records it: write, attend; the lengths and the table change between the replays."""
+    import torch
+    from paper_2410_09397_amd import attn
+    print("case stream and graph", kind, d, flush=True)
+    lens = [800, 33, 400]
+    c = Cache("bf16", kind, lens, 2, d, 16, seed=9)
+    Q = torch.randn(3, 8, d, device="cuda").to(torch.bfloat16)
+    K, V = (torch.randn(3, 2, d, device="cuda").to(torch.bfloat16) for _ in range(2))
+
+    def step(out=None, workspace=None, stream=None):
+        attn.attn_cache_write(K, V, *c.args(), stream=stream, **c.exps())
+        return attn.attn_paged_fwd(Q, *c.args(), 0.1, out=out, workspace=workspace, stream=stream, **c.exps())
+
+    want = step()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = step(stream=side)
+    side.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    out = tuple(torch.empty_like(x) for x in want)
+    workspace = torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step(out=out, workspace=workspace)
+    for cut in (1, 17, 300):
+        Q.copy_(torch.randn(3, 8, d, device="cuda"))
+        K.copy_(torch.randn(3, 2, d, device="cuda"))
+        c.lens.copy_(torch.tensor([max(1, l - cut) for l in lens], dtype=torch.int32))
+        want = step()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1]), cut
+
+
+def test_empty_calls():
+    import torch
+    from paper_2410_09397_amd import attn
+    c = Cache("bf16", "plain", [5], 2, 64, 16)
+    x = torch.empty(0, 2, 64, dtype=torch.bfloat16, device="cuda")
+    attn.attn_cache_write(x, x, *c.args())
+    assert attn.attn_paged_fwd(x, *c.args(), 1.0)[0].shape == x.shape
+    assert attn.attn_cache_read(*c.args(), torch.bfloat16, 0)[0].shape == x.shape
