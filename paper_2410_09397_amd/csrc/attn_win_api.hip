@@ -147,19 +147,20 @@ attn_status check_cache(const attn_paged_desc* d, const attn_cache* c) {
     return ATTN_OK;
 }
 
-// Keys of a tile, rows of a row block, and workgroups per CU of the forward's kernels.
-int fwd_tile(const attn_paged_desc*) { return 32; }
-int64_t fwd_rows(const attn_paged_desc*) { return 128; }
+// Whether the rows of a (sequence, key head) are taken 32 at a time, by workgroups whose waves share the keys out among themselves.
+bool few_rows(const attn_paged_desc* d) { return is_wide(d->dtype, d->d) && (int64_t)d->max_q * (d->heads / d->kv_heads) <= 64; }
 
 // How the keys of a row block are shared out: with fewer row blocks than the chip has places for, a workgroup takes `chunk` tiles.
 void set_splits(WinParams& p, const attn_paged_desc* d) {
-    const int64_t blocks = (((int64_t)p.n * p.group + fwd_rows(d) - 1) / fwd_rows(d)) * p.batch * p.kv_heads;
-    const int64_t keys = std::min<int64_t>(p.max_len, (int64_t)p.window + p.n) + p.sinks, tiles = keys / fwd_tile(d) + 2;
+    const bool few = few_rows(d);
+    const int64_t rows = few ? 32 : 128, tile = is_wide(d->dtype, d->d) && !few ? 64 : 32;
+    const int64_t blocks = (((int64_t)p.n * p.group + rows - 1) / rows) * p.batch * p.kv_heads;
+    const int64_t keys = std::min<int64_t>(p.max_len, (int64_t)p.window + p.n) + p.sinks, tiles = keys / tile + 2;
     p.splits = 1;
     p.chunk = 0x7fffffff;
-    const int64_t want = std::min<int64_t>(64, 1024 / std::max<int64_t>(1, blocks));
+    const int64_t want = std::min<int64_t>(64, (few ? 2048 : 1024) / std::max<int64_t>(1, blocks));
     if (want > 1 && tiles > 8) {
-        p.chunk = (int)std::max<int64_t>(4, (tiles + want - 1) / want);
+        p.chunk = (int)std::max<int64_t>(few ? 8 : 4, (tiles + want - 1) / want);
         p.splits = (int)((tiles + p.chunk - 1) / p.chunk);
         if (p.splits <= 1) {
             p.splits = 1;
@@ -238,7 +239,8 @@ attn_status attn_win_fwd(const attn_win_desc* desc, const int32_t* lens, const v
     p.V = V;
     p.O = O;
     p.LSE = LSE;
-    return status_of(attn::launch_win_plain_fwd(bf16, false, p, static_cast<hipStream_t>(stream)));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return status_of(is_wide(desc->dtype, desc->d) ? attn::launch_win_fwd(false, false, p, s) : attn::launch_win_plain_fwd(bf16, false, p, s));
 }
 
 attn_status attn_win_bwd(const attn_win_desc* desc, const int32_t* lens, const void* Q, const void* K, const void* V, const void* O,
@@ -319,7 +321,8 @@ attn_status attn_paged_fwd(const attn_paged_desc* desc, const attn_cache* cache,
     p.part_ml = static_cast<float*>(workspace);
     p.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + part_ml_bytes(desc, p));
     hipStream_t s = static_cast<hipStream_t>(stream);
-    hipError_t e = attn::launch_win_plain_fwd(bf16, desc->kind == ATTN_CACHE_FP8, p, s);
+    const bool fp8 = desc->kind == ATTN_CACHE_FP8;
+    hipError_t e = is_wide(desc->dtype, desc->d) ? attn::launch_win_fwd(fp8, few_rows(desc), p, s) : attn::launch_win_plain_fwd(bf16, fp8, p, s);
     if (e == hipSuccess && p.splits > 1) e = attn::launch_win_join(bf16, p, s);
     return status_of(e);
 }
