@@ -65,7 +65,7 @@ void set_window(WinParams& p, int32_t window, int32_t sinks, int32_t longest) {
 }
 
 // Keys of a tile of the backward's key owners.
-int key_tile(const attn_win_desc*) { return 32; }
+int key_tile(const attn_win_desc* d) { return is_wide(d->dtype, d->d) ? 64 : 32; }
 
 // A key owner streams window + tile tokens per head, one of sink keys all of them: its tokens are shared out over as many workgroups
 // as make the shares about as long (at most 64, and fewer where there are many sink tiles).
@@ -268,8 +268,13 @@ attn_status attn_win_bwd(const attn_win_desc* desc, const int32_t* lens, const v
     p.delta = static_cast<float*>(workspace);
     p.part_kv = reinterpret_cast<float*>(static_cast<char*>(workspace) + rows_bytes(desc));
     hipStream_t s = static_cast<hipStream_t>(stream);
-    hipError_t e = attn::launch_win_rows(bf16, p, s);
-    if (e == hipSuccess) e = attn::launch_win_plain_bwd(bf16, p, s);
+    hipError_t e;
+    if (is_wide(desc->dtype, desc->d)) {
+        e = attn::launch_win_bwd(p, s);
+    } else {
+        e = attn::launch_win_rows(bf16, p, s);
+        if (e == hipSuccess) e = attn::launch_win_plain_bwd(bf16, p, s);
+    }
     if (e == hipSuccess && p.parts > 1) e = attn::launch_win_sinks(bf16, key_tile(desc), p, s);
     return status_of(e);
 }
