@@ -44,28 +44,22 @@ __device__ __forceinline__ void store8(float* at, int count, f32x8 v) {
     }
 }
 
-__device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
-
-// Which row a lane works on: row u of the new tokens' rows of a sequence, u = (t * kv_heads + kvh) * 2 + (0: K, 1: V).
+// The rows of a token and head that a lane works on, K and V alike: u = t * kv_heads + kvh counts those of a sequence.
 struct CacheRow {
     bool inside, in_page;  // a row of this sequence; that has a place in the pages
-    int t, kvh, which;
-    long at, exp;
+    long given, at, exp;   // its offset among the new tokens' rows, in the pages, among the exponents
 };
-__device__ __forceinline__ CacheRow cache_row(const WinParams& p, const WinSeq& s, int b, long u) {
+__device__ __forceinline__ CacheRow cache_row(const WinParams& p, const WinSeq& s, int b, int row0, long u, long s_n, long s_h) {
     CacheRow r;
-    r.which = (int)(u & 1);
-    const long x = u >> 1;
-    r.t = (int)(x / p.kv_heads);
-    r.kvh = (int)(x - (long)r.t * p.kv_heads);
-    r.inside = r.t < s.nq;
+    const int t = (int)(u / p.kv_heads), kvh = (int)(u - (long)t * p.kv_heads), pos = s.first + t;
+    r.inside = t < s.nq;
     r.in_page = false;
+    r.given = (row0 + (long)t) * s_n + (long)kvh * s_h;
     r.at = r.exp = 0;
-    const int pos = s.first + r.t;
     if (r.inside && pos >= 0) {
         const int page = p.table[(long)b * p.table_stride + (pos >> p.page_shift)];
         if ((unsigned)page < (unsigned)p.num_pages) {
-            const PageRow at = win_page_row(p, page, r.kvh, pos);
+            const PageRow at = win_page_row(p, page, kvh, pos);
             r.at = at.at;
             r.exp = at.exp;
             r.in_page = true;
@@ -73,87 +67,129 @@ __device__ __forceinline__ CacheRow cache_row(const WinParams& p, const WinSeq& 
     }
     return r;
 }
+// Rows per thread: K and V of kRowsPerThread tokens or heads are on the way at a time (one row at a time, the 88 MB of a batch of prompts took 37 us
+// to write and 27 to read, a chain of dependent loads each).
+constexpr int kRowsPerThread = 4;
+
+__device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
+
+// Codes and exponent of a row that `lanes` lanes share.
+__device__ __forceinline__ u32x2 quantise(f32x8 v, int lanes, int& e2) {
+    constexpr uint32_t kInf = 0x7f800000u;
+    uint32_t top = 0;  // magnitudes order as their bits do
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t a = magnitude(v[e]);
+        if (a < kInf) top = a > top ? a : top;
+    }
+    for (int x = 1; x < lanes; x <<= 1) {
+        const uint32_t other = (uint32_t)__shfl_xor((int)top, x, 64);
+        top = other > top ? other : top;
+    }
+    // top = f 2^k with 1 <= f < 2, and 448 = 1.75 2^8
+    e2 = (int)(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
+    e2 = top == 0 ? 0 : e2 < -126 ? -126 : e2;
+    const float scale = __builtin_bit_cast(float, (uint32_t)(127 - e2) << 23);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = magnitude(v[e]) < kInf ? v[e] * scale : __builtin_nanf("");
+    int lo = 0, hi = 0;
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], lo, false);
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], lo, true);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[4], v[5], hi, false);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[6], v[7], hi, true);
+    return u32x2{(uint32_t)lo, (uint32_t)hi};
+}
+__device__ __forceinline__ f32x8 dequantise(u32x2 codes, float scale) {
+    f32x8 v;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[x], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[x], true);
+        v[4 * x] = lo[0] * scale;
+        v[4 * x + 1] = lo[1] * scale;
+        v[4 * x + 2] = hi[0] * scale;
+        v[4 * x + 3] = hi[1] * scale;
+    }
+    return v;
+}
+
+__device__ __forceinline__ int first_row(const WinParams& p, int b) { return p.q_ptr ? min(max(p.q_ptr[b], 0), p.total_q) : b * p.n; }
 
 template <typename T, bool FP8>
 __global__ void __launch_bounds__(kThreads) cache_write_kernel(WinParams p, const void* K, const void* V, long s_n, long s_h, int lanes) {
-    const int b = blockIdx.y;
+    const int b = blockIdx.y, row0 = first_row(p, b), per = kThreads / lanes;
     const WinSeq s = win_sequence(p, b);
-    const long u = ((long)blockIdx.x * kThreads + threadIdx.x) / lanes;
+    const long u0 = (long)blockIdx.x * (per * kRowsPerThread);
+    if (u0 >= (long)s.nq * p.kv_heads) return;
     const int c = 8 * (int)(threadIdx.x & (lanes - 1));
-    const CacheRow r = cache_row(p, s, b, u);
-    const bool mine = r.in_page && c < p.d;
-    f32x8 v = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const int row0 = p.q_ptr ? min(max(p.q_ptr[b], 0), p.total_q) : b * p.n;
-    if (mine) v = load8(static_cast<const T*>(r.which ? V : K) + (row0 + (long)r.t) * s_n + (long)r.kvh * s_h + c, p.d - c);
-    void* pages = const_cast<void*>(r.which ? p.V : p.K);
-    if constexpr (FP8) {
-        constexpr uint32_t kInf = 0x7f800000u;
-        uint32_t top = 0;  // magnitudes order as their bits do
+    CacheRow r[kRowsPerThread];
+    f32x8 k[kRowsPerThread], v[kRowsPerThread];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t a = magnitude(v[e]);
-            if (a < kInf) top = a > top ? a : top;
-        }
-        for (int x = 1; x < lanes; x <<= 1) {
-            const uint32_t other = (uint32_t)__shfl_xor((int)top, x, 64);
-            top = other > top ? other : top;
-        }
-        // top = f 2^k with 1 <= f < 2, and 448 = 1.75 2^8
-        int e2 = (int)(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
-        e2 = top == 0 ? 0 : e2 < -126 ? -126 : e2;
-        const float scale = __builtin_bit_cast(float, (uint32_t)(127 - e2) << 23);
+    for (int x = 0; x < kRowsPerThread; ++x) r[x] = cache_row(p, s, b, row0, u0 + x * per + threadIdx.x / lanes, s_n, s_h);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            v[e] = magnitude(v[e]) < kInf ? v[e] * scale : __builtin_nanf("");
+    for (int x = 0; x < kRowsPerThread; ++x) {
+        k[x] = v[x] = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (r[x].in_page && c < p.d) {
+            k[x] = load8(static_cast<const T*>(K) + r[x].given + c, p.d - c);
+            v[x] = load8(static_cast<const T*>(V) + r[x].given + c, p.d - c);
         }
-        if (mine) {
-            int lo = 0, hi = 0;
-            lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], lo, false);
-            lo = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], lo, true);
-            hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[4], v[5], hi, false);
-            hi = __builtin_amdgcn_cvt_pk_fp8_f32(v[6], v[7], hi, true);
-            *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(pages) + r.at + c) = u32x2{(uint32_t)lo, (uint32_t)hi};
-            if (c == 0) const_cast<uint8_t*>(r.which ? p.V_exp : p.K_exp)[r.exp] = (uint8_t)(e2 + 127);
+    }
+#pragma unroll
+    for (int x = 0; x < kRowsPerThread; ++x) {
+        const bool mine = r[x].in_page && c < p.d;
+        if constexpr (FP8) {
+            int ke, ve;
+            const u32x2 kc = quantise(k[x], lanes, ke), vc = quantise(v[x], lanes, ve);
+            if (mine) {
+                *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(const_cast<void*>(p.K)) + r[x].at + c) = kc;
+                *reinterpret_cast<u32x2*>(static_cast<uint8_t*>(const_cast<void*>(p.V)) + r[x].at + c) = vc;
+                if (c == 0) {
+                    const_cast<uint8_t*>(p.K_exp)[r[x].exp] = (uint8_t)(ke + 127);
+                    const_cast<uint8_t*>(p.V_exp)[r[x].exp] = (uint8_t)(ve + 127);
+                }
+            }
+        } else if (mine) {
+            store8(static_cast<T*>(const_cast<void*>(p.K)) + r[x].at + c, p.d - c, k[x]);
+            store8(static_cast<T*>(const_cast<void*>(p.V)) + r[x].at + c, p.d - c, v[x]);
         }
-    } else if (mine) {
-        store8(static_cast<T*>(pages) + r.at + c, p.d - c, v);
     }
 }
 
 // Rows without a place in the pages (a position in front of the first token, a page that is gone) come back as zeros.
 template <typename T, bool FP8>
 __global__ void __launch_bounds__(kThreads) cache_read_kernel(WinParams p, void* K, void* V, long s_n, long s_h, int lanes) {
-    const int b = blockIdx.y;
+    const int b = blockIdx.y, row0 = first_row(p, b), per = kThreads / lanes;
     const WinSeq s = win_sequence(p, b);
-    const long u = ((long)blockIdx.x * kThreads + threadIdx.x) / lanes;
+    const long u0 = (long)blockIdx.x * (per * kRowsPerThread);
     const int c = 8 * (int)(threadIdx.x & (lanes - 1));
-    const CacheRow r = cache_row(p, s, b, u);
-    if (!r.inside || c >= p.d) return;
-    f32x8 v = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const void* pages = r.which ? p.V : p.K;
-    if (r.in_page) {
-        if constexpr (FP8) {
-            const u32x2 codes = *reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(pages) + r.at + c);
-            const float scale = exp_value((r.which ? p.V_exp : p.K_exp)[r.exp]);
+    if (u0 >= (long)s.nq * p.kv_heads || c >= p.d) return;
+    CacheRow r[kRowsPerThread];
+    f32x8 k[kRowsPerThread], v[kRowsPerThread];
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[x], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[x], true);
-                v[4 * x] = lo[0] * scale;
-                v[4 * x + 1] = lo[1] * scale;
-                v[4 * x + 2] = hi[0] * scale;
-                v[4 * x + 3] = hi[1] * scale;
-            }
+    for (int x = 0; x < kRowsPerThread; ++x) r[x] = cache_row(p, s, b, row0, u0 + x * per + threadIdx.x / lanes, s_n, s_h);
+#pragma unroll
+    for (int x = 0; x < kRowsPerThread; ++x) {
+        k[x] = v[x] = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (!r[x].in_page) continue;
+        if constexpr (FP8) {
+            k[x] = dequantise(*reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(p.K) + r[x].at + c), exp_value(p.K_exp[r[x].exp]));
+            v[x] = dequantise(*reinterpret_cast<const u32x2*>(static_cast<const uint8_t*>(p.V) + r[x].at + c), exp_value(p.V_exp[r[x].exp]));
         } else {
-            v = load8(static_cast<const T*>(pages) + r.at + c, p.d - c);
+            k[x] = load8(static_cast<const T*>(p.K) + r[x].at + c, p.d - c);
+            v[x] = load8(static_cast<const T*>(p.V) + r[x].at + c, p.d - c);
         }
     }
-    const int row0 = p.q_ptr ? min(max(p.q_ptr[b], 0), p.total_q) : b * p.n;
-    store8(static_cast<T*>(r.which ? V : K) + (row0 + (long)r.t) * s_n + (long)r.kvh * s_h + c, p.d - c, v);
+#pragma unroll
+    for (int x = 0; x < kRowsPerThread; ++x) {
+        if (!r[x].inside) continue;
+        store8(static_cast<T*>(K) + r[x].given + c, p.d - c, k[x]);
+        store8(static_cast<T*>(V) + r[x].given + c, p.d - c, v[x]);
+    }
 }
 
 int lanes_of(int d) { return d <= 64 ? 8 : d <= 128 ? 16 : 32; }
 dim3 grid_of(const WinParams& p) {
-    return dim3((unsigned)(((long)p.n * p.kv_heads * 2 * lanes_of(p.d) + kThreads - 1) / kThreads), (unsigned)p.batch);
+    const long rows = kThreads / lanes_of(p.d) * kRowsPerThread;
+    return dim3((unsigned)(((long)p.n * p.kv_heads + rows - 1) / rows), (unsigned)p.batch);
 }
 
 }  // namespace

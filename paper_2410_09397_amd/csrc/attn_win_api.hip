@@ -154,11 +154,16 @@ bool few_rows(const attn_paged_desc* d) { return is_wide(d->dtype, d->d) && (int
 void set_splits(WinParams& p, const attn_paged_desc* d) {
     const bool few = few_rows(d);
     const int64_t rows = few ? 32 : 128, tile = is_wide(d->dtype, d->d) && !few ? 64 : 32;
-    const int64_t blocks = (((int64_t)p.n * p.group + rows - 1) / rows) * p.batch * p.kv_heads;
+    // (total_q bounds the row blocks that have rows where the sequences' new tokens differ in number)
+    const int64_t blocks = std::min((((int64_t)p.n * p.group + rows - 1) / rows) * p.batch, (int64_t)p.total_q * p.group / rows + p.batch) * p.kv_heads;
     const int64_t keys = std::min<int64_t>(p.max_len, (int64_t)p.window + p.n) + p.sinks, tiles = keys / tile + 2;
     p.splits = 1;
     p.chunk = 0x7fffffff;
-    const int64_t want = std::min<int64_t>(64, (few ? 2048 : 1024) / std::max<int64_t>(1, blocks));
+    #ifdef WANT_FEW
+    const int64_t want = std::min<int64_t>(64, (few ? WANT_FEW : WANT_OUT) / std::max<int64_t>(1, blocks));
+#else
+    const int64_t want = std::min<int64_t>(64, (few ? 2048 : 512) / std::max<int64_t>(1, blocks));
+#endif
     if (want > 1 && tiles > 8) {
         p.chunk = (int)std::max<int64_t>(few ? 8 : 4, (tiles + want - 1) / want);
         p.splits = (int)((tiles + p.chunk - 1) / p.chunk);

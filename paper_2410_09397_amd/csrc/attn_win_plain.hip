@@ -235,15 +235,17 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) win_plain_out_ker
             none ? -__builtin_inff() : (m_run + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// The sums of the parts of a row: O = sum_k 2^(m_k - m) O_k / l, l = sum_k 2^(m_k - m) l_k, in the order of the parts.  One wave per
-// row; every wave reads all maxima (at most 64, one per lane), then the O_k of the parts that saw a key.
-template <typename T>
+// The sums of the parts of a row: O = sum_k 2^(m_k - m) O_k / l, l = sum_k 2^(m_k - m) l_k, always in the same order.  WAVES waves per row; every
+// one reads all m_k, l_k (at most 64, one per lane); 16 to 64 lanes share a part's O_k, so that a row has 1 to 16 parts on the way
+// at a time.  Parts that saw no key have no O_k.  (One wave per row and one part at a time: 21 us for 32 rows of 63 parts, now 5.)
+template <typename T, int WAVES>
 __global__ void __launch_bounds__(kThreads) win_join_kernel(WinParams p) {
-    const int lane = threadIdx.x & 63, b = blockIdx.y;
+    __shared__ f32x4 meet[kThreads];
+    const int lane = threadIdx.x & 63, in_row = threadIdx.x % (64 * WAVES), b = blockIdx.y;
     const WinSeq s = win_sequence(p, b);
-    const long f = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const long f = ((long)blockIdx.x * kThreads + threadIdx.x) / (64 * WAVES);
     const int t = (int)(f / p.heads), head = (int)(f % p.heads);
-    if (t >= s.nq) return;
+    if (t >= s.nq) return;  // (of all waves of a row)
     const long row = s.lse_base + (long)t * p.heads + head;
     const float* ml = p.part_ml + row * p.splits * 2;
     const bool mine = lane < p.splits;
@@ -252,22 +254,42 @@ __global__ void __launch_bounds__(kThreads) win_join_kernel(WinParams p) {
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) m = __builtin_elementwise_maximum(m, __shfl_xor(m, x, 64));
     const float m_use = m == -__builtin_inff() ? 0.f : m;
-    const float f_k = __builtin_amdgcn_exp2f(m_k - m_use);
+    const float f_k = l_k != 0.f ? __builtin_amdgcn_exp2f(m_k - m_use) : 0.f;  // (NaN: not 0)
     float l = f_k * l_k;
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) l += __shfl_xor(l, x, 64);
     const bool none = l == 0.f;
     const float inv = none ? 0.f : 1.f / l;
-    const unsigned long parts = __builtin_amdgcn_ballot_w64(l_k > 0.f || l_k != l_k);
+    const int lanes = p.d <= 64 ? 16 : p.d <= 128 ? 32 : 64, slots = 64 * WAVES / lanes, slot = in_row / lanes, c = 4 * (in_row % lanes);
     const float* src = p.part_o + row * p.splits * p.d;
-    T* dst = static_cast<T*>(p.O) + s.q_base + (long)head * p.q_h + (long)t * p.q_n;
-    const int c = 4 * lane;  // d <= 256
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (unsigned long todo = parts; todo; todo &= todo - 1) {
-        const int k = __builtin_ctzl(todo);
-        const float weight = __shfl(f_k, k, 64);  // (by all lanes)
-        if (c < p.d) sum += load4(src + (long)k * p.d, c, p.d) * weight;
+    constexpr int kAhead = 4;  // parts per lane on the way
+    for (int k0 = 0; k0 < p.splits; k0 += kAhead * slots) {
+        f32x4 part[kAhead];
+        float weight[kAhead];
+#pragma unroll
+        for (int x = 0; x < kAhead; ++x) {
+            const int k = k0 + x * slots + slot, kc = min(k, p.splits - 1);
+            weight[x] = __shfl(f_k, kc, 64);  // (by all lanes)
+            if (k >= p.splits) weight[x] = 0.f;
+            part[x] = load4(src + (long)kc * p.d, c, p.d);
+        }
+#pragma unroll
+        for (int x = 0; x < kAhead; ++x)
+            if (weight[x] != 0.f) sum += part[x] * weight[x];
     }
+    for (int x = lanes; x < 64; x <<= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], x, 64);
+    if constexpr (WAVES > 1) {
+        meet[threadIdx.x] = sum;
+        __syncthreads();
+        if (in_row >= 64) return;
+#pragma unroll
+        for (int x = 1; x < WAVES; ++x) sum += meet[threadIdx.x + 64 * x];
+    }
+    if (lane >= lanes) return;
+    T* dst = static_cast<T*>(p.O) + s.q_base + (long)head * p.q_h + (long)t * p.q_n;
     if (c < p.d) store4(dst, c, p.d, sum * inv);
     if (lane == 0) p.LSE[row] = none ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
@@ -515,9 +537,12 @@ hipError_t launch_win_plain_bwd(bool is_bf16, const WinParams& p, hipStream_t st
     return is_bf16 ? bwd<__bf16>(p, stream) : bwd<float>(p, stream);
 }
 hipError_t launch_win_join(bool is_bf16, const WinParams& p, hipStream_t stream) {
-    const dim3 grid((unsigned)(((long)p.n * p.heads + 3) / 4), (unsigned)p.batch);
-    if (is_bf16) hipLaunchKernelGGL(win_join_kernel<__bf16>, grid, dim3(kThreads), 0, stream, p);
-    else hipLaunchKernelGGL(win_join_kernel<float>, grid, dim3(kThreads), 0, stream, p);
+    // four waves for a row that has many parts
+    const int waves = p.splits > 8 ? 4 : 1;
+    const dim3 grid((unsigned)(((long)p.n * p.heads * waves + 3) / 4), (unsigned)p.batch);
+    auto fn = is_bf16 ? (waves == 4 ? win_join_kernel<__bf16, 4> : win_join_kernel<__bf16, 1>)
+                      : (waves == 4 ? win_join_kernel<float, 4> : win_join_kernel<float, 1>);
+    hipLaunchKernelGGL(fn, grid, dim3(kThreads), 0, stream, p);
     return hipGetLastError();
 }
 hipError_t launch_win_rows(bool is_bf16, const WinParams& p, hipStream_t stream) {
