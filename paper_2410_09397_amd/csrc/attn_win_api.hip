@@ -130,7 +130,7 @@ attn_status check_paged(const attn_paged_desc* d) {
     if (d->batch > 65535 || d->max_len > kMostTokens) return ATTN_ERR_UNSUPPORTED;
     if (d->heads == 0) return ATTN_OK;
     const int64_t rows = (int64_t)d->max_q * (d->heads / d->kv_heads);
-    if (rows > kMostTokens || ((rows + 31) / 32) * d->batch * d->kv_heads > kMostGroups || ((int64_t)d->max_q * d->heads + 3) / 4 * d->batch > kMostGroups ||
+    if (rows > kMostTokens || ((rows + 15) / 16) * d->batch * d->kv_heads > kMostGroups || ((int64_t)d->max_q * d->heads + 3) / 4 * d->batch > kMostGroups ||
         (int64_t)d->max_q * d->kv_heads / 4 * d->batch > kMostGroups)
         return ATTN_ERR_UNSUPPORTED;
     return ATTN_OK;
@@ -147,13 +147,16 @@ attn_status check_cache(const attn_paged_desc* d, const attn_cache* c) {
     return ATTN_OK;
 }
 
-// Whether the rows of a (sequence, key head) are taken 32 at a time, by workgroups whose waves share the keys out among themselves.
-bool few_rows(const attn_paged_desc* d) { return is_wide(d->dtype, d->d) && (int64_t)d->max_q * (d->heads / d->kv_heads) <= 64; }
+// Rows of a workgroup of the paged forward: see attn_win_fwd.hip.
+int paged_rows(const attn_paged_desc* d) {
+    const int64_t rows = (int64_t)d->max_q * (d->heads / d->kv_heads);
+    return !is_wide(d->dtype, d->d) || rows > 64 ? 128 : rows > 16 ? 32 : 16;
+}
 
 // How the keys of a row block are shared out: with fewer row blocks than the chip has places for, a workgroup takes `chunk` tiles.
 void set_splits(WinParams& p, const attn_paged_desc* d) {
-    const bool few = few_rows(d);
-    const int64_t rows = few ? 32 : 128, tile = is_wide(d->dtype, d->d) && !few ? 64 : 32;
+    const int64_t rows = paged_rows(d), tile = is_wide(d->dtype, d->d) && rows == 128 ? 64 : 32;
+    const bool few = rows < 128;
     // (total_q bounds the row blocks that have rows where the sequences' new tokens differ in number)
     const int64_t blocks = std::min((((int64_t)p.n * p.group + rows - 1) / rows) * p.batch, (int64_t)p.total_q * p.group / rows + p.batch) * p.kv_heads;
     const int64_t keys = std::min<int64_t>(p.max_len, (int64_t)p.window + p.n) + p.sinks, tiles = keys / tile + 2;
@@ -245,7 +248,7 @@ attn_status attn_win_fwd(const attn_win_desc* desc, const int32_t* lens, const v
     p.O = O;
     p.LSE = LSE;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return status_of(is_wide(desc->dtype, desc->d) ? attn::launch_win_fwd(false, false, p, s) : attn::launch_win_plain_fwd(bf16, false, p, s));
+    return status_of(is_wide(desc->dtype, desc->d) ? attn::launch_win_fwd(false, 128, p, s) : attn::launch_win_plain_fwd(bf16, false, p, s));
 }
 
 attn_status attn_win_bwd(const attn_win_desc* desc, const int32_t* lens, const void* Q, const void* K, const void* V, const void* O,
@@ -332,7 +335,7 @@ attn_status attn_paged_fwd(const attn_paged_desc* desc, const attn_cache* cache,
     p.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + part_ml_bytes(desc, p));
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool fp8 = desc->kind == ATTN_CACHE_FP8;
-    hipError_t e = is_wide(desc->dtype, desc->d) ? attn::launch_win_fwd(fp8, few_rows(desc), p, s) : attn::launch_win_plain_fwd(bf16, fp8, p, s);
+    hipError_t e = is_wide(desc->dtype, desc->d) ? attn::launch_win_fwd(fp8, paged_rows(desc), p, s) : attn::launch_win_plain_fwd(bf16, fp8, p, s);
     if (e == hipSuccess && p.splits > 1) e = attn::launch_win_join(bf16, p, s);
     return status_of(e);
 }

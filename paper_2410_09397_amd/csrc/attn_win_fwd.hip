@@ -3,8 +3,9 @@
 //   win_out_kernel  128 rows per workgroup (rows r = t * group + head of the group: see attn_window.hpp), 64-key tiles shared by its
 //                   four waves.  Many rows: a prompt, a chunk, training
 //   win_few_kernel  32 rows per workgroup, whose waves take 32-key tiles in turn, each with LDS and softmax state of its own, and meet at
-//                   the end.  Few rows: single tokens, where the time is that of the keys' way from memory
-// Either can share the keys of a row block out over workgroups (p.splits), whose sums win_join_kernel brings together.
+//                   the end.  A few tokens of a sequence
+//   win_one_kernel  the same with 16 rows.  Single tokens, where the time is that of the keys' way from memory
+// Each can share the keys of a row block out over workgroups (p.splits), whose sums win_join_kernel brings together.
 //
 // Per tile: S^T = K Q^T (lane <-> query), P^T = exp2(S^T - m) with a running reference m, O^T += V^T P^T, with V^T from transposing LDS
 // reads and P^T straight from the accumulators.  P is rounded to bf16 for the second product (2^-9 of each weight; O is rounded as far
@@ -335,6 +336,46 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_out_kernel(Win
     }
 }
 
+// Rows r0 .. r1 of a workgroup from its waves' sums in LDS ([wave][ROWS][D + 4] fp32 and [wave][ROWS][m, l]): to O and LSE, or to the parts.
+template <int D, int NW, int ROWS>
+__device__ __forceinline__ void few_store(const WinParams& p, const WinSeq& s, const char* smem, const float* ml, int kvh, int r0, int r1) {
+    constexpr int kPitch = D * 4 + 16;
+    const int tid = threadIdx.x;
+    constexpr int kLanes = D / 4;  // threads per row
+    for (int row = tid / kLanes; row < ROWS; row += 64 * NW / kLanes) {
+        const int r = r0 + row, c = 4 * (tid % kLanes);
+        if (r > r1) break;
+        float m = -__builtin_inff();
+#pragma unroll
+        for (int x = 0; x < NW; ++x) m = __builtin_elementwise_maximum(m, ml[(x * ROWS + row) * 2]);
+        const float m_use = m == -__builtin_inff() ? 0.f : m;
+        float sum_l = 0.f;
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < NW; ++x) {
+            const float f = __builtin_amdgcn_exp2f(ml[(x * ROWS + row) * 2] - m_use);
+            sum_l += f * ml[(x * ROWS + row) * 2 + 1];
+            sum += *reinterpret_cast<const f32x4*>(smem + (x * ROWS + row) * kPitch + c * 4) * f;
+        }
+        int rt, rh;
+        win_place(p, kvh, r, rt, rh);
+        const long at = s.lse_base + (long)rt * p.heads + rh;
+        const bool some = sum_l != 0.f;
+        if (p.splits > 1) {
+            if (c == 0) {
+                p.part_ml[(at * p.splits + blockIdx.y) * 2] = m;
+                p.part_ml[(at * p.splits + blockIdx.y) * 2 + 1] = sum_l;
+            }
+            if (some) *reinterpret_cast<f32x4*>(p.part_o + (at * p.splits + blockIdx.y) * D + c) = sum;
+        } else {
+            const float inv = some ? 1.f / sum_l : 0.f;
+            if (c == 0) p.LSE[at] = some ? (m + __builtin_amdgcn_logf(sum_l)) * kLn2 : -__builtin_inff();
+            *reinterpret_cast<u32x2*>(static_cast<__bf16*>(p.O) + s.q_base + (long)rh * p.q_h + (long)rt * p.q_n + c) =
+                u32x2{pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
+        }
+    }
+}
+
 // -------------------------------------------------------------------------------------------------------- few rows
 template <int D, int SRC>
 constexpr int kFewWaves = D == 256 && SRC == kPages ? 2 : 4;
@@ -469,39 +510,184 @@ __global__ void __launch_bounds__((64 * kFewWaves<D, SRC>), (D == 256 ? 1 : 2)) 
             *reinterpret_cast<f32x4*>(smem + (w * 32 + l32) * kPitch + (32 * mt + 8 * g + 4 * h) * 4) =
                 f32x4{acc.o[mt][4 * g], acc.o[mt][4 * g + 1], acc.o[mt][4 * g + 2], acc.o[mt][4 * g + 3]};
     __syncthreads();
-    constexpr int kLanes = D / 4;  // threads per row
-    for (int row = tid / kLanes; row < 32; row += 64 * NW / kLanes) {
-        const int r = r0 + row, c = 4 * (tid % kLanes);
-        if (r > r1) break;
-        float m = -__builtin_inff();
+    few_store<D, NW, 32>(p, s, smem, ml, kvh, r0, r1);
+}
+
+// ---------------------------------------------------------------------------------------------------------- a row tile
+// Single tokens: at most 16 rows of a (sequence, key head), on 16x16x32 products, with half the registers, half the matrix cycles and half the
+// softmax arithmetic of 32 rows.  K goes from memory straight into operands: lane (l % 16, q = l / 16) reads 16 bytes of key l % 16, and
+// 64 bytes of each of 16 rows make an instruction.  The order of d inside a product is free as long as Q has the same:
+//   bf16   product ks: columns 32 ks + 8 q ..             codes   products 2 kk, 2 kk + 1: columns 64 kk + 16 q .., + 8 ..
+// V goes through 32 rows of LDS that only this wave uses, for the transposing reads.  The next tile is in registers or on its way to them while
+// this one is worked on.  C: column l % 16 (query), register i of group g <-> key 16 g + 4 q + i, and as an operand with k = 4 g + i.
+template <int D, int SRC>
+constexpr int kOneLds = 4 * (32 * D * 2 > 16 * (D * 4 + 16) + 128 ? 32 * D * 2 : 16 * (D * 4 + 16) + 128);
+// workgroups of four waves on a CU that the registers allow
+template <int D, int SRC>
+constexpr int kOnePerCu = D == 64 ? 4 : D == 128 ? 3 : SRC == kCodes ? 2 : 1;
+
+template <int D, int SRC>
+__global__ void __launch_bounds__(kThreads, (kOnePerCu<D, SRC>)) win_one_kernel(WinParams p, int row_blocks) {
+    constexpr int NW = 4, MT = D / 16, KS = D / 32, kTile = 32 * D * 2;
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, l16 = lane & 15;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int bk = blockIdx.x / row_blocks, b = bk / p.kv_heads, kvh = bk % p.kv_heads;
+    const WinSeq s = win_sequence(p, b);
+    const int rows = s.nq * p.group, r0 = (blockIdx.x % row_blocks) * 16;
+    if (r0 >= rows) return;
+    const int r1 = min(r0 + 15, rows - 1);
+    int t, head;
+    win_place(p, kvh, min(r0 + l16, r1), t, head);
+    const int t_lo = s.first + (int)((unsigned)r0 / (unsigned)p.group), t_hi = s.first + (int)((unsigned)r1 / (unsigned)p.group);
+    LaneBounds see;
+    see.init(p, s.first + t, s.len);
+    WinTiles<32> tiles;
+    tiles.init(p, s.len, t_lo, t_hi);
+    const int it0 = blockIdx.y * p.chunk, it1 = (int)min((long)tiles.count, (long)it0 + p.chunk);
+
+    PageWindow pages;
+    pages.init();
+    // bf16: kr[g * KS + ks], vr[x]: 16 bytes of rows x * 64 / (D / 8) ..   codes: kr[g * KS / 2 + kk], with the scales of the rows
+    constexpr int kK = SRC == kCodes ? KS : 2 * KS, kV = SRC == kCodes ? D / 32 : D / 16, kChunksPerRow = SRC == kCodes ? D / 16 : D / 8;
+    u32x4 kr[kK], vr[kV];
+    uint8_t ke[2], ve[SRC == kCodes ? kV : 1];
+    auto request = [&](int it) {
+        constexpr int es = SRC == kCodes ? 1 : 2;
+        const int j0 = tiles.start(it);
+        pages.cover(p, b, tiles.row(p, j0), tiles.row(p, j0 + 31), tiles.end, lane);
 #pragma unroll
-        for (int x = 0; x < NW; ++x) m = __builtin_elementwise_maximum(m, ml[(x * 32 + row) * 2]);
-        const float m_use = m == -__builtin_inff() ? 0.f : m;
-        float sum_l = 0.f;
-        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        for (int g = 0; g < 2; ++g) {
+            const int j = tiles.row(p, j0 + 16 * g + l16);
+            const PageRow r = win_page_row(p, pages.page(p, j), kvh, j);
+            const char* src = static_cast<const char*>(p.K) + r.at * es + 16 * q;
 #pragma unroll
-        for (int x = 0; x < NW; ++x) {
-            const float f = __builtin_amdgcn_exp2f(ml[(x * 32 + row) * 2] - m_use);
-            sum_l += f * ml[(x * 32 + row) * 2 + 1];
-            sum += *reinterpret_cast<const f32x4*>(smem + (x * 32 + row) * kPitch + c * 4) * f;
+            for (int x = 0; x < kK / 2; ++x) kr[g * (kK / 2) + x] = *reinterpret_cast<const u32x4*>(src + 64 * x);
+            if constexpr (SRC == kCodes) ke[g] = p.K_exp[r.exp];
         }
-        int rt, rh;
-        win_place(p, kvh, r, rt, rh);
-        const long at = s.lse_base + (long)rt * p.heads + rh;
-        const bool some = sum_l != 0.f;
-        if (p.splits > 1) {
-            if (c == 0) {
-                p.part_ml[(at * p.splits + blockIdx.y) * 2] = m;
-                p.part_ml[(at * p.splits + blockIdx.y) * 2 + 1] = sum_l;
+#pragma unroll
+        for (int x = 0; x < kV; ++x) {
+            const int idx = x * 64 + lane, j = tiles.row(p, j0 + idx / kChunksPerRow);
+            const PageRow r = win_page_row(p, pages.page(p, j), kvh, j);
+            vr[x] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.V) + r.at * es + 16 * (idx % kChunksPerRow));
+            if constexpr (SRC == kCodes) ve[x] = p.V_exp[r.exp];
+        }
+    };
+    int it = it0 + w;
+    if (it < it1) request(it);
+
+    bf16x8 qf[KS];
+    const __bf16* qrow = static_cast<const __bf16*>(p.Q) + s.q_base + (long)head * p.q_h + (long)t * p.q_n;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+        qf[ks] = *reinterpret_cast<const bf16x8*>(qrow + (SRC == kCodes ? 64 * (ks >> 1) + 16 * q + 8 * (ks & 1) : 32 * ks + 8 * q));
+    win_sign(p.scale, qf);
+    const float cs = win_scale(p.scale);
+    f32x4 o[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) o[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -__builtin_inff(), l = 0.f;  // l: this lane's quarter of the sum
+    char* mine = smem + w * kTile;
+    // column 16 mt + l % 16 of keys 4 q .. + 3 (and 16 further): see load_frag_t
+    const int tr_row = 4 * q + (l16 >> 2), tr = tile_off<D>(tr_row, (l16 & 3) >> 1) + ((l16 & 1) << 3);
+
+    for (; it < it1; it += NW) {
+        const int j0 = tiles.start(it);
+        f32x4 st[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+#pragma unroll
+            for (int x = 0; x < kK / 2; ++x) {
+                const u32x4 v = kr[g * (kK / 2) + x];
+                if constexpr (SRC == kCodes) {
+                    const float scale = exp_value(ke[g]);
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        u32x4 a;
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 * half + y], scale, false);
+                            const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 * half + y], scale, true);
+                            a[2 * y] = __builtin_bit_cast(uint32_t, lo);
+                            a[2 * y + 1] = __builtin_bit_cast(uint32_t, hi);
+                        }
+                        st[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), qf[2 * x + half], st[g], 0, 0, 0);
+                    }
+                } else {
+                    st[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), qf[x], st[g], 0, 0, 0);
+                }
             }
-            if (some) *reinterpret_cast<f32x4*>(p.part_o + (at * p.splits + blockIdx.y) * D + c) = sum;
-        } else {
-            const float inv = some ? 1.f / sum_l : 0.f;
-            if (c == 0) p.LSE[at] = some ? (m + __builtin_amdgcn_logf(sum_l)) * kLn2 : -__builtin_inff();
-            *reinterpret_cast<u32x2*>(static_cast<__bf16*>(p.O) + s.q_base + (long)rh * p.q_h + (long)rt * p.q_n + c) =
-                u32x2{pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
         }
+#pragma unroll
+        for (int x = 0; x < kV; ++x) {
+            const int idx = x * 64 + lane, row = idx / kChunksPerRow, c = idx % kChunksPerRow;
+            if constexpr (SRC == kCodes) {
+                CodeChunk chunk;
+                chunk.codes = vr[x];
+                chunk.scale = exp_value(ve[x]);
+                chunk.to_lds(mine + tile_off<D>(row, 2 * c), mine + tile_off<D>(row, 2 * c + 1));
+            } else {
+                *reinterpret_cast<u32x4*>(mine + tile_off<D>(row, c)) = vr[x];
+            }
+        }
+        wave_exchange();
+        if (it + NW < it1) request(it + NW);
+        const bool all = j0 + 31 <= t_lo && t_hi < s.len && (t_hi - j0 < p.window || j0 + 31 < p.sinks);
+        if (!all) {
+            const int j = j0 + 4 * q, hi = see.hi - j, lo = see.lo - j, sink = p.sinks - j;
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int c = 16 * g + i;
+                    st[g][i] = c <= hi && (c >= lo || c < sink) ? st[g][i] : -__builtin_inff();
+                }
+        }
+        float mx = max3(max3(st[0][0], st[0][1], st[0][2]), max3(st[0][3], st[1][0], st[1][1]), __builtin_elementwise_maximum(st[1][2], st[1][3]));
+        constexpr float kSlack = 8.f;  // see WinRows
+        if (__builtin_amdgcn_ballot_w64(mx * cs > m + kSlack) != 0) {
+            mx = __builtin_elementwise_maximum(mx, __shfl_xor(mx, 16, 64));
+            mx = __builtin_elementwise_maximum(mx, __shfl_xor(mx, 32, 64));
+            const float cand = mx * cs, m_new = cand > m + kSlack ? cand : m;
+            const float alpha = __builtin_amdgcn_exp2f(m - (m_new == -__builtin_inff() ? 0.f : m_new));
+            l *= alpha;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) o[mt] *= alpha;
+            m = m_new;
+        }
+        const float m_use = m == -__builtin_inff() ? 0.f : m;
+        float f[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            f[x] = __builtin_amdgcn_exp2f(fmaf(st[x >> 2][x & 3], cs, -m_use));
+            l += f[x];
+        }
+        const u32x4 pb = {pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7])};
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            const int at = (tr ^ ((mt & 7) << 5)) + 256 * (mt >> 3);
+            const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((i16x4 ATTN_LDS*)(mine + at));
+            const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((i16x4 ATTN_LDS*)(mine + at + 16 * D * 2));
+            typedef short i16x8 __attribute__((ext_vector_type(8)));
+            const i16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            o[mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, pb), o[mt], 0, 0, 0);
+        }
+        wave_exchange();
     }
+
+    constexpr int kPitch = D * 4 + 16;  // the waves meet: [wave][16 rows][D + 4] fp32, then [wave][16][m, l]
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    __syncthreads();
+    float* ml = reinterpret_cast<float*>(smem + NW * 16 * kPitch);
+    if (q == 0) {
+        ml[(w * 16 + l16) * 2] = m;
+        ml[(w * 16 + l16) * 2 + 1] = l;
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) *reinterpret_cast<f32x4*>(smem + (w * 16 + l16) * kPitch + (16 * mt + 4 * q) * 4) = o[mt];
+    __syncthreads();
+    few_store<D, NW, 16>(p, s, smem, ml, kvh, r0, r1);
 }
 
 template <int D, int SRC>
@@ -523,20 +709,31 @@ hipError_t few(const WinParams& p, hipStream_t stream) {
                        stream, p, blocks);
     return hipGetLastError();
 }
+template <int D, int SRC>
+hipError_t one(const WinParams& p, hipStream_t stream) {
+    constexpr int lds = kOneLds<D, SRC>;
+    const hipError_t e = allow_lds(win_one_kernel<D, SRC>, lds);
+    if (e != hipSuccess) return e;
+    const int blocks = (int)(((long)p.n * p.group + 15) / 16);
+    hipLaunchKernelGGL((win_one_kernel<D, SRC>), dim3((unsigned)((long)blocks * p.batch * p.kv_heads), (unsigned)p.splits), dim3(kThreads), lds, stream, p,
+                       blocks);
+    return hipGetLastError();
+}
 template <int D>
-hipError_t launch(bool fp8, bool few_rows, const WinParams& p, hipStream_t stream) {
+hipError_t launch(bool fp8, int rows, const WinParams& p, hipStream_t stream) {
     if (!p.table) return out<D, kTensors>(p, stream);
-    if (few_rows) return fp8 ? few<D, kCodes>(p, stream) : few<D, kPages>(p, stream);
+    if (rows == 16) return fp8 ? one<D, kCodes>(p, stream) : one<D, kPages>(p, stream);
+    if (rows == 32) return fp8 ? few<D, kCodes>(p, stream) : few<D, kPages>(p, stream);
     return fp8 ? out<D, kCodes>(p, stream) : out<D, kPages>(p, stream);
 }
 
 }  // namespace
 
-hipError_t launch_win_fwd(bool fp8, bool few_rows, const WinParams& p, hipStream_t stream) {
+hipError_t launch_win_fwd(bool fp8, int rows, const WinParams& p, hipStream_t stream) {
     switch (p.d) {
-        case 64: return launch<64>(fp8, few_rows, p, stream);
-        case 128: return launch<128>(fp8, few_rows, p, stream);
-        case 256: return launch<256>(fp8, few_rows, p, stream);
+        case 64: return launch<64>(fp8, rows, p, stream);
+        case 128: return launch<128>(fp8, rows, p, stream);
+        case 256: return launch<256>(fp8, rows, p, stream);
         default: return hipErrorInvalidValue;
     }
 }

@@ -112,7 +112,8 @@ __device__ __forceinline__ float exp_value(uint8_t e) { return __builtin_bit_cas
 // ------------------------------------------------------------------------------------------------------------- host
 // is_bf16: the type of Q, O and of tensors, and of pages that are not quantised (fp8).  The arguments have been checked.
 hipError_t launch_win_plain_fwd(bool is_bf16, bool fp8, const WinParams& p, hipStream_t stream);
-hipError_t launch_win_fwd(bool fp8, bool few_rows, const WinParams& p, hipStream_t stream);  // bf16, d in {64, 128, 256}
+// bf16, d in {64, 128, 256}; rows of a workgroup: 16, 32 (pages), 128
+hipError_t launch_win_fwd(bool fp8, int rows, const WinParams& p, hipStream_t stream);
 hipError_t launch_win_bwd(const WinParams& p, hipStream_t stream);                                // the same; forms delta itself
 hipError_t launch_win_plain_bwd(bool is_bf16, const WinParams& p, hipStream_t stream);
 hipError_t launch_win_join(bool is_bf16, const WinParams& p, hipStream_t stream);
