@@ -7,6 +7,7 @@ is missing, loading raises.
 """
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -92,7 +93,7 @@ def lib():
         L.attn_blockmask_validate.argtypes = [ctypes.c_int32] * 4 + [i32p] * 4
         L.attn_mfma_ceiling.restype = ctypes.c_int
         L.attn_mfma_ceiling.argtypes = [ctypes.c_int32, ctypes.c_int32, vp, ctypes.POINTER(ctypes.c_double), vp]
-        wp, pp, cp = ctypes.POINTER(attn_win_desc), ctypes.POINTER(attn_paged_desc), ctypes.POINTER(attn_cache)
+        wp = pp = cp = vp  # descriptors as packed bytes or as the structures above
         L.attn_win_workspace_bytes.restype = L.attn_paged_workspace_bytes.restype = ctypes.c_size_t
         L.attn_win_workspace_bytes.argtypes = [wp]
         L.attn_paged_workspace_bytes.argtypes = [pp]
@@ -326,22 +327,29 @@ def attn_mfma_ceiling(iters, operands=0, stream=None):
 
 
 # ------------------------------------------------------------------------- windowed attention with shared heads
-def _dtype(x):
+# A call of a few tokens takes 6 us on the GPU, so its marshalling is kept short as well: descriptors are packed as bytes (the layouts of attn_win_desc,
+# attn_paged_desc and attn_cache; half the time of filling the structures), and every tensor is asked once for its shape, strides and device.
+_WIN_DESC = struct.Struct("@5if4i6q")
+_PAGED_DESC = struct.Struct("@10if5i8q")
+_CACHE = struct.Struct("@7P")
+
+
+def _dtype(dtype):
     import torch
-    if x.dtype is torch.bfloat16:
+    if dtype is torch.bfloat16:
         return ATTN_BF16
-    if x.dtype is torch.float32:
+    if dtype is torch.float32:
         return ATTN_F32
-    raise ValueError("expected a bfloat16 or float32 tensor, got %s" % x.dtype)
+    raise ValueError("expected bfloat16 or float32 tensors, got %s" % dtype)
 
 
-def _int32(name, t, shape, device):
-    """Device address of an int32 tensor that the kernels index."""
-    import torch
+def _int32(name, t, count, device):
+    """Device address of an int32 vector that the kernels index."""
     if t is None:
         return None
-    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
-        raise ValueError("%s must be a contiguous int32 tensor of shape %s on the device of the other tensors" % (name, shape))
+    import torch
+    if t.dtype is not torch.int32 or t.shape != (count,) or not t.is_contiguous() or t.device != device:
+        raise ValueError("%s must be a contiguous int32 tensor of %d entries on the device of the other tensors" % (name, count))
     return t.data_ptr()
 
 
@@ -355,32 +363,41 @@ def _scratch(nbytes, device, stream):
 
 
 def _win_desc(Q, K, scale, window, sinks):
-    if Q.dim() != 4 or K.dim() != 4 or Q.stride(3) != 1 or K.stride(3) != 1:
-        raise ValueError("expected [batch, heads, n, d] tensors with unit stride along d")
-    b, h, n, d = Q.shape
-    if (K.shape[0], K.shape[2], K.shape[3]) != (b, n, d) or K.dtype != Q.dtype or K.device != Q.device:
+    if Q.dim() != 4 or K.dim() != 4:
+        raise ValueError("expected [batch, heads, n, d] tensors")
+    (b, h, n, d), (kb, kh, kn, kd), dtype = Q.shape, K.shape, Q.dtype
+    (qsb, qsh, qsn, qsd), (ksb, ksh, ksn, ksd) = Q.stride(), K.stride()
+    if qsd != 1 or ksd != 1:
+        raise ValueError("expected unit stride along d")
+    if (kb, kn, kd) != (b, n, d) or K.dtype != dtype or K.device != Q.device:
         raise ValueError("Q and K must share batch, n, d, dtype and device")
-    return attn_win_desc(b, h, K.shape[1], n, d, float(scale), int(window), int(sinks), _dtype(Q), 0, *Q.stride()[:3], *K.stride()[:3])
+    return _WIN_DESC.pack(b, h, kh, n, d, scale, window, sinks, _dtype(dtype), 0, qsb, qsh, qsn, ksb, ksh, ksn)
+
+
+def _as_argument(desc):
+    return desc if isinstance(desc, bytes) else ctypes.byref(desc)
 
 
 def attn_win_workspace_bytes(desc):
-    return lib().attn_win_workspace_bytes(ctypes.byref(desc))
+    return lib().attn_win_workspace_bytes(_as_argument(desc))
 
 
 def attn_win_fwd(Q, K, V, scale, window=0, sinks=0, lens=None, stream=None, out=None):
     """O, LSE of causal attention in which a query sees itself, the window - 1 keys in front of it (window = 0: all of them) and the
     first `sinks` keys.  Q: [batch, heads, n, d]; K, V: [batch, kv_heads, n, d], heads a multiple of kv_heads; lens: the
     sequences' lengths (int32 [batch]), rows from there on are padding."""
-    import torch
-    _same_layout(K, V)
     desc = _win_desc(Q, K, scale, window, sinks)
+    _same_layout(K, V)
     if out is None:
-        out = torch.empty_like(Q), torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device)
-    O, LSE = out
-    _same_layout(Q, O)
-    _check_lse(LSE, Q)
-    st = lib().attn_win_fwd(ctypes.byref(desc), _int32("lens", lens, (Q.shape[0],), Q.device), Q.data_ptr(), K.data_ptr(), V.data_ptr(),
-                            O.data_ptr(), LSE.data_ptr(), _stream(stream))
+        import torch
+        O, LSE = torch.empty_like(Q), torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device)
+        _same_layout(Q, O)  # (of an expanded Q there is no dense tensor of the same strides)
+    else:
+        O, LSE = out
+        _same_layout(Q, O)
+        _check_lse(LSE, Q)
+    st = lib().attn_win_fwd(desc, _int32("lens", lens, Q.shape[0], Q.device), Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(),
+                            LSE.data_ptr(), _stream(stream))
     if st != ATTN_OK:
         raise AttnError(st, "attn_win_fwd")
     return O, LSE
@@ -394,20 +411,19 @@ def _check_lse(LSE, Q):
 
 def attn_win_bwd(Q, K, V, O, dO, LSE, scale, window=0, sinks=0, lens=None, stream=None, out=None, workspace=None):
     """dQ, dK, dV of attn_win_fwd from its O and LSE; dK and dV are sums over the query heads that share a key head."""
-    import torch
-    _same_layout(K, V)
     desc = _win_desc(Q, K, scale, window, sinks)
     if out is None:
+        import torch
         out = torch.empty_like(Q), torch.empty_like(K), torch.empty_like(K)
     dQ, dK, dV = out
     _same_layout(Q, O, dO, dQ)
-    _same_layout(K, dK, dV)
+    _same_layout(K, V, dK, dV)
     _check_lse(LSE, Q)
     if workspace is None:
         workspace = _scratch(max(attn_win_workspace_bytes(desc), 256), Q.device, stream)
-    st = lib().attn_win_bwd(ctypes.byref(desc), _int32("lens", lens, (Q.shape[0],), Q.device), Q.data_ptr(), K.data_ptr(), V.data_ptr(),
-                            O.data_ptr(), dO.data_ptr(), LSE.data_ptr(), dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(),
-                            workspace.data_ptr(), workspace.numel(), _stream(stream))
+    st = lib().attn_win_bwd(desc, _int32("lens", lens, Q.shape[0], Q.device), Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(),
+                            dO.data_ptr(), LSE.data_ptr(), dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), workspace.data_ptr(),
+                            workspace.numel(), _stream(stream))
     if st != ATTN_OK:
         raise AttnError(st, "attn_win_bwd")
     return dQ, dK, dV
@@ -424,37 +440,41 @@ def attn_cache_pages(num_pages, kv_heads, page_size, d, dtype, device="cuda"):
     return K, V, *(torch.full((num_pages, kv_heads, page_size), 127, dtype=torch.uint8, device=device) for _ in range(2))
 
 
-def _paged(name, x, heads_of, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp, scale=1.0, window=0, sinks=0):
-    """The descriptor and the cache structure of a call whose rows are x: [total, heads, d] (heads_of "q": the queries' heads)."""
+def _paged(name, x, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp, kv_rows, scale=1.0, window=0, sinks=0):
+    """The descriptor and the cache structure of a call whose rows are x: [total, heads, d]; kv_rows: x has the pages' heads."""
     import torch
-    if x.dim() != 3 or x.stride(2) != 1 or K_pages.dim() != 4 or K_pages.stride(3) != 1:
-        raise ValueError("%s: expected rows [total, heads, d] and pages [num_pages, kv_heads, page_size, d] with unit stride along d" % name)
-    _same_layout(K_pages, V_pages)
-    num, kvh, page, d = K_pages.shape
-    total, h, dx = x.shape
-    if dx != d or (heads_of == "kv" and h != kvh) or x.device != K_pages.device:
-        raise ValueError("%s: rows and pages must agree in their heads, d and device" % name)
-    fp8 = K_pages.dtype is torch.float8_e4m3fn
-    if not fp8 and K_pages.dtype != x.dtype:
+    if x.dim() != 3 or K_pages.dim() != 4 or table.dim() != 2:
+        raise ValueError("%s: expected rows [total, heads, d], pages [num_pages, kv_heads, page_size, d] and a table [batch, pages]" % name)
+    (total, h, dx), (sn, sh, sd), dtype, device = x.shape, x.stride(), x.dtype, x.device
+    shape, strides, kind = K_pages.shape, K_pages.stride(), K_pages.dtype
+    (num, kvh, page, d), (psp, psh, psn, psd) = shape, strides
+    if sd != 1 or psd != 1:
+        raise ValueError("%s: expected unit stride along d" % name)
+    if V_pages.shape != shape or V_pages.stride() != strides or V_pages.dtype != kind or V_pages.device != device or K_pages.device != device:
+        raise ValueError("%s: K_pages and V_pages must share shape, strides, dtype and the rows' device" % name)
+    if dx != d or (kv_rows and h != kvh):
+        raise ValueError("%s: rows and pages must agree in d and in their heads" % name)
+    fp8 = kind is torch.float8_e4m3fn
+    if fp8:
+        for e in (K_exp, V_exp):
+            if e is None or e.dtype is not torch.uint8 or e.shape != shape[:3] or not e.is_contiguous() or e.device != device:
+                raise ValueError("%s: quantised pages need contiguous uint8 exponents [num_pages, kv_heads, page_size]" % name)
+    elif kind is not dtype:
         raise ValueError("%s: pages hold the rows' type, or float8_e4m3fn with exponents" % name)
-    for e in (K_exp, V_exp) if fp8 else ():
-        if e is None or e.dtype != torch.uint8 or tuple(e.shape) != (num, kvh, page) or not e.is_contiguous() or e.device != x.device:
-            raise ValueError("%s: quantised pages need contiguous uint8 exponents [num_pages, kv_heads, page_size]" % name)
-    if table.dim() != 2 or table.dtype != torch.int32 or table.stride(1) != 1 or table.device != x.device:
-        raise ValueError("%s: the table must be an int32 tensor [batch, pages] with unit stride along the pages" % name)
     batch, width = table.shape
-    if q_ptr is None and max_q is None:
+    ts, t1 = table.stride()
+    if table.dtype is not torch.int32 or t1 != 1 or table.device != device:
+        raise ValueError("%s: the table must be an int32 tensor with unit stride along the pages" % name)
+    if max_q is None:
+        if q_ptr is not None:
+            raise ValueError("%s: q_ptr needs max_q, the largest number of new tokens of a sequence" % name)
         if batch and total % batch:
             raise ValueError("%s: without q_ptr every sequence has the same number of rows" % name)
         max_q = total // batch if batch else 0
-    if max_q is None:
-        raise ValueError("%s: q_ptr needs max_q, the largest number of new tokens of a sequence" % name)
-    sn, sh, _ = x.stride()
-    kind = ATTN_CACHE_FP8 if fp8 else ATTN_CACHE_PLAIN
-    desc = attn_paged_desc(batch, h, kvh, d, total, int(max_q), width * page if max_len is None else int(max_len), page, num, width,
-                           float(scale), int(window), int(sinks), _dtype(x), kind, 0, sn, sh, sn, sh, *K_pages.stride()[:3], table.stride(0))
-    cache = attn_cache(K_pages.data_ptr(), V_pages.data_ptr(), K_exp.data_ptr() if fp8 else None, V_exp.data_ptr() if fp8 else None,
-                       table.data_ptr(), _int32("lens", lens, (batch,), x.device), _int32("q_ptr", q_ptr, (batch + 1,), x.device))
+    desc = _PAGED_DESC.pack(batch, h, kvh, d, total, max_q, width * page if max_len is None else max_len, page, num, width, scale, window, sinks,
+                            _dtype(dtype), ATTN_CACHE_FP8 if fp8 else ATTN_CACHE_PLAIN, 0, sn, sh, sn, sh, psp, psh, psn, ts)
+    cache = _CACHE.pack(K_pages.data_ptr(), V_pages.data_ptr(), K_exp.data_ptr() if fp8 else 0, V_exp.data_ptr() if fp8 else 0,
+                        table.data_ptr(), _int32("lens", lens, batch, device) or 0, _int32("q_ptr", q_ptr, batch + 1, device) or 0)
     return desc, cache
 
 
@@ -462,46 +482,54 @@ def attn_cache_write(K, V, K_pages, V_pages, table, lens, q_ptr=None, max_q=None
     """The new tokens' K and V ([total, kv_heads, d]) into the pages of their sequences, quantised where the pages are float8_e4m3fn.
     lens (int32 [batch]) counts the new tokens already; rows q_ptr[b] .. q_ptr[b + 1] - 1 belong to sequence b (None: the same number each)."""
     _same_layout(K, V)
-    desc, cache = _paged("attn_cache_write", K, "kv", K_pages, V_pages, table, lens, q_ptr, max_q, None, K_exp, V_exp)
-    st = lib().attn_cache_write(ctypes.byref(desc), ctypes.byref(cache), K.data_ptr(), V.data_ptr(), _stream(stream))
+    desc, cache = _paged("attn_cache_write", K, K_pages, V_pages, table, lens, q_ptr, max_q, None, K_exp, V_exp, True)
+    st = lib().attn_cache_write(desc, cache, K.data_ptr(), V.data_ptr(), _stream(stream))
     if st != ATTN_OK:
         raise AttnError(st, "attn_cache_write")
 
 
 def attn_cache_read(K_pages, V_pages, table, lens, dtype, total, q_ptr=None, max_q=None, K_exp=None, V_exp=None, stream=None, out=None):
     """K, V ([total, kv_heads, d]): the last tokens of every sequence, as many as q_ptr says (None: total / batch each)."""
-    import torch
     if out is None:
+        import torch
+        if K_pages.dim() != 4:
+            raise ValueError("attn_cache_read: expected pages [num_pages, kv_heads, page_size, d]")
         shape = (total, K_pages.shape[1], K_pages.shape[3])
-        out = tuple(torch.empty(shape, dtype=dtype, device=K_pages.device) for _ in range(2))
+        out = torch.empty(shape, dtype=dtype, device=K_pages.device), torch.empty(shape, dtype=dtype, device=K_pages.device)
     K, V = out
     _same_layout(K, V)
-    desc, cache = _paged("attn_cache_read", K, "kv", K_pages, V_pages, table, lens, q_ptr, max_q, None, K_exp, V_exp)
-    st = lib().attn_cache_read(ctypes.byref(desc), ctypes.byref(cache), K.data_ptr(), V.data_ptr(), _stream(stream))
+    desc, cache = _paged("attn_cache_read", K, K_pages, V_pages, table, lens, q_ptr, max_q, None, K_exp, V_exp, True)
+    st = lib().attn_cache_read(desc, cache, K.data_ptr(), V.data_ptr(), _stream(stream))
     if st != ATTN_OK:
         raise AttnError(st, "attn_cache_read")
     return K, V
 
 
 def attn_paged_workspace_bytes(desc):
-    return lib().attn_paged_workspace_bytes(ctypes.byref(desc))
+    return lib().attn_paged_workspace_bytes(_as_argument(desc))
 
 
 def attn_paged_fwd(Q, K_pages, V_pages, table, lens, scale, q_ptr=None, max_q=None, max_len=None, window=0, sinks=0, K_exp=None,
                    V_exp=None, stream=None, out=None, workspace=None):
     """O [total, heads, d], LSE [total, heads] of the new tokens Q [total, heads, d] over the paged cache that their keys and values have
     been written to.  max_len bounds the lengths (None: what the table can hold; a tighter bound gives better launches)."""
-    import torch
-    desc, cache = _paged("attn_paged_fwd", Q, "q", K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp, scale, window, sinks)
+    desc, cache = _paged("attn_paged_fwd", Q, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp, False, scale, window, sinks)
     if out is None:
-        out = torch.empty_like(Q), torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device)
-    O, LSE = out
-    _same_layout(Q, O)
-    _check_lse(LSE, Q)
+        import torch
+        O, LSE = torch.empty_like(Q), torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device)
+        _same_layout(Q, O)
+    else:
+        O, LSE = out
+        _same_layout(Q, O)
+        _check_lse(LSE, Q)
+    where = size = 0
     if workspace is None:
-        workspace = _scratch(max(attn_paged_workspace_bytes(desc), 256), Q.device, stream)
-    st = lib().attn_paged_fwd(ctypes.byref(desc), ctypes.byref(cache), Q.data_ptr(), O.data_ptr(), LSE.data_ptr(), workspace.data_ptr(),
-                              workspace.numel(), _stream(stream))
+        size = attn_paged_workspace_bytes(desc)
+        if size > 256:  # (256: nothing is kept there)
+            workspace = _scratch(size, Q.device, stream)
+    if workspace is not None:
+        where, size = workspace.data_ptr(), workspace.numel()
+    st = lib().attn_paged_fwd(desc, cache, Q.data_ptr(), O.data_ptr(), LSE.data_ptr(), where, size, _stream(stream))
     if st != ATTN_OK:
         raise AttnError(st, "attn_paged_fwd")
     return O, LSE

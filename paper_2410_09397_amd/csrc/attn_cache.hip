@@ -67,9 +67,10 @@ __device__ __forceinline__ CacheRow cache_row(const WinParams& p, const WinSeq& 
     }
     return r;
 }
-// Rows per thread: K and V of kRowsPerThread tokens or heads are on the way at a time (one row at a time, the 88 MB of a batch of prompts took 37 us
+// Rows per thread: K and V of several tokens or heads are on the way at a time (one row at a time, the 88 MB of a batch of prompts took 37 us
 // to write and 27 to read, a chain of dependent loads each).
-constexpr int kRowsPerThread = 4;
+// (A call of few rows, a decoding step, has one each: 3.6 us against 6.5 with four for 64 tokens of 8 heads.)
+constexpr int kManyRows = 4;
 
 __device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
 
@@ -114,7 +115,7 @@ __device__ __forceinline__ f32x8 dequantise(u32x2 codes, float scale) {
 
 __device__ __forceinline__ int first_row(const WinParams& p, int b) { return p.q_ptr ? min(max(p.q_ptr[b], 0), p.total_q) : b * p.n; }
 
-template <typename T, bool FP8>
+template <typename T, bool FP8, int kRowsPerThread>
 __global__ void __launch_bounds__(kThreads) cache_write_kernel(WinParams p, const void* K, const void* V, long s_n, long s_h, int lanes) {
     const int b = blockIdx.y, row0 = first_row(p, b), per = kThreads / lanes;
     const WinSeq s = win_sequence(p, b);
@@ -155,7 +156,7 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(WinParams p, cons
 }
 
 // Rows without a place in the pages (a position in front of the first token, a page that is gone) come back as zeros.
-template <typename T, bool FP8>
+template <typename T, bool FP8, int kRowsPerThread>
 __global__ void __launch_bounds__(kThreads) cache_read_kernel(WinParams p, void* K, void* V, long s_n, long s_h, int lanes) {
     const int b = blockIdx.y, row0 = first_row(p, b), per = kThreads / lanes;
     const WinSeq s = win_sequence(p, b);
@@ -187,23 +188,36 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(WinParams p, void*
 }
 
 int lanes_of(int d) { return d <= 64 ? 8 : d <= 128 ? 16 : 32; }
+template <int ROWS>
 dim3 grid_of(const WinParams& p) {
-    const long rows = kThreads / lanes_of(p.d) * kRowsPerThread;
+    const long rows = kThreads / lanes_of(p.d) * ROWS;
     return dim3((unsigned)(((long)p.n * p.kv_heads + rows - 1) / rows), (unsigned)p.batch);
 }
+// whether the rows fill the chip with several per thread: about one workgroup of eight waves' rows for every CU
+bool many_rows(const WinParams& p) { return (long)p.total_q * p.kv_heads * lanes_of(p.d) > 256L * 2 * kThreads; }
 
 }  // namespace
 
 hipError_t launch_cache_write(bool is_bf16, bool fp8, const WinParams& p, const void* K, const void* V, long s_n, long s_h, hipStream_t stream) {
-    auto fn = is_bf16 ? (fp8 ? cache_write_kernel<__bf16, true> : cache_write_kernel<__bf16, false>)
-                      : (fp8 ? cache_write_kernel<float, true> : cache_write_kernel<float, false>);
-    hipLaunchKernelGGL(fn, grid_of(p), dim3(kThreads), 0, stream, p, K, V, s_n, s_h, lanes_of(p.d));
+    auto launch = [&](auto rows) {
+        constexpr int R = decltype(rows)::value;
+        auto fn = is_bf16 ? (fp8 ? cache_write_kernel<__bf16, true, R> : cache_write_kernel<__bf16, false, R>)
+                          : (fp8 ? cache_write_kernel<float, true, R> : cache_write_kernel<float, false, R>);
+        hipLaunchKernelGGL(fn, grid_of<R>(p), dim3(kThreads), 0, stream, p, K, V, s_n, s_h, lanes_of(p.d));
+    };
+    if (many_rows(p)) launch(std::integral_constant<int, kManyRows>{});
+    else launch(std::integral_constant<int, 1>{});
     return hipGetLastError();
 }
 hipError_t launch_cache_read(bool is_bf16, bool fp8, const WinParams& p, void* K, void* V, long s_n, long s_h, hipStream_t stream) {
-    auto fn = is_bf16 ? (fp8 ? cache_read_kernel<__bf16, true> : cache_read_kernel<__bf16, false>)
-                      : (fp8 ? cache_read_kernel<float, true> : cache_read_kernel<float, false>);
-    hipLaunchKernelGGL(fn, grid_of(p), dim3(kThreads), 0, stream, p, K, V, s_n, s_h, lanes_of(p.d));
+    auto launch = [&](auto rows) {
+        constexpr int R = decltype(rows)::value;
+        auto fn = is_bf16 ? (fp8 ? cache_read_kernel<__bf16, true, R> : cache_read_kernel<__bf16, false, R>)
+                          : (fp8 ? cache_read_kernel<float, true, R> : cache_read_kernel<float, false, R>);
+        hipLaunchKernelGGL(fn, grid_of<R>(p), dim3(kThreads), 0, stream, p, K, V, s_n, s_h, lanes_of(p.d));
+    };
+    if (many_rows(p)) launch(std::integral_constant<int, kManyRows>{});
+    else launch(std::integral_constant<int, 1>{});
     return hipGetLastError();
 }
 

@@ -47,7 +47,7 @@ attn_status check_win(const attn_win_desc* d) {
     // the tile copies address a tile's rows with 32-bit byte offsets from its first row
     if (d->q_stride_n >= (int64_t)1 << 22 || d->kv_stride_n >= (int64_t)1 << 22) return ATTN_ERR_UNSUPPORTED;
     const int64_t group = d->heads / d->kv_heads, rows = d->n * group, bk = (int64_t)d->batch * d->kv_heads;
-    if (rows > kMostTokens || bk > kMostGroups || ((rows + 63) / 64 + 64) * bk > kMostGroups ||
+    if (rows > kMostTokens || bk > kMostGroups || ((rows + 31) / 32 + 64) * bk > kMostGroups ||
         (int64_t)d->batch * d->heads > kMostGroups || (int64_t)d->batch * d->heads * d->n > kMostGroups * 32)
         return ATTN_ERR_UNSUPPORTED;
     return ATTN_OK;
@@ -150,12 +150,12 @@ attn_status check_cache(const attn_paged_desc* d, const attn_cache* c) {
 // Rows of a workgroup of the paged forward: see attn_win_fwd.hip.
 int paged_rows(const attn_paged_desc* d) {
     const int64_t rows = (int64_t)d->max_q * (d->heads / d->kv_heads);
-    return !is_wide(d->dtype, d->d) || rows > 64 ? 128 : rows > 16 ? 32 : 16;
+    return !is_wide(d->dtype, d->d) ? 32 : rows > 64 ? 128 : rows > 16 ? 32 : 16;
 }
 
 // How the keys of a row block are shared out: with fewer row blocks than the chip has places for, a workgroup takes `chunk` tiles.
 void set_splits(WinParams& p, const attn_paged_desc* d) {
-    const int64_t rows = paged_rows(d), tile = is_wide(d->dtype, d->d) && rows == 128 ? 64 : 32;
+    const int64_t rows = paged_rows(d), tile = rows == 128 ? 64 : 32;
     const bool few = rows < 128;
     // (total_q bounds the row blocks that have rows where the sequences' new tokens differ in number)
     const int64_t blocks = std::min((((int64_t)p.n * p.group + rows - 1) / rows) * p.batch, (int64_t)p.total_q * p.group / rows + p.batch) * p.kv_heads;

@@ -5,9 +5,9 @@
 // bf16 form (column l % 32, register i <-> row 8 (i / 4) + 4 h + i % 4).  The order of k is free as long as both operands have the same:
 //   contraction over d     step (c, e) takes columns 8 c + e (h = 0) and 8 c + 4 + e (h = 1): a lane reads 4 values at a time
 //   contraction over rows  step i takes the rows of accumulator register i, which is then an operand as it stands
-// Every wave works by itself, on 32 rows of queries or keys, and reads its operands straight from memory (the four waves of a
-// workgroup read the same tiles, which L1 holds): no LDS, no barrier, and any layout of the rows.  A step of the second kind has one
-// 4-byte load per lane for 64 cycles of the matrix pipe.
+// A workgroup owns 32 rows of queries or keys; its four waves take the tiles that stream past in turn, each reading its operands straight from memory
+// (any layout of the rows will do) into accumulators of its own, which meet in LDS at the end: a short window is only a handful of tiles, and a tile
+// takes a wave 64 cycles for every 2 x 32 of its products.
 #include <type_traits>
 
 #include "attn_internal.hpp"
@@ -21,7 +21,56 @@ __device__ __forceinline__ f32x16 mfma_f32(float a, float b, f32x16 c) { return 
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef __bf16 bf16x4u __attribute__((ext_vector_type(4), aligned(8)));
 
-// columns c .. c + 3 of a row (0 from d on); c is a multiple of 4
+// A kernel of width DP serves head dimensions in (kFull<DP>, DP]: the columns below kFull<DP> exist without a question.  The others are read from inside
+// the row and replaced by 0 where they do not exist: a load behind a condition is waited for where it stands, and the loads of a tile have
+// to be on their way together.
+template <int DP>
+constexpr int kFull = DP == 192 ? 128 : DP == 256 ? 192 : DP - 32;
+
+// columns c .. c + 3 of a row, c a multiple of 4
+template <int DP>
+__device__ __forceinline__ f32x4 load4(const float* row, int c, bool exists, int d) {
+    if (exists) return *reinterpret_cast<const f32x4u*>(row + c);
+    f32x4 v;
+    if constexpr (DP == 32) {  // (d may be less than 4)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = row[min(c + e, d - 1)];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = c + e < d ? v[e] : 0.f;
+    } else {
+        // four values that end with the row's last one, moved down by as many places as they start early
+        const int start = min(c, d - 4), s = c - start;
+        v = *reinterpret_cast<const f32x4u*>(row + start);
+        if (s & 1) v = f32x4{v[1], v[2], v[3], 0.f};
+        if (s & 2) v = f32x4{v[2], v[3], 0.f, 0.f};
+        if (s >= 4) v = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    return v;
+}
+template <int DP>
+__device__ __forceinline__ f32x4 load4(const __bf16* row, int c, bool exists, int d) {  // (d is a multiple of 8)
+    const f32x4 v = __builtin_convertvector(*reinterpret_cast<const bf16x4u*>(row + (exists ? c : min(c, d - 4))), f32x4), zero = {0.f, 0.f, 0.f, 0.f};
+    return exists || c < d ? v : zero;
+}
+template <int DP>
+__device__ __forceinline__ f32x4 load4(const uint8_t* row, int c, bool exists, int d) {
+    int u = *reinterpret_cast<const int*>(row + (exists ? c : min(c, d - 4)));
+    u = exists || c < d ? u : 0;
+    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(u, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(u, true);
+    return f32x4{lo[0], lo[1], hi[0], hi[1]};
+}
+__device__ __forceinline__ float value(float x) { return x; }
+__device__ __forceinline__ float value(__bf16 x) { return (float)x; }
+__device__ __forceinline__ float value(uint8_t x) { return __builtin_amdgcn_cvt_f32_fp8((int)x, 0); }
+// column 32 m + l of a row; CHECK, first: m counts from a group of columns that the compiler does not know
+template <int DP, bool CHECK = false, typename E>
+__device__ __forceinline__ float load1(const E* row, int m, int l, int d, int first = 0) {
+    const int c = 32 * (first + m) + l;
+    if (!CHECK && 32 * m + 32 <= kFull<DP>) return value(row[c]);
+    const float v = value(row[min(c, d - 1)]);
+    return c < d ? v : 0.f;
+}
+// of any width, for the small kernels
 __device__ __forceinline__ f32x4 load4(const float* row, int c, int d) {
     if (c + 4 <= d) return *reinterpret_cast<const f32x4u*>(row + c);
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
@@ -30,25 +79,7 @@ __device__ __forceinline__ f32x4 load4(const float* row, int c, int d) {
         if (c + e < d) v[e] = row[c + e];
     return v;
 }
-__device__ __forceinline__ f32x4 load4(const __bf16* row, int c, int d) {  // (d is a multiple of 8)
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (c < d) v = __builtin_convertvector(*reinterpret_cast<const bf16x4u*>(row + c), f32x4);
-    return v;
-}
-__device__ __forceinline__ f32x4 load4(const uint8_t* row, int c, int d) {
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (c < d) {
-        const int u = *reinterpret_cast<const int*>(row + c);
-        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(u, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(u, true);
-        v = f32x4{lo[0], lo[1], hi[0], hi[1]};
-    }
-    return v;
-}
-__device__ __forceinline__ float load1(const float* row, int c, int d) { return c < d ? row[c] : 0.f; }
-__device__ __forceinline__ float load1(const __bf16* row, int c, int d) { return c < d ? (float)row[c] : 0.f; }
-__device__ __forceinline__ float load1(const uint8_t* row, int c, int d) {
-    return c < d ? __builtin_amdgcn_cvt_f32_fp8((int)row[c], 0) : 0.f;
-}
+__device__ __forceinline__ f32x4 load4(const __bf16* row, int c, int d) { return load4<32>(row, c, false, d); }
 __device__ __forceinline__ void store4(float* row, int c, int d, f32x4 v) {
     if (c + 4 <= d) {
         *reinterpret_cast<f32x4u*>(row + c) = v;
@@ -62,14 +93,15 @@ __device__ __forceinline__ void store4(__bf16* row, int c, int d, f32x4 v) {
     if (c < d) *reinterpret_cast<u32x2*>(row + c) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
 }
 
-// A resident row as the contraction over d takes it: 4 values of columns 8 c + 4 h .. for every c.  bf16 rows stay packed; fp32 rows of
-// more than 128 columns have no registers to stay in and are read again for every tile.
-template <typename T, int DP, bool kResident = std::is_same_v<T, __bf16> || DP <= 128>
+// A resident row as the contraction over d takes it: 4 values of columns 8 c + 4 h .. for every c.  bf16 rows stay packed; rows that
+// have no registers to stay in are read again for every tile.
+template <typename T, int DP, bool kResident = DP <= (std::is_same_v<T, __bf16> ? 192 : 128)>
 struct RowOperand {
     typedef std::conditional_t<std::is_same_v<T, __bf16>, u32x2, f32x4> Chunk;
     Chunk v[kResident ? DP / 8 : 1];
     const T* row;
     int d, h;
+    __device__ __forceinline__ f32x4 load(int c) const { return load4<DP>(row, 8 * c + 4 * h, 8 * c + 8 <= kFull<DP>, d); }
     __device__ __forceinline__ void init(const T* row_, int d_, int h_) {
         row = row_;
         d = d_;
@@ -77,28 +109,32 @@ struct RowOperand {
         if constexpr (kResident) {
 #pragma unroll
             for (int c = 0; c < DP / 8; ++c) {
-                const f32x4 x = load4(row, 8 * c + 4 * h, d);
+                const f32x4 x = load(c);
                 if constexpr (std::is_same_v<T, __bf16>) v[c] = u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
                 else v[c] = x;
             }
         }
     }
     __device__ __forceinline__ f32x4 get(int c) const {
-        if constexpr (!kResident) return load4(row, 8 * c + 4 * h, d);
+        if constexpr (!kResident) return load(c);
         else if constexpr (std::is_same_v<T, __bf16>) return __builtin_convertvector(__builtin_bit_cast(bf16x4, v[c]), f32x4);
         else return v[c];
     }
 };
 
-// The 32 rows of a key tile as a lane sees them: row l % 32 for the contraction over d, every row for the contraction over keys.
-template <typename E>
+// The 32 rows of a key tile as a lane sees them: row l % 32 for the contraction over d, every row for the contraction over keys.  Rows of
+// tensors are 32-bit offsets from the tile's first (q_n, k_n < 2^22), rows of pages lie anywhere.
+template <typename E, bool PAGED>
 struct KeyTile {
     static constexpr bool kCodes = std::is_same_v<E, uint8_t>;
-    long at;      // element offset of row l % 32 in K and V
+    std::conditional_t<PAGED, long, unsigned> at;  // element offset of row l % 32
+    const E *K, *V;
     float sk, sv;  // quantised: what its codes are multiplied with
     __device__ __forceinline__ void init(const WinParams& p, const WinTiles<32>& tiles, int b, int kvh, int j0, int l32) {
         const int j = tiles.row(p, j0 + l32);
-        if (p.table) {
+        K = static_cast<const E*>(p.K);
+        V = static_cast<const E*>(p.V);
+        if constexpr (PAGED) {
             const PageRow r = win_page_row(p, win_page(p, b, j), kvh, j);
             at = r.at;
             if constexpr (kCodes) {
@@ -106,25 +142,40 @@ struct KeyTile {
                 sv = exp_value(p.V_exp[r.exp]);
             }
         } else {
-            at = (long)b * p.k_b + (long)kvh * p.k_h + (long)j * p.k_n;
+            const long base = (long)b * p.k_b + (long)kvh * p.k_h + (long)j0 * p.k_n;
+            K += base;
+            V += base;
+            at = (unsigned)(j - j0) * (unsigned)p.k_n;
         }
     }
-    static __device__ __forceinline__ long row_of(long at, int row) {  // of the lane that holds `row`
-        const int lo = __shfl((int)at, row, 64), hi = __shfl((int)(at >> 32), row, 64);
-        return ((long)hi << 32) | (unsigned)lo;
+    // offset of the row that another lane holds
+    __device__ __forceinline__ auto row_of(int row) const {
+        if constexpr (PAGED) {
+            const int lo = __shfl((int)at, row, 64), hi = __shfl((int)(at >> 32), row, 64);
+            return ((long)hi << 32) | (unsigned)lo;
+        } else {
+            return (unsigned)__shfl((int)at, row, 64);
+        }
     }
 };
+
+// Wide rows: the loads of at most `every` steps are on the way together (of more the compiler spills the addresses).
+template <int DP>
+__device__ __forceinline__ void pause(int step, int every) {
+    if (DP >= 192 && step % every == every - 1) __builtin_amdgcn_sched_barrier(0);
+}
 
 // s += A B^T over d: rows of `a` (l % 32) are the tile's, rows of b the resident ones
 template <typename E, typename T, int DP, bool R>
 __device__ __forceinline__ void scores(f32x16& s, const E* row, float scale, const RowOperand<T, DP, R>& b, int d, int h) {
 #pragma unroll
     for (int c = 0; c < DP / 8; ++c) {
-        f32x4 a = load4(row, 8 * c + 4 * h, d);
+        f32x4 a = load4<DP>(row, 8 * c + 4 * h, 8 * c + 8 <= kFull<DP>, d);
         if constexpr (std::is_same_v<E, uint8_t>) a *= scale;
         const f32x4 q = b.get(c);
 #pragma unroll
         for (int e = 0; e < 4; ++e) s = mfma_f32(a[e], q[e], s);
+        pause<DP>(c, 8);
     }
 }
 
@@ -136,14 +187,40 @@ __device__ __forceinline__ RowPlace place(const WinParams& p, int kvh, int r) {
     return {t, kvh * p.group + r - t * p.group};
 }
 
+// a: the sum of the four waves' accumulators, for wave 0, in the order of the waves; `meet`: 4 MT KB
+template <int MT>
+__device__ __forceinline__ void meet_waves(f32x16 (&a)[MT], float* meet, int w, int lane) {
+    auto slot = [&](int m, int x) { return reinterpret_cast<f32x4*>(meet) + (m * 4 + x) * 64 + lane; };
+    for (int from = 1; from < 4; ++from) {
+        if (w == from) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) *slot(m, x) = f32x4{a[m][4 * x], a[m][4 * x + 1], a[m][4 * x + 2], a[m][4 * x + 3]};
+        }
+        __syncthreads();
+        if (w == 0) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const f32x4 other = *slot(m, x);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) a[m][4 * x + e] += other[e];
+                }
+        }
+        __syncthreads();
+    }
+}
+
 // --------------------------------------------------------------------------------------------------------- forward
-template <typename T, typename E, int DP>
+template <typename T, typename E, int DP, bool PAGED>
 __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) win_plain_out_kernel(WinParams p, int row_blocks) {
     constexpr int MT = DP / 32;
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int bk = blockIdx.x / row_blocks, b = bk / p.kv_heads, kvh = bk % p.kv_heads;
     const WinSeq s = win_sequence(p, b);
-    const int rows = s.nq * p.group, r0 = ((blockIdx.x % row_blocks) * 4 + w) * 32;
+    const int rows = s.nq * p.group, r0 = (blockIdx.x % row_blocks) * 32;
     if (r0 >= rows) return;
     const int r = min(r0 + l32, rows - 1);
     const RowPlace at = place(p, kvh, r);
@@ -162,14 +239,14 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) win_plain_out_ker
         for (int e = 0; e < 16; ++e) o[m][e] = 0.f;
     float m_run = -__builtin_inff(), l_run = 0.f;  // of scale log2(e) s; this lane's half of the sum
     const float cs = p.scale * kLog2e;
-    for (int it = it0; it < it1; ++it) {
+    for (int it = it0 + w; it < it1; it += 4) {
         const int j0 = tiles.start(it);
-        KeyTile<E> keys;
+        KeyTile<E, PAGED> keys;
         keys.init(p, tiles, b, kvh, j0, l32);
         f32x16 st;
 #pragma unroll
         for (int e = 0; e < 16; ++e) st[e] = 0.f;
-        scores(st, static_cast<const E*>(p.K) + keys.at, keys.sk, q, p.d, h);
+        scores(st, keys.K + keys.at, keys.sk, q, p.d, h);
         float mx = -__builtin_inff();
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -195,15 +272,37 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) win_plain_out_ker
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const int row = acc_row(e, h);
-            const E* v = static_cast<const E*>(p.V) + KeyTile<E>::row_of(keys.at, row);
+            const E* v = keys.V + keys.row_of(row);
             float f = st[e];
-            if constexpr (KeyTile<E>::kCodes) f *= __shfl(keys.sv, row, 64);
+            if constexpr (KeyTile<E, PAGED>::kCodes) f *= __shfl(keys.sv, row, 64);
 #pragma unroll
-            for (int m = 0; m < MT; ++m) o[m] = mfma_f32(load1(v, 32 * m + l32, p.d), f, o[m]);
+            for (int m = 0; m < MT; ++m) o[m] = mfma_f32(load1<DP>(v, m, l32, p.d), f, o[m]);
+            pause<DP>(e, 4);
         }
     }
-    const float l = l_run + __shfl_xor(l_run, 32, 64);
-    if (r0 + l32 >= rows) return;
+    // every wave's m and l, then its O in units of the common reference
+    float l = l_run + __shfl_xor(l_run, 32, 64);
+    extern __shared__ __attribute__((aligned(16))) float meet[];  // [MT][4][64] x 16 bytes, [4][m, l][32]
+    float* stats = meet + MT * 4 * 64 * 4;
+    if (h == 0) {
+        stats[w * 64 + l32] = m_run;
+        stats[w * 64 + 32 + l32] = l;
+    }
+    __syncthreads();
+    float m_all = stats[l32];
+#pragma unroll
+    for (int x = 1; x < 4; ++x) m_all = __builtin_elementwise_maximum(m_all, stats[x * 64 + l32]);
+    const float m_ref = m_all == -__builtin_inff() ? 0.f : m_all, mine = __builtin_amdgcn_exp2f(m_run - m_ref);
+    l = 0.f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) l += __builtin_amdgcn_exp2f(stats[x * 64 + l32] - m_ref) * stats[x * 64 + 32 + l32];
+    m_run = m_all;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[m][e] *= mine;
+    meet_waves<MT>(o, meet, w, lane);
+    if (w != 0 || r0 + l32 >= rows) return;
     if (p.splits > 1) {
         const long row = s.lse_base + (long)at.t * p.heads + at.head;
         float* ml = p.part_ml + (row * p.splits + blockIdx.y) * 2;
@@ -322,7 +421,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) win_plain_dq_kerne
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int bk = blockIdx.x / row_blocks, b = bk / p.kv_heads, kvh = bk % p.kv_heads;
     const WinSeq s = win_sequence(p, b);
-    const int rows = s.nq * p.group, r0 = ((blockIdx.x % row_blocks) * 4 + w) * 32;
+    const int rows = s.nq * p.group, r0 = (blockIdx.x % row_blocks) * 32;
     if (r0 >= rows) return;
     const int r = min(r0 + l32, rows - 1);
     const RowPlace at = place(p, kvh, r);
@@ -341,26 +440,29 @@ __global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) win_plain_dq_kerne
 #pragma unroll
         for (int e = 0; e < 16; ++e) dq[m][e] = 0.f;
     const float cs = p.scale * kLog2e;
-    for (int it = 0; it < tiles.count; ++it) {
+    for (int it = w; it < tiles.count; it += 4) {
         const int j0 = tiles.start(it);
-        KeyTile<T> keys;
+        KeyTile<T, false> keys;
         keys.init(p, tiles, b, kvh, j0, l32);
         f32x16 st, dp;
 #pragma unroll
         for (int e = 0; e < 16; ++e) st[e] = dp[e] = 0.f;
-        scores(st, static_cast<const T*>(p.K) + keys.at, 1.f, q, p.d, h);
-        scores(dp, static_cast<const T*>(p.V) + keys.at, 1.f, g, p.d, h);
+        scores(st, keys.K + keys.at, 1.f, q, p.d, h);
+        scores(dp, keys.V + keys.at, 1.f, g, p.d, h);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const int row = acc_row(e, h), j = j0 + row;
             const bool seen = j <= hi && (j >= lo || j < p.sinks);
             const float ds = seen ? __builtin_amdgcn_exp2f(fmaf(st[e], cs, -lse)) * (dp[e] - delta) : 0.f;
-            const T* k = static_cast<const T*>(p.K) + KeyTile<T>::row_of(keys.at, row);
+            const T* k = keys.K + keys.row_of(row);
 #pragma unroll
-            for (int m = 0; m < MT; ++m) dq[m] = mfma_f32(load1(k, 32 * m + l32, p.d), ds, dq[m]);
+            for (int m = 0; m < MT; ++m) dq[m] = mfma_f32(load1<DP>(k, m, l32, p.d), ds, dq[m]);
+            pause<DP>(e, 4);
         }
     }
-    if (r0 + l32 >= rows) return;
+    extern __shared__ __attribute__((aligned(16))) float meet[];
+    meet_waves<MT>(dq, meet, w, lane);
+    if (w != 0 || r0 + l32 >= rows) return;
     T* dst = static_cast<T*>(p.dQ) + off;
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -372,13 +474,13 @@ __global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) win_plain_dq_kerne
 
 // dK, dV: a workgroup owns 32 keys; its waves take the 32-token tiles of all heads of the group in turn, with scores [query][key], which
 // are the operands of dV^T += dO^T P and dK^T += Q^T dS as they stand.  The waves' sums meet in LDS.  Blocks 0 .. sink_tiles * parts - 1 of a
-// head work on the sink tiles, a share of the tokens each.  d > 192: the columns of the gradients are shared by two workgroups
+// head work on the sink tiles, a share of the tokens each.  d > 128: the columns of the gradients are shared by two workgroups
 // (blockIdx.y), which both form the scores; one would need 600 registers per lane.
 template <typename T, int DP>
 __global__ void __launch_bounds__(kThreads, 1) win_plain_dkdv_kernel(WinParams p, int key_blocks) {
-    constexpr int MT = DP == 256 ? 4 : DP / 32;
-    extern __shared__ __attribute__((aligned(16))) float meet[];  // [2 MT][4][64] x 16 bytes
-    const int c0 = 32 * MT * blockIdx.y;  // first column of the gradients
+    constexpr int MT = DP >= 192 ? DP / 64 : DP / 32;
+    extern __shared__ __attribute__((aligned(16))) float meet[];  // [MT][4][64] x 16 bytes
+    const int m0 = MT * blockIdx.y, c0 = 32 * m0;  // first column of the gradients
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int bk = blockIdx.x / key_blocks, b = bk / p.kv_heads, kvh = bk % p.kv_heads;
     const int blk = blockIdx.x % key_blocks, shared = p.sink_tiles * p.parts;
@@ -408,55 +510,37 @@ __global__ void __launch_bounds__(kThreads, 1) win_plain_dkdv_kernel(WinParams p
     const float cs = p.scale * kLog2e;
     for (int job = w; job < jobs; job += 4) {
         const int head = kvh * p.group + job / t_tiles, t0 = i0 + 32 * (job % t_tiles);
-        const long base = s.q_base + (long)head * p.q_h;
+        // 32-bit offsets from the tile's first row; rows past the end repeat the last one
+        const long base = s.q_base + (long)head * p.q_h + (long)t0 * p.q_n, stat = s.lse_base + (long)head * s.lse_h + t0;
         const T *Q = static_cast<const T*>(p.Q) + base, *G = static_cast<const T*>(p.dO) + base;
-        const long stat = s.lse_base + (long)head * s.lse_h;
-        const int tr = min(t0 + l32, i1 - 1);
+        const float *lse = p.LSE_in + stat, *delta = p.delta + stat;
+        const int last = i1 - 1 - t0;
+        const unsigned q_n = (unsigned)p.q_n, mine = (unsigned)min(l32, last) * q_n;
         f32x16 st, dp;
 #pragma unroll
         for (int e = 0; e < 16; ++e) st[e] = dp[e] = 0.f;
-        scores(st, Q + (long)tr * p.q_n, 1.f, k, p.d, h);
-        scores(dp, G + (long)tr * p.q_n, 1.f, v, p.d, h);
+        scores(st, Q + mine, 1.f, k, p.d, h);
+        scores(dp, G + mine, 1.f, v, p.d, h);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            const int i = t0 + acc_row(e, h), ic = min(i, i1 - 1);
-            const bool seen = i < i1 && j <= i && (i - j < p.window || j < p.sinks);
-            const float f = seen ? __builtin_amdgcn_exp2f(fmaf(st[e], cs, -p.LSE_in[stat + ic] * kLog2e)) : 0.f;
-            const float ds = seen ? f * (dp[e] - p.delta[stat + ic]) : 0.f;
+            const int x = acc_row(e, h), xc = min(x, last), i = t0 + x;
+            const bool seen = x <= last && j <= i && (i - j < p.window || j < p.sinks);
+            st[e] = seen ? __builtin_amdgcn_exp2f(fmaf(st[e], cs, -lse[xc] * kLog2e)) : 0.f;
+            dp[e] = seen ? st[e] * (dp[e] - delta[xc]) : 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const unsigned row = (unsigned)min(acc_row(e, h), last) * q_n;
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                dv[m] = mfma_f32(load1(G + (long)ic * p.q_n, c0 + 32 * m + l32, p.d), f, dv[m]);
-                dk[m] = mfma_f32(load1(Q + (long)ic * p.q_n, c0 + 32 * m + l32, p.d), ds, dk[m]);
+                dv[m] = mfma_f32(load1<DP, (DP >= 192)>(G + row, m, l32, p.d, m0), st[e], dv[m]);
+                dk[m] = mfma_f32(load1<DP, (DP >= 192)>(Q + row, m, l32, p.d, m0), dp[e], dk[m]);
             }
+            pause<DP>(e, 4);
         }
     }
-    auto slot = [&](int m, int x) { return reinterpret_cast<f32x4*>(meet) + (m * 4 + x) * 64 + lane; };
-    for (int from = 1; from < 4; ++from) {
-        if (w == from) {
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    *slot(m, x) = f32x4{dk[m][4 * x], dk[m][4 * x + 1], dk[m][4 * x + 2], dk[m][4 * x + 3]};
-                    *slot(MT + m, x) = f32x4{dv[m][4 * x], dv[m][4 * x + 1], dv[m][4 * x + 2], dv[m][4 * x + 3]};
-                }
-        }
-        __syncthreads();
-        if (w == 0) {
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const f32x4 a = *slot(m, x), c = *slot(MT + m, x);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        dk[m][4 * x + e] += a[e];
-                        dv[m][4 * x + e] += c[e];
-                    }
-                }
-        }
-        __syncthreads();
-    }
+    meet_waves<MT>(dk, meet, w, lane);
+    meet_waves<MT>(dv, meet, w, lane);
     if (w != 0 || j >= p.n) return;
     if (part >= 0) {
         float* dst = p.part_kv + (((long)bk * p.sink_tiles + j0 / 32) * p.parts + part) * 2 * 32 * p.d + (long)l32 * p.d;
@@ -495,9 +579,10 @@ __global__ void __launch_bounds__(kThreads) win_sink_kernel(WinParams p, int til
     }
 }
 
-// f(width): head dimensions are taken in widths of 64, 96, 128, 192 and 256
+// f(width): see kFull
 template <typename F>
 hipError_t with_width(int d, F f) {
+    if (d <= 32) return f(std::integral_constant<int, 32>{});
     if (d <= 64) return f(std::integral_constant<int, 64>{});
     if (d <= 96) return f(std::integral_constant<int, 96>{});
     if (d <= 128) return f(std::integral_constant<int, 128>{});
@@ -505,24 +590,24 @@ hipError_t with_width(int d, F f) {
     return f(std::integral_constant<int, 256>{});
 }
 
-template <typename T, typename E>
+template <typename T, typename E, bool PAGED>
 hipError_t fwd(const WinParams& p, hipStream_t stream) {
-    const int blocks = (int)(((long)p.n * p.group + 127) / 128);
+    const int blocks = (int)(((long)p.n * p.group + 31) / 32);
     return with_width(p.d, [&](auto width) {
-        hipLaunchKernelGGL((win_plain_out_kernel<T, E, decltype(width)::value>), dim3((unsigned)((long)blocks * p.batch * p.kv_heads), (unsigned)p.splits),
-                           dim3(kThreads), 0, stream, p, blocks);
+        hipLaunchKernelGGL((win_plain_out_kernel<T, E, decltype(width)::value, PAGED>), dim3((unsigned)((long)blocks * p.batch * p.kv_heads), (unsigned)p.splits),
+                           dim3(kThreads), decltype(width)::value * 128 + 1024, stream, p, blocks);
         return hipGetLastError();
     });
 }
 
 template <typename T>
 hipError_t bwd(const WinParams& p, hipStream_t stream) {
-    const int blocks = (int)(((long)p.n * p.group + 127) / 128), keys = (p.n + 31) / 32 - p.sink_tiles + p.sink_tiles * p.parts;
+    const int blocks = (int)(((long)p.n * p.group + 31) / 32), keys = (p.n + 31) / 32 - p.sink_tiles + p.sink_tiles * p.parts;
     return with_width(p.d, [&](auto width) {
         constexpr int DP = decltype(width)::value;
-        hipLaunchKernelGGL((win_plain_dq_kernel<T, DP>), dim3((unsigned)((long)blocks * p.batch * p.kv_heads)), dim3(kThreads), 0, stream, p, blocks);
-        hipLaunchKernelGGL((win_plain_dkdv_kernel<T, DP>), dim3((unsigned)((long)keys * p.batch * p.kv_heads), DP == 256 ? 2 : 1), dim3(kThreads),
-                           (DP == 256 ? 128 : DP) * 256, stream, p, keys);
+        hipLaunchKernelGGL((win_plain_dq_kernel<T, DP>), dim3((unsigned)((long)blocks * p.batch * p.kv_heads)), dim3(kThreads), DP * 128, stream, p, blocks);
+        hipLaunchKernelGGL((win_plain_dkdv_kernel<T, DP>), dim3((unsigned)((long)keys * p.batch * p.kv_heads), DP >= 192 ? 2 : 1), dim3(kThreads),
+                           (DP >= 192 ? DP / 2 : DP) * 128, stream, p, keys);
         return hipGetLastError();
     });
 }
@@ -530,8 +615,9 @@ hipError_t bwd(const WinParams& p, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_win_plain_fwd(bool is_bf16, bool fp8, const WinParams& p, hipStream_t stream) {
-    if (fp8) return is_bf16 ? fwd<__bf16, uint8_t>(p, stream) : fwd<float, uint8_t>(p, stream);
-    return is_bf16 ? fwd<__bf16, __bf16>(p, stream) : fwd<float, float>(p, stream);
+    if (fp8) return is_bf16 ? fwd<__bf16, uint8_t, true>(p, stream) : fwd<float, uint8_t, true>(p, stream);
+    if (p.table) return is_bf16 ? fwd<__bf16, __bf16, true>(p, stream) : fwd<float, float, true>(p, stream);
+    return is_bf16 ? fwd<__bf16, __bf16, false>(p, stream) : fwd<float, float, false>(p, stream);
 }
 hipError_t launch_win_plain_bwd(bool is_bf16, const WinParams& p, hipStream_t stream) {
     return is_bf16 ? bwd<__bf16>(p, stream) : bwd<float>(p, stream);
