@@ -250,7 +250,7 @@ typedef struct {
     int64_t kv_stride_b, kv_stride_h, kv_stride_n;
 } attn_win_desc;
 
-/* Device scratch of attn_win_bwd (row sums v, and sums of the sink keys); attn_win_fwd needs none.  0 if desc is invalid. */
+/* Device scratch of attn_win_bwd (row sums v, and partial sums of keys whose work is shared out); attn_win_fwd needs none.  0 if desc is invalid. */
 size_t attn_win_workspace_bytes(const attn_win_desc *desc);
 attn_status attn_win_fwd(const attn_win_desc *desc, const int32_t *lens, const void *Q, const void *K, const void *V,
                          void *O, float *LSE, void *stream);

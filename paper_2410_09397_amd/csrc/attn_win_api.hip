@@ -66,20 +66,29 @@ void set_window(WinParams& p, int32_t window, int32_t sinks, int32_t longest) {
 
 // Keys of a tile of the backward's key owners.
 int key_tile(const attn_win_desc* d) { return is_wide(d->dtype, d->d) ? 64 : 32; }
-
-// A key owner streams window + tile tokens per head, one of sink keys all of them: its tokens are shared out over as many workgroups
-// as make the shares about as long (at most 64, and fewer where there are many sink tiles).
-void set_sinks(WinParams& p, int tile) {
-    p.sink_tiles = p.sinks > 0 ? (std::min(p.sinks, p.n) + tile - 1) / tile : 0;
-    p.parts = 1;
-    if (p.sink_tiles > 0) {
-        const int64_t shares = ((int64_t)p.n + p.window + tile - 1) / ((int64_t)p.window + tile);
-        p.parts = (int)std::min<int64_t>(std::min<int64_t>(shares, 64), std::max(1, 256 / p.sink_tiles));
+// Workgroups of the key owners.  One streams window + tile tokens per head of its group, one of sink keys all of them: those are shared out over as
+// many workgroups as make the shares about as long (at most 64, and fewer where there are many sink tiles).  Where all of them
+// together are fewer than the places on the chip, the tokens of every tile are shared out: at least two tiles of tokens to each, and enough of
+// them over all heads of the group (ten; the 32-bit kernels, whose waves take them in turn, six) to pay for the sums' way through memory
+// and the launch behind.  us of the backward, one workgroup per tile -> shared, h heads on k key heads:
+//   d = 128, no window   h8 k2 n512 63 -> 39   h8 k2 n1024 114 -> 55   h16 k2 n2048 380 -> 128      d = 256, no window  h8 k2 n1024 211 -> 104
+//   d = 128, window      h4 k1 n4096 w1024 135 -> 76   h16 k4 n2048 w512 85 -> 77   h8 k8 n1024 w256 (too few tiles) 35 -> 45
+//   d = 64               h4 k4 n300 (too few tiles) 20 -> 22      d = 256, window     h8 k4 n2048 w300 (too few tiles) 73 -> 77
+void set_parts(WinParams& p, int tile) {
+    const bool wide = tile == 64;
+    const int64_t places = wide && p.d == 256 ? 256 : 512;
+    const int64_t tiles = (p.n + tile - 1) / tile, bk = (int64_t)p.batch * p.kv_heads;
+    const int64_t span = std::min<int64_t>((int64_t)p.window + tile, p.n), token_tiles = (span + tile - 1) / tile;
+    p.sink_tiles = p.sinks > 0 ? (int)std::min<int64_t>((p.sinks + tile - 1) / tile, tiles) : 0;
+    p.parts = p.rest_parts = 1;
+    if (p.sink_tiles > 0) p.parts = (int)std::min<int64_t>(std::min<int64_t>((p.n + span - 1) / span, 64), std::max(1, 256 / p.sink_tiles));
+    const int64_t rest = std::min(std::min(places / std::max<int64_t>(1, tiles * bk), token_tiles / 2), token_tiles * p.group / (wide ? 10 : 6));
+    if (rest > 1) {
+        p.rest_parts = (int)rest;
+        p.parts = std::min(64, (int)rest * p.parts);
     }
-    if (p.parts <= 1) {
-        p.sink_tiles = 0;
-        p.parts = 1;
-    }
+    if (p.parts <= 1) p.sink_tiles = 0;
+    p.slots = p.sink_tiles * (p.parts > 1 ? p.parts : 0) + (p.rest_parts > 1 ? (int)(tiles - p.sink_tiles) * p.rest_parts : 0);
 }
 
 WinParams win_params(const attn_win_desc* d) {
@@ -99,16 +108,14 @@ WinParams win_params(const attn_win_desc* d) {
     p.d = d->d;
     p.scale = d->scale;
     set_window(p, d->window, d->sinks, d->n);
-    set_sinks(p, key_tile(d));
+    set_parts(p, key_tile(d));
     p.splits = 1;
     p.chunk = 0x7fffffff;
     return p;
 }
 
 size_t rows_bytes(const attn_win_desc* d) { return round_up((size_t)d->batch * d->heads * d->n * sizeof(float), 256); }
-size_t sinks_bytes(const WinParams& p, int tile) {
-    return (size_t)p.batch * p.kv_heads * p.sink_tiles * (p.parts > 1 ? p.parts : 0) * 2 * tile * p.d * sizeof(float);
-}
+size_t parts_bytes(const WinParams& p, int tile) { return (size_t)p.batch * p.kv_heads * p.slots * 2 * tile * p.d * sizeof(float); }
 
 attn_status check_paged(const attn_paged_desc* d) {
     if (!d) return ATTN_ERR_INVALID_ARG;
@@ -207,7 +214,7 @@ WinParams paged_params(const attn_paged_desc* d, const attn_cache* c) {
     p.max_len = d->max_len;
     p.scale = d->scale;
     set_window(p, d->window, d->sinks, d->max_len);
-    p.parts = 1;
+    p.parts = p.rest_parts = 1;
     set_splits(p, d);
     return p;
 }
@@ -229,7 +236,7 @@ extern "C" {
 size_t attn_win_workspace_bytes(const attn_win_desc* desc) {
     if (check_win(desc) != ATTN_OK) return 0;
     if (is_empty(desc)) return 256;
-    return rows_bytes(desc) + sinks_bytes(win_params(desc), key_tile(desc));
+    return rows_bytes(desc) + parts_bytes(win_params(desc), key_tile(desc));
 }
 
 attn_status attn_win_fwd(const attn_win_desc* desc, const int32_t* lens, const void* Q, const void* K, const void* V, void* O,
@@ -283,7 +290,7 @@ attn_status attn_win_bwd(const attn_win_desc* desc, const int32_t* lens, const v
         e = attn::launch_win_rows(bf16, p, s);
         if (e == hipSuccess) e = attn::launch_win_plain_bwd(bf16, p, s);
     }
-    if (e == hipSuccess && p.parts > 1) e = attn::launch_win_sinks(bf16, key_tile(desc), p, s);
+    if (e == hipSuccess && p.slots > 0) e = attn::launch_win_keys(bf16, key_tile(desc), p, s);
     return status_of(e);
 }
 

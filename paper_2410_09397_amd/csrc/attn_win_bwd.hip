@@ -4,7 +4,8 @@
 //   win_dkdv_kernel  a workgroup owns 64 keys and streams the 64-token tiles that see them, of one head of the group after the other: the sum
 //                    over the heads that share the keys is a longer stream into the same accumulators
 // No atomics, so the same call gives the same bits.  A key that is a sink is seen by every token behind it: the tokens that see a tile
-// with sinks are shared out over p.parts workgroups, whose fp32 sums win_sink_kernel brings together.  P and dS are rounded to bf16 for the
+// with sinks are shared out over p.parts workgroups, whose fp32 sums win_keys_kernel brings together; where there are fewer key tiles than
+// places on the chip, those of the other tiles over p.rest_parts.  P and dS are rounded to bf16 for the
 // products that use them (2^-9 of each weight), sums are fp32.
 #include <type_traits>
 
@@ -210,19 +211,12 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dkdv_kernel(Wi
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wk = w & 1, wx = w >> 1;
     int bk, blk;
     decode_block(blockIdx.x, key_blocks, p.batch * p.kv_heads, bk, blk);
-    const int b = bk / p.kv_heads, kvh = bk % p.kv_heads, shared = p.sink_tiles * p.parts;
-    const int part = blk < shared ? blk % p.parts : -1;
-    const int j0 = 64 * (blk < shared ? blk / p.parts : blk - shared + p.sink_tiles);
+    const int b = bk / p.kv_heads, kvh = bk % p.kv_heads;
     const WinSeq s = win_sequence(p, b);
-    // tokens i0 .. i1 - 1 see some key of the block
-    int i0 = j0, i1 = s.len;
-    if (j0 >= p.sinks) i1 = (int)min((long)s.len, (long)j0 + 63 + p.window);
-    if (part >= 0) {
-        const int share = ((s.len - j0 + p.parts - 1) / p.parts + 63) & ~63;
-        i0 = min(s.len, j0 + part * share);
-        i1 = min(s.len, i0 + share);
-    }
-    const int t_tiles = j0 < s.len && i0 < i1 ? (i1 - i0 + 63) / 64 : 0, jobs = t_tiles * p.group;
+    WinKeys keys;
+    keys.init(p, blk, 64, s.len);
+    const int j0 = keys.j0, i0 = keys.i0, i1 = keys.i1;
+    const int t_tiles = (i1 - i0 + 63) / 64, jobs = t_tiles * p.group;
     const long kv = (long)b * p.k_b + (long)kvh * p.k_h;
 
     f32x16 acc[MH][2];
@@ -405,8 +399,8 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dkdv_kernel(Wi
         }
     }
 
-    if (part >= 0) {  // fp32 sums of this part: [dK, dV][64 keys][d]
-        float* dst = p.part_kv + ((((long)bk * p.sink_tiles + j0 / 64) * p.parts + part) * 2 + (wx == 0 ? 1 : 0)) * 64 * D;
+    if (keys.slot >= 0) {  // fp32 sums of this part: [dK, dV][64 keys][d]
+        float* dst = p.part_kv + (((long)bk * p.slots + keys.slot) * 2 + (wx == 0 ? 1 : 0)) * 64 * D;
         const float f = wx == 0 ? 1.f : p.scale;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
@@ -446,7 +440,7 @@ hipError_t launch(const WinParams& p, hipStream_t stream) {
     hipError_t e = allow_lds(win_dq_kernel<D>, q_lds);
     if (e == hipSuccess) e = allow_lds(win_dkdv_kernel<D>, k_lds);
     if (e != hipSuccess) return e;
-    const int rows = (int)(((long)p.n * p.group + 127) / 128), keys = (p.n + 63) / 64 - p.sink_tiles + p.sink_tiles * p.parts;
+    const int rows = (int)(((long)p.n * p.group + 127) / 128), keys = p.sink_tiles * p.parts + ((p.n + 63) / 64 - p.sink_tiles) * p.rest_parts;
     const long bk = (long)p.batch * p.kv_heads;
     hipLaunchKernelGGL(win_dq_kernel<D>, dim3((unsigned)(rows * bk)), dim3(kThreads), q_lds, stream, p, rows);
     hipLaunchKernelGGL(win_dkdv_kernel<D>, dim3((unsigned)(keys * bk)), dim3(kThreads), k_lds, stream, p, keys);

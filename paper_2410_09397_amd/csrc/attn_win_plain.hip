@@ -165,17 +165,64 @@ __device__ __forceinline__ void pause(int step, int every) {
     if (DP >= 192 && step % every == every - 1) __builtin_amdgcn_sched_barrier(0);
 }
 
-// s += A B^T over d: rows of `a` (l % 32) are the tile's, rows of b the resident ones
+// A row of the tile (l % 32) for the contraction over d.  Narrow widths: all of its loads are requested by init(), so that those of
+// several rows and of what follows are on their way together; wide ones read it as they go.
+template <typename E, int DP>
+struct TileRow {
+    static constexpr bool kAhead = DP <= 128;
+    f32x4 v[kAhead ? DP / 8 : 1];
+    const E* row;
+    int d, h;
+    __device__ __forceinline__ f32x4 load(int c) const { return load4<DP>(row, 8 * c + 4 * h, 8 * c + 8 <= kFull<DP>, d); }
+    __device__ __forceinline__ void init(const E* row_, int d_, int h_) {
+        row = row_;
+        d = d_;
+        h = h_;
+        if constexpr (kAhead) {
+#pragma unroll
+            for (int c = 0; c < DP / 8; ++c) v[c] = load(c);
+        }
+    }
+    __device__ __forceinline__ f32x4 get(int c) const {
+        if constexpr (kAhead) return v[c];
+        else return load(c);
+    }
+};
+
+// s += A B^T over d: a's rows are the tile's, b's the resident ones
 template <typename E, typename T, int DP, bool R>
-__device__ __forceinline__ void scores(f32x16& s, const E* row, float scale, const RowOperand<T, DP, R>& b, int d, int h) {
+__device__ __forceinline__ void scores(f32x16& s, const TileRow<E, DP>& row, float scale, const RowOperand<T, DP, R>& b) {
 #pragma unroll
     for (int c = 0; c < DP / 8; ++c) {
-        f32x4 a = load4<DP>(row, 8 * c + 4 * h, 8 * c + 8 <= kFull<DP>, d);
+        f32x4 a = row.get(c);
         if constexpr (std::is_same_v<E, uint8_t>) a *= scale;
         const f32x4 q = b.get(c);
 #pragma unroll
         for (int e = 0; e < 4; ++e) s = mfma_f32(a[e], q[e], s);
         pause<DP>(c, 8);
+    }
+}
+
+// Products over the rows of a tile, in groups of 4 accumulator registers: use(e, x) has what load(e, x) gave for x < N (columns of one or two tensors);
+// the loads of a group are requested in front of the products of the one before.
+template <int N, int DP, typename Load, typename Use>
+__device__ __forceinline__ void by_rows(Load load, Use use) {
+    float v[2][4][N];
+    auto request = [&](int g) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int x = 0; x < N; ++x) v[g & 1][e][x] = load(4 * g + e, x);
+    };
+    request(0);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        if (g < 3) request(g + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int x = 0; x < N; ++x) use(4 * g + e, x, v[g & 1][e][x]);
     }
 }
 
@@ -215,7 +262,7 @@ __device__ __forceinline__ void meet_waves(f32x16 (&a)[MT], float* meet, int w, 
 
 // --------------------------------------------------------------------------------------------------------- forward
 template <typename T, typename E, int DP, bool PAGED>
-__global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) win_plain_out_kernel(WinParams p, int row_blocks) {
+__global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) win_plain_out_kernel(WinParams p, int row_blocks) {
     constexpr int MT = DP / 32;
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int bk = blockIdx.x / row_blocks, b = bk / p.kv_heads, kvh = bk % p.kv_heads;
@@ -246,7 +293,9 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) win_plain_out_ker
         f32x16 st;
 #pragma unroll
         for (int e = 0; e < 16; ++e) st[e] = 0.f;
-        scores(st, keys.K + keys.at, keys.sk, q, p.d, h);
+        TileRow<E, DP> key;
+        key.init(keys.K + keys.at, p.d, h);
+        scores(st, key, keys.sk, q);
         float mx = -__builtin_inff();
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -269,16 +318,12 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) win_plain_out_ker
             st[e] = __builtin_amdgcn_exp2f(st[e] - m_use);
             l_run += st[e];
         }
+        if constexpr (KeyTile<E, PAGED>::kCodes) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int row = acc_row(e, h);
-            const E* v = keys.V + keys.row_of(row);
-            float f = st[e];
-            if constexpr (KeyTile<E, PAGED>::kCodes) f *= __shfl(keys.sv, row, 64);
-#pragma unroll
-            for (int m = 0; m < MT; ++m) o[m] = mfma_f32(load1<DP>(v, m, l32, p.d), f, o[m]);
-            pause<DP>(e, 4);
+            for (int e = 0; e < 16; ++e) st[e] *= __shfl(keys.sv, acc_row(e, h), 64);
         }
+        by_rows<MT, DP>([&](int e, int m) { return load1<DP>(keys.V + keys.row_of(acc_row(e, h)), m, l32, p.d); },
+                        [&](int e, int m, float v) { o[m] = mfma_f32(v, st[e], o[m]); });
     }
     // every wave's m and l, then its O in units of the common reference
     float l = l_run + __shfl_xor(l_run, 32, 64);
@@ -416,7 +461,7 @@ __global__ void __launch_bounds__(kThreads) win_rows_kernel(WinParams p) {
 
 // dQ: a wave owns 32 query rows; dS^T = P^T o (V dO^T - delta), dQ^T += K^T dS^T.
 template <typename T, int DP>
-__global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) win_plain_dq_kernel(WinParams p, int row_blocks) {
+__global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) win_plain_dq_kernel(WinParams p, int row_blocks) {
     constexpr int MT = DP / 32;
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int bk = blockIdx.x / row_blocks, b = bk / p.kv_heads, kvh = bk % p.kv_heads;
@@ -447,18 +492,19 @@ __global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) win_plain_dq_kerne
         f32x16 st, dp;
 #pragma unroll
         for (int e = 0; e < 16; ++e) st[e] = dp[e] = 0.f;
-        scores(st, keys.K + keys.at, 1.f, q, p.d, h);
-        scores(dp, keys.V + keys.at, 1.f, g, p.d, h);
+        TileRow<T, DP> key, val;
+        key.init(keys.K + keys.at, p.d, h);
+        val.init(keys.V + keys.at, p.d, h);
+        scores(st, key, 1.f, q);
+        scores(dp, val, 1.f, g);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            const int row = acc_row(e, h), j = j0 + row;
+            const int j = j0 + acc_row(e, h);
             const bool seen = j <= hi && (j >= lo || j < p.sinks);
-            const float ds = seen ? __builtin_amdgcn_exp2f(fmaf(st[e], cs, -lse)) * (dp[e] - delta) : 0.f;
-            const T* k = keys.K + keys.row_of(row);
-#pragma unroll
-            for (int m = 0; m < MT; ++m) dq[m] = mfma_f32(load1<DP>(k, m, l32, p.d), ds, dq[m]);
-            pause<DP>(e, 4);
+            dp[e] = seen ? __builtin_amdgcn_exp2f(fmaf(st[e], cs, -lse)) * (dp[e] - delta) : 0.f;
         }
+        by_rows<MT, DP>([&](int e, int m) { return load1<DP>(keys.K + keys.row_of(acc_row(e, h)), m, l32, p.d); },
+                        [&](int e, int m, float v) { dq[m] = mfma_f32(v, dp[e], dq[m]); });
     }
     extern __shared__ __attribute__((aligned(16))) float meet[];
     meet_waves<MT>(dq, meet, w, lane);
@@ -473,8 +519,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) win_plain_dq_kerne
 }
 
 // dK, dV: a workgroup owns 32 keys; its waves take the 32-token tiles of all heads of the group in turn, with scores [query][key], which
-// are the operands of dV^T += dO^T P and dK^T += Q^T dS as they stand.  The waves' sums meet in LDS.  Blocks 0 .. sink_tiles * parts - 1 of a
-// head work on the sink tiles, a share of the tokens each.  d > 128: the columns of the gradients are shared by two workgroups
+// are the operands of dV^T += dO^T P and dK^T += Q^T dS as they stand.  The waves' sums meet in LDS.  d > 128: the columns of the gradients are shared by two workgroups
 // (blockIdx.y), which both form the scores; one would need 600 registers per lane.
 template <typename T, int DP>
 __global__ void __launch_bounds__(kThreads, 1) win_plain_dkdv_kernel(WinParams p, int key_blocks) {
@@ -483,21 +528,12 @@ __global__ void __launch_bounds__(kThreads, 1) win_plain_dkdv_kernel(WinParams p
     const int m0 = MT * blockIdx.y, c0 = 32 * m0;  // first column of the gradients
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int bk = blockIdx.x / key_blocks, b = bk / p.kv_heads, kvh = bk % p.kv_heads;
-    const int blk = blockIdx.x % key_blocks, shared = p.sink_tiles * p.parts;
-    const int part = blk < shared ? blk % p.parts : -1;
-    const int j0 = 32 * (blk < shared ? blk / p.parts : blk - shared + p.sink_tiles);
     const WinSeq s = win_sequence(p, b);
-    const int j = j0 + l32;
+    WinKeys own;
+    own.init(p, blockIdx.x % key_blocks, 32, s.len);
+    const int j0 = own.j0, i0 = own.i0, i1 = own.i1, j = j0 + l32;
     const long kv = (long)b * p.k_b + (long)kvh * p.k_h;
-    // tokens i0 .. i1 - 1 see some key of the block
-    int i0 = j0, i1 = s.len;
-    if (j0 >= p.sinks) i1 = (int)min((long)s.len, (long)j0 + 31 + p.window);
-    if (part >= 0) {
-        const int share = ((s.len - j0 + p.parts - 1) / p.parts + 31) & ~31;
-        i0 = min(s.len, j0 + part * share);
-        i1 = min(s.len, i0 + share);
-    }
-    const int t_tiles = j0 < s.len ? (i1 - i0 + 31) / 32 : 0, jobs = max(0, t_tiles) * p.group;
+    const int t_tiles = (i1 - i0 + 31) / 32, jobs = t_tiles * p.group;
     const int jr = max(0, min(j, s.len - 1));
     RowOperand<T, DP, DP <= 128> k, v;
     k.init(static_cast<const T*>(p.K) + kv + (long)jr * p.k_n, p.d, h);
@@ -519,31 +555,40 @@ __global__ void __launch_bounds__(kThreads, 1) win_plain_dkdv_kernel(WinParams p
         f32x16 st, dp;
 #pragma unroll
         for (int e = 0; e < 16; ++e) st[e] = dp[e] = 0.f;
-        scores(st, Q + mine, 1.f, k, p.d, h);
-        scores(dp, G + mine, 1.f, v, p.d, h);
+        TileRow<T, DP> query, grad;
+        query.init(Q + mine, p.d, h);
+        grad.init(G + mine, p.d, h);
+        float lse_x[16], delta_x[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            const int x = acc_row(e, h), xc = min(x, last), i = t0 + x;
+            lse_x[e] = lse[min(acc_row(e, h), last)];
+            delta_x[e] = delta[min(acc_row(e, h), last)];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        scores(st, query, 1.f, k);
+        scores(dp, grad, 1.f, v);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int x = acc_row(e, h), i = t0 + x;
             const bool seen = x <= last && j <= i && (i - j < p.window || j < p.sinks);
-            st[e] = seen ? __builtin_amdgcn_exp2f(fmaf(st[e], cs, -lse[xc] * kLog2e)) : 0.f;
-            dp[e] = seen ? st[e] * (dp[e] - delta[xc]) : 0.f;
+            st[e] = seen ? __builtin_amdgcn_exp2f(fmaf(st[e], cs, -lse_x[e] * kLog2e)) : 0.f;
+            dp[e] = seen ? st[e] * (dp[e] - delta_x[e]) : 0.f;
         }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const unsigned row = (unsigned)min(acc_row(e, h), last) * q_n;
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                dv[m] = mfma_f32(load1<DP, (DP >= 192)>(G + row, m, l32, p.d, m0), st[e], dv[m]);
-                dk[m] = mfma_f32(load1<DP, (DP >= 192)>(Q + row, m, l32, p.d, m0), dp[e], dk[m]);
-            }
-            pause<DP>(e, 4);
-        }
+        by_rows<2 * MT, DP>(
+            [&](int e, int x) {
+                const unsigned row = (unsigned)min(acc_row(e, h), last) * q_n;
+                return load1<DP, (DP >= 192)>((x < MT ? G : Q) + row, x % MT, l32, p.d, m0);
+            },
+            [&](int e, int x, float y) {
+                if (x < MT) dv[x] = mfma_f32(y, st[e], dv[x]);
+                else dk[x - MT] = mfma_f32(y, dp[e], dk[x - MT]);
+            });
     }
     meet_waves<MT>(dk, meet, w, lane);
     meet_waves<MT>(dv, meet, w, lane);
     if (w != 0 || j >= p.n) return;
-    if (part >= 0) {
-        float* dst = p.part_kv + (((long)bk * p.sink_tiles + j0 / 32) * p.parts + part) * 2 * 32 * p.d + (long)l32 * p.d;
+    if (own.slot >= 0) {
+        float* dst = p.part_kv + ((long)bk * p.slots + own.slot) * 2 * 32 * p.d + (long)l32 * p.d;
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -563,20 +608,29 @@ __global__ void __launch_bounds__(kThreads, 1) win_plain_dkdv_kernel(WinParams p
         }
 }
 
-// dK and dV of the keys in sink tiles: the sum of the parts, in their order.  Eight lanes per row.
+// dK and dV of keys whose tiles several workgroups work on: the sum of the parts, in their order.  16 to 64 lanes per row.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) win_sink_kernel(WinParams p, int tile) {
-    const int keys = min(p.sink_tiles * tile, p.n);
-    const long f = ((long)blockIdx.x * kThreads + threadIdx.x) >> 3;
-    if (f >= (long)p.batch * p.kv_heads * keys * 2) return;
-    const int which = (int)(f & 1), j = (int)((f >> 1) % keys), bk = (int)((f >> 1) / keys);
-    const float* src = p.part_kv + (((long)bk * p.sink_tiles + j / tile) * p.parts * 2 + which) * tile * p.d + (long)(j % tile) * p.d;
+__global__ void __launch_bounds__(kThreads) win_keys_kernel(WinParams p, int tile, int keys) {
+    const int lanes = p.d <= 64 ? 16 : p.d <= 128 ? 32 : 64;
+    const long f = ((long)blockIdx.x * kThreads + threadIdx.x) / lanes;
+    const int c = 4 * (int)(threadIdx.x & (lanes - 1));
+    if (f >= (long)p.batch * p.kv_heads * keys * 2 || c >= p.d) return;
+    const int which = (int)(f & 1), j = (int)((f >> 1) % keys), bk = (int)((f >> 1) / keys), x = j / tile;
+    const bool sink = x < p.sink_tiles;
+    const int parts = sink ? p.parts : p.rest_parts, slot = sink ? x * p.parts : p.sink_tiles * p.parts + (x - p.sink_tiles) * p.rest_parts;
+    const float* src = p.part_kv + (((long)bk * p.slots + slot) * 2 + which) * tile * p.d + (long)(j % tile) * p.d;
     T* dst = static_cast<T*>(which ? p.dV : p.dK) + (long)(bk / p.kv_heads) * p.k_b + (long)(bk % p.kv_heads) * p.k_h + (long)j * p.k_n;
-    for (int c = 4 * (threadIdx.x & 7); c < p.d; c += 32) {
-        f32x4 sum = load4(src, c, p.d);
-        for (int k = 1; k < p.parts; ++k) sum += load4(src + (long)k * 2 * tile * p.d, c, p.d);
-        store4(dst, c, p.d, sum);
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    constexpr int kAhead = 8;  // parts on the way
+    for (int k0 = 0; k0 < parts; k0 += kAhead) {
+        f32x4 v[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) v[k] = load4(src + (long)min(k0 + k, parts - 1) * 2 * tile * p.d, c, p.d);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (k0 + k < parts) sum += v[k];
     }
+    store4(dst, c, p.d, sum);
 }
 
 // f(width): see kFull
@@ -602,7 +656,7 @@ hipError_t fwd(const WinParams& p, hipStream_t stream) {
 
 template <typename T>
 hipError_t bwd(const WinParams& p, hipStream_t stream) {
-    const int blocks = (int)(((long)p.n * p.group + 31) / 32), keys = (p.n + 31) / 32 - p.sink_tiles + p.sink_tiles * p.parts;
+    const int blocks = (int)(((long)p.n * p.group + 31) / 32), keys = p.sink_tiles * p.parts + ((p.n + 31) / 32 - p.sink_tiles) * p.rest_parts;
     return with_width(p.d, [&](auto width) {
         constexpr int DP = decltype(width)::value;
         hipLaunchKernelGGL((win_plain_dq_kernel<T, DP>), dim3((unsigned)((long)blocks * p.batch * p.kv_heads)), dim3(kThreads), DP * 128, stream, p, blocks);
@@ -637,11 +691,11 @@ hipError_t launch_win_rows(bool is_bf16, const WinParams& p, hipStream_t stream)
     else hipLaunchKernelGGL(win_rows_kernel<float>, grid, dim3(kThreads), 0, stream, p);
     return hipGetLastError();
 }
-hipError_t launch_win_sinks(bool is_bf16, int tile, const WinParams& p, hipStream_t stream) {
-    const long rows = (long)p.batch * p.kv_heads * (p.sink_tiles * tile < p.n ? p.sink_tiles * tile : p.n) * 2;
-    const dim3 grid((unsigned)((rows * 8 + kThreads - 1) / kThreads));
-    if (is_bf16) hipLaunchKernelGGL(win_sink_kernel<__bf16>, grid, dim3(kThreads), 0, stream, p, tile);
-    else hipLaunchKernelGGL(win_sink_kernel<float>, grid, dim3(kThreads), 0, stream, p, tile);
+hipError_t launch_win_keys(bool is_bf16, int tile, const WinParams& p, hipStream_t stream) {
+    const int keys = p.rest_parts > 1 || p.sink_tiles * tile > p.n ? p.n : p.sink_tiles * tile;
+    const dim3 grid((unsigned)(((long)p.batch * p.kv_heads * keys * 2 * (p.d <= 64 ? 16 : p.d <= 128 ? 32 : 64) + kThreads - 1) / kThreads));
+    if (is_bf16) hipLaunchKernelGGL(win_keys_kernel<__bf16>, grid, dim3(kThreads), 0, stream, p, tile, keys);
+    else hipLaunchKernelGGL(win_keys_kernel<float>, grid, dim3(kThreads), 0, stream, p, tile, keys);
     return hipGetLastError();
 }
 

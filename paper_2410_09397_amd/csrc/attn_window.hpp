@@ -29,9 +29,11 @@ struct WinParams {
     // forward: work of a row block shared out over `splits` workgroups of `chunk` tiles each; their sums meet in win_join_kernel
     int splits, chunk;
     float *part_o, *part_ml;  // [row][split][d], [row][split][2], row = token row * heads + head
-    // backward: the key tiles that hold sinks are each worked on by `parts` workgroups; their sums meet in win_sink_kernel
-    int sink_tiles, parts;
-    float* part_kv;  // [batch * kv_heads][sink tile][part][dK, dV][keys of a tile][d]
+    // backward: the first `sink_tiles` key tiles are each worked on by `parts` workgroups, the others by `rest_parts`, each of which takes a
+    // share of the tokens; where there are several, their sums meet in win_keys_kernel
+    int sink_tiles, parts, rest_parts;
+    int slots;  // workgroups of a (sequence, key head) whose sums are parts
+    float* part_kv;  // [batch * kv_heads][slot][dK, dV][keys of a tile][d]
 };
 
 // What a workgroup knows of its sequence.  Everything is uniform; lengths from device memory are brought into the range that the
@@ -109,6 +111,26 @@ __device__ __forceinline__ PageRow win_page_row(const WinParams& p, int page, in
 // 2^(e - 127) for an exponent byte e of 1 .. 254 (0 and 255, which no row is written with, give 0 and infinity).
 __device__ __forceinline__ float exp_value(uint8_t e) { return __builtin_bit_cast(float, (uint32_t)e << 23); }
 
+// What a key owner of the backward works on: keys j0 .. and tokens i0 .. i1 - 1 (which see some of them); slot < 0: all of those, else one part.
+struct WinKeys {
+    int j0, i0, i1, slot;
+    __device__ __forceinline__ void init(const WinParams& p, int blk, int tile, int len) {
+        const int shared = p.sink_tiles * p.parts, r = blk - shared;
+        const int parts = r < 0 ? p.parts : p.rest_parts, part = (r < 0 ? blk : r) % parts;
+        j0 = tile * (r < 0 ? blk / parts : p.sink_tiles + r / parts);
+        slot = parts > 1 ? blk : -1;
+        i1 = j0 < p.sinks ? len : (int)min((long)len, (long)j0 + tile - 1 + p.window);
+        i0 = j0;
+        if (j0 >= len) {
+            i1 = i0;
+        } else if (parts > 1) {
+            const int share = ((i1 - j0 + parts - 1) / parts + tile - 1) / tile * tile;
+            i0 = min(i1, j0 + part * share);
+            i1 = min(i1, i0 + share);
+        }
+    }
+};
+
 // ------------------------------------------------------------------------------------------------------------- host
 // is_bf16: the type of Q, O and of tensors, and of pages that are not quantised (fp8).  The arguments have been checked.
 hipError_t launch_win_plain_fwd(bool is_bf16, bool fp8, const WinParams& p, hipStream_t stream);
@@ -117,7 +139,7 @@ hipError_t launch_win_fwd(bool fp8, int rows, const WinParams& p, hipStream_t st
 hipError_t launch_win_bwd(const WinParams& p, hipStream_t stream);                                // the same; forms delta itself
 hipError_t launch_win_plain_bwd(bool is_bf16, const WinParams& p, hipStream_t stream);
 hipError_t launch_win_join(bool is_bf16, const WinParams& p, hipStream_t stream);
-hipError_t launch_win_sinks(bool is_bf16, int tile, const WinParams& p, hipStream_t stream);
+hipError_t launch_win_keys(bool is_bf16, int tile, const WinParams& p, hipStream_t stream);
 hipError_t launch_win_rows(bool is_bf16, const WinParams& p, hipStream_t stream);  // delta
 hipError_t launch_cache_write(bool is_bf16, bool fp8, const WinParams& p, const void* K, const void* V, long s_n, long s_h, hipStream_t stream);
 hipError_t launch_cache_read(bool is_bf16, bool fp8, const WinParams& p, void* K, void* V, long s_n, long s_h, hipStream_t stream);
