@@ -64,6 +64,13 @@ void set_window(WinParams& p, int32_t window, int32_t sinks, int32_t longest) {
     p.sinks = limits ? sinks : 0;
 }
 
+// Rows of a workgroup: 128, or 64 where blocks of 128 would not be more than the CUs.  us, forward / backward, 128 -> 64 rows, h heads on k key heads:
+//   d = 64    h4 k4 n300 9.4 / 19.8 -> 8.4 / 17.7                d = 256   h8 k2 n1024 55 / 110 -> 36 / 87
+//   d = 128   h8 k2 n1024 26 / 60 -> 20 / 50     h4 k1 n4096 w1024 31 / 74 -> 23 / 62     h16 k2 n2048 48 / 128 -> 39 / 115
+//   beyond the line: d = 64 b2 h16 k4 n2048 w256 16.6 / 56 -> 18.3 / 59
+int block_rows(int64_t blocks128) { return blocks128 <= 256 ? 64 : 128; }
+int win_rows(const attn_win_desc* d) { return block_rows(((int64_t)d->n * (d->heads / d->kv_heads) + 127) / 128 * d->batch * d->kv_heads); }
+
 // Keys of a tile of the backward's key owners.
 int key_tile(const attn_win_desc* d) { return is_wide(d->dtype, d->d) ? 64 : 32; }
 // Workgroups of the key owners.  One streams window + tile tokens per head of its group, one of sink keys all of them: those are shared out over as
@@ -157,15 +164,20 @@ attn_status check_cache(const attn_paged_desc* d, const attn_cache* c) {
 // Rows of a workgroup of the paged forward: see attn_win_fwd.hip.
 int paged_rows(const attn_paged_desc* d) {
     const int64_t rows = (int64_t)d->max_q * (d->heads / d->kv_heads);
-    return !is_wide(d->dtype, d->d) ? 32 : rows > 64 ? 128 : rows > 16 ? 32 : 16;
+    if (!is_wide(d->dtype, d->d)) return 32;
+    // (total_q bounds the row blocks that have rows where the sequences' new tokens differ in number)
+    if (rows > 64)
+        return block_rows(std::min((rows + 127) / 128 * d->batch, (int64_t)d->total_q * (d->heads / d->kv_heads) / 128 + d->batch) * d->kv_heads);
+    return rows > 16 ? 32 : 16;
 }
 
 // How the keys of a row block are shared out: with fewer row blocks than the chip has places for, a workgroup takes `chunk` tiles.
 void set_splits(WinParams& p, const attn_paged_desc* d) {
-    const int64_t rows = paged_rows(d), tile = rows == 128 ? 64 : 32;
-    const bool few = rows < 128;
-    // (total_q bounds the row blocks that have rows where the sequences' new tokens differ in number)
-    const int64_t blocks = std::min((((int64_t)p.n * p.group + rows - 1) / rows) * p.batch, (int64_t)p.total_q * p.group / rows + p.batch) * p.kv_heads;
+    const int64_t rows = paged_rows(d), tile = rows >= 64 ? 64 : 32;
+    const bool few = rows < 64;
+    p.row_blocks = (int)(((int64_t)p.n * p.group + rows - 1) / rows);
+    p.blocks = (int)std::min((int64_t)p.row_blocks * p.batch, (int64_t)p.total_q * p.group / rows + p.batch);
+    const int64_t blocks = (int64_t)p.blocks * p.kv_heads;
     const int64_t keys = std::min<int64_t>(p.max_len, (int64_t)p.window + p.n) + p.sinks, tiles = keys / tile + 2;
     p.splits = 1;
     p.chunk = 0x7fffffff;
@@ -255,7 +267,7 @@ attn_status attn_win_fwd(const attn_win_desc* desc, const int32_t* lens, const v
     p.O = O;
     p.LSE = LSE;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return status_of(is_wide(desc->dtype, desc->d) ? attn::launch_win_fwd(false, 128, p, s) : attn::launch_win_plain_fwd(bf16, false, p, s));
+    return status_of(is_wide(desc->dtype, desc->d) ? attn::launch_win_fwd(false, win_rows(desc), p, s) : attn::launch_win_plain_fwd(bf16, false, p, s));
 }
 
 attn_status attn_win_bwd(const attn_win_desc* desc, const int32_t* lens, const void* Q, const void* K, const void* V, const void* O,
@@ -285,7 +297,7 @@ attn_status attn_win_bwd(const attn_win_desc* desc, const int32_t* lens, const v
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e;
     if (is_wide(desc->dtype, desc->d)) {
-        e = attn::launch_win_bwd(p, s);
+        e = attn::launch_win_bwd(win_rows(desc), p, s);
     } else {
         e = attn::launch_win_rows(bf16, p, s);
         if (e == hipSuccess) e = attn::launch_win_plain_bwd(bf16, p, s);

@@ -1,6 +1,7 @@
 // Windowed attention, backward, bf16 at d in {64, 128, 256}, in the tiling of the backward without a window (attn_bwd.hip), whose
 // layouts, phases and wave priorities these kernels share:
-//   win_dq_kernel    a workgroup owns 128 rows r = t * group + head of the group and streams the 64-key tiles that they see
+//   win_dq_kernel    a workgroup owns 128 rows r = t * group + head of the group and streams the 64-key tiles that they see (SPLIT = 2: 64 rows,
+//                    two waves for 32 of them with a key half of every tile each)
 //   win_dkdv_kernel  a workgroup owns 64 keys and streams the 64-token tiles that see them, of one head of the group after the other: the sum
 //                    over the heads that share the keys is a longer stream into the same accumulators
 // No atomics, so the same call gives the same bits.  A key that is a sink is seen by every token behind it: the tokens that see a tile
@@ -18,18 +19,18 @@ namespace {
 constexpr int kPrioScores = 3, kPrioSoftmax = 0, kPrioProducts = 1;
 
 // ------------------------------------------------------------------------------------------------------------- dQ
-template <int D>
+template <int D, int SPLIT>
 __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dq_kernel(WinParams p, int row_blocks) {
-    constexpr int KS = D / 16, MT = D / 32, kTile = 64 * D * 2;
+    constexpr int KS = D / 16, MT = D / 32, kTile = 64 * D * 2, BR = 128 / SPLIT;
     extern __shared__ __attribute__((aligned(1024))) char smem[];  // [stage][K, V]
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
-    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wq = SPLIT == 1 ? w : w & 1, wk = SPLIT == 1 ? 0 : w >> 1;
     int bk, blk;
     decode_block(blockIdx.x, row_blocks, p.batch * p.kv_heads, bk, blk);
     const int b = bk / p.kv_heads, kvh = bk % p.kv_heads;
     const WinSeq s = win_sequence(p, b);
-    const int rows = s.nq * p.group, r0 = (row_blocks - 1 - blk) * 128;
-    const int w0 = min(r0 + 32 * w, rows - 1), w1 = min(r0 + 32 * w + 31, rows - 1);  // rows of this wave (repeated past the end)
+    const int rows = s.nq * p.group, r0 = (row_blocks - 1 - blk) * BR;
+    const int w0 = min(r0 + 32 * wq, rows - 1), w1 = min(r0 + 32 * wq + 31, rows - 1);  // rows of this wave (repeated past the end)
     auto place = [&](int r, int& t, int& head) {
         t = (int)((unsigned)r / (unsigned)p.group);
         head = kvh * p.group + r - t * p.group;
@@ -40,7 +41,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dq_kernel(WinP
     LaneBounds see;
     see.init(p, t, s.len);
     WinTiles<64> tiles;
-    tiles.init(p, s.len, (int)((unsigned)r0 / (unsigned)p.group), (int)((unsigned)min(r0 + 127, rows - 1) / (unsigned)p.group));
+    tiles.init(p, s.len, (int)((unsigned)r0 / (unsigned)p.group), (int)((unsigned)min(r0 + BR - 1, rows - 1) / (unsigned)p.group));
 
     // Q and dO rows of a wave come through 16 KB (d = 128) of the stages that only this wave reads, then O for delta = rowsum(dO o O), which stays in
     // the workspace for the key owners.  Queries outside their sequence have delta 0.
@@ -80,7 +81,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dq_kernel(WinP
     }
     dl += __shfl_xor(dl, 32, 64);
     if (see.hi < 0) dl = 0.f;
-    if (h == 0 && r0 + 32 * w + l32 < rows) p.delta[stat] = dl;
+    if (h == 0 && wk == 0 && r0 + 32 * wq + l32 < rows) p.delta[stat] = dl;
     settle(lse);
     settle(dl);
     __syncthreads();  // the stages are free
@@ -112,6 +113,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dq_kernel(WinP
         for (int i = 0; i < 16; ++i) dq[mt][i] = 0.f;
     FragAddrs<D> fo;
     fo.init(offsets);
+    if constexpr (SPLIT > 1) fo.shift_rows(32 * wk);
     const float c = p.scale * kLog2e;
     wait_direct_loads();
     __syncthreads();
@@ -119,7 +121,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dq_kernel(WinP
     auto tile = [&](auto stage_off, int j0, bool masked) {
         const int off = stage_off;
 #pragma unroll
-        for (int T = 0; T < 2; ++T) {
+        for (int T = 0; T < 2 / SPLIT; ++T) {
             __builtin_amdgcn_s_setprio(kPrioScores);
             f32x16 st, dp;
 #pragma unroll
@@ -161,10 +163,11 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dq_kernel(WinP
         }
     };
     auto step = [&](auto stage_off, int it) {
-        const int off = stage_off, j0 = tiles.start(it);
+        const int off = stage_off, j0 = tiles.start(it) + 32 * wk;  // (of the keys that this wave looks at)
         if (it + 1 < n_it) request(tiles.start(it + 1), smem + (2 * kTile - off));
-        const bool none = j0 > t_hi || (j0 + 63 < t_lo - p.window + 1 && j0 >= p.sinks) || r0 + 32 * w >= rows;
-        const bool all = j0 + 63 <= t_lo && t_hi < s.len && (t_hi - j0 < p.window || j0 + 63 < p.sinks);
+        constexpr int kLast = 64 / SPLIT - 1;
+        const bool none = j0 > t_hi || (j0 + kLast < t_lo - p.window + 1 && j0 >= p.sinks) || r0 + 32 * wq >= rows;
+        const bool all = j0 + kLast <= t_lo && t_hi < s.len && (t_hi - j0 < p.window || j0 + kLast < p.sinks);
         if (D == 256 || !none) tile(stage_off, j0, !all);  // (see win_out_kernel)
         wait_direct_loads();
         __syncthreads();
@@ -177,8 +180,28 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dq_kernel(WinP
         if (it + 1 < n_it) step(std::integral_constant<int, 2 * kTile>{}, it + 1);
     }
 
+    constexpr int kMeet = SPLIT == 2 ? 2 * 4 * MT * 1024 : 0;
+    if constexpr (SPLIT == 2) {  // the two waves of a row meet in LDS (see win_out_kernel)
+        auto slot = [&](int g) { return reinterpret_cast<f32x4*>(smem) + (wq * 4 * MT + g) * 64 + lane; };
+        if (wk == 1) {
+#pragma unroll
+            for (int g = 0; g < 4 * MT; ++g) {
+                const f32x16& a = dq[g / 4];
+                *slot(g) = f32x4{a[4 * (g % 4)], a[4 * (g % 4) + 1], a[4 * (g % 4) + 2], a[4 * (g % 4) + 3]};
+            }
+        }
+        __syncthreads();
+        if (wk == 1) return;
+#pragma unroll
+        for (int g = 0; g < 4 * MT; ++g) {
+            const f32x4 a = *slot(g);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) dq[g / 4][4 * (g % 4) + e] += a[e];
+        }
+    }
     typedef RowStage<D> Rows;
-    char* out = smem + w * Rows::kBytes;
+    static_assert(kMeet + 4 / SPLIT * Rows::kBytes <= 4 * kTile, "the rows fit the stages");
+    char* out = smem + kMeet + wq * Rows::kBytes;
 #pragma unroll
     for (int g = 0; g < 4 * MT; ++g) {
         const f32x16& a = dq[g / 4];
@@ -190,7 +213,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dq_kernel(WinP
     wave_exchange();
 #pragma unroll
     for (int x = 0; x < 32; x += 64 / Rows::kLanes) {
-        const int row = x + lane / Rows::kLanes, cc = lane % Rows::kLanes, r = r0 + 32 * w + row;
+        const int row = x + lane / Rows::kLanes, cc = lane % Rows::kLanes, r = r0 + 32 * wq + row;
         if (r < rows) {
             int qt, qh;
             place(r, qt, qh);
@@ -434,26 +457,26 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dkdv_kernel(Wi
     Rows::template store<64, 4>(smem + kGrad, static_cast<__bf16*>(p.dK) + out, p.k_n, p.n - j0, lane, w);
 }
 
-template <int D>
+template <int D, int SPLIT>
 hipError_t launch(const WinParams& p, hipStream_t stream) {
-    constexpr int q_lds = 4 * 64 * D * 2, k_lds = q_lds + 2 * 64 * 64 * 2;
-    hipError_t e = allow_lds(win_dq_kernel<D>, q_lds);
+    constexpr int q_lds = 4 * 64 * D * 2, k_lds = q_lds + 2 * 64 * 64 * 2, BR = 128 / SPLIT;
+    hipError_t e = allow_lds(win_dq_kernel<D, SPLIT>, q_lds);
     if (e == hipSuccess) e = allow_lds(win_dkdv_kernel<D>, k_lds);
     if (e != hipSuccess) return e;
-    const int rows = (int)(((long)p.n * p.group + 127) / 128), keys = p.sink_tiles * p.parts + ((p.n + 63) / 64 - p.sink_tiles) * p.rest_parts;
+    const int rows = (int)(((long)p.n * p.group + BR - 1) / BR), keys = p.sink_tiles * p.parts + ((p.n + 63) / 64 - p.sink_tiles) * p.rest_parts;
     const long bk = (long)p.batch * p.kv_heads;
-    hipLaunchKernelGGL(win_dq_kernel<D>, dim3((unsigned)(rows * bk)), dim3(kThreads), q_lds, stream, p, rows);
+    hipLaunchKernelGGL((win_dq_kernel<D, SPLIT>), dim3((unsigned)(rows * bk)), dim3(kThreads), q_lds, stream, p, rows);
     hipLaunchKernelGGL(win_dkdv_kernel<D>, dim3((unsigned)(keys * bk)), dim3(kThreads), k_lds, stream, p, keys);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_win_bwd(const WinParams& p, hipStream_t stream) {
+hipError_t launch_win_bwd(int rows, const WinParams& p, hipStream_t stream) {
     switch (p.d) {
-        case 64: return launch<64>(p, stream);
-        case 128: return launch<128>(p, stream);
-        case 256: return launch<256>(p, stream);
+        case 64: return rows == 64 ? launch<64, 2>(p, stream) : launch<64, 1>(p, stream);
+        case 128: return rows == 64 ? launch<128, 2>(p, stream) : launch<128, 1>(p, stream);
+        case 256: return rows == 64 ? launch<256, 2>(p, stream) : launch<256, 1>(p, stream);
         default: return hipErrorInvalidValue;
     }
 }

@@ -1,7 +1,8 @@
 // Windowed attention, forward, bf16 at d in {64, 128, 256}: over tensors, bf16 pages or quantised pages.
 //
 //   win_out_kernel  128 rows per workgroup (rows r = t * group + head of the group: see attn_window.hpp), 64-key tiles shared by its
-//                   four waves.  Many rows: a prompt, a chunk, training
+//                   four waves.  Many rows: a prompt, a chunk, training.  SPLIT = 2: 64 rows, two waves for 32 of them with a key half
+//                   of every tile each, where blocks of 128 would leave the chip half idle
 //   win_few_kernel  32 rows per workgroup, whose waves take 32-key tiles in turn, each with LDS and softmax state of its own, and meet at
 //                   the end.  A few tokens of a sequence
 //   win_one_kernel  the same with 16 rows.  Single tokens, where the time is that of the keys' way from memory
@@ -176,19 +177,31 @@ struct TileFeed {
     }
 };
 
-template <int D, int SRC>
+template <int D, int SRC, int SPLIT>
 __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_out_kernel(WinParams p, int row_blocks) {
-    constexpr int KS = D / 16, MT = D / 32, kTile = 64 * D * 2;
+    constexpr int KS = D / 16, MT = D / 32, kTile = 64 * D * 2, BR = 128 / SPLIT;
     extern __shared__ __attribute__((aligned(1024))) char smem[];  // [K stage 0][K stage 1][V stage 0][V stage 1]
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
-    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    int bk, blk;
-    decode_block(blockIdx.x, row_blocks, p.batch * p.kv_heads, bk, blk);
-    const int b = bk / p.kv_heads, kvh = bk % p.kv_heads;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wq = SPLIT == 1 ? w : w & 1, wk = SPLIT == 1 ? 0 : w >> 1;
+    int b, kvh, blk;
+    if constexpr (SRC == kTensors) {
+        int bk;
+        decode_block(blockIdx.x, row_blocks, p.batch * p.kv_heads, bk, blk);
+        b = bk / p.kv_heads;
+        kvh = bk % p.kv_heads;
+        blk = row_blocks - 1 - blk;  // the last rows see most keys
+    } else {  // (a key head's blocks on as few XCDs as its number allows)
+        WinBlock at;
+        at.init(p, p.blocks - 1 - (int)(blockIdx.x / p.kv_heads), BR, lane);
+        if (!at.any) return;
+        b = at.b;
+        kvh = blockIdx.x % p.kv_heads;
+        blk = at.blk;
+    }
     const WinSeq s = win_sequence(p, b);
-    const int rows = s.nq * p.group, r0 = (row_blocks - 1 - blk) * 128;  // the last rows see most keys without a window
+    const int rows = s.nq * p.group, r0 = blk * BR;
     if (r0 >= rows) return;
-    const int w0 = min(r0 + 32 * w, rows - 1), w1 = min(r0 + 32 * w + 31, rows - 1);  // rows of this wave (repeated past the end)
+    const int w0 = min(r0 + 32 * wq, rows - 1), w1 = min(r0 + 32 * wq + 31, rows - 1);  // rows of this wave (repeated past the end)
     int t, head, t_lo, t_hi;
     win_place(p, kvh, min(w0 + l32, rows - 1), t, head);
     t_lo = s.first + (int)((unsigned)w0 / (unsigned)p.group);  // positions of its first and last
@@ -197,7 +210,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_out_kernel(Win
     see.init(p, s.first + t, s.len);
     WinTiles<64> tiles;
     tiles.init(p, s.len, s.first + (int)((unsigned)r0 / (unsigned)p.group),
-               s.first + (int)((unsigned)min(r0 + 127, rows - 1) / (unsigned)p.group));
+               s.first + (int)((unsigned)min(r0 + BR - 1, rows - 1) / (unsigned)p.group));
     const int it0 = blockIdx.y * p.chunk, it1 = (int)min((long)tiles.count, (long)it0 + p.chunk);
 
     TileFeed<D, SRC> feed;
@@ -227,13 +240,14 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_out_kernel(Win
     acc.init();
     FragAddrs<D> fo;
     fo.init(offsets);
+    if constexpr (SPLIT > 1) fo.shift_rows(32 * wk);
     fo.shift_transposed(2 * kTile);
     if (it0 < it1) feed.arrive(smem, tid);
     __syncthreads();
 
     constexpr int kPrioScores = 2, kPrioSoftmax = 0, kPrioPV = 1;  // see the forward without a window
     // d = 256: the 32-key halves of a tile one after the other (both at once need 530 registers)
-    constexpr int kTurns = D == 256 ? 2 : 1, NT = 2 / kTurns;
+    constexpr int kTurns = D == 256 && SPLIT == 1 ? 2 : 1, NT = SPLIT == 2 ? 1 : 2 / kTurns;
     auto tile = [&](auto stage_off, int j0, bool masked) {
         const int off = stage_off;
 #pragma unroll
@@ -275,11 +289,12 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_out_kernel(Win
     };
     auto step = [&](auto stage_off, int it) {
         const int off = stage_off;
-        const int j0 = tiles.start(it);
+        const int j0 = tiles.start(it) + 32 * wk;  // of the keys that this wave looks at
         if (it + 1 < it1) feed.request(p, tiles, b, kvh, tiles.start(it + 1), smem + (kTile - off), tid);
         // what this wave's rows see of the tile: nothing, all of it, or a part
-        const bool none = j0 > t_hi || (j0 + 63 < t_lo - p.window + 1 && j0 >= p.sinks) || r0 + 32 * w >= rows;
-        const bool all = j0 + 63 <= t_lo && t_hi < s.len && (t_hi - j0 < p.window || j0 + 63 < p.sinks);
+        constexpr int kLast = 64 / SPLIT - 1;
+        const bool none = j0 > t_hi || (j0 + kLast < t_lo - p.window + 1 && j0 >= p.sinks) || r0 + 32 * wq >= rows;
+        const bool all = j0 + kLast <= t_lo && t_hi < s.len && (t_hi - j0 < p.window || j0 + kLast < p.sinks);
         if (D == 256 || !none) tile(stage_off, j0, !all);  // (d = 256: the branch costs 150 to 420 bytes of scratch)
         if (it + 1 < it1) feed.arrive(smem + (kTile - off), tid);
         __syncthreads();
@@ -292,8 +307,34 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_out_kernel(Win
         if (it + 1 < it1) step(std::integral_constant<int, kTile>{}, it + 1);
     }
 
-    const float l = acc.l + __shfl_xor(acc.l, 32, 64);
-    const bool ok = r0 + 32 * w + l32 < rows, some = l != 0.f;  // (NaN: some)
+    float l = acc.l + __shfl_xor(acc.l, 32, 64);
+    if constexpr (SPLIT == 2) {
+        // the two waves of a row meet in LDS (the stages are free: every wave is past the last barrier): [wave][4 MT groups][64 lanes] x 16 bytes, m, l
+        auto slot = [&](int g) { return reinterpret_cast<f32x4*>(smem) + (wq * 4 * MT + g) * 64 + lane; };
+        float* ml = reinterpret_cast<float*>(smem + 2 * 4 * MT * 1024) + wq * 128;
+        if (wk == 1) {
+#pragma unroll
+            for (int g = 0; g < 4 * MT; ++g) {
+                const f32x16& a = acc.o[g / 4];
+                *slot(g) = f32x4{a[4 * (g % 4)], a[4 * (g % 4) + 1], a[4 * (g % 4) + 2], a[4 * (g % 4) + 3]};
+            }
+            ml[lane] = acc.m;
+            ml[64 + lane] = l;
+        }
+        __syncthreads();
+        if (wk == 1) return;
+        const float m_other = ml[lane], m = __builtin_elementwise_maximum(acc.m, m_other), m_use = m == -__builtin_inff() ? 0.f : m;
+        const float mine = __builtin_amdgcn_exp2f(acc.m - m_use), other = __builtin_amdgcn_exp2f(m_other - m_use);
+        l = l * mine + ml[64 + lane] * other;
+        acc.m = m;
+#pragma unroll
+        for (int g = 0; g < 4 * MT; ++g) {
+            const f32x4 a = *slot(g);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc.o[g / 4][4 * (g % 4) + e] = acc.o[g / 4][4 * (g % 4) + e] * mine + a[e] * other;
+        }
+    }
+    const bool ok = r0 + 32 * wq + l32 < rows, some = l != 0.f;  // (NaN: some)
     if (p.splits > 1) {
         const long row = s.lse_base + (long)t * p.heads + head;
         if (!ok) return;
@@ -315,9 +356,10 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_out_kernel(Win
     const float inv = some ? 1.f / l : 0.f;
     if (ok && h == 0)
         p.LSE[s.lse_base + (long)head * s.lse_h + (long)t * s.lse_t] = some ? (acc.m + __builtin_amdgcn_logf(l)) * kLn2 : -__builtin_inff();
-    typedef RowStage<D> Rows;  // (the stages are free: every wave is past the last barrier)
-    static_assert(4 * Rows::kBytes <= 4 * kTile, "the rows of four waves fit the stages");
-    char* out = smem + w * Rows::kBytes;
+    typedef RowStage<D> Rows;  // (behind what the waves of a row exchange)
+    constexpr int kMeet = SPLIT == 2 ? 2 * 4 * MT * 1024 + 1024 : 0;
+    static_assert(kMeet + 4 / SPLIT * Rows::kBytes <= 4 * kTile, "the rows fit the stages");
+    char* out = smem + kMeet + wq * Rows::kBytes;
 #pragma unroll
     for (int g = 0; g < 4 * MT; ++g) {
         const f32x16& a = acc.o[g / 4];
@@ -326,7 +368,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_out_kernel(Win
     wave_exchange();
 #pragma unroll
     for (int x = 0; x < 32; x += 64 / Rows::kLanes) {
-        const int row = x + lane / Rows::kLanes, c = lane % Rows::kLanes, r = r0 + 32 * w + row;
+        const int row = x + lane / Rows::kLanes, c = lane % Rows::kLanes, r = r0 + 32 * wq + row;
         if (r < rows) {
             int qt, qh;
             win_place(p, kvh, r, qt, qh);
@@ -389,14 +431,17 @@ constexpr int kFewLds = [] {
 }();
 
 template <int D, int SRC>
-__global__ void __launch_bounds__((64 * kFewWaves<D, SRC>), (D == 256 ? 1 : 2)) win_few_kernel(WinParams p, int row_blocks) {
+__global__ void __launch_bounds__((64 * kFewWaves<D, SRC>), (D == 256 ? 1 : 2)) win_few_kernel(WinParams p) {
     constexpr int NW = kFewWaves<D, SRC>, KS = D / 16, MT = D / 32, kTile = 32 * D * 2;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int bk = blockIdx.x / row_blocks, b = bk / p.kv_heads, kvh = bk % p.kv_heads;
+    WinBlock at;
+    at.init(p, (int)(blockIdx.x / p.kv_heads), 32, lane);
+    if (!at.any) return;
+    const int b = at.b, kvh = blockIdx.x % p.kv_heads;
     const WinSeq s = win_sequence(p, b);
-    const int rows = s.nq * p.group, r0 = (blockIdx.x % row_blocks) * 32;
+    const int rows = s.nq * p.group, r0 = at.blk * 32;
     if (r0 >= rows) return;
     const int r1 = min(r0 + 31, rows - 1);
     int t, head;
@@ -527,14 +572,17 @@ template <int D, int SRC>
 constexpr int kOnePerCu = D == 64 ? 4 : D == 128 ? 3 : SRC == kCodes ? 2 : 1;
 
 template <int D, int SRC>
-__global__ void __launch_bounds__(kThreads, (kOnePerCu<D, SRC>)) win_one_kernel(WinParams p, int row_blocks) {
+__global__ void __launch_bounds__(kThreads, (kOnePerCu<D, SRC>)) win_one_kernel(WinParams p) {
     constexpr int NW = 4, MT = D / 16, KS = D / 32, kTile = 32 * D * 2;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, l16 = lane & 15;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int bk = blockIdx.x / row_blocks, b = bk / p.kv_heads, kvh = bk % p.kv_heads;
+    WinBlock at;
+    at.init(p, (int)(blockIdx.x / p.kv_heads), 16, lane);
+    if (!at.any) return;
+    const int b = at.b, kvh = blockIdx.x % p.kv_heads;
     const WinSeq s = win_sequence(p, b);
-    const int rows = s.nq * p.group, r0 = (blockIdx.x % row_blocks) * 16;
+    const int rows = s.nq * p.group, r0 = at.blk * 16;
     if (r0 >= rows) return;
     const int r1 = min(r0 + 15, rows - 1);
     int t, head;
@@ -690,13 +738,14 @@ __global__ void __launch_bounds__(kThreads, (kOnePerCu<D, SRC>)) win_one_kernel(
     few_store<D, NW, 16>(p, s, smem, ml, kvh, r0, r1);
 }
 
-template <int D, int SRC>
+template <int D, int SRC, int SPLIT>
 hipError_t out(const WinParams& p, hipStream_t stream) {
-    constexpr int lds = 4 * 64 * D * 2;
-    const hipError_t e = allow_lds(win_out_kernel<D, SRC>, lds);
+    constexpr int lds = 4 * 64 * D * 2, BR = 128 / SPLIT;
+    const hipError_t e = allow_lds(win_out_kernel<D, SRC, SPLIT>, lds);
     if (e != hipSuccess) return e;
-    const int blocks = (int)(((long)p.n * p.group + 127) / 128);
-    hipLaunchKernelGGL((win_out_kernel<D, SRC>), dim3((unsigned)((long)blocks * p.batch * p.kv_heads), (unsigned)p.splits), dim3(kThreads), lds, stream, p, blocks);
+    const int row_blocks = (int)(((long)p.n * p.group + BR - 1) / BR);
+    const long blocks = SRC == kTensors ? (long)row_blocks * p.batch : p.blocks;
+    hipLaunchKernelGGL((win_out_kernel<D, SRC, SPLIT>), dim3((unsigned)(blocks * p.kv_heads), (unsigned)p.splits), dim3(kThreads), lds, stream, p, row_blocks);
     return hipGetLastError();
 }
 template <int D, int SRC>
@@ -704,9 +753,7 @@ hipError_t few(const WinParams& p, hipStream_t stream) {
     constexpr int lds = kFewLds<D, SRC>;
     const hipError_t e = allow_lds(win_few_kernel<D, SRC>, lds);
     if (e != hipSuccess) return e;
-    const int blocks = (int)(((long)p.n * p.group + 31) / 32);
-    hipLaunchKernelGGL((win_few_kernel<D, SRC>), dim3((unsigned)((long)blocks * p.batch * p.kv_heads), (unsigned)p.splits), dim3(64 * kFewWaves<D, SRC>), lds,
-                       stream, p, blocks);
+    hipLaunchKernelGGL((win_few_kernel<D, SRC>), dim3((unsigned)((long)p.blocks * p.kv_heads), (unsigned)p.splits), dim3(64 * kFewWaves<D, SRC>), lds, stream, p);
     return hipGetLastError();
 }
 template <int D, int SRC>
@@ -714,17 +761,16 @@ hipError_t one(const WinParams& p, hipStream_t stream) {
     constexpr int lds = kOneLds<D, SRC>;
     const hipError_t e = allow_lds(win_one_kernel<D, SRC>, lds);
     if (e != hipSuccess) return e;
-    const int blocks = (int)(((long)p.n * p.group + 15) / 16);
-    hipLaunchKernelGGL((win_one_kernel<D, SRC>), dim3((unsigned)((long)blocks * p.batch * p.kv_heads), (unsigned)p.splits), dim3(kThreads), lds, stream, p,
-                       blocks);
+    hipLaunchKernelGGL((win_one_kernel<D, SRC>), dim3((unsigned)((long)p.blocks * p.kv_heads), (unsigned)p.splits), dim3(kThreads), lds, stream, p);
     return hipGetLastError();
 }
 template <int D>
 hipError_t launch(bool fp8, int rows, const WinParams& p, hipStream_t stream) {
-    if (!p.table) return out<D, kTensors>(p, stream);
+    if (!p.table) return rows == 64 ? out<D, kTensors, 2>(p, stream) : out<D, kTensors, 1>(p, stream);
     if (rows == 16) return fp8 ? one<D, kCodes>(p, stream) : one<D, kPages>(p, stream);
     if (rows == 32) return fp8 ? few<D, kCodes>(p, stream) : few<D, kPages>(p, stream);
-    return fp8 ? out<D, kCodes>(p, stream) : out<D, kPages>(p, stream);
+    if (rows == 64) return fp8 ? out<D, kCodes, 2>(p, stream) : out<D, kPages, 2>(p, stream);
+    return fp8 ? out<D, kCodes, 1>(p, stream) : out<D, kPages, 1>(p, stream);
 }
 
 }  // namespace

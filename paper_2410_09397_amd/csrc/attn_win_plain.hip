@@ -265,9 +265,22 @@ template <typename T, typename E, int DP, bool PAGED>
 __global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) win_plain_out_kernel(WinParams p, int row_blocks) {
     constexpr int MT = DP / 32;
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int bk = blockIdx.x / row_blocks, b = bk / p.kv_heads, kvh = bk % p.kv_heads;
+    int b, kvh, blk;
+    if constexpr (PAGED) {
+        WinBlock block;
+        block.init(p, (int)(blockIdx.x / p.kv_heads), 32, lane);
+        if (!block.any) return;
+        b = block.b;
+        kvh = blockIdx.x % p.kv_heads;
+        blk = block.blk;
+    } else {
+        const int bk = blockIdx.x / row_blocks;
+        b = bk / p.kv_heads;
+        kvh = bk % p.kv_heads;
+        blk = blockIdx.x % row_blocks;
+    }
     const WinSeq s = win_sequence(p, b);
-    const int rows = s.nq * p.group, r0 = (blockIdx.x % row_blocks) * 32;
+    const int rows = s.nq * p.group, r0 = blk * 32;
     if (r0 >= rows) return;
     const int r = min(r0 + l32, rows - 1);
     const RowPlace at = place(p, kvh, r);
@@ -385,12 +398,14 @@ __global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) win_plain_out_kern
 template <typename T, int WAVES>
 __global__ void __launch_bounds__(kThreads) win_join_kernel(WinParams p) {
     __shared__ f32x4 meet[kThreads];
-    const int lane = threadIdx.x & 63, in_row = threadIdx.x % (64 * WAVES), b = blockIdx.y;
+    const int lane = threadIdx.x & 63, in_row = threadIdx.x % (64 * WAVES);
+    const long row = ((long)blockIdx.x * kThreads + threadIdx.x) / (64 * WAVES);
+    const int token = (int)(row / p.heads), head = (int)(row % p.heads);
+    const int b = token < p.total_q ? win_sequence_of(p, __builtin_amdgcn_readfirstlane(token), lane) : -1;
+    if (b < 0) return;  // (of all waves of a row)
     const WinSeq s = win_sequence(p, b);
-    const long f = ((long)blockIdx.x * kThreads + threadIdx.x) / (64 * WAVES);
-    const int t = (int)(f / p.heads), head = (int)(f % p.heads);
-    if (t >= s.nq) return;  // (of all waves of a row)
-    const long row = s.lse_base + (long)t * p.heads + head;
+    const int t = token - (int)(s.lse_base / p.heads);
+    if (t < 0 || t >= s.nq) return;
     const float* ml = p.part_ml + row * p.splits * 2;
     const bool mine = lane < p.splits;
     const float m_k = mine ? ml[2 * lane] : -__builtin_inff(), l_k = mine ? ml[2 * lane + 1] : 0.f;
@@ -461,7 +476,7 @@ __global__ void __launch_bounds__(kThreads) win_rows_kernel(WinParams p) {
 
 // dQ: a wave owns 32 query rows; dS^T = P^T o (V dO^T - delta), dQ^T += K^T dS^T.
 template <typename T, int DP>
-__global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) win_plain_dq_kernel(WinParams p, int row_blocks) {
+__global__ void __launch_bounds__(kThreads, DP <= 64 || (DP == 96 && std::is_same_v<T, float>) ? 2 : 1) win_plain_dq_kernel(WinParams p, int row_blocks) {
     constexpr int MT = DP / 32;
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int bk = blockIdx.x / row_blocks, b = bk / p.kv_heads, kvh = bk % p.kv_heads;
@@ -648,7 +663,7 @@ template <typename T, typename E, bool PAGED>
 hipError_t fwd(const WinParams& p, hipStream_t stream) {
     const int blocks = (int)(((long)p.n * p.group + 31) / 32);
     return with_width(p.d, [&](auto width) {
-        hipLaunchKernelGGL((win_plain_out_kernel<T, E, decltype(width)::value, PAGED>), dim3((unsigned)((long)blocks * p.batch * p.kv_heads), (unsigned)p.splits),
+        hipLaunchKernelGGL((win_plain_out_kernel<T, E, decltype(width)::value, PAGED>), dim3((unsigned)((PAGED ? (long)p.blocks : (long)blocks * p.batch) * p.kv_heads), (unsigned)p.splits),
                            dim3(kThreads), decltype(width)::value * 128 + 1024, stream, p, blocks);
         return hipGetLastError();
     });
@@ -679,7 +694,7 @@ hipError_t launch_win_plain_bwd(bool is_bf16, const WinParams& p, hipStream_t st
 hipError_t launch_win_join(bool is_bf16, const WinParams& p, hipStream_t stream) {
     // four waves for a row that has many parts
     const int waves = p.splits > 8 ? 4 : 1;
-    const dim3 grid((unsigned)(((long)p.n * p.heads * waves + 3) / 4), (unsigned)p.batch);
+    const dim3 grid((unsigned)(((long)p.total_q * p.heads * waves + 3) / 4));
     auto fn = is_bf16 ? (waves == 4 ? win_join_kernel<__bf16, 4> : win_join_kernel<__bf16, 1>)
                       : (waves == 4 ? win_join_kernel<float, 4> : win_join_kernel<float, 1>);
     hipLaunchKernelGGL(fn, grid, dim3(kThreads), 0, stream, p);

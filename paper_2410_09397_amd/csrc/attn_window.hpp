@@ -26,6 +26,7 @@ struct WinParams {
     int page_shift, num_pages, total_q, max_len;
     float scale;
     int window, sinks;  // window > 0; no window: larger than any distance, and no sinks
+    int row_blocks, blocks;  // paged: row blocks of the longest sequence, and at most of all of them
     // forward: work of a row block shared out over `splits` workgroups of `chunk` tiles each; their sums meet in win_join_kernel
     int splits, chunk;
     float *part_o, *part_ml;  // [row][split][d], [row][split][2], row = token row * heads + head
@@ -64,6 +65,57 @@ __device__ __forceinline__ WinSeq win_sequence(const WinParams& p, int b) {
         s.lse_t = 1;
     }
     return s;
+}
+
+// Row block `idx` of all sequences of a paged call, counting only those that have rows: the host knows no more than their number's bound, and a workgroup
+// for every block that the longest sequence could have costs a batch of mixed lengths more than its work (16 sequences of 1 to 256 new tokens:
+// 744 of 1024 without rows).  A wave adds up the sequences' blocks 64 at a time.
+struct WinBlock {
+    int b, blk;
+    bool any;
+    __device__ __forceinline__ void init(const WinParams& p, int idx, int rows_per_block, int lane) {
+        any = true;
+        if (!p.q_ptr || p.row_blocks == 1) {
+            b = idx / p.row_blocks;
+            blk = idx - b * p.row_blocks;
+            return;
+        }
+        for (int base = 0; base < p.batch; base += 64) {
+            const int mine = base + lane;
+            int own = 0;
+            if (mine < p.batch) {
+                const int row0 = min(max(p.q_ptr[mine], 0), p.total_q), rows = min(max(p.q_ptr[mine + 1] - row0, 0), p.total_q - row0);
+                own = (min(rows, p.n) * p.group + rows_per_block - 1) / rows_per_block;
+            }
+            int upto = own;
+#pragma unroll
+            for (int x = 1; x < 64; x <<= 1) {
+                const int before = __shfl_up(upto, x, 64);
+                upto += lane >= x ? before : 0;
+            }
+            const int all = __builtin_amdgcn_readlane(upto, 63);
+            if (idx < all) {
+                const int who = __builtin_ctzl(__builtin_amdgcn_ballot_w64(upto > idx));
+                b = base + who;
+                blk = idx - __builtin_amdgcn_readlane(upto - own, who);
+                return;
+            }
+            idx -= all;
+        }
+        any = false;
+        b = blk = 0;
+    }
+};
+// The sequence that row `row` of a paged call belongs to, or -1.
+__device__ __forceinline__ int win_sequence_of(const WinParams& p, int row, int lane) {
+    if (!p.q_ptr) return row < p.batch * p.n ? row / p.n : -1;
+    for (int base = 0; base < p.batch; base += 64) {
+        const int mine = base + lane;
+        const bool hit = mine < p.batch && row >= p.q_ptr[mine] && row < p.q_ptr[mine + 1];
+        const unsigned long who = __builtin_amdgcn_ballot_w64(hit);
+        if (who) return base + __builtin_ctzl(who);
+    }
+    return -1;
 }
 
 // The key tiles of BC keys that queries at positions i_min .. i_max see some key of: those of the sinks, then those of the windows.
@@ -134,9 +186,9 @@ struct WinKeys {
 // ------------------------------------------------------------------------------------------------------------- host
 // is_bf16: the type of Q, O and of tensors, and of pages that are not quantised (fp8).  The arguments have been checked.
 hipError_t launch_win_plain_fwd(bool is_bf16, bool fp8, const WinParams& p, hipStream_t stream);
-// bf16, d in {64, 128, 256}; rows of a workgroup: 16, 32 (pages), 128
+// bf16, d in {64, 128, 256}; rows of a workgroup: 16, 32 (pages), 64, 128
 hipError_t launch_win_fwd(bool fp8, int rows, const WinParams& p, hipStream_t stream);
-hipError_t launch_win_bwd(const WinParams& p, hipStream_t stream);                                // the same; forms delta itself
+hipError_t launch_win_bwd(int rows, const WinParams& p, hipStream_t stream);                                // rows: 64, 128; forms delta itself
 hipError_t launch_win_plain_bwd(bool is_bf16, const WinParams& p, hipStream_t stream);
 hipError_t launch_win_join(bool is_bf16, const WinParams& p, hipStream_t stream);
 hipError_t launch_win_keys(bool is_bf16, int tile, const WinParams& p, hipStream_t stream);
