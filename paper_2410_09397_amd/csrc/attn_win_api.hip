@@ -47,7 +47,7 @@ attn_status check_win(const attn_win_desc* d) {
     // the tile copies address a tile's rows with 32-bit byte offsets from its first row
     if (d->q_stride_n >= (int64_t)1 << 22 || d->kv_stride_n >= (int64_t)1 << 22) return ATTN_ERR_UNSUPPORTED;
     const int64_t group = d->heads / d->kv_heads, rows = d->n * group, bk = (int64_t)d->batch * d->kv_heads;
-    if (rows > kMostTokens || bk > kMostGroups || ((rows + 31) / 32 + 64) * bk > kMostGroups ||
+    if (rows > kMostTokens || bk > kMostGroups || ((rows + 31) / 32 + 320) * bk > kMostGroups ||
         (int64_t)d->batch * d->heads > kMostGroups || (int64_t)d->batch * d->heads * d->n > kMostGroups * 32)
         return ATTN_ERR_UNSUPPORTED;
     return ATTN_OK;
@@ -64,11 +64,12 @@ void set_window(WinParams& p, int32_t window, int32_t sinks, int32_t longest) {
     p.sinks = limits ? sinks : 0;
 }
 
-// Rows of a workgroup: 128, or 64 where blocks of 128 would not be more than the CUs.  us, forward / backward, 128 -> 64 rows, h heads on k key heads:
+// Rows of a workgroup: 128, or 64 where blocks of 128 would not be more than three for two CUs.  us, forward / backward, 128 -> 64 rows, h heads on k key heads:
 //   d = 64    h4 k4 n300 9.4 / 19.8 -> 8.4 / 17.7                d = 256   h8 k2 n1024 55 / 110 -> 36 / 87
 //   d = 128   h8 k2 n1024 26 / 60 -> 20 / 50     h4 k1 n4096 w1024 31 / 74 -> 23 / 62     h16 k2 n2048 48 / 128 -> 39 / 115
+//   16 sequences of 1 to 256 new tokens, h32 k8 w1024 d = 128 (280 to 336 blocks) 54 -> 44
 //   beyond the line: d = 64 b2 h16 k4 n2048 w256 16.6 / 56 -> 18.3 / 59
-int block_rows(int64_t blocks128) { return blocks128 <= 256 ? 64 : 128; }
+int block_rows(int64_t blocks128) { return blocks128 <= 384 ? 64 : 128; }
 int win_rows(const attn_win_desc* d) { return block_rows(((int64_t)d->n * (d->heads / d->kv_heads) + 127) / 128 * d->batch * d->kv_heads); }
 
 // Keys of a tile of the backward's key owners.
@@ -94,6 +95,8 @@ void set_parts(WinParams& p, int tile) {
         p.rest_parts = (int)rest;
         p.parts = std::min(64, (int)rest * p.parts);
     }
+    // (the sums of the parts are a launch of up to 64 lanes for every key and gradient)
+    if (bk * (p.rest_parts > 1 ? p.n : (int64_t)p.sink_tiles * tile) / 2 > kMostGroups) p.parts = p.rest_parts = 1;
     if (p.parts <= 1) p.sink_tiles = 0;
     p.slots = p.sink_tiles * (p.parts > 1 ? p.parts : 0) + (p.rest_parts > 1 ? (int)(tiles - p.sink_tiles) * p.rest_parts : 0);
 }
@@ -141,7 +144,7 @@ attn_status check_paged(const attn_paged_desc* d) {
         !good_stride(d->page_stride_p, d->num_pages, d->d, page_unit) || !good_stride(d->page_stride_h, d->kv_heads, d->d, page_unit) ||
         !good_stride(d->page_stride_n, d->page_size, d->d, page_unit))
         return ATTN_ERR_INVALID_ARG;
-    if (d->batch > 65535 || d->max_len > kMostTokens) return ATTN_ERR_UNSUPPORTED;
+    if (d->batch > 65535 || d->max_len > kMostTokens || d->total_q > kMostTokens) return ATTN_ERR_UNSUPPORTED;
     if (d->heads == 0) return ATTN_OK;
     const int64_t rows = (int64_t)d->max_q * (d->heads / d->kv_heads);
     if (rows > kMostTokens || ((rows + 15) / 16) * d->batch * d->kv_heads > kMostGroups || ((int64_t)d->max_q * d->heads + 3) / 4 * d->batch > kMostGroups ||
@@ -186,7 +189,7 @@ void set_splits(WinParams& p, const attn_paged_desc* d) {
 #else
     const int64_t want = std::min<int64_t>(64, (few ? 2048 : 512) / std::max<int64_t>(1, blocks));
 #endif
-    if (want > 1 && tiles > 8) {
+    if (want > 1 && tiles > 8 && (int64_t)p.total_q * p.heads <= kMostGroups) {
         p.chunk = (int)std::max<int64_t>(few ? 8 : 4, (tiles + want - 1) / want);
         p.splits = (int)((tiles + p.chunk - 1) / p.chunk);
         if (p.splits <= 1) {

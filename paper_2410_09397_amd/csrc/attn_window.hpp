@@ -134,10 +134,10 @@ struct WinTiles {
     }
     __device__ __forceinline__ int start(int it) const { return (it < ns ? it : it - ns + first) * BC; }
     // The row that is read for key j of a tile: rows that no query of the block sees (behind the end, before the windows, where pages
-    // may be gone) are replaced by one that some query sees.
+    // may be gone) are replaced by one of the same tile that some query sees.
     __device__ __forceinline__ int row(const WinParams& p, int j) const {
         j = min(j, end - 1);
-        return j < lo && j >= p.sinks ? lo : j;
+        return j < lo && j >= p.sinks ? ((j & -BC) < p.sinks ? p.sinks - 1 : lo) : j;
     }
     __device__ __forceinline__ bool whole(const WinParams& p, int j0) const {  // every row of the tile is its own
         return j0 + BC <= end && (j0 >= lo || j0 + BC <= p.sinks);

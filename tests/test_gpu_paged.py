@@ -150,8 +150,8 @@ def test_pages_behind_the_window_may_be_gone(kind, d, new):
     import torch
     from paper_2410_09397_amd import attn
     print("case pages gone", kind, d, new, flush=True)
-    window, sinks, page, lens = 100, 4, 16, [900, 300, 120]
-    c, Q, O, LSE = _paged_case("bf16", kind, lens, [new] * 3, 4, 2, d, page, window, sinks, ragged=False)
+    window, sinks, page, lens = 100, 4, 16, [900, 300, 5000, 120]
+    c, Q, O, LSE = _paged_case("bf16", kind, lens, [new] * 4, 4, 2, d, page, window, sinks, ragged=False)
     for b, l in enumerate(lens):
         first = max(0, l - new - window + 1) // page  # the oldest page that a window reaches into
         for x in range(1, first):
@@ -231,6 +231,17 @@ def test_writing_and_reading_back(dtype, kind, d, page, layout):
         y = window_ref.values(*codes[which]).to(dt).cuda()
         assert same(got[which][:25], y[:25])
         assert not bool(got[which][25].any())  # no page: zeros
+
+
+@pytest.mark.parametrize("kind,d", [("plain", 128), ("fp8", 64), ("plain", 48)])
+def test_a_batch_of_more_than_64_sequences_of_different_numbers_of_new_tokens(kind, d):
+    """Row blocks are counted 64 sequences at a time; some have no new token."""
+    print("case many sequences", kind, d, flush=True)
+    lens = [1 + (37 * i) % 300 for i in range(150)]
+    new = [min(l, (0, 1, 0, 3, 40, 1)[i % 6]) for i, l in enumerate(lens)]
+    _paged_case("bf16", kind, lens, new, 8, 2, d, 16)
+    _paged_case("bf16", kind, lens, [min(1, q) for q in new], 8, 2, d, 16)
+    _paged_case("bf16", kind, [l + 2000 for l in lens], [min(9, q) for q in new], 4, 1, d, 16, window=50, sinks=3)
 
 
 def test_without_row_offsets_every_sequence_has_the_same_number_of_tokens():
