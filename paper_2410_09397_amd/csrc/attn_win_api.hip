@@ -55,8 +55,8 @@ attn_status check_win(const attn_win_desc* d) {
 
 bool is_empty(const attn_win_desc* d) { return d->batch == 0 || d->heads == 0 || d->n == 0; }
 
-// bf16 at these head dimensions has kernels of its own
-bool is_wide(int32_t dtype, int32_t d) { return dtype == ATTN_BF16 && (d == 64 || d == 128 || d == 256); }
+// Whether the bf16-MFMA kernels take a call: bf16 of any head dimension, quantised pages of those that fill a kernel's width.
+bool is_wide(int32_t dtype, int32_t d, bool fp8 = false) { return dtype == ATTN_BF16 && (!fp8 || d == 64 || d == 128 || d == 256); }
 
 void set_window(WinParams& p, int32_t window, int32_t sinks, int32_t longest) {
     const bool limits = window > 0 && window < longest && sinks < longest;
@@ -77,20 +77,20 @@ int key_tile(const attn_win_desc* d) { return is_wide(d->dtype, d->d) ? 64 : 32;
 // Workgroups of the key owners.  One streams window + tile tokens per head of its group, one of sink keys all of them: those are shared out over as
 // many workgroups as make the shares about as long (at most 64, and fewer where there are many sink tiles).  Where all of them
 // together are fewer than the places on the chip, the tokens of every tile are shared out: at least two tiles of tokens to each, and enough of
-// them over all heads of the group (ten; the 32-bit kernels, whose waves take them in turn, six) to pay for the sums' way through memory
+// them over all heads of the group (twelve; the 32-bit kernels, whose waves take them in turn, six) to pay for the sums' way through memory
 // and the launch behind.  us of the backward, one workgroup per tile -> shared, h heads on k key heads:
 //   d = 128, no window   h8 k2 n512 63 -> 39   h8 k2 n1024 114 -> 55   h16 k2 n2048 380 -> 128      d = 256, no window  h8 k2 n1024 211 -> 104
 //   d = 128, window      h4 k1 n4096 w1024 135 -> 76   h16 k4 n2048 w512 85 -> 77   h8 k8 n1024 w256 (too few tiles) 35 -> 45
 //   d = 64               h4 k4 n300 (too few tiles) 20 -> 22      d = 256, window     h8 k4 n2048 w300 (too few tiles) 73 -> 77
 void set_parts(WinParams& p, int tile) {
     const bool wide = tile == 64;
-    const int64_t places = wide && p.d == 256 ? 256 : 512;
+    const int64_t places = wide && p.d > 128 ? 256 : 512;
     const int64_t tiles = (p.n + tile - 1) / tile, bk = (int64_t)p.batch * p.kv_heads;
     const int64_t span = std::min<int64_t>((int64_t)p.window + tile, p.n), token_tiles = (span + tile - 1) / tile;
     p.sink_tiles = p.sinks > 0 ? (int)std::min<int64_t>((p.sinks + tile - 1) / tile, tiles) : 0;
     p.parts = p.rest_parts = 1;
     if (p.sink_tiles > 0) p.parts = (int)std::min<int64_t>(std::min<int64_t>((p.n + span - 1) / span, 64), std::max(1, 256 / p.sink_tiles));
-    const int64_t rest = std::min(std::min(places / std::max<int64_t>(1, tiles * bk), token_tiles / 2), token_tiles * p.group / (wide ? 10 : 6));
+    const int64_t rest = std::min(std::min(places / std::max<int64_t>(1, tiles * bk), token_tiles / 2), token_tiles * p.group / (wide ? 12 : 6));
     if (rest > 1) {
         p.rest_parts = (int)rest;
         p.parts = std::min(64, (int)rest * p.parts);
@@ -167,7 +167,7 @@ attn_status check_cache(const attn_paged_desc* d, const attn_cache* c) {
 // Rows of a workgroup of the paged forward: see attn_win_fwd.hip.
 int paged_rows(const attn_paged_desc* d) {
     const int64_t rows = (int64_t)d->max_q * (d->heads / d->kv_heads);
-    if (!is_wide(d->dtype, d->d)) return 32;
+    if (!is_wide(d->dtype, d->d, d->kind == ATTN_CACHE_FP8)) return 32;
     // (total_q bounds the row blocks that have rows where the sequences' new tokens differ in number)
     if (rows > 64)
         return block_rows(std::min((rows + 127) / 128 * d->batch, (int64_t)d->total_q * (d->heads / d->kv_heads) / 128 + d->batch) * d->kv_heads);
@@ -181,21 +181,19 @@ void set_splits(WinParams& p, const attn_paged_desc* d) {
     p.row_blocks = (int)(((int64_t)p.n * p.group + rows - 1) / rows);
     p.blocks = (int)std::min((int64_t)p.row_blocks * p.batch, (int64_t)p.total_q * p.group / rows + p.batch);
     const int64_t blocks = (int64_t)p.blocks * p.kv_heads;
-    const int64_t keys = std::min<int64_t>(p.max_len, (int64_t)p.window + p.n) + p.sinks, tiles = keys / tile + 2;
+    // (the windows of a block reach over window + its tokens - 1 keys, which lie in one tile more than they fill, as the sinks do)
+    const int64_t keys = std::min<int64_t>(p.max_len, (int64_t)p.window + p.n) + p.sinks, tiles = keys / tile + 3;
+    // How many: as many as there are places (some more for few rows, whose lengths differ), but not in pieces so small that the launch that
+    // joins them costs more than they save.  us, split -> not: one token of b sequences of L keys, d = 128, quantised: b1 L600 11.0 -> 10.4,
+    // b1 L1000 11.2 -> 13.6, b64 L1000 33 -> 24; d = 256: b1 L300 12.9 -> 11.4, b1 L600 13.0 -> 14.9
+    const int64_t want = std::min<int64_t>(64, (few ? 2048 : 512) / std::max<int64_t>(1, blocks));
+    const int64_t least = !few ? 16 : blocks >= 256 ? 32 : p.d > 128 ? 8 : 12;  // tiles
+    const int64_t splits = (int64_t)p.total_q * p.heads <= kMostGroups ? std::min(want, tiles / least) : 1;
     p.splits = 1;
     p.chunk = 0x7fffffff;
-    #ifdef WANT_FEW
-    const int64_t want = std::min<int64_t>(64, (few ? WANT_FEW : WANT_OUT) / std::max<int64_t>(1, blocks));
-#else
-    const int64_t want = std::min<int64_t>(64, (few ? 2048 : 512) / std::max<int64_t>(1, blocks));
-#endif
-    if (want > 1 && tiles > 8 && (int64_t)p.total_q * p.heads <= kMostGroups) {
-        p.chunk = (int)std::max<int64_t>(few ? 8 : 4, (tiles + want - 1) / want);
+    if (splits > 1) {
+        p.chunk = (int)((tiles + splits - 1) / splits);
         p.splits = (int)((tiles + p.chunk - 1) / p.chunk);
-        if (p.splits <= 1) {
-            p.splits = 1;
-            p.chunk = 0x7fffffff;
-        }
     }
 }
 
@@ -299,11 +297,11 @@ attn_status attn_win_bwd(const attn_win_desc* desc, const int32_t* lens, const v
     p.part_kv = reinterpret_cast<float*>(static_cast<char*>(workspace) + rows_bytes(desc));
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e;
-    if (is_wide(desc->dtype, desc->d)) {
+    if (bf16) {
         e = attn::launch_win_bwd(win_rows(desc), p, s);
     } else {
-        e = attn::launch_win_rows(bf16, p, s);
-        if (e == hipSuccess) e = attn::launch_win_plain_bwd(bf16, p, s);
+        e = attn::launch_win_rows(p, s);
+        if (e == hipSuccess) e = attn::launch_win_plain_bwd(p, s);
     }
     if (e == hipSuccess && p.slots > 0) e = attn::launch_win_keys(bf16, key_tile(desc), p, s);
     return status_of(e);
@@ -357,7 +355,7 @@ attn_status attn_paged_fwd(const attn_paged_desc* desc, const attn_cache* cache,
     p.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + part_ml_bytes(desc, p));
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool fp8 = desc->kind == ATTN_CACHE_FP8;
-    hipError_t e = is_wide(desc->dtype, desc->d) ? attn::launch_win_fwd(fp8, paged_rows(desc), p, s) : attn::launch_win_plain_fwd(bf16, fp8, p, s);
+    hipError_t e = is_wide(desc->dtype, desc->d, fp8) ? attn::launch_win_fwd(fp8, paged_rows(desc), p, s) : attn::launch_win_plain_fwd(bf16, fp8, p, s);
     if (e == hipSuccess && p.splits > 1) e = attn::launch_win_join(bf16, p, s);
     return status_of(e);
 }

@@ -1,4 +1,4 @@
-// Windowed attention, backward, bf16 at d in {64, 128, 256}, in the tiling of the backward without a window (attn_bwd.hip), whose
+// Windowed attention, backward, bf16 (widths of 64, 128 and 256 columns, other rows padded: see attn_win_fwd.hip), in the tiling of the backward without a window (attn_bwd.hip), whose
 // layouts, phases and wave priorities these kernels share:
 //   win_dq_kernel    a workgroup owns 128 rows r = t * group + head of the group and streams the 64-key tiles that they see (SPLIT = 2: 64 rows,
 //                    two waves for 32 of them with a key half of every tile each)
@@ -19,7 +19,7 @@ namespace {
 constexpr int kPrioScores = 3, kPrioSoftmax = 0, kPrioProducts = 1;
 
 // ------------------------------------------------------------------------------------------------------------- dQ
-template <int D, int SPLIT>
+template <int D, int SPLIT, bool PAD>
 __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dq_kernel(WinParams p, int row_blocks) {
     constexpr int KS = D / 16, MT = D / 32, kTile = 64 * D * 2, BR = 128 / SPLIT;
     extern __shared__ __attribute__((aligned(1024))) char smem[];  // [stage][K, V]
@@ -52,8 +52,8 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dq_kernel(WinP
             const int row = CopyLane<D>::row_of(u, lane);
             int qt, qh;
             place(min(w0 + row, rows - 1), qt, qh);
-            copy_row(reinterpret_cast<const char*>(static_cast<const __bf16*>(base) + s.q_base + (long)qh * p.q_h + (long)qt * p.q_n) + CopyLane<D>::byte_of(row, lane),
-                     lds_address(to + u * 1024));
+            const __bf16* from = static_cast<const __bf16*>(base) + s.q_base + (long)qh * p.q_h + (long)qt * p.q_n;
+            copy_row(CopyLane<D>::template at<PAD>(reinterpret_cast<const char*>(from), row, lane, p.d), lds_address(to + u * 1024));
         }
     };
     copy_rows(p.Q, mine);
@@ -91,16 +91,16 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dq_kernel(WinP
     const long kv = (long)b * p.k_b + (long)kvh * p.k_h;
     const __bf16 *K = static_cast<const __bf16*>(p.K) + kv, *V = static_cast<const __bf16*>(p.V) + kv;
     auto request = [&](int j0, char* stage) {
-        if (tiles.whole(p, j0)) {
+        if (!PAD && tiles.whole(p, j0)) {
             loader.load(K + (long)j0 * p.k_n, stage);
             loader.load(V + (long)j0 * p.k_n, stage + kTile);
         } else {
 #pragma unroll
             for (int u = 0; u < 64 / (4 * CopyLane<D>::kRows); ++u) {
                 const int inst = u * 4 + w, row = CopyLane<D>::row_of(inst, lane);
-                const long at = (long)tiles.row(p, j0 + row) * p.k_n * 2 + CopyLane<D>::byte_of(row, lane);
-                copy_row(reinterpret_cast<const char*>(K) + at, lds_address(stage + inst * 1024));
-                copy_row(reinterpret_cast<const char*>(V) + at, lds_address(stage + kTile + inst * 1024));
+                const long at = (long)tiles.row(p, j0 + row) * p.k_n;
+                copy_row(CopyLane<D>::template at<PAD>(reinterpret_cast<const char*>(K + at), row, lane, p.d), lds_address(stage + inst * 1024));
+                copy_row(CopyLane<D>::template at<PAD>(reinterpret_cast<const char*>(V + at), row, lane, p.d), lds_address(stage + kTile + inst * 1024));
             }
         }
     };
@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dq_kernel(WinP
 #pragma unroll
     for (int x = 0; x < 32; x += 64 / Rows::kLanes) {
         const int row = x + lane / Rows::kLanes, cc = lane % Rows::kLanes, r = r0 + 32 * wq + row;
-        if (r < rows) {
+        if (r < rows && (!PAD || 8 * cc < p.d)) {
             int qt, qh;
             place(r, qt, qh);
             *reinterpret_cast<u32x4*>(static_cast<__bf16*>(p.dQ) + s.q_base + (long)qh * p.q_h + (long)qt * p.q_n + 8 * cc) =
@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dq_kernel(WinP
 // --------------------------------------------------------------------------------------------------------- dK, dV
 // Phase 1, wave (wk, wx): S^T and dP^T for key half wk and token half wx; P and dS to LDS as [token][key] tiles.
 // Phase 2: dV^T (wx = 0) or dK^T (wx = 1) for the half wk of d, all 64 keys and tokens.
-template <int D>
+template <int D, bool PAD>
 __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dkdv_kernel(WinParams p, int key_blocks) {
     constexpr int KS = D / 16, MT = D / 32, MH = MT / 2, kTile = 64 * D * 2, kStage = 2 * kTile, kP = 64 * 64 * 2;
     extern __shared__ __attribute__((aligned(1024))) char smem[];  // [stage][Q, dO], P, dS
@@ -265,9 +265,24 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dkdv_kernel(Wi
             lse_raw = lse_g[(long)g_next * s.lse_h + i];
             delta_raw = delta_g[(long)g_next * s.lse_h + i];
         };
+        // 64 rows from `row0` on; rows from `end` on repeat the last one
+        auto load_rows = [&](const TileLoader<D, 64>& by, const __bf16* base, long ld, int row0, int end, char* to) {
+            if constexpr (PAD) {
+                int l = lane;  // (formed again for every tile: d > 128 has no registers to keep what a lane copies)
+                asm volatile("" : "+v"(l));
+#pragma unroll
+                for (int u = 0; u < 64 / (4 * CopyLane<D>::kRows); ++u) {
+                    const int inst = u * 4 + w, row = CopyLane<D>::row_of(inst, l);
+                    const __bf16* from = base + (long)min(row0 + row, end - 1) * ld;
+                    copy_row(CopyLane<D>::template at<PAD>(reinterpret_cast<const char*>(from), row, l, p.d), lds_address(to + inst * 1024));
+                }
+            } else {
+                by.load(base, ld, row0, end, to, tid);
+            }
+        };
         auto fetch = [&](char* stage) {
-            loader.load(Qh + (long)g_next * p.q_h, p.q_n, ti_next, i1, stage, tid);
-            loader.load(Gh + (long)g_next * p.q_h, p.q_n, ti_next, i1, stage + kTile, tid);
+            load_rows(loader, Qh + (long)g_next * p.q_h, p.q_n, ti_next, i1, stage);
+            load_rows(loader, Gh + (long)g_next * p.q_h, p.q_n, ti_next, i1, stage + kTile);
             fetch_rows();
         };
         auto advance = [&] {
@@ -282,8 +297,8 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dkdv_kernel(Wi
             // the owned rows come through the second stage; rows past the sequence repeat its last one, which nothing sees
             TileLoader<D, 64> own;
             own.init(tid, p.k_n);
-            own.load(static_cast<const __bf16*>(p.K) + kv, p.k_n, j0, s.len, smem + kStage, tid);
-            own.load(static_cast<const __bf16*>(p.V) + kv, p.k_n, j0, s.len, smem + kStage + kTile, tid);
+            load_rows(own, static_cast<const __bf16*>(p.K) + kv, p.k_n, j0, s.len, smem + kStage);
+            load_rows(own, static_cast<const __bf16*>(p.V) + kv, p.k_n, j0, s.len, smem + kStage + kTile);
         }
         fetch(smem);
         FragOffsets<D> fo;
@@ -327,7 +342,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dkdv_kernel(Wi
             char* next_stage = smem + (kStage - q_off);
             if (it + 1 < jobs) {
                 advance();
-                spread = ti_next + 64 <= i1;
+                spread = !PAD && ti_next + 64 <= i1;
                 if (spread) {
                     next_q = Qh + (long)g_next * p.q_h + (long)ti_next * p.q_n;
                     next_g = Gh + (long)g_next * p.q_h + (long)ti_next * p.q_n;
@@ -423,7 +438,8 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dkdv_kernel(Wi
     }
 
     if (keys.slot >= 0) {  // fp32 sums of this part: [dK, dV][64 keys][d]
-        float* dst = p.part_kv + (((long)bk * p.slots + keys.slot) * 2 + (wx == 0 ? 1 : 0)) * 64 * D;
+        const int d = PAD ? p.d : D;
+        float* dst = p.part_kv + (((long)bk * p.slots + keys.slot) * 2 + (wx == 0 ? 1 : 0)) * 64 * d;
         const float f = wx == 0 ? 1.f : p.scale;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
@@ -432,7 +448,8 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dkdv_kernel(Wi
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     const f32x16& a = acc[m][kt];
-                    *reinterpret_cast<f32x4*>(dst + (32 * kt + l32) * D + 32 * (MH * wk + m) + 8 * g + 4 * h) =
+                    if (32 * (MH * wk + m) + 8 * g < d)
+                        *reinterpret_cast<f32x4*>(dst + (32 * kt + l32) * d + 32 * (MH * wk + m) + 8 * g + 4 * h) =
                         f32x4{a[4 * g] * f, a[4 * g + 1] * f, a[4 * g + 2] * f, a[4 * g + 3] * f};
                 }
         return;
@@ -453,32 +470,33 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dkdv_kernel(Wi
             }
     __syncthreads();
     const long out = kv + (long)j0 * p.k_n;
+    if (PAD && 8 * (lane % Rows::kLanes) >= p.d) return;  // (the columns of a lane are the same in every row that it stores)
     Rows::template store<64, 4>(smem, static_cast<__bf16*>(p.dV) + out, p.k_n, p.n - j0, lane, w);
     Rows::template store<64, 4>(smem + kGrad, static_cast<__bf16*>(p.dK) + out, p.k_n, p.n - j0, lane, w);
 }
 
-template <int D, int SPLIT>
+template <int D, int SPLIT, bool PAD>
 hipError_t launch(const WinParams& p, hipStream_t stream) {
     constexpr int q_lds = 4 * 64 * D * 2, k_lds = q_lds + 2 * 64 * 64 * 2, BR = 128 / SPLIT;
-    hipError_t e = allow_lds(win_dq_kernel<D, SPLIT>, q_lds);
-    if (e == hipSuccess) e = allow_lds(win_dkdv_kernel<D>, k_lds);
+    hipError_t e = allow_lds(win_dq_kernel<D, SPLIT, PAD>, q_lds);
+    if (e == hipSuccess) e = allow_lds(win_dkdv_kernel<D, PAD>, k_lds);
     if (e != hipSuccess) return e;
     const int rows = (int)(((long)p.n * p.group + BR - 1) / BR), keys = p.sink_tiles * p.parts + ((p.n + 63) / 64 - p.sink_tiles) * p.rest_parts;
     const long bk = (long)p.batch * p.kv_heads;
-    hipLaunchKernelGGL((win_dq_kernel<D, SPLIT>), dim3((unsigned)(rows * bk)), dim3(kThreads), q_lds, stream, p, rows);
-    hipLaunchKernelGGL(win_dkdv_kernel<D>, dim3((unsigned)(keys * bk)), dim3(kThreads), k_lds, stream, p, keys);
+    hipLaunchKernelGGL((win_dq_kernel<D, SPLIT, PAD>), dim3((unsigned)(rows * bk)), dim3(kThreads), q_lds, stream, p, rows);
+    hipLaunchKernelGGL((win_dkdv_kernel<D, PAD>), dim3((unsigned)(keys * bk)), dim3(kThreads), k_lds, stream, p, keys);
     return hipGetLastError();
+}
+template <int D>
+hipError_t launch(int rows, const WinParams& p, hipStream_t stream) {
+    if (p.d < D) return rows == 64 ? launch<D, 2, true>(p, stream) : launch<D, 1, true>(p, stream);
+    return rows == 64 ? launch<D, 2, false>(p, stream) : launch<D, 1, false>(p, stream);
 }
 
 }  // namespace
 
 hipError_t launch_win_bwd(int rows, const WinParams& p, hipStream_t stream) {
-    switch (p.d) {
-        case 64: return rows == 64 ? launch<64, 2>(p, stream) : launch<64, 1>(p, stream);
-        case 128: return rows == 64 ? launch<128, 2>(p, stream) : launch<128, 1>(p, stream);
-        case 256: return rows == 64 ? launch<256, 2>(p, stream) : launch<256, 1>(p, stream);
-        default: return hipErrorInvalidValue;
-    }
+    return p.d <= 64 ? launch<64>(rows, p, stream) : p.d <= 128 ? launch<128>(rows, p, stream) : launch<256>(rows, p, stream);
 }
 
 }  // namespace attn

@@ -1,4 +1,5 @@
-// Windowed attention, forward, bf16 at d in {64, 128, 256}: over tensors, bf16 pages or quantised pages.
+// Windowed attention, forward, bf16: over tensors, bf16 pages or (d in {64, 128, 256}) quantised pages.  Kernels have widths of 64, 128 and 256
+// columns; rows of another d are padded with zeros on their way into LDS and registers (PAD).
 //
 //   win_out_kernel  128 rows per workgroup (rows r = t * group + head of the group: see attn_window.hpp), 64-key tiles shared by its
 //                   four waves.  Many rows: a prompt, a chunk, training.  SPLIT = 2: 64 rows, two waves for 32 of them with a key half
@@ -109,7 +110,7 @@ __device__ __forceinline__ void win_sign(float scale, bf16x8 (&qf)[KS]) {
 
 // ------------------------------------------------------------------------------------------------------- many rows
 // Tiles of 64 keys for a workgroup of four waves, K and V at once.
-template <int D, int SRC>
+template <int D, int SRC, bool PAD>
 struct TileFeed {
     static constexpr int kBytes = 64 * D * 2, kInst = 64 / (4 * CopyLane<D>::kRows);
     static constexpr int kChunks = D / 64;  // 16-code chunks per thread and tensor
@@ -126,16 +127,17 @@ struct TileFeed {
         if constexpr (SRC == kTensors) {
             const long base = (long)b * p.k_b + (long)kvh * p.k_h;
             const __bf16 *K = static_cast<const __bf16*>(p.K) + base, *V = static_cast<const __bf16*>(p.V) + base;
-            if (tiles.whole(p, j0)) {
+            if (!PAD && tiles.whole(p, j0)) {
                 loader.load(K + (long)j0 * p.k_n, stage);
                 loader.load(V + (long)j0 * p.k_n, stage + 2 * kBytes);
             } else {
 #pragma unroll
                 for (int u = 0; u < kInst; ++u) {
                     const int inst = u * 4 + w, row = CopyLane<D>::row_of(inst, lane);
-                    const long at = (long)tiles.row(p, j0 + row) * p.k_n * 2 + CopyLane<D>::byte_of(row, lane);
-                    copy_row(reinterpret_cast<const char*>(K) + at, lds_address(stage + inst * 1024));
-                    copy_row(reinterpret_cast<const char*>(V) + at, lds_address(stage + 2 * kBytes + inst * 1024));
+                    const long at = (long)tiles.row(p, j0 + row) * p.k_n;
+                    copy_row(CopyLane<D>::template at<PAD>(reinterpret_cast<const char*>(K + at), row, lane, p.d), lds_address(stage + inst * 1024));
+                    copy_row(CopyLane<D>::template at<PAD>(reinterpret_cast<const char*>(V + at), row, lane, p.d),
+                             lds_address(stage + 2 * kBytes + inst * 1024));
                 }
             }
         } else {
@@ -144,9 +146,10 @@ struct TileFeed {
 #pragma unroll
                 for (int u = 0; u < kInst; ++u) {
                     const int inst = u * 4 + w, row = CopyLane<D>::row_of(inst, lane), j = tiles.row(p, j0 + row);
-                    const long at = win_page_row(p, pages.page(p, j), kvh, j).at * 2 + CopyLane<D>::byte_of(row, lane);
-                    copy_row(static_cast<const char*>(p.K) + at, lds_address(stage + inst * 1024));
-                    copy_row(static_cast<const char*>(p.V) + at, lds_address(stage + 2 * kBytes + inst * 1024));
+                    const long at = win_page_row(p, pages.page(p, j), kvh, j).at * 2;
+                    copy_row(CopyLane<D>::template at<PAD>(static_cast<const char*>(p.K) + at, row, lane, p.d), lds_address(stage + inst * 1024));
+                    copy_row(CopyLane<D>::template at<PAD>(static_cast<const char*>(p.V) + at, row, lane, p.d),
+                             lds_address(stage + 2 * kBytes + inst * 1024));
                 }
             } else {
 #pragma unroll
@@ -177,7 +180,7 @@ struct TileFeed {
     }
 };
 
-template <int D, int SRC, int SPLIT>
+template <int D, int SRC, int SPLIT, bool PAD>
 __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_out_kernel(WinParams p, int row_blocks) {
     constexpr int KS = D / 16, MT = D / 32, kTile = 64 * D * 2, BR = 128 / SPLIT;
     extern __shared__ __attribute__((aligned(1024))) char smem[];  // [K stage 0][K stage 1][V stage 0][V stage 1]
@@ -213,7 +216,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_out_kernel(Win
                s.first + (int)((unsigned)min(r0 + BR - 1, rows - 1) / (unsigned)p.group));
     const int it0 = blockIdx.y * p.chunk, it1 = (int)min((long)tiles.count, (long)it0 + p.chunk);
 
-    TileFeed<D, SRC> feed;
+    TileFeed<D, SRC, PAD> feed;
     feed.init(p, tid);
     // the Q rows come through a piece of the second stage that only this wave reads
     char* mine = smem + (w < 2 ? 1 : 3) * kTile + (w & 1) * (32 * D * 2);
@@ -222,8 +225,8 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_out_kernel(Win
         const int row = CopyLane<D>::row_of(u, lane);
         int qt, qh;
         win_place(p, kvh, min(w0 + row, rows - 1), qt, qh);
-        copy_row(reinterpret_cast<const char*>(static_cast<const __bf16*>(p.Q) + s.q_base + (long)qh * p.q_h + (long)qt * p.q_n) + CopyLane<D>::byte_of(row, lane),
-                 lds_address(mine + u * 1024));
+        const __bf16* from = static_cast<const __bf16*>(p.Q) + s.q_base + (long)qh * p.q_h + (long)qt * p.q_n;
+        copy_row(CopyLane<D>::template at<PAD>(reinterpret_cast<const char*>(from), row, lane, p.d), lds_address(mine + u * 1024));
     }
     if (it0 < it1) feed.request(p, tiles, b, kvh, tiles.start(it0), smem, tid);
     FragOffsets<D> offsets;
@@ -344,12 +347,14 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_out_kernel(Win
             ml[1] = l;
         }
         if (some) {
-            float* dst = p.part_o + (row * p.splits + blockIdx.y) * D + 4 * h;
+            const int d = PAD ? p.d : D;
+            float* dst = p.part_o + (row * p.splits + blockIdx.y) * d + 4 * h;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
-                    *reinterpret_cast<f32x4*>(dst + 32 * mt + 8 * g) = f32x4{acc.o[mt][4 * g], acc.o[mt][4 * g + 1], acc.o[mt][4 * g + 2], acc.o[mt][4 * g + 3]};
+                    if (32 * mt + 8 * g < d)
+                        *reinterpret_cast<f32x4*>(dst + 32 * mt + 8 * g) = f32x4{acc.o[mt][4 * g], acc.o[mt][4 * g + 1], acc.o[mt][4 * g + 2], acc.o[mt][4 * g + 3]};
         }
         return;
     }
@@ -369,7 +374,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_out_kernel(Win
 #pragma unroll
     for (int x = 0; x < 32; x += 64 / Rows::kLanes) {
         const int row = x + lane / Rows::kLanes, c = lane % Rows::kLanes, r = r0 + 32 * wq + row;
-        if (r < rows) {
+        if (r < rows && (!PAD || 8 * c < p.d)) {
             int qt, qh;
             win_place(p, kvh, r, qt, qh);
             *reinterpret_cast<u32x4*>(static_cast<__bf16*>(p.O) + s.q_base + (long)qh * p.q_h + (long)qt * p.q_n + 8 * c) =
@@ -379,14 +384,14 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_out_kernel(Win
 }
 
 // Rows r0 .. r1 of a workgroup from its waves' sums in LDS ([wave][ROWS][D + 4] fp32 and [wave][ROWS][m, l]): to O and LSE, or to the parts.
-template <int D, int NW, int ROWS>
+template <int D, int NW, int ROWS, bool PAD>
 __device__ __forceinline__ void few_store(const WinParams& p, const WinSeq& s, const char* smem, const float* ml, int kvh, int r0, int r1) {
     constexpr int kPitch = D * 4 + 16;
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, d = PAD ? p.d : D;
     constexpr int kLanes = D / 4;  // threads per row
     for (int row = tid / kLanes; row < ROWS; row += 64 * NW / kLanes) {
         const int r = r0 + row, c = 4 * (tid % kLanes);
-        if (r > r1) break;
+        if (r > r1 || c >= d) break;
         float m = -__builtin_inff();
 #pragma unroll
         for (int x = 0; x < NW; ++x) m = __builtin_elementwise_maximum(m, ml[(x * ROWS + row) * 2]);
@@ -408,7 +413,7 @@ __device__ __forceinline__ void few_store(const WinParams& p, const WinSeq& s, c
                 p.part_ml[(at * p.splits + blockIdx.y) * 2] = m;
                 p.part_ml[(at * p.splits + blockIdx.y) * 2 + 1] = sum_l;
             }
-            if (some) *reinterpret_cast<f32x4*>(p.part_o + (at * p.splits + blockIdx.y) * D + c) = sum;
+            if (some) *reinterpret_cast<f32x4*>(p.part_o + (at * p.splits + blockIdx.y) * d + c) = sum;
         } else {
             const float inv = some ? 1.f / sum_l : 0.f;
             if (c == 0) p.LSE[at] = some ? (m + __builtin_amdgcn_logf(sum_l)) * kLn2 : -__builtin_inff();
@@ -430,7 +435,7 @@ constexpr int kFewLds = [] {
     return stages > meet ? stages : meet;
 }();
 
-template <int D, int SRC>
+template <int D, int SRC, bool PAD>
 __global__ void __launch_bounds__((64 * kFewWaves<D, SRC>), (D == 256 ? 1 : 2)) win_few_kernel(WinParams p) {
     constexpr int NW = kFewWaves<D, SRC>, KS = D / 16, MT = D / 32, kTile = 32 * D * 2;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -454,9 +459,9 @@ __global__ void __launch_bounds__((64 * kFewWaves<D, SRC>), (D == 256 ? 1 : 2)) 
     const int it0 = blockIdx.y * p.chunk, it1 = (int)min((long)tiles.count, (long)it0 + p.chunk);
 
     bf16x8 qf[KS];
-    const __bf16* q = static_cast<const __bf16*>(p.Q) + s.q_base + (long)head * p.q_h + (long)t * p.q_n + 8 * h;
+    const char* q = reinterpret_cast<const char*>(static_cast<const __bf16*>(p.Q) + s.q_base + (long)head * p.q_h + (long)t * p.q_n);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8*>(q + 16 * ks);
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = __builtin_bit_cast(bf16x8, load_chunk<PAD>(q, 2 * ks + h, p.d));
     win_sign(p.scale, qf);
     const float cs = win_scale(p.scale);
     WinRows<D> acc;
@@ -480,9 +485,9 @@ __global__ void __launch_bounds__((64 * kFewWaves<D, SRC>), (D == 256 ? 1 : 2)) 
 #pragma unroll
             for (int u = 0; u < kInst; ++u) {
                 const int row = CopyLane<D>::row_of(u, lane), j = tiles.row(p, j0 + row);
-                const long at = win_page_row(p, pages.page(p, j), kvh, j).at * 2 + CopyLane<D>::byte_of(row, lane);
-                copy_row(static_cast<const char*>(p.K) + at, lds_address(stage + u * 1024));
-                copy_row(static_cast<const char*>(p.V) + at, lds_address(stage + kTile + u * 1024));
+                const long at = win_page_row(p, pages.page(p, j), kvh, j).at * 2;
+                copy_row(CopyLane<D>::template at<PAD>(static_cast<const char*>(p.K) + at, row, lane, p.d), lds_address(stage + u * 1024));
+                copy_row(CopyLane<D>::template at<PAD>(static_cast<const char*>(p.V) + at, row, lane, p.d), lds_address(stage + kTile + u * 1024));
             }
         } else {
 #pragma unroll
@@ -555,7 +560,7 @@ __global__ void __launch_bounds__((64 * kFewWaves<D, SRC>), (D == 256 ? 1 : 2)) 
             *reinterpret_cast<f32x4*>(smem + (w * 32 + l32) * kPitch + (32 * mt + 8 * g + 4 * h) * 4) =
                 f32x4{acc.o[mt][4 * g], acc.o[mt][4 * g + 1], acc.o[mt][4 * g + 2], acc.o[mt][4 * g + 3]};
     __syncthreads();
-    few_store<D, NW, 32>(p, s, smem, ml, kvh, r0, r1);
+    few_store<D, NW, 32, PAD>(p, s, smem, ml, kvh, r0, r1);
 }
 
 // ---------------------------------------------------------------------------------------------------------- a row tile
@@ -571,7 +576,7 @@ constexpr int kOneLds = 4 * (32 * D * 2 > 16 * (D * 4 + 16) + 128 ? 32 * D * 2 :
 template <int D, int SRC>
 constexpr int kOnePerCu = D == 64 ? 4 : D == 128 ? 3 : SRC == kCodes ? 2 : 1;
 
-template <int D, int SRC>
+template <int D, int SRC, bool PAD>
 __global__ void __launch_bounds__(kThreads, (kOnePerCu<D, SRC>)) win_one_kernel(WinParams p) {
     constexpr int NW = 4, MT = D / 16, KS = D / 32, kTile = 32 * D * 2;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -608,16 +613,16 @@ __global__ void __launch_bounds__(kThreads, (kOnePerCu<D, SRC>)) win_one_kernel(
         for (int g = 0; g < 2; ++g) {
             const int j = tiles.row(p, j0 + 16 * g + l16);
             const PageRow r = win_page_row(p, pages.page(p, j), kvh, j);
-            const char* src = static_cast<const char*>(p.K) + r.at * es + 16 * q;
+            const char* src = static_cast<const char*>(p.K) + r.at * es;
 #pragma unroll
-            for (int x = 0; x < kK / 2; ++x) kr[g * (kK / 2) + x] = *reinterpret_cast<const u32x4*>(src + 64 * x);
+            for (int x = 0; x < kK / 2; ++x) kr[g * (kK / 2) + x] = load_chunk<PAD>(src, 4 * x + q, p.d);
             if constexpr (SRC == kCodes) ke[g] = p.K_exp[r.exp];
         }
 #pragma unroll
         for (int x = 0; x < kV; ++x) {
             const int idx = x * 64 + lane, j = tiles.row(p, j0 + idx / kChunksPerRow);
             const PageRow r = win_page_row(p, pages.page(p, j), kvh, j);
-            vr[x] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p.V) + r.at * es + 16 * (idx % kChunksPerRow));
+            vr[x] = load_chunk<PAD>(static_cast<const char*>(p.V) + r.at * es, idx % kChunksPerRow, p.d);
             if constexpr (SRC == kCodes) ve[x] = p.V_exp[r.exp];
         }
     };
@@ -625,10 +630,10 @@ __global__ void __launch_bounds__(kThreads, (kOnePerCu<D, SRC>)) win_one_kernel(
     if (it < it1) request(it);
 
     bf16x8 qf[KS];
-    const __bf16* qrow = static_cast<const __bf16*>(p.Q) + s.q_base + (long)head * p.q_h + (long)t * p.q_n;
+    const char* qrow = reinterpret_cast<const char*>(static_cast<const __bf16*>(p.Q) + s.q_base + (long)head * p.q_h + (long)t * p.q_n);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
-        qf[ks] = *reinterpret_cast<const bf16x8*>(qrow + (SRC == kCodes ? 64 * (ks >> 1) + 16 * q + 8 * (ks & 1) : 32 * ks + 8 * q));
+        qf[ks] = __builtin_bit_cast(bf16x8, load_chunk<PAD>(qrow, SRC == kCodes ? 8 * (ks >> 1) + 2 * q + (ks & 1) : 4 * ks + q, p.d));
     win_sign(p.scale, qf);
     const float cs = win_scale(p.scale);
     f32x4 o[MT];
@@ -735,53 +740,57 @@ __global__ void __launch_bounds__(kThreads, (kOnePerCu<D, SRC>)) win_one_kernel(
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) *reinterpret_cast<f32x4*>(smem + (w * 16 + l16) * kPitch + (16 * mt + 4 * q) * 4) = o[mt];
     __syncthreads();
-    few_store<D, NW, 16>(p, s, smem, ml, kvh, r0, r1);
+    few_store<D, NW, 16, PAD>(p, s, smem, ml, kvh, r0, r1);
 }
 
-template <int D, int SRC, int SPLIT>
+template <int D, int SRC, int SPLIT, bool PAD>
 hipError_t out(const WinParams& p, hipStream_t stream) {
     constexpr int lds = 4 * 64 * D * 2, BR = 128 / SPLIT;
-    const hipError_t e = allow_lds(win_out_kernel<D, SRC, SPLIT>, lds);
+    const hipError_t e = allow_lds(win_out_kernel<D, SRC, SPLIT, PAD>, lds);
     if (e != hipSuccess) return e;
     const int row_blocks = (int)(((long)p.n * p.group + BR - 1) / BR);
     const long blocks = SRC == kTensors ? (long)row_blocks * p.batch : p.blocks;
-    hipLaunchKernelGGL((win_out_kernel<D, SRC, SPLIT>), dim3((unsigned)(blocks * p.kv_heads), (unsigned)p.splits), dim3(kThreads), lds, stream, p, row_blocks);
+    hipLaunchKernelGGL((win_out_kernel<D, SRC, SPLIT, PAD>), dim3((unsigned)(blocks * p.kv_heads), (unsigned)p.splits), dim3(kThreads), lds, stream, p,
+                       row_blocks);
     return hipGetLastError();
 }
-template <int D, int SRC>
+template <int D, int SRC, bool PAD>
 hipError_t few(const WinParams& p, hipStream_t stream) {
     constexpr int lds = kFewLds<D, SRC>;
-    const hipError_t e = allow_lds(win_few_kernel<D, SRC>, lds);
+    const hipError_t e = allow_lds(win_few_kernel<D, SRC, PAD>, lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((win_few_kernel<D, SRC>), dim3((unsigned)((long)p.blocks * p.kv_heads), (unsigned)p.splits), dim3(64 * kFewWaves<D, SRC>), lds, stream, p);
+    hipLaunchKernelGGL((win_few_kernel<D, SRC, PAD>), dim3((unsigned)((long)p.blocks * p.kv_heads), (unsigned)p.splits), dim3(64 * kFewWaves<D, SRC>), lds,
+                       stream, p);
     return hipGetLastError();
 }
-template <int D, int SRC>
+template <int D, int SRC, bool PAD>
 hipError_t one(const WinParams& p, hipStream_t stream) {
     constexpr int lds = kOneLds<D, SRC>;
-    const hipError_t e = allow_lds(win_one_kernel<D, SRC>, lds);
+    const hipError_t e = allow_lds(win_one_kernel<D, SRC, PAD>, lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((win_one_kernel<D, SRC>), dim3((unsigned)((long)p.blocks * p.kv_heads), (unsigned)p.splits), dim3(kThreads), lds, stream, p);
+    hipLaunchKernelGGL((win_one_kernel<D, SRC, PAD>), dim3((unsigned)((long)p.blocks * p.kv_heads), (unsigned)p.splits), dim3(kThreads), lds, stream, p);
     return hipGetLastError();
+}
+template <int D, int SRC, bool PAD>
+hipError_t launch_from(int rows, const WinParams& p, hipStream_t stream) {
+    if constexpr (SRC != kTensors) {
+        if (rows == 16) return one<D, SRC, PAD>(p, stream);
+        if (rows == 32) return few<D, SRC, PAD>(p, stream);
+    }
+    return rows == 64 ? out<D, SRC, 2, PAD>(p, stream) : out<D, SRC, 1, PAD>(p, stream);
 }
 template <int D>
 hipError_t launch(bool fp8, int rows, const WinParams& p, hipStream_t stream) {
-    if (!p.table) return rows == 64 ? out<D, kTensors, 2>(p, stream) : out<D, kTensors, 1>(p, stream);
-    if (rows == 16) return fp8 ? one<D, kCodes>(p, stream) : one<D, kPages>(p, stream);
-    if (rows == 32) return fp8 ? few<D, kCodes>(p, stream) : few<D, kPages>(p, stream);
-    if (rows == 64) return fp8 ? out<D, kCodes, 2>(p, stream) : out<D, kPages, 2>(p, stream);
-    return fp8 ? out<D, kCodes, 1>(p, stream) : out<D, kPages, 1>(p, stream);
+    if (fp8) return launch_from<D, kCodes, false>(rows, p, stream);
+    if (p.d < D) return p.table ? launch_from<D, kPages, true>(rows, p, stream) : launch_from<D, kTensors, true>(rows, p, stream);
+    return p.table ? launch_from<D, kPages, false>(rows, p, stream) : launch_from<D, kTensors, false>(rows, p, stream);
 }
 
 }  // namespace
 
 hipError_t launch_win_fwd(bool fp8, int rows, const WinParams& p, hipStream_t stream) {
-    switch (p.d) {
-        case 64: return launch<64>(fp8, rows, p, stream);
-        case 128: return launch<128>(fp8, rows, p, stream);
-        case 256: return launch<256>(fp8, rows, p, stream);
-        default: return hipErrorInvalidValue;
-    }
+    if (fp8 && p.d != 64 && p.d != 128 && p.d != 256) return hipErrorInvalidValue;
+    return p.d <= 64 ? launch<64>(fp8, rows, p, stream) : p.d <= 128 ? launch<128>(fp8, rows, p, stream) : launch<256>(fp8, rows, p, stream);
 }
 
 }  // namespace attn

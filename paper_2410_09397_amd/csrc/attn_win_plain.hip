@@ -1,5 +1,5 @@
-// Windowed attention in 32-bit arithmetic: forward over tensors or pages, backward, for fp32 storage at any d <= 256 and for bf16 (and
-// quantised pages) at the head dimensions that attn_win_fwd.hip and attn_win_bwd.hip do not have.
+// Windowed attention in 32-bit arithmetic: forward over tensors or pages and backward for fp32 storage at any d <= 256, and the forward
+// over quantised pages at the head dimensions that attn_win_fwd.hip does not have.
 //
 // Products are v_mfma_f32_32x32x2_f32.  Operand layout (lane l, h = l / 32): A row l % 32, k = h; B column l % 32, k = h; C as for the
 // bf16 form (column l % 32, register i <-> row 8 (i / 4) + 4 h + i % 4).  The order of k is free as long as both operands have the same:
@@ -685,12 +685,9 @@ hipError_t bwd(const WinParams& p, hipStream_t stream) {
 
 hipError_t launch_win_plain_fwd(bool is_bf16, bool fp8, const WinParams& p, hipStream_t stream) {
     if (fp8) return is_bf16 ? fwd<__bf16, uint8_t, true>(p, stream) : fwd<float, uint8_t, true>(p, stream);
-    if (p.table) return is_bf16 ? fwd<__bf16, __bf16, true>(p, stream) : fwd<float, float, true>(p, stream);
-    return is_bf16 ? fwd<__bf16, __bf16, false>(p, stream) : fwd<float, float, false>(p, stream);
+    return p.table ? fwd<float, float, true>(p, stream) : fwd<float, float, false>(p, stream);
 }
-hipError_t launch_win_plain_bwd(bool is_bf16, const WinParams& p, hipStream_t stream) {
-    return is_bf16 ? bwd<__bf16>(p, stream) : bwd<float>(p, stream);
-}
+hipError_t launch_win_plain_bwd(const WinParams& p, hipStream_t stream) { return bwd<float>(p, stream); }
 hipError_t launch_win_join(bool is_bf16, const WinParams& p, hipStream_t stream) {
     // four waves for a row that has many parts
     const int waves = p.splits > 8 ? 4 : 1;
@@ -700,10 +697,9 @@ hipError_t launch_win_join(bool is_bf16, const WinParams& p, hipStream_t stream)
     hipLaunchKernelGGL(fn, grid, dim3(kThreads), 0, stream, p);
     return hipGetLastError();
 }
-hipError_t launch_win_rows(bool is_bf16, const WinParams& p, hipStream_t stream) {
+hipError_t launch_win_rows(const WinParams& p, hipStream_t stream) {
     const dim3 grid((unsigned)(((long)p.batch * p.heads * p.n * 8 + kThreads - 1) / kThreads));
-    if (is_bf16) hipLaunchKernelGGL(win_rows_kernel<__bf16>, grid, dim3(kThreads), 0, stream, p);
-    else hipLaunchKernelGGL(win_rows_kernel<float>, grid, dim3(kThreads), 0, stream, p);
+    hipLaunchKernelGGL(win_rows_kernel<float>, grid, dim3(kThreads), 0, stream, p);
     return hipGetLastError();
 }
 hipError_t launch_win_keys(bool is_bf16, int tile, const WinParams& p, hipStream_t stream) {

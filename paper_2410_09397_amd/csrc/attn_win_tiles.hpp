@@ -7,14 +7,26 @@ namespace attn {
 
 enum WinSource { kTensors = 0, kPages = 1, kCodes = 2 };  // bf16 tensors, bf16 pages, quantised pages
 
-// Byte offset, inside a [rows x D] tile, of what lane `lane` of copy instruction `inst` (1 KB each) fetches: row and chunk.
+// What lane `lane` of copy instruction `inst` (1 KB of a [rows x D] tile) fetches: its row, and where in the row.  PAD: the rows have d < D
+// columns (a multiple of 8); the others are filled with zeros, which change no product.
+static __device__ const u32x4 win_zeros = {0, 0, 0, 0};
 template <int D>
 struct CopyLane {
     static constexpr int kRows = 512 / D;  // rows per instruction
-    int row, byte;                         // row inside the instruction's rows; byte offset inside the row for even / odd swizzle: see at()
     __device__ __forceinline__ static int row_of(int inst, int lane) { return inst * kRows + lane / (D / 8); }
-    __device__ __forceinline__ static int byte_of(int row, int lane) { return ((lane % (D / 8)) ^ swz<D>(row)) * 16; }
+    // from: the first byte of row `row` of the tile
+    template <bool PAD>
+    __device__ __forceinline__ static const char* at(const char* from, int row, int lane, int d) {
+        const int c = (lane % (D / 8)) ^ swz<D>(row);
+        if (PAD && 8 * c >= d) return reinterpret_cast<const char*>(&win_zeros);
+        return from + 16 * c;
+    }
 };
+// 16 bytes from column 8 c on of a row
+template <bool PAD>
+__device__ __forceinline__ u32x4 load_chunk(const char* row, int c, int d) {
+    return *reinterpret_cast<const u32x4*>(PAD && 8 * c >= d ? reinterpret_cast<const char*>(&win_zeros) : row + 16 * c);
+}
 
 // 16 bytes per lane from `src` to LDS at dst + 16 lane.  Inline assembly as in load_tile_direct: the wait is the caller's.
 __device__ __forceinline__ void copy_row(const char* src, unsigned dst) {

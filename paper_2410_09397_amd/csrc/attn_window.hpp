@@ -186,13 +186,13 @@ struct WinKeys {
 // ------------------------------------------------------------------------------------------------------------- host
 // is_bf16: the type of Q, O and of tensors, and of pages that are not quantised (fp8).  The arguments have been checked.
 hipError_t launch_win_plain_fwd(bool is_bf16, bool fp8, const WinParams& p, hipStream_t stream);
-// bf16, d in {64, 128, 256}; rows of a workgroup: 16, 32 (pages), 64, 128
+// bf16; quantised pages: d in {64, 128, 256}; rows of a workgroup: 16, 32 (pages), 64, 128
 hipError_t launch_win_fwd(bool fp8, int rows, const WinParams& p, hipStream_t stream);
 hipError_t launch_win_bwd(int rows, const WinParams& p, hipStream_t stream);                                // rows: 64, 128; forms delta itself
-hipError_t launch_win_plain_bwd(bool is_bf16, const WinParams& p, hipStream_t stream);
+hipError_t launch_win_plain_bwd(const WinParams& p, hipStream_t stream);  // fp32
 hipError_t launch_win_join(bool is_bf16, const WinParams& p, hipStream_t stream);
 hipError_t launch_win_keys(bool is_bf16, int tile, const WinParams& p, hipStream_t stream);
-hipError_t launch_win_rows(bool is_bf16, const WinParams& p, hipStream_t stream);  // delta
+hipError_t launch_win_rows(const WinParams& p, hipStream_t stream);       // fp32: delta
 hipError_t launch_cache_write(bool is_bf16, bool fp8, const WinParams& p, const void* K, const void* V, long s_n, long s_h, hipStream_t stream);
 hipError_t launch_cache_read(bool is_bf16, bool fp8, const WinParams& p, void* K, void* V, long s_n, long s_h, hipStream_t stream);
 
