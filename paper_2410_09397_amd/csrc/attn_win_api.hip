@@ -101,6 +101,13 @@ void set_parts(WinParams& p, int tile) {
     p.slots = p.sink_tiles * (p.parts > 1 ? p.parts : 0) + (p.rest_parts > 1 ? (int)(tiles - p.sink_tiles) * p.rest_parts : 0);
 }
 
+void set_heads(WinParams& p, int32_t heads, int32_t kv_heads) {
+    p.heads = heads;
+    p.kv_heads = kv_heads;
+    p.group = heads / kv_heads;
+    p.group_inv = p.group > 1 ? (unsigned)((((uint64_t)1 << 32) + p.group - 1) / p.group) : 0;
+}
+
 WinParams win_params(const attn_win_desc* d) {
     WinParams p;
     std::memset(&p, 0, sizeof(p));
@@ -111,9 +118,7 @@ WinParams win_params(const attn_win_desc* d) {
     p.k_h = d->kv_stride_h;
     p.k_n = d->kv_stride_n;
     p.batch = d->batch;
-    p.heads = d->heads;
-    p.kv_heads = d->kv_heads;
-    p.group = d->heads / d->kv_heads;
+    set_heads(p, d->heads, d->kv_heads);
     p.n = d->n;
     p.d = d->d;
     p.scale = d->scale;
@@ -216,9 +221,7 @@ WinParams paged_params(const attn_paged_desc* d, const attn_cache* c) {
     }
     p.table_stride = d->table_stride;
     p.batch = d->batch;
-    p.heads = d->heads;
-    p.kv_heads = d->kv_heads;
-    p.group = d->heads / d->kv_heads;
+    set_heads(p, d->heads, d->kv_heads);
     p.n = d->max_q;
     p.d = d->d;
     while ((1 << p.page_shift) < d->page_size) ++p.page_shift;

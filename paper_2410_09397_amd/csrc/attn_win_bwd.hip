@@ -32,16 +32,16 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dq_kernel(WinP
     const int rows = s.nq * p.group, r0 = (row_blocks - 1 - blk) * BR;
     const int w0 = min(r0 + 32 * wq, rows - 1), w1 = min(r0 + 32 * wq + 31, rows - 1);  // rows of this wave (repeated past the end)
     auto place = [&](int r, int& t, int& head) {
-        t = (int)((unsigned)r / (unsigned)p.group);
+        t = win_token(p, r);
         head = kvh * p.group + r - t * p.group;
     };
     int t, head;
     place(min(w0 + l32, rows - 1), t, head);
-    const int t_lo = (int)((unsigned)w0 / (unsigned)p.group), t_hi = (int)((unsigned)w1 / (unsigned)p.group);
+    const int t_lo = win_token(p, w0), t_hi = win_token(p, w1);
     LaneBounds see;
     see.init(p, t, s.len);
     WinTiles<64> tiles;
-    tiles.init(p, s.len, (int)((unsigned)r0 / (unsigned)p.group), (int)((unsigned)min(r0 + BR - 1, rows - 1) / (unsigned)p.group));
+    tiles.init(p, s.len, win_token(p, r0), win_token(p, min(r0 + BR - 1, rows - 1)));
 
     // Q and dO rows of a wave come through 16 KB (d = 128) of the stages that only this wave reads, then O for delta = rowsum(dO o O), which stays in
     // the workspace for the key owners.  Queries outside their sequence have delta 0.
@@ -115,6 +115,11 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dq_kernel(WinP
     fo.init(offsets);
     if constexpr (SPLIT > 1) fo.shift_rows(32 * wk);
     const float c = p.scale * kLog2e;
+    // the dP chains start from -delta (not at d = 256, which has no 16 registers for it)
+    constexpr bool kDeltaInAcc = D == 128;
+    f32x16 ndl;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) ndl[i] = kDeltaInAcc ? -dl : 0.f;
     wait_direct_loads();
     __syncthreads();
 
@@ -123,9 +128,10 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dq_kernel(WinP
 #pragma unroll
         for (int T = 0; T < 2 / SPLIT; ++T) {
             __builtin_amdgcn_s_setprio(kPrioScores);
-            f32x16 st, dp;
+            if (D < 256 && SPLIT == 1 && T == 1 && j0 + 32 >= p.sinks && j0 + 63 < t_lo - p.window + 1) break;  // (of a tile of sinks: nothing is seen of this half)
+            f32x16 st, dp = ndl;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) st[i] = dp[i] = 0.f;
+            for (int i = 0; i < 16; ++i) st[i] = 0.f;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
                 const bf16x8 kf = fo.frag(smem, off, 32 * T, ks), vf = fo.frag(smem, off + kTile, 32 * T, ks);
@@ -135,7 +141,7 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_dq_kernel(WinP
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(kPrioSoftmax);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) dp[i] = __builtin_amdgcn_exp2f(fmaf(st[i], c, -lse)) * (dp[i] - dl);
+            for (int i = 0; i < 16; ++i) dp[i] = __builtin_amdgcn_exp2f(fmaf(st[i], c, -lse)) * (kDeltaInAcc ? dp[i] : dp[i] - dl);
             if (masked) {
                 const int j = j0 + 32 * T + 4 * h, hi = see.hi - j, lo = see.lo - j, sink = p.sinks - j;
 #pragma unroll

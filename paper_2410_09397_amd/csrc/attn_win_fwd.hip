@@ -21,7 +21,7 @@ namespace attn {
 namespace {
 
 __device__ __forceinline__ void win_place(const WinParams& p, int kvh, int r, int& t, int& head) {
-    t = (int)((unsigned)r / (unsigned)p.group);
+    t = win_token(p, r);
     head = kvh * p.group + r - t * p.group;
 }
 
@@ -207,13 +207,13 @@ __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) win_out_kernel(Win
     const int w0 = min(r0 + 32 * wq, rows - 1), w1 = min(r0 + 32 * wq + 31, rows - 1);  // rows of this wave (repeated past the end)
     int t, head, t_lo, t_hi;
     win_place(p, kvh, min(w0 + l32, rows - 1), t, head);
-    t_lo = s.first + (int)((unsigned)w0 / (unsigned)p.group);  // positions of its first and last
-    t_hi = s.first + (int)((unsigned)w1 / (unsigned)p.group);
+    t_lo = s.first + win_token(p, w0);  // positions of its first and last
+    t_hi = s.first + win_token(p, w1);
     LaneBounds see;
     see.init(p, s.first + t, s.len);
     WinTiles<64> tiles;
-    tiles.init(p, s.len, s.first + (int)((unsigned)r0 / (unsigned)p.group),
-               s.first + (int)((unsigned)min(r0 + BR - 1, rows - 1) / (unsigned)p.group));
+    tiles.init(p, s.len, s.first + win_token(p, r0),
+               s.first + win_token(p, min(r0 + BR - 1, rows - 1)));
     const int it0 = blockIdx.y * p.chunk, it1 = (int)min((long)tiles.count, (long)it0 + p.chunk);
 
     TileFeed<D, SRC, PAD> feed;
@@ -451,7 +451,7 @@ __global__ void __launch_bounds__((64 * kFewWaves<D, SRC>), (D == 256 ? 1 : 2)) 
     const int r1 = min(r0 + 31, rows - 1);
     int t, head;
     win_place(p, kvh, min(r0 + l32, r1), t, head);
-    const int t_lo = s.first + (int)((unsigned)r0 / (unsigned)p.group), t_hi = s.first + (int)((unsigned)r1 / (unsigned)p.group);
+    const int t_lo = s.first + win_token(p, r0), t_hi = s.first + win_token(p, r1);
     LaneBounds see;
     see.init(p, s.first + t, s.len);
     WinTiles<32> tiles;
@@ -592,7 +592,7 @@ __global__ void __launch_bounds__(kThreads, (kOnePerCu<D, SRC>)) win_one_kernel(
     const int r1 = min(r0 + 15, rows - 1);
     int t, head;
     win_place(p, kvh, min(r0 + l16, r1), t, head);
-    const int t_lo = s.first + (int)((unsigned)r0 / (unsigned)p.group), t_hi = s.first + (int)((unsigned)r1 / (unsigned)p.group);
+    const int t_lo = s.first + win_token(p, r0), t_hi = s.first + win_token(p, r1);
     LaneBounds see;
     see.init(p, s.first + t, s.len);
     WinTiles<32> tiles;

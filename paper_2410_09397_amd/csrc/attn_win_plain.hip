@@ -230,7 +230,7 @@ struct RowPlace {  // of query row r of a (sequence, key head)
     int t, head;
 };
 __device__ __forceinline__ RowPlace place(const WinParams& p, int kvh, int r) {
-    const int t = (int)((unsigned)r / (unsigned)p.group);
+    const int t = win_token(p, r);
     return {t, kvh * p.group + r - t * p.group};
 }
 

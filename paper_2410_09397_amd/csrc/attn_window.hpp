@@ -22,6 +22,7 @@ struct WinParams {
     const uint8_t *K_exp, *V_exp;  // [page][kv head][token of the page]; nullptr: pages hold values
     const int32_t *table, *lens, *q_ptr;  // table == nullptr: tensors
     long table_stride;
+    unsigned group_inv;     // ceil(2^32 / group) for group > 1: see win_token
     int batch, heads, kv_heads, group, n, d;  // n: tokens (tensors), largest number of new tokens of a sequence (paged)
     int page_shift, num_pages, total_q, max_len;
     float scale;
@@ -36,6 +37,14 @@ struct WinParams {
     int slots;  // workgroups of a (sequence, key head) whose sums are parts
     float* part_kv;  // [batch * kv_heads][slot][dK, dV][keys of a tile][d]
 };
+
+// r / group for 0 <= r < 2^31: the product with ceil(2^32 / group) is the quotient or one more (a division takes some 25 instructions, and the rows of a
+// block are placed one by one when they are read and written).
+__device__ __forceinline__ int win_token(const WinParams& p, int r) {
+    if (p.group == 1) return r;
+    const unsigned q = __umulhi((unsigned)r, p.group_inv);
+    return (int)(q - (q * (unsigned)p.group > (unsigned)r ? 1u : 0u));
+}
 
 // What a workgroup knows of its sequence.  Everything is uniform; lengths from device memory are brought into the range that the
 // buffers allow, so that no value in them leads outside.
