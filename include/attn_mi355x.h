@@ -235,8 +235,9 @@ attn_status attn_mfma_ceiling(int32_t iters, int32_t operands, float *clock_ghz,
  * Q, O, dO, dQ are [batch, heads, n, d] with the q_ strides, K, V, dK, dV [batch, kv_heads, n, d] with the kv_ strides (in
  * elements, d axis 1); LSE is contiguous [batch, heads, n].  Outputs are overwritten and overlap nothing else; a stride of
  * an axis with more than one entry is at least d.
- * Supported: 1 <= d <= 256; ATTN_F32; ATTN_BF16 with d, strides and pointers as for attn_fwd.  ATTN_BF16 with d in {64, 128, 256} runs
- * bf16-MFMA kernels with fp32 accumulation, everything else fp32 arithmetic on the matrix cores.  The same call gives the same bits.
+ * Supported: 1 <= d <= 256; ATTN_F32; ATTN_BF16 with d, strides and pointers as for attn_fwd.  ATTN_BF16 runs bf16-MFMA kernels with fp32
+ * accumulation (d = 64, 128 and 256 fill them, other d run at the next of these), ATTN_F32 fp32 arithmetic on the matrix cores.  The same call
+ * gives the same bits.
  * A NaN or an infinity in a row inside a sequence may reach every query whose tile of keys it lies in, also those that do not see it.
  * The work goes with the number of visible pairs: tiles that no query of a block sees are neither read nor computed.
  */
@@ -279,7 +280,7 @@ attn_status attn_win_bwd(const attn_win_desc *desc, const int32_t *lens, const v
  * attn_cache_write skips such tokens, attn_cache_read gives zeros for them.  Rows beyond the sequences' own are not written.
  * Supported: page_size a power of two from 8 to 4096, 1 <= d <= 256, d % 8 == 0 for ATTN_BF16 and ATTN_CACHE_FP8, batch <= 65535; with
  * ATTN_BF16 strides are multiples of 8 and pointers 16-byte aligned, strides of quantised pages are multiples of 8 (of 16 for d a multiple
- * of 64).  ATTN_BF16 with d in {64, 128, 256} runs bf16-MFMA kernels, everything else fp32 arithmetic.
+ * of 64).  ATTN_BF16 runs bf16-MFMA kernels (quantised pages: with d in {64, 128, 256}), everything else fp32 arithmetic.
  */
 typedef enum { ATTN_CACHE_PLAIN = 0, ATTN_CACHE_FP8 = 1 } attn_cache_kind;
 
