@@ -67,10 +67,10 @@ __device__ __forceinline__ CacheRow cache_row(const WinParams& p, const WinSeq& 
     }
     return r;
 }
-// Rows per thread: K and V of several tokens or heads are on the way at a time (one row at a time, the 88 MB of a batch of prompts took 37 us
-// to write and 27 to read, a chain of dependent loads each).
-// (A call of few rows, a decoding step, has one each: 3.6 us against 6.5 with four for 64 tokens of 8 heads.)
-constexpr int kManyRows = 4;
+// Rows per thread: K and V of kManyRows tokens or heads are on the way at a time.  us of 88 MB of prompts, 1 row of K or V / 2 / 4 / 8 rows of both to a
+// thread: write 37 / 22 / 25 / 38, read 27 / 17 / 18 / 21.  A call of few rows, a decoding step, has one each: 4.2 us
+// against 6.5 with four for 64 tokens of 8 heads.
+constexpr int kManyRows = 2;
 
 __device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
 

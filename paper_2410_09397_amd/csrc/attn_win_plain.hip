@@ -401,14 +401,14 @@ __global__ void __launch_bounds__(kThreads) win_join_kernel(WinParams p) {
     const int lane = threadIdx.x & 63, in_row = threadIdx.x % (64 * WAVES);
     const long row = ((long)blockIdx.x * kThreads + threadIdx.x) / (64 * WAVES);
     const int token = (int)(row / p.heads), head = (int)(row % p.heads);
-    const int b = token < p.total_q ? win_sequence_of(p, __builtin_amdgcn_readfirstlane(token), lane) : -1;
-    if (b < 0) return;  // (of all waves of a row)
-    const WinSeq s = win_sequence(p, b);
-    const int t = token - (int)(s.lse_base / p.heads);
-    if (t < 0 || t >= s.nq) return;
+    if (token >= p.total_q) return;  // (all waves of a row)
     const float* ml = p.part_ml + row * p.splits * 2;
     const bool mine = lane < p.splits;
     const float m_k = mine ? ml[2 * lane] : -__builtin_inff(), l_k = mine ? ml[2 * lane + 1] : 0.f;
+    // which sequence the row belongs to is looked up while its sums are on their way; of a row of no sequence they mean nothing, and nothing is written
+    const int b = win_sequence_of(p, __builtin_amdgcn_readfirstlane(token), lane);
+    const WinSeq s = win_sequence(p, max(b, 0));
+    const int t = b < 0 ? -1 : token - (int)(s.lse_base / p.heads);
     float m = m_k;
 #pragma unroll
     for (int x = 1; x < 64; x <<= 1) m = __builtin_elementwise_maximum(m, __shfl_xor(m, x, 64));
@@ -447,7 +447,7 @@ __global__ void __launch_bounds__(kThreads) win_join_kernel(WinParams p) {
 #pragma unroll
         for (int x = 1; x < WAVES; ++x) sum += meet[threadIdx.x + 64 * x];
     }
-    if (lane >= lanes) return;
+    if (t < 0 || t >= s.nq || lane >= lanes) return;
     T* dst = static_cast<T*>(p.O) + s.q_base + (long)head * p.q_h + (long)t * p.q_n;
     if (c < p.d) store4(dst, c, p.d, sum * inv);
     if (lane == 0) p.LSE[row] = none ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
