@@ -353,13 +353,19 @@ def _int32(name, t, count, device):
     return t.data_ptr()
 
 
-def _scratch(nbytes, device, stream):
-    """A workspace allocated on the stream that the kernels will run on (see _workspace)."""
+def _made_on(stream, make):
+    """make()'s tensors, allocated on the stream that the kernels will run on: memory that was freed on another one may still be in use there
+    when they write to it, and theirs may be handed out there while they do."""
+    if stream is None:
+        return make()
     import torch
-    if stream is not None:
-        with torch.cuda.stream(stream):
-            return torch.empty(nbytes, dtype=torch.uint8, device=device)
-    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return make()
+
+
+def _scratch(nbytes, device, stream):
+    import torch
+    return _made_on(stream, lambda: torch.empty(nbytes, dtype=torch.uint8, device=device))
 
 
 def _win_desc(Q, K, scale, window, sinks):
@@ -390,7 +396,7 @@ def attn_win_fwd(Q, K, V, scale, window=0, sinks=0, lens=None, stream=None, out=
     _same_layout(K, V)
     if out is None:
         import torch
-        O, LSE = torch.empty_like(Q), torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device)
+        O, LSE = _made_on(stream, lambda: (torch.empty_like(Q), torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device)))
         _same_layout(Q, O)  # (of an expanded Q there is no dense tensor of the same strides)
     else:
         O, LSE = out
@@ -414,7 +420,7 @@ def attn_win_bwd(Q, K, V, O, dO, LSE, scale, window=0, sinks=0, lens=None, strea
     desc = _win_desc(Q, K, scale, window, sinks)
     if out is None:
         import torch
-        out = torch.empty_like(Q), torch.empty_like(K), torch.empty_like(K)
+        out = _made_on(stream, lambda: (torch.empty_like(Q), torch.empty_like(K), torch.empty_like(K)))
     dQ, dK, dV = out
     _same_layout(Q, O, dO, dQ)
     _same_layout(K, V, dK, dV)
@@ -495,7 +501,8 @@ def attn_cache_read(K_pages, V_pages, table, lens, dtype, total, q_ptr=None, max
         if K_pages.dim() != 4:
             raise ValueError("attn_cache_read: expected pages [num_pages, kv_heads, page_size, d]")
         shape = (total, K_pages.shape[1], K_pages.shape[3])
-        out = torch.empty(shape, dtype=dtype, device=K_pages.device), torch.empty(shape, dtype=dtype, device=K_pages.device)
+        device = K_pages.device
+        out = _made_on(stream, lambda: (torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device)))
     K, V = out
     _same_layout(K, V)
     desc, cache = _paged("attn_cache_read", K, K_pages, V_pages, table, lens, q_ptr, max_q, None, K_exp, V_exp, True)
@@ -516,7 +523,7 @@ def attn_paged_fwd(Q, K_pages, V_pages, table, lens, scale, q_ptr=None, max_q=No
     desc, cache = _paged("attn_paged_fwd", Q, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp, False, scale, window, sinks)
     if out is None:
         import torch
-        O, LSE = torch.empty_like(Q), torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device)
+        O, LSE = _made_on(stream, lambda: (torch.empty_like(Q), torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device)))
         _same_layout(Q, O)
     else:
         O, LSE = out
