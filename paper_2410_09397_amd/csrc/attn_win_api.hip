@@ -151,9 +151,10 @@ attn_status check_paged(const attn_paged_desc* d) {
         return ATTN_ERR_INVALID_ARG;
     if (d->batch > 65535 || d->max_len > kMostTokens || d->total_q > kMostTokens) return ATTN_ERR_UNSUPPORTED;
     if (d->heads == 0) return ATTN_OK;
-    const int64_t rows = (int64_t)d->max_q * (d->heads / d->kv_heads);
-    if (rows > kMostTokens || ((rows + 15) / 16) * d->batch * d->kv_heads > kMostGroups || ((int64_t)d->max_q * d->heads + 3) / 4 * d->batch > kMostGroups ||
-        (int64_t)d->max_q * d->kv_heads / 4 * d->batch > kMostGroups)
+    // (every factor is bounded before it is multiplied further)
+    const int64_t rows = (int64_t)d->max_q * (d->heads / d->kv_heads), bh = (int64_t)d->batch * d->heads, bk = (int64_t)d->batch * d->kv_heads;
+    if (rows > kMostTokens || (d->max_q > 0 && (bk > kMostGroups || bh > 4 * kMostGroups)) || (rows + 15) / 16 * bk > kMostGroups ||
+        ((int64_t)d->max_q * d->heads + 3) / 4 * d->batch > kMostGroups || (int64_t)d->max_q * d->kv_heads / 4 * d->batch > kMostGroups)
         return ATTN_ERR_UNSUPPORTED;
     return ATTN_OK;
 }
