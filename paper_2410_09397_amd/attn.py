@@ -363,6 +363,21 @@ def _made_on(stream, make):
         return make()
 
 
+def _empty_as(x):
+    """An uninitialised tensor of x's shape and strides.  A view of a wider tensor (the queries of a fused projection) has gaps between its
+    rows, and so has its image; views whose entries share memory have none."""
+    import torch
+    y = torch.empty_like(x)
+    if y.stride() == x.stride():
+        return y
+    reach = 0  # of the axes with smaller strides
+    for stride, size in sorted((a, n) for a, n in zip(x.stride(), x.shape) if n > 1):
+        if stride <= reach:
+            raise ValueError("expected a tensor whose entries do not share memory, got strides %s of shape %s" % (x.stride(), tuple(x.shape)))
+        reach += stride * (size - 1)
+    return torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
+
+
 def _scratch(nbytes, device, stream):
     import torch
     return _made_on(stream, lambda: torch.empty(nbytes, dtype=torch.uint8, device=device))
@@ -391,13 +406,12 @@ def attn_win_workspace_bytes(desc):
 def attn_win_fwd(Q, K, V, scale, window=0, sinks=0, lens=None, stream=None, out=None):
     """O, LSE of causal attention in which a query sees itself, the window - 1 keys in front of it (window = 0: all of them) and the
     first `sinks` keys.  Q: [batch, heads, n, d]; K, V: [batch, kv_heads, n, d], heads a multiple of kv_heads; lens: the
-    sequences' lengths (int32 [batch]), rows from there on are padding."""
+    sequences' lengths (int32 [batch]), rows from there on are padding.  Q, K and V may be views of one wider tensor; O has Q's strides."""
     desc = _win_desc(Q, K, scale, window, sinks)
     _same_layout(K, V)
     if out is None:
         import torch
-        O, LSE = _made_on(stream, lambda: (torch.empty_like(Q), torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device)))
-        _same_layout(Q, O)  # (of an expanded Q there is no dense tensor of the same strides)
+        O, LSE = _made_on(stream, lambda: (_empty_as(Q), torch.empty(Q.shape[:3], dtype=torch.float32, device=Q.device)))
     else:
         O, LSE = out
         _same_layout(Q, O)
@@ -416,11 +430,11 @@ def _check_lse(LSE, Q):
 
 
 def attn_win_bwd(Q, K, V, O, dO, LSE, scale, window=0, sinks=0, lens=None, stream=None, out=None, workspace=None):
-    """dQ, dK, dV of attn_win_fwd from its O and LSE; dK and dV are sums over the query heads that share a key head."""
+    """dQ, dK, dV of attn_win_fwd from its O and LSE; dK and dV are sums over the query heads that share a key head.  O, dO and dQ have Q's
+    strides, V, dK and dV those of K."""
     desc = _win_desc(Q, K, scale, window, sinks)
     if out is None:
-        import torch
-        out = _made_on(stream, lambda: (torch.empty_like(Q), torch.empty_like(K), torch.empty_like(K)))
+        out = _made_on(stream, lambda: (_empty_as(Q), _empty_as(K), _empty_as(K)))
     dQ, dK, dV = out
     _same_layout(Q, O, dO, dQ)
     _same_layout(K, V, dK, dV)
@@ -519,12 +533,12 @@ def attn_paged_workspace_bytes(desc):
 def attn_paged_fwd(Q, K_pages, V_pages, table, lens, scale, q_ptr=None, max_q=None, max_len=None, window=0, sinks=0, K_exp=None,
                    V_exp=None, stream=None, out=None, workspace=None):
     """O [total, heads, d], LSE [total, heads] of the new tokens Q [total, heads, d] over the paged cache that their keys and values have
-    been written to.  max_len bounds the lengths (None: what the table can hold; a tighter bound gives better launches)."""
+    been written to.  max_len bounds the lengths (None: what the table can hold; a tighter bound gives better launches).  Q may be a view of a
+    wider tensor; O has its strides."""
     desc, cache = _paged("attn_paged_fwd", Q, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp, False, scale, window, sinks)
     if out is None:
         import torch
-        O, LSE = _made_on(stream, lambda: (torch.empty_like(Q), torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device)))
-        _same_layout(Q, O)
+        O, LSE = _made_on(stream, lambda: (_empty_as(Q), torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device)))
     else:
         O, LSE = out
         _same_layout(Q, O)
