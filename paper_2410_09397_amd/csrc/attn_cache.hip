@@ -7,6 +7,7 @@
 //
 // Bound by memory: every value is read once and written once.  8 to 32 lanes share a row, 16 bytes of it each.
 #include "attn_internal.hpp"
+#include "attn_win_rules.hpp"
 #include "attn_window.hpp"
 
 namespace attn {
@@ -67,10 +68,6 @@ __device__ __forceinline__ CacheRow cache_row(const WinParams& p, const WinSeq& 
     }
     return r;
 }
-// Rows per thread: K and V of kManyRows tokens or heads are on the way at a time.  us of 88 MB of prompts, 1 row of K or V / 2 / 4 / 8 rows of both to a
-// thread: write 37 / 22 / 25 / 38, read 27 / 17 / 18 / 21.  A call of few rows, a decoding step, has one each: 4.2 us
-// against 6.5 with four for 64 tokens of 8 heads.
-constexpr int kManyRows = 2;
 
 __device__ __forceinline__ uint32_t magnitude(float x) { return __builtin_bit_cast(uint32_t, x) & 0x7fffffffu; }
 
@@ -187,14 +184,11 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(WinParams p, void*
     }
 }
 
-int lanes_of(int d) { return d <= 64 ? 8 : d <= 128 ? 16 : 32; }
 template <int ROWS>
 dim3 grid_of(const WinParams& p) {
-    const long rows = kThreads / lanes_of(p.d) * ROWS;
+    const long rows = kThreads / cache_lanes(p.d) * ROWS;
     return dim3((unsigned)(((long)p.n * p.kv_heads + rows - 1) / rows), (unsigned)p.batch);
 }
-// whether the rows fill the chip with several per thread: about one workgroup of eight waves' rows for every CU
-bool many_rows(const WinParams& p) { return (long)p.total_q * p.kv_heads * lanes_of(p.d) > 256L * 2 * kThreads; }
 
 }  // namespace
 
@@ -203,9 +197,9 @@ hipError_t launch_cache_write(bool is_bf16, bool fp8, const WinParams& p, const 
         constexpr int R = decltype(rows)::value;
         auto fn = is_bf16 ? (fp8 ? cache_write_kernel<__bf16, true, R> : cache_write_kernel<__bf16, false, R>)
                           : (fp8 ? cache_write_kernel<float, true, R> : cache_write_kernel<float, false, R>);
-        hipLaunchKernelGGL(fn, grid_of<R>(p), dim3(kThreads), 0, stream, p, K, V, s_n, s_h, lanes_of(p.d));
+        hipLaunchKernelGGL(fn, grid_of<R>(p), dim3(kThreads), 0, stream, p, K, V, s_n, s_h, cache_lanes(p.d));
     };
-    if (many_rows(p)) launch(std::integral_constant<int, kManyRows>{});
+    if (cache_rows_per_thread(p.kv_heads, p.total_q, p.d) > 1) launch(std::integral_constant<int, kManyRows>{});
     else launch(std::integral_constant<int, 1>{});
     return hipGetLastError();
 }
@@ -214,9 +208,9 @@ hipError_t launch_cache_read(bool is_bf16, bool fp8, const WinParams& p, void* K
         constexpr int R = decltype(rows)::value;
         auto fn = is_bf16 ? (fp8 ? cache_read_kernel<__bf16, true, R> : cache_read_kernel<__bf16, false, R>)
                           : (fp8 ? cache_read_kernel<float, true, R> : cache_read_kernel<float, false, R>);
-        hipLaunchKernelGGL(fn, grid_of<R>(p), dim3(kThreads), 0, stream, p, K, V, s_n, s_h, lanes_of(p.d));
+        hipLaunchKernelGGL(fn, grid_of<R>(p), dim3(kThreads), 0, stream, p, K, V, s_n, s_h, cache_lanes(p.d));
     };
-    if (many_rows(p)) launch(std::integral_constant<int, kManyRows>{});
+    if (cache_rows_per_thread(p.kv_heads, p.total_q, p.d) > 1) launch(std::integral_constant<int, kManyRows>{});
     else launch(std::integral_constant<int, 1>{});
     return hipGetLastError();
 }

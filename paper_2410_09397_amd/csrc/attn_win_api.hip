@@ -6,15 +6,15 @@
 
 #include "../../include/attn_mi355x.h"
 #include "attn_internal.hpp"
+#include "attn_win_rules.hpp"
 #include "attn_window.hpp"
 
 namespace {
 
+using attn::kMostGroups;
 using attn::WinParams;
 
-constexpr int kNoWindow = 0x3fffffff;       // larger than any distance; a position plus or minus it stays in range
 constexpr int64_t kMostTokens = 1 << 29;    // positions, rows of a (sequence, key head), and sums of two of them in 32 bits
-constexpr int64_t kMostGroups = (1 << 24) - 1;  // workgroups of 256 threads in a launch
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
@@ -55,51 +55,16 @@ attn_status check_win(const attn_win_desc* d) {
 
 bool is_empty(const attn_win_desc* d) { return d->batch == 0 || d->heads == 0 || d->n == 0; }
 
-// Whether the bf16-MFMA kernels take a call: bf16 of any head dimension, quantised pages of those that fill a kernel's width.
-bool is_wide(int32_t dtype, int32_t d, bool fp8 = false) { return dtype == ATTN_BF16 && (!fp8 || d == 64 || d == 128 || d == 256); }
-
 void set_window(WinParams& p, int32_t window, int32_t sinks, int32_t longest) {
-    const bool limits = window > 0 && window < longest && sinks < longest;
-    p.window = limits ? window : kNoWindow;
-    p.sinks = limits ? sinks : 0;
+    const attn::WinReach r = attn::win_reach(window, sinks, longest);
+    p.window = r.window;
+    p.sinks = r.sinks;
 }
 
-// Rows of a workgroup: 128, or 64 where blocks of 128 would not be more than three for two CUs.  us, forward / backward, 128 -> 64 rows, h heads on k key heads:
-//   d = 64    h4 k4 n300 9.4 / 19.8 -> 8.4 / 17.7                d = 256   h8 k2 n1024 55 / 110 -> 36 / 87
-//   d = 128   h8 k2 n1024 26 / 60 -> 20 / 50     h4 k1 n4096 w1024 31 / 74 -> 23 / 62     h16 k2 n2048 48 / 128 -> 39 / 115
-//   16 sequences of 1 to 256 new tokens, h32 k8 w1024 d = 128 (280 to 336 blocks) 54 -> 44
-//   beyond the line: d = 64 b2 h16 k4 n2048 w256 16.6 / 56 -> 18.3 / 59
-int block_rows(int64_t blocks128) { return blocks128 <= 384 ? 64 : 128; }
-int win_rows(const attn_win_desc* d) { return block_rows(((int64_t)d->n * (d->heads / d->kv_heads) + 127) / 128 * d->batch * d->kv_heads); }
-
-// Keys of a tile of the backward's key owners.
-int key_tile(const attn_win_desc* d) { return is_wide(d->dtype, d->d) ? 64 : 32; }
-// Workgroups of the key owners.  One streams window + tile tokens per head of its group, one of sink keys all of them: those are shared out over as
-// many workgroups as make the shares about as long (at most 64, and fewer where there are many sink tiles).  Where all of them
-// together are fewer than the places on the chip, the tokens of every tile are shared out: at least two tiles of tokens to each, and enough of
-// them over all heads of the group (twelve; the 32-bit kernels, whose waves take them in turn, six) to pay for the sums' way through memory
-// and the launch behind.  us of the backward, one workgroup per tile -> shared, h heads on k key heads:
-//   d = 128, no window   h8 k2 n512 63 -> 39   h8 k2 n1024 114 -> 55   h16 k2 n2048 380 -> 128      d = 256, no window  h8 k2 n1024 211 -> 104
-//   d = 128, window      h4 k1 n4096 w1024 135 -> 76   h16 k4 n2048 w512 85 -> 77   h8 k8 n1024 w256 (too few tiles) 35 -> 45
-//   d = 64               h4 k4 n300 (too few tiles) 20 -> 22      d = 256, window     h8 k4 n2048 w300 (too few tiles) 73 -> 77
-void set_parts(WinParams& p, int tile) {
-    const bool wide = tile == 64;
-    const int64_t places = wide && p.d > 128 ? 256 : 512;
-    const int64_t tiles = (p.n + tile - 1) / tile, bk = (int64_t)p.batch * p.kv_heads;
-    const int64_t span = std::min<int64_t>((int64_t)p.window + tile, p.n), token_tiles = (span + tile - 1) / tile;
-    p.sink_tiles = p.sinks > 0 ? (int)std::min<int64_t>((p.sinks + tile - 1) / tile, tiles) : 0;
-    p.parts = p.rest_parts = 1;
-    if (p.sink_tiles > 0) p.parts = (int)std::min<int64_t>(std::min<int64_t>((p.n + span - 1) / span, 64), std::max(1, 256 / p.sink_tiles));
-    const int64_t rest = std::min(std::min(places / std::max<int64_t>(1, tiles * bk), token_tiles / 2), token_tiles * p.group / (wide ? 12 : 6));
-    if (rest > 1) {
-        p.rest_parts = (int)rest;
-        p.parts = std::min(64, (int)rest * p.parts);
-    }
-    // (the sums of the parts are a launch of up to 64 lanes for every key and gradient)
-    if (bk * (p.rest_parts > 1 ? p.n : (int64_t)p.sink_tiles * tile) / 2 > kMostGroups) p.parts = p.rest_parts = 1;
-    if (p.parts <= 1) p.sink_tiles = 0;
-    p.slots = p.sink_tiles * (p.parts > 1 ? p.parts : 0) + (p.rest_parts > 1 ? (int)(tiles - p.sink_tiles) * p.rest_parts : 0);
-}
+bool is_wide(const attn_win_desc* d) { return attn::win_is_wide(d->dtype == ATTN_BF16, d->d); }
+bool is_wide(const attn_paged_desc* d) { return attn::win_is_wide(d->dtype == ATTN_BF16, d->d, d->kind == ATTN_CACHE_FP8); }
+int win_rows(const attn_win_desc* d) { return attn::win_rows(d->batch, d->heads, d->kv_heads, d->n); }
+int key_tile(const attn_win_desc* d) { return attn::win_key_tile(is_wide(d)); }
 
 void set_heads(WinParams& p, int32_t heads, int32_t kv_heads) {
     p.heads = heads;
@@ -123,7 +88,11 @@ WinParams win_params(const attn_win_desc* d) {
     p.d = d->d;
     p.scale = d->scale;
     set_window(p, d->window, d->sinks, d->n);
-    set_parts(p, key_tile(d));
+    const attn::WinParts parts = attn::win_parts(is_wide(d), d->batch, d->heads, d->kv_heads, d->n, d->d, p.window, p.sinks);
+    p.sink_tiles = parts.sink_tiles;
+    p.parts = parts.parts;
+    p.rest_parts = parts.rest_parts;
+    p.slots = parts.slots;
     p.splits = 1;
     p.chunk = 0x7fffffff;
     return p;
@@ -170,38 +139,7 @@ attn_status check_cache(const attn_paged_desc* d, const attn_cache* c) {
     return ATTN_OK;
 }
 
-// Rows of a workgroup of the paged forward: see attn_win_fwd.hip.
-int paged_rows(const attn_paged_desc* d) {
-    const int64_t rows = (int64_t)d->max_q * (d->heads / d->kv_heads);
-    if (!is_wide(d->dtype, d->d, d->kind == ATTN_CACHE_FP8)) return 32;
-    // (total_q bounds the row blocks that have rows where the sequences' new tokens differ in number)
-    if (rows > 64)
-        return block_rows(std::min((rows + 127) / 128 * d->batch, (int64_t)d->total_q * (d->heads / d->kv_heads) / 128 + d->batch) * d->kv_heads);
-    return rows > 16 ? 32 : 16;
-}
-
-// How the keys of a row block are shared out: with fewer row blocks than the chip has places for, a workgroup takes `chunk` tiles.
-void set_splits(WinParams& p, const attn_paged_desc* d) {
-    const int64_t rows = paged_rows(d), tile = rows >= 64 ? 64 : 32;
-    const bool few = rows < 64;
-    p.row_blocks = (int)(((int64_t)p.n * p.group + rows - 1) / rows);
-    p.blocks = (int)std::min((int64_t)p.row_blocks * p.batch, (int64_t)p.total_q * p.group / rows + p.batch);
-    const int64_t blocks = (int64_t)p.blocks * p.kv_heads;
-    // (the windows of a block reach over window + its tokens - 1 keys, which lie in one tile more than they fill, as the sinks do)
-    const int64_t keys = std::min<int64_t>(p.max_len, (int64_t)p.window + p.n) + p.sinks, tiles = keys / tile + 3;
-    // How many: as many as there are places (some more for few rows, whose lengths differ), but not in pieces so small that the launch that
-    // joins them costs more than they save.  us, split -> not: one token of b sequences of L keys, d = 128, quantised: b1 L600 11.0 -> 10.4,
-    // b1 L1000 11.2 -> 13.6, b64 L1000 33 -> 24; d = 256: b1 L300 12.9 -> 11.4, b1 L600 13.0 -> 14.9
-    const int64_t want = std::min<int64_t>(64, (few ? 2048 : 512) / std::max<int64_t>(1, blocks));
-    const int64_t least = !few ? 16 : blocks >= 256 ? 32 : p.d > 128 ? 8 : 12;  // tiles
-    const int64_t splits = (int64_t)p.total_q * p.heads <= kMostGroups ? std::min(want, tiles / least) : 1;
-    p.splits = 1;
-    p.chunk = 0x7fffffff;
-    if (splits > 1) {
-        p.chunk = (int)((tiles + splits - 1) / splits);
-        p.splits = (int)((tiles + p.chunk - 1) / p.chunk);
-    }
-}
+int paged_rows(const attn_paged_desc* d) { return attn::paged_rows(is_wide(d), d->batch, d->heads, d->kv_heads, d->total_q, d->max_q); }
 
 WinParams paged_params(const attn_paged_desc* d, const attn_cache* c) {
     WinParams p;
@@ -232,7 +170,11 @@ WinParams paged_params(const attn_paged_desc* d, const attn_cache* c) {
     p.scale = d->scale;
     set_window(p, d->window, d->sinks, d->max_len);
     p.parts = p.rest_parts = 1;
-    set_splits(p, d);
+    const attn::PagedSplits splits = attn::paged_splits(is_wide(d), d->batch, d->heads, d->kv_heads, d->d, d->total_q, d->max_q, d->max_len, p.window, p.sinks);
+    p.row_blocks = splits.row_blocks;
+    p.blocks = splits.blocks;
+    p.splits = splits.splits;
+    p.chunk = splits.chunk;
     return p;
 }
 
@@ -272,7 +214,7 @@ attn_status attn_win_fwd(const attn_win_desc* desc, const int32_t* lens, const v
     p.O = O;
     p.LSE = LSE;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return status_of(is_wide(desc->dtype, desc->d) ? attn::launch_win_fwd(false, win_rows(desc), p, s) : attn::launch_win_plain_fwd(bf16, false, p, s));
+    return status_of(is_wide(desc) ? attn::launch_win_fwd(false, win_rows(desc), p, s) : attn::launch_win_plain_fwd(bf16, false, p, s));
 }
 
 attn_status attn_win_bwd(const attn_win_desc* desc, const int32_t* lens, const void* Q, const void* K, const void* V, const void* O,
@@ -359,7 +301,7 @@ attn_status attn_paged_fwd(const attn_paged_desc* desc, const attn_cache* cache,
     p.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + part_ml_bytes(desc, p));
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool fp8 = desc->kind == ATTN_CACHE_FP8;
-    hipError_t e = is_wide(desc->dtype, desc->d, fp8) ? attn::launch_win_fwd(fp8, paged_rows(desc), p, s) : attn::launch_win_plain_fwd(bf16, fp8, p, s);
+    hipError_t e = is_wide(desc) ? attn::launch_win_fwd(fp8, paged_rows(desc), p, s) : attn::launch_win_plain_fwd(bf16, fp8, p, s);
     if (e == hipSuccess && p.splits > 1) e = attn::launch_win_join(bf16, p, s);
     return status_of(e);
 }
