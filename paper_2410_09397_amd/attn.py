@@ -383,6 +383,16 @@ def _scratch(nbytes, device, stream):
     return _made_on(stream, lambda: torch.empty(nbytes, dtype=torch.uint8, device=device))
 
 
+def _on_gpu(x):
+    if not x.is_cuda:  # (the kernels would be given a host address)
+        raise ValueError("expected tensors on a GPU, got %s" % x.device)
+
+
+def _check_workspace(workspace, device):
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError("the workspace must be a contiguous tensor on the device of the other tensors")
+
+
 def _win_desc(Q, K, scale, window, sinks):
     if Q.dim() != 4 or K.dim() != 4:
         raise ValueError("expected [batch, heads, n, d] tensors")
@@ -392,6 +402,7 @@ def _win_desc(Q, K, scale, window, sinks):
         raise ValueError("expected unit stride along d")
     if (kb, kn, kd) != (b, n, d) or K.dtype != dtype or K.device != Q.device:
         raise ValueError("Q and K must share batch, n, d, dtype and device")
+    _on_gpu(Q)
     return _WIN_DESC.pack(b, h, kh, n, d, scale, window, sinks, _dtype(dtype), 0, qsb, qsh, qsn, ksb, ksh, ksn)
 
 
@@ -441,6 +452,8 @@ def attn_win_bwd(Q, K, V, O, dO, LSE, scale, window=0, sinks=0, lens=None, strea
     _check_lse(LSE, Q)
     if workspace is None:
         workspace = _scratch(max(attn_win_workspace_bytes(desc), 256), Q.device, stream)
+    else:
+        _check_workspace(workspace, Q.device)
     st = lib().attn_win_bwd(desc, _int32("lens", lens, Q.shape[0], Q.device), Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(),
                             dO.data_ptr(), LSE.data_ptr(), dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), workspace.data_ptr(),
                             workspace.numel(), _stream(stream))
@@ -491,6 +504,7 @@ def _paged(name, x, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp,
         if batch and total % batch:
             raise ValueError("%s: without q_ptr every sequence has the same number of rows" % name)
         max_q = total // batch if batch else 0
+    _on_gpu(x)
     desc = _PAGED_DESC.pack(batch, h, kvh, d, total, max_q, width * page if max_len is None else max_len, page, num, width, scale, window, sinks,
                             _dtype(dtype), ATTN_CACHE_FP8 if fp8 else ATTN_CACHE_PLAIN, 0, sn, sh, sn, sh, psp, psh, psn, ts)
     cache = _CACHE.pack(K_pages.data_ptr(), V_pages.data_ptr(), K_exp.data_ptr() if fp8 else 0, V_exp.data_ptr() if fp8 else 0,
@@ -548,6 +562,8 @@ def attn_paged_fwd(Q, K_pages, V_pages, table, lens, scale, q_ptr=None, max_q=No
         size = attn_paged_workspace_bytes(desc)
         if size > 256:  # (256: nothing is kept there)
             workspace = _scratch(size, Q.device, stream)
+    else:
+        _check_workspace(workspace, Q.device)
     if workspace is not None:
         where, size = workspace.data_ptr(), workspace.numel()
     st = lib().attn_paged_fwd(desc, cache, Q.data_ptr(), O.data_ptr(), LSE.data_ptr(), where, size, _stream(stream))

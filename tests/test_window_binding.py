@@ -1,0 +1,37 @@
+"""What the binding of windowed attention and the paged cache turns down before the library is called: tensors whose addresses mean nothing on
+the GPU."""
+import pytest
+
+from paper_2410_09397_amd import attn
+
+
+def _tensors(device):
+    import torch
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16, device=device)
+    pages = [bf(4, 2, 16, 64), bf(4, 2, 16, 64)]
+    table, lens = torch.arange(4, dtype=torch.int32, device=device).view(2, 2), torch.full((2,), 20, dtype=torch.int32, device=device)
+    return bf(2, 4, 20, 64), bf(2, 2, 20, 64), pages, table, lens, bf(2, 4, 64), bf(2, 2, 64), torch.zeros(2, 4, 20, device=device)
+
+
+def test_host_tensors_are_refused():
+    import torch
+    Q, K, pages, table, lens, q, k, LSE = _tensors("cpu")
+    for call in (lambda: attn.attn_win_fwd(Q, K, K, 1.0, out=(Q, LSE)), lambda: attn.attn_win_bwd(Q, K, K, Q, Q, LSE, 1.0, out=(Q, K, K)),
+                 lambda: attn.attn_cache_write(k, k, *pages, table, lens), lambda: attn.attn_cache_read(*pages, table, lens, torch.bfloat16, 2),
+                 lambda: attn.attn_paged_fwd(q, *pages, table, lens, 1.0, out=(q, LSE[:, :, 0].contiguous()))):
+        with pytest.raises(ValueError, match="on a GPU"):
+            call()
+
+
+@pytest.mark.gpu
+def test_workspaces_elsewhere_are_refused():
+    import torch
+    Q, K, pages, table, lens, q, k, LSE = _tensors("cuda")
+    size = 1 << 20
+    for bad in (torch.zeros(size, dtype=torch.uint8), torch.zeros(1, dtype=torch.uint8, device="cuda").expand(size),
+                torch.zeros(2 * size, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError, match="workspace"):
+            attn.attn_win_bwd(Q, K, K, Q, Q, LSE, 1.0, workspace=bad)
+        with pytest.raises(ValueError, match="workspace"):
+            attn.attn_paged_fwd(q, *pages, table, lens, 1.0, workspace=bad)
+    attn.attn_paged_fwd(q, *pages, table, lens, 1.0, workspace=torch.zeros(size, dtype=torch.uint8, device="cuda"))
