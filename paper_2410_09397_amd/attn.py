@@ -524,14 +524,16 @@ def attn_cache_write(K, V, K_pages, V_pages, table, lens, q_ptr=None, max_q=None
 
 def attn_cache_read(K_pages, V_pages, table, lens, dtype, total, q_ptr=None, max_q=None, K_exp=None, V_exp=None, stream=None, out=None):
     """K, V ([total, kv_heads, d]): the last tokens of every sequence, as many as q_ptr says (None: total / batch each)."""
+    if K_pages.dim() != 4:
+        raise ValueError("attn_cache_read: expected pages [num_pages, kv_heads, page_size, d]")
+    shape = (total, K_pages.shape[1], K_pages.shape[3])
     if out is None:
         import torch
-        if K_pages.dim() != 4:
-            raise ValueError("attn_cache_read: expected pages [num_pages, kv_heads, page_size, d]")
-        shape = (total, K_pages.shape[1], K_pages.shape[3])
         device = K_pages.device
         out = _made_on(stream, lambda: (torch.empty(shape, dtype=dtype, device=device), torch.empty(shape, dtype=dtype, device=device)))
     K, V = out
+    if K.shape != shape or K.dtype != dtype:
+        raise ValueError("attn_cache_read: out must hold tensors [total, kv_heads, d] of the given type")
     _same_layout(K, V)
     desc, cache = _paged("attn_cache_read", K, K_pages, V_pages, table, lens, q_ptr, max_q, None, K_exp, V_exp, True)
     st = lib().attn_cache_read(desc, cache, K.data_ptr(), V.data_ptr(), _stream(stream))

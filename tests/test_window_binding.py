@@ -23,6 +23,18 @@ def test_host_tensors_are_refused():
             call()
 
 
+def test_tensors_to_read_into_agree_with_the_call():
+    """More rows than `total` would be filled with earlier tokens, and another type would go unnoticed."""
+    import torch
+    pages = [torch.zeros(4, 2, 16, 64) for _ in range(2)]
+    table, lens = torch.arange(4, dtype=torch.int32).view(2, 2), torch.full((2,), 20, dtype=torch.int32)
+    for shape, dtype in (((6, 2, 64), torch.float32), ((2, 2, 64), torch.float32), ((4, 3, 64), torch.float32), ((4, 2, 32), torch.float32)):
+        with pytest.raises(ValueError, match="out must hold"):
+            attn.attn_cache_read(*pages, table, lens, dtype, 4, out=tuple(torch.zeros(shape) for _ in range(2)))
+    with pytest.raises(ValueError, match="out must hold"):
+        attn.attn_cache_read(*pages, table, lens, torch.bfloat16, 4, out=tuple(torch.zeros(4, 2, 64) for _ in range(2)))
+
+
 @pytest.mark.gpu
 def test_workspaces_elsewhere_are_refused():
     import torch
