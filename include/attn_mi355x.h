@@ -233,8 +233,8 @@ attn_status attn_mfma_ceiling(int32_t iters, int32_t operands, float *clock_ghz,
  *     padding: keys there are visible to nobody and never read into a sum, queries there get O = 0, LSE = -inf and gradients 0.
  *     (Values below 0 or above n count as 0 and n.)
  * Q, O, dO, dQ are [batch, heads, n, d] with the q_ strides, K, V, dK, dV [batch, kv_heads, n, d] with the kv_ strides (in
- * elements, d axis 1); LSE is contiguous [batch, heads, n].  Outputs are overwritten and overlap nothing else; a stride of
- * an axis with more than one entry is at least d.
+ * elements, d axis 1); LSE is contiguous [batch, heads, n].  Outputs are overwritten and overlap nothing else (a call with batch, heads or n
+ * 0 has nothing to do: it writes nothing, not dK and dV of keys that no head reads either); a stride of an axis with more than one entry is at least d.
  * Supported: 1 <= d <= 256; ATTN_F32; ATTN_BF16 with d, strides and pointers as for attn_fwd.  ATTN_BF16 runs bf16-MFMA kernels with fp32
  * accumulation (d = 64, 128 and 256 fill them, other d run at the next of these), ATTN_F32 fp32 arithmetic on the matrix cores.  The same call
  * gives the same bits.

@@ -459,6 +459,8 @@ def attn_win_bwd(Q, K, V, O, dO, LSE, scale, window=0, sinks=0, lens=None, strea
                             workspace.numel(), _stream(stream))
     if st != ATTN_OK:
         raise AttnError(st, "attn_win_bwd")
+    if Q.shape[1] == 0:  # nothing is launched: keys that no head reads
+        _made_on(stream, lambda: (dK.zero_(), dV.zero_()))
     return dQ, dK, dV
 
 

@@ -47,3 +47,17 @@ def test_workspaces_elsewhere_are_refused():
         with pytest.raises(ValueError, match="workspace"):
             attn.attn_paged_fwd(q, *pages, table, lens, 1.0, workspace=bad)
     attn.attn_paged_fwd(q, *pages, table, lens, 1.0, workspace=torch.zeros(size, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("side", [False, True])
+def test_keys_that_no_head_reads_have_gradients_of_zero(side):
+    import torch
+    Q, K = torch.zeros(2, 0, 30, 64, device="cuda"), torch.randn(2, 3, 30, 64, device="cuda")
+    LSE, stream = torch.zeros(2, 0, 30, device="cuda"), torch.cuda.Stream() if side else None
+    out = (torch.empty_like(Q), torch.full_like(K, 7.0), torch.full_like(K, 7.0))
+    torch.cuda.synchronize()
+    attn.attn_win_bwd(Q, K, K, Q, Q, LSE, 1.0, stream=stream, out=out)
+    torch.cuda.synchronize()
+    assert not bool(out[1].any()) and not bool(out[2].any())
+    assert attn.attn_win_fwd(Q, K, K, 1.0, stream=stream)[0].shape == Q.shape
