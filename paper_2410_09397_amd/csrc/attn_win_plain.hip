@@ -60,7 +60,6 @@ __device__ __forceinline__ f32x4 load4(const uint8_t* row, int c, bool exists, i
     return f32x4{lo[0], lo[1], hi[0], hi[1]};
 }
 __device__ __forceinline__ float value(float x) { return x; }
-__device__ __forceinline__ float value(__bf16 x) { return (float)x; }
 __device__ __forceinline__ float value(uint8_t x) { return __builtin_amdgcn_cvt_f32_fp8((int)x, 0); }
 // column 32 m + l of a row; CHECK, first: m counts from a group of columns that the compiler does not know
 template <int DP, bool CHECK = false, typename E>
@@ -79,7 +78,6 @@ __device__ __forceinline__ f32x4 load4(const float* row, int c, int d) {
         if (c + e < d) v[e] = row[c + e];
     return v;
 }
-__device__ __forceinline__ f32x4 load4(const __bf16* row, int c, int d) { return load4<32>(row, c, false, d); }
 __device__ __forceinline__ void store4(float* row, int c, int d, f32x4 v) {
     if (c + 4 <= d) {
         *reinterpret_cast<f32x4u*>(row + c) = v;
@@ -95,8 +93,9 @@ __device__ __forceinline__ void store4(__bf16* row, int c, int d, f32x4 v) {
 
 // A resident row as the contraction over d takes it: 4 values of columns 8 c + 4 h .. for every c.  bf16 rows stay packed; rows that
 // have no registers to stay in are read again for every tile.
-template <typename T, int DP, bool kResident = DP <= (std::is_same_v<T, __bf16> ? 192 : 128)>
+template <typename T, int DP>
 struct RowOperand {
+    static constexpr bool kResident = DP <= (std::is_same_v<T, __bf16> ? 192 : 128);
     typedef std::conditional_t<std::is_same_v<T, __bf16>, u32x2, f32x4> Chunk;
     Chunk v[kResident ? DP / 8 : 1];
     const T* row;
@@ -190,8 +189,8 @@ struct TileRow {
 };
 
 // s += A B^T over d: a's rows are the tile's, b's the resident ones
-template <typename E, typename T, int DP, bool R>
-__device__ __forceinline__ void scores(f32x16& s, const TileRow<E, DP>& row, float scale, const RowOperand<T, DP, R>& b) {
+template <typename E, typename T, int DP>
+__device__ __forceinline__ void scores(f32x16& s, const TileRow<E, DP>& row, float scale, const RowOperand<T, DP>& b) {
 #pragma unroll
     for (int c = 0; c < DP / 8; ++c) {
         f32x4 a = row.get(c);
@@ -455,7 +454,6 @@ __global__ void __launch_bounds__(kThreads) win_join_kernel(WinParams p) {
 
 // -------------------------------------------------------------------------------------------------------- backward
 // delta = rowsum(dO o O) of every query inside its sequence, [batch, heads, n]; eight lanes per row.
-template <typename T>
 __global__ void __launch_bounds__(kThreads) win_rows_kernel(WinParams p) {
     const long f = ((long)blockIdx.x * kThreads + threadIdx.x) >> 3, rows = (long)p.batch * p.heads * p.n;
     const int c0 = 4 * (threadIdx.x & 7);
@@ -465,7 +463,7 @@ __global__ void __launch_bounds__(kThreads) win_rows_kernel(WinParams p) {
         const long at = (long)(bh / p.heads) * p.q_b + (long)(bh % p.heads) * p.q_h + (long)t * p.q_n;
         if (!p.lens || t < p.lens[bh / p.heads])
             for (int c = c0; c < p.d; c += 32) {
-                const f32x4 x = load4(static_cast<const T*>(p.O_in) + at, c, p.d), g = load4(static_cast<const T*>(p.dO) + at, c, p.d);
+                const f32x4 x = load4(static_cast<const float*>(p.O_in) + at, c, p.d), g = load4(static_cast<const float*>(p.dO) + at, c, p.d);
                 sum += x[0] * g[0] + x[1] * g[1] + x[2] * g[2] + x[3] * g[3];
             }
     }
@@ -474,9 +472,9 @@ __global__ void __launch_bounds__(kThreads) win_rows_kernel(WinParams p) {
     if (f < rows && (threadIdx.x & 7) == 0) p.delta[f] = sum;
 }
 
-// dQ: a wave owns 32 query rows; dS^T = P^T o (V dO^T - delta), dQ^T += K^T dS^T.
-template <typename T, int DP>
-__global__ void __launch_bounds__(kThreads, DP <= 64 || (DP == 96 && std::is_same_v<T, float>) ? 2 : 1) win_plain_dq_kernel(WinParams p, int row_blocks) {
+// dQ: a workgroup owns 32 query rows, its waves take the key tiles in turn and their sums meet in LDS; dS^T = P^T o (V dO^T - delta), dQ^T += K^T dS^T.
+template <int DP>
+__global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) win_plain_dq_kernel(WinParams p, int row_blocks) {
     constexpr int MT = DP / 32;
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int bk = blockIdx.x / row_blocks, b = bk / p.kv_heads, kvh = bk % p.kv_heads;
@@ -490,9 +488,9 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 || (DP == 96 && std::is_sam
     WinTiles<32> tiles;
     tiles.init(p, s.len, s.first + place(p, kvh, r0).t, s.first + place(p, kvh, min(r0 + 31, rows - 1)).t);
     const long off = s.q_base + (long)at.head * p.q_h + (long)at.t * p.q_n, stat = s.lse_base + (long)at.head * s.lse_h + at.t;
-    RowOperand<T, DP> q, g;
-    q.init(static_cast<const T*>(p.Q) + off, p.d, h);
-    g.init(static_cast<const T*>(p.dO) + off, p.d, h);
+    RowOperand<float, DP> q, g;
+    q.init(static_cast<const float*>(p.Q) + off, p.d, h);
+    g.init(static_cast<const float*>(p.dO) + off, p.d, h);
     const float lse = hi >= 0 ? p.LSE_in[stat] * kLog2e : 0.f, delta = hi >= 0 ? p.delta[stat] : 0.f;
     f32x16 dq[MT];
 #pragma unroll
@@ -502,12 +500,12 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 || (DP == 96 && std::is_sam
     const float cs = p.scale * kLog2e;
     for (int it = w; it < tiles.count; it += 4) {
         const int j0 = tiles.start(it);
-        KeyTile<T, false> keys;
+        KeyTile<float, false> keys;
         keys.init(p, tiles, b, kvh, j0, l32);
         f32x16 st, dp;
 #pragma unroll
         for (int e = 0; e < 16; ++e) st[e] = dp[e] = 0.f;
-        TileRow<T, DP> key, val;
+        TileRow<float, DP> key, val;
         key.init(keys.K + keys.at, p.d, h);
         val.init(keys.V + keys.at, p.d, h);
         scores(st, key, 1.f, q);
@@ -524,7 +522,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 || (DP == 96 && std::is_sam
     extern __shared__ __attribute__((aligned(16))) float meet[];
     meet_waves<MT>(dq, meet, w, lane);
     if (w != 0 || r0 + l32 >= rows) return;
-    T* dst = static_cast<T*>(p.dQ) + off;
+    float* dst = static_cast<float*>(p.dQ) + off;
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -536,7 +534,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 || (DP == 96 && std::is_sam
 // dK, dV: a workgroup owns 32 keys; its waves take the 32-token tiles of all heads of the group in turn, with scores [query][key], which
 // are the operands of dV^T += dO^T P and dK^T += Q^T dS as they stand.  The waves' sums meet in LDS.  d > 128: the columns of the gradients are shared by two workgroups
 // (blockIdx.y), which both form the scores; one would need 600 registers per lane.
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(kThreads, 1) win_plain_dkdv_kernel(WinParams p, int key_blocks) {
     constexpr int MT = DP >= 192 ? DP / 64 : DP / 32;
     extern __shared__ __attribute__((aligned(16))) float meet[];  // [MT][4][64] x 16 bytes
@@ -550,9 +548,9 @@ __global__ void __launch_bounds__(kThreads, 1) win_plain_dkdv_kernel(WinParams p
     const long kv = (long)b * p.k_b + (long)kvh * p.k_h;
     const int t_tiles = (i1 - i0 + 31) / 32, jobs = t_tiles * p.group;
     const int jr = max(0, min(j, s.len - 1));
-    RowOperand<T, DP, DP <= 128> k, v;
-    k.init(static_cast<const T*>(p.K) + kv + (long)jr * p.k_n, p.d, h);
-    v.init(static_cast<const T*>(p.V) + kv + (long)jr * p.k_n, p.d, h);
+    RowOperand<float, DP> k, v;
+    k.init(static_cast<const float*>(p.K) + kv + (long)jr * p.k_n, p.d, h);
+    v.init(static_cast<const float*>(p.V) + kv + (long)jr * p.k_n, p.d, h);
     f32x16 dk[MT], dv[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -563,14 +561,14 @@ __global__ void __launch_bounds__(kThreads, 1) win_plain_dkdv_kernel(WinParams p
         const int head = kvh * p.group + job / t_tiles, t0 = i0 + 32 * (job % t_tiles);
         // 32-bit offsets from the tile's first row; rows past the end repeat the last one
         const long base = s.q_base + (long)head * p.q_h + (long)t0 * p.q_n, stat = s.lse_base + (long)head * s.lse_h + t0;
-        const T *Q = static_cast<const T*>(p.Q) + base, *G = static_cast<const T*>(p.dO) + base;
+        const float *Q = static_cast<const float*>(p.Q) + base, *G = static_cast<const float*>(p.dO) + base;
         const float *lse = p.LSE_in + stat, *delta = p.delta + stat;
         const int last = i1 - 1 - t0;
         const unsigned q_n = (unsigned)p.q_n, mine = (unsigned)min(l32, last) * q_n;
         f32x16 st, dp;
 #pragma unroll
         for (int e = 0; e < 16; ++e) st[e] = dp[e] = 0.f;
-        TileRow<T, DP> query, grad;
+        TileRow<float, DP> query, grad;
         query.init(Q + mine, p.d, h);
         grad.init(G + mine, p.d, h);
         float lse_x[16], delta_x[16];
@@ -618,8 +616,8 @@ __global__ void __launch_bounds__(kThreads, 1) win_plain_dkdv_kernel(WinParams p
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-            store4(static_cast<T*>(p.dK) + out, c0 + 32 * m + 8 * x + 4 * h, p.d, f32x4{dk[m][4 * x], dk[m][4 * x + 1], dk[m][4 * x + 2], dk[m][4 * x + 3]} * p.scale);
-            store4(static_cast<T*>(p.dV) + out, c0 + 32 * m + 8 * x + 4 * h, p.d, f32x4{dv[m][4 * x], dv[m][4 * x + 1], dv[m][4 * x + 2], dv[m][4 * x + 3]});
+            store4(static_cast<float*>(p.dK) + out, c0 + 32 * m + 8 * x + 4 * h, p.d, f32x4{dk[m][4 * x], dk[m][4 * x + 1], dk[m][4 * x + 2], dk[m][4 * x + 3]} * p.scale);
+            store4(static_cast<float*>(p.dV) + out, c0 + 32 * m + 8 * x + 4 * h, p.d, f32x4{dv[m][4 * x], dv[m][4 * x + 1], dv[m][4 * x + 2], dv[m][4 * x + 3]});
         }
 }
 
@@ -669,13 +667,12 @@ hipError_t fwd(const WinParams& p, hipStream_t stream) {
     });
 }
 
-template <typename T>
 hipError_t bwd(const WinParams& p, hipStream_t stream) {
     const int blocks = (int)(((long)p.n * p.group + 31) / 32), keys = p.sink_tiles * p.parts + ((p.n + 31) / 32 - p.sink_tiles) * p.rest_parts;
     return with_width(p.d, [&](auto width) {
         constexpr int DP = decltype(width)::value;
-        hipLaunchKernelGGL((win_plain_dq_kernel<T, DP>), dim3((unsigned)((long)blocks * p.batch * p.kv_heads)), dim3(kThreads), DP * 128, stream, p, blocks);
-        hipLaunchKernelGGL((win_plain_dkdv_kernel<T, DP>), dim3((unsigned)((long)keys * p.batch * p.kv_heads), DP >= 192 ? 2 : 1), dim3(kThreads),
+        hipLaunchKernelGGL((win_plain_dq_kernel<DP>), dim3((unsigned)((long)blocks * p.batch * p.kv_heads)), dim3(kThreads), DP * 128, stream, p, blocks);
+        hipLaunchKernelGGL((win_plain_dkdv_kernel<DP>), dim3((unsigned)((long)keys * p.batch * p.kv_heads), DP >= 192 ? 2 : 1), dim3(kThreads),
                            (DP >= 192 ? DP / 2 : DP) * 128, stream, p, keys);
         return hipGetLastError();
     });
@@ -687,7 +684,7 @@ hipError_t launch_win_plain_fwd(bool is_bf16, bool fp8, const WinParams& p, hipS
     if (fp8) return is_bf16 ? fwd<__bf16, uint8_t, true>(p, stream) : fwd<float, uint8_t, true>(p, stream);
     return p.table ? fwd<float, float, true>(p, stream) : fwd<float, float, false>(p, stream);
 }
-hipError_t launch_win_plain_bwd(const WinParams& p, hipStream_t stream) { return bwd<float>(p, stream); }
+hipError_t launch_win_plain_bwd(const WinParams& p, hipStream_t stream) { return bwd(p, stream); }
 hipError_t launch_win_join(bool is_bf16, const WinParams& p, hipStream_t stream) {
     // four waves for a row that has many parts
     const int waves = p.splits > 8 ? 4 : 1;
@@ -699,7 +696,7 @@ hipError_t launch_win_join(bool is_bf16, const WinParams& p, hipStream_t stream)
 }
 hipError_t launch_win_rows(const WinParams& p, hipStream_t stream) {
     const dim3 grid((unsigned)(((long)p.batch * p.heads * p.n * 8 + kThreads - 1) / kThreads));
-    hipLaunchKernelGGL(win_rows_kernel<float>, grid, dim3(kThreads), 0, stream, p);
+    hipLaunchKernelGGL(win_rows_kernel, grid, dim3(kThreads), 0, stream, p);
     return hipGetLastError();
 }
 hipError_t launch_win_keys(bool is_bf16, int tile, const WinParams& p, hipStream_t stream) {
