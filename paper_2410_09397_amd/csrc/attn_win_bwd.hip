@@ -7,7 +7,7 @@
 // No atomics, so the same call gives the same bits.  A key that is a sink is seen by every token behind it: the tokens that see a tile
 // with sinks are shared out over p.parts workgroups, whose fp32 sums win_keys_kernel brings together; where there are fewer key tiles than
 // places on the chip, those of the other tiles over p.rest_parts.  P and dS are rounded to bf16 for the
-// products that use them (2^-9 of each weight), sums are fp32.
+// products that use them (2^-9 of each weight; at the padded head dimensions by choice: see attn_win_fwd.hip), sums are fp32.
 #include <type_traits>
 
 #include "attn_internal.hpp"
