@@ -36,12 +36,16 @@ inline int win_key_tile(bool wide) { return wide ? 64 : 32; }
 
 // Workgroups of the key owners.  One streams window + tile tokens per head of its group, one of sink keys all of them: those are shared out over as
 // many workgroups as make the shares about as long (at most 64, and fewer where there are many sink tiles).  Where all of them
-// together are fewer than the places on the chip, the tokens of every tile are shared out: at least two tiles of tokens to each, and enough of
-// them over all heads of the group (twelve; the 32-bit kernels, whose waves take them in turn, six) to pay for the sums' way through memory
-// and the launch behind.  us of the backward, one workgroup per tile -> shared, h heads on k key heads:
+// together are no more than half of the places that are counted here (512 up to d = 128, two on a CU; 256 beyond, one on a CU), the tokens of every tile are shared out: at least two
+// tiles of tokens to each, and enough of them over all heads of the group (twelve; the 32-bit kernels, whose waves take them in turn, six) to pay for the
+// sums' way through memory and the launch behind.  us of the backward, one workgroup per tile -> shared, h heads on k key heads:
 //   d = 128, no window   h8 k2 n512 63 -> 39   h8 k2 n1024 114 -> 55   h16 k2 n2048 380 -> 128      d = 256, no window  h8 k2 n1024 211 -> 104
 //   d = 128, window      h4 k1 n4096 w1024 135 -> 76   h16 k4 n2048 w512 85 -> 77   h8 k8 n1024 w256 (too few tiles) 35 -> 45
 //   d = 64               h4 k4 n300 (too few tiles) 20 -> 22      d = 256, window     h8 k4 n2048 w300 (too few tiles) 73 -> 77
+// Both numbers are one line for all calls, and other lines suit some of them better.  Twelve tiles -> ten: d = 64 w256, h16 k4 n2048 two sequences 42 -> 45
+// (with sinks, whose sums make the launch anyway, 52 -> 53), one sequence 40 -> 37 (with sinks 48 -> 42); d = 128, the same, one sequence 52 -> 50 (59 -> 56); d = 40 h8 k2 n1031 42 -> 38.
+// 512 places -> the 768 that the registers and LDS of d = 64 allow: no window h8 k2 n8192 462 -> 388, h6 k3 n2500 63 -> 62, w700 h12 k3 n6000 108 -> 91, w256 as it was.
+// 256 places -> 512 for the padded rows of 129 to 255: h8 k2 n2048 d = 160 187 -> 166, h16 k4 n2048 d = 200 w512 173 -> 165.
 // sink_tiles: how many of the first key tiles are shared out over `parts` workgroups each (0 where parts is 1); the others over rest_parts;
 // slots: workgroups of a (sequence, key head) whose sums are parts.  window, sinks: as win_reach gives them.
 struct WinParts {
