@@ -240,7 +240,8 @@ attn_status attn_mfma_ceiling(int32_t iters, int32_t operands, float *clock_ghz,
  * gives the same bits.
  * Precision, ATTN_BF16: the weights P and dS are rounded to bf16 for the products that use them, at every d.  attn_fwd and attn_bwd round them at d = 64, 128
  * and 256 only: at other d a causal call without a window or shared heads is more exact through those (distance from 64 bits over the norm 1.6 to
- * 1.7e-3, of O and of the gradients, against 2.0 and 2.4e-3 here), in about the same time.
+ * 1.7e-3, of O and of the gradients, against 2.0 and 2.4e-3 here), in about the same time.  ATTN_F32: a step takes longer than the full causal one of attn_fwd
+ * and attn_bwd where the window is more than about a tenth of the sequence (three times as long without a window).
  * A NaN or an infinity in a row inside a sequence may reach every query whose tile of keys it lies in, also those that do not see it.
  * The work goes with the number of visible pairs: tiles that no query of a block sees are neither read nor computed.
  */

@@ -7,7 +7,10 @@
 //   contraction over rows  step i takes the rows of accumulator register i, which is then an operand as it stands
 // A workgroup owns 32 rows of queries or keys; its four waves take the tiles that stream past in turn, each reading its operands straight from memory
 // (any layout of the rows will do) into accumulators of its own, which meet in LDS at the end: a short window is only a handful of tiles, and a tile
-// takes a wave 64 cycles for every 2 x 32 of its products.
+// takes a wave 64 cycles for every 2 x 32 of its products.  What bounds them is the wait for those reads, not the products (four dependent trips to a tile: 49 to 63 % of the
+// wave cycles wait, the matrix pipe is 16 to 19 % busy; the kernels of attn_stream.hip, which stage whole rows in LDS, keep it 45 to 65 % busy).  us of a step, full causal
+// through those -> windowed through these, b2 h6: n777 d80 w128 81 -> 101 (two key heads) and 118 (six), w64 81 -> 81, n1500 d64 w128 159 -> 135,
+// n2048 d64 w128 278 -> 149; without a window b2 h16 n1000 d96 287 -> 840.
 #include <type_traits>
 
 #include "attn_internal.hpp"
