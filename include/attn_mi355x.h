@@ -320,6 +320,80 @@ size_t attn_paged_workspace_bytes(const attn_paged_desc *desc);
 attn_status attn_paged_fwd(const attn_paged_desc *desc, const attn_cache *cache, const void *Q, void *O, float *LSE,
                            void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Trees of drafted tokens over the paged cache (speculative decoding).  The new tokens of a sequence are not one continuation but several that
+ * share their beginnings: each follows the context or an earlier one of them.  The order of a step is attn_cache_write (lens counts all
+ * drafted tokens), attn_tree_mask once, attn_tree_fwd for every layer, and attn_tree_commit for the branch that was accepted.
+ *   parents  DEVICE int32 [total_q]: the number, among the new tokens of its sequence, of the token that a row follows; -1 (or any number that is
+ *            not an earlier token's): it follows the context
+ *   mask     DEVICE words [total_q] x [(max_q + 31) / 32], rows mask_stride words apart: bit u % 32 of word u / 32 of a row says that it sees new token
+ *            u of its sequence.  attn_tree_mask sets the bits of a row's own token and of those that lead to it; any other bits may be set instead
+ * A query sees the tokens in front of the new ones (the context) and the new ones of its mask.  The r-th of these, in their order, is at
+ * position r and the query at the last one's: under a window it sees those less than `window` away from it, and the first `sinks`.  Of the context
+ * the last `window` tokens and the first `sinks` are read.  A query that sees nothing: O = 0, LSE = -inf.  max_q <= 1024.
+ * attn_tree_mask takes batch, total_q, max_q and q_ptr as in attn_paged_desc and attn_cache; rows of no sequence, and rows from max_q on, are not written.
+ * attn_tree_fwd is attn_paged_fwd with the mask in the place of the order of the new tokens: a mask whose row t has bits 0 .. t gives what that gives
+ * (not the same bits: its key tiles differ).  Its workspace is attn_tree_workspace_bytes.
+ */
+attn_status attn_tree_mask(int32_t batch, int32_t total_q, int32_t max_q, const int32_t *q_ptr, const int32_t *parents, uint32_t *mask,
+                           int64_t mask_stride, void *stream);
+size_t attn_tree_workspace_bytes(const attn_paged_desc *desc);
+attn_status attn_tree_fwd(const attn_paged_desc *desc, const attn_cache *cache, const uint32_t *mask, int64_t mask_stride, const void *Q, void *O,
+                          float *LSE, void *workspace, size_t workspace_bytes, void *stream);
+/* Of the new tokens those that row leaf[b] of a sequence sees stay, behind the context, in their order: their rows move there, and new_lens[b] (DEVICE
+ * int32 [batch], overlaps no input) is the number of tokens that are left.  leaf[b] (DEVICE int32 [batch]) counts within the sequence's new tokens; any other
+ * number, -1 say: none stays.  The slots behind the new length hold what they held.  A token whose page, or the page that it moves to, is outside the
+ * cache does not move.  Of desc the sizes of Q, O, K and V, scale and window do not matter (heads may be kv_heads).  A call with batch, heads, total_q or
+ * max_q 0 has nothing to do and writes nothing, not new_lens either. */
+attn_status attn_tree_commit(const attn_paged_desc *desc, const attn_cache *cache, const uint32_t *mask, int64_t mask_stride, const int32_t *leaf,
+                             int32_t *new_lens, void *stream);
+
+/*
+ * Eviction from the paged cache by accumulated attention weight.  weight[b][h][j] is what the queries have paid to the token in slot j of key head h so far:
+ *     out[b][h][j] = decay * in[b][h][j] + sum exp(scale <Q, K_j> - LSE)     over the new tokens that see j and the query heads of the group,
+ * by attn_cache_weigh, with the visibility and the LSE of attn_paged_fwd (a query with LSE = -inf adds nothing).  New tokens start at zero: `in` is read
+ * for the tokens in front of them only, and may be NULL (zeros).  Slots below lens[b] are written, others not.  `out` may be `in` (with the same strides).
+ * Every token of the cache is worked on, those of sequences without new tokens too: they keep decay times their weight.  Q and LSE (contiguous [total_q,
+ * heads]) may be NULL if total_q or max_q is 0.  batch * kv_heads * ceil(max_len / 128) < 2^24.  Arithmetic as attn_paged_fwd, weights in fp32.
+ */
+typedef struct { /* DEVICE memory; strides in elements, the slots' is 1 and those of batches and heads at least max_len */
+    const float *in;
+    float *out;
+    int64_t in_stride_b, in_stride_h, out_stride_b, out_stride_h;
+    float decay;      /* finite */
+    int32_t reserved; /* 0 */
+} attn_weights;
+attn_status attn_cache_weigh(const attn_paged_desc *desc, const attn_cache *cache, const void *Q, const float *LSE, const attn_weights *weights,
+                             void *stream);
+
+/*
+ * attn_cache_evict: of every sequence of more than `budget` tokens each key head keeps `budget`, for itself: those at positions in front of `first`, the
+ * `recent` latest ones, and of the others those with the largest weights (a tie: the lower slot; NaN is less than anything).  Kept tokens in slots from
+ * `budget` on move into slots that have become free below, both in ascending order; all others stay where they are, so that what moves is as little as can
+ * be.  Their weights and positions move with them.  Attention without a window does not depend on the order of the keys; under a window, slots are not
+ * positions any more.
+ * Positions: a token in slot s < kept[b] is at pos[b][h][s], one behind at seen[b] - lens[b] + s: slots from kept[b] on hold the latest tokens, in their order, the
+ * last at position seen[b] - 1.  seen counts all tokens that the sequence has had; NULL: lens.  kept: new_lens of the last eviction; NULL: 0, and so it is
+ * without pos.  weight_out and pos_out (may be NULL without pos) get the values of the tokens that stay, in slots 0 .. new_lens[b] - 1; they may be weight
+ * and pos themselves, with the same strides.  new_lens[b] = min(lens[b], budget), in memory of its own.  A token whose page, or the page that it moves to, is
+ * outside the cache does not move.
+ * A call with batch, kv_heads or max_len 0 writes nothing.  first + recent <= budget, budget >= 1.  Of desc batch, kv_heads, d, max_len, the pages' fields, dtype and kind matter.
+ */
+typedef struct { /* DEVICE memory; strides in elements, that of the slots is 1 */
+    int32_t budget, first, recent;
+    int32_t reserved; /* 0 */
+    const float *weight;
+    const int32_t *pos, *kept, *seen;
+    float *weight_out;
+    int32_t *pos_out, *new_lens;
+    int64_t stride_b, stride_h;         /* weight, pos: at least max_len */
+    int64_t out_stride_b, out_stride_h; /* weight_out, pos_out: at least min(max_len, budget) */
+} attn_eviction;
+/* Device scratch of attn_cache_evict: the slots between which tokens move.  0 if desc or budget is invalid. */
+size_t attn_evict_workspace_bytes(const attn_paged_desc *desc, int32_t budget);
+attn_status attn_cache_evict(const attn_paged_desc *desc, const attn_cache *cache, const attn_eviction *eviction, void *workspace,
+                             size_t workspace_bytes, void *stream);
+
 /* Static description of a status code. */
 const char *attn_status_str(attn_status s);
 

@@ -23,7 +23,8 @@ ATTN_CACHE_PLAIN, ATTN_CACHE_FP8 = 0, 1
 EXPORTS = ("attn_workspace_bytes", "attn_fwd", "attn_bwd", "attn_bwd_noalloc", "attn_bwd_blocksparse",
            "attn_wgrad_workspace_bytes", "attn_bwd_wgrad", "attn_blockmask_validate", "attn_mfma_ceiling",
            "attn_win_workspace_bytes", "attn_win_fwd", "attn_win_bwd", "attn_cache_write", "attn_cache_read",
-           "attn_paged_workspace_bytes", "attn_paged_fwd", "attn_status_str")
+           "attn_paged_workspace_bytes", "attn_paged_fwd", "attn_tree_mask", "attn_tree_workspace_bytes", "attn_tree_fwd", "attn_tree_commit",
+           "attn_cache_weigh", "attn_evict_workspace_bytes", "attn_cache_evict", "attn_status_str")
 
 
 class attn_desc(ctypes.Structure):
@@ -55,6 +56,18 @@ class attn_paged_desc(ctypes.Structure):
 
 class attn_cache(ctypes.Structure):
     _fields_ = [(f, ctypes.c_void_p) for f in ("K", "V", "K_exp", "V_exp", "table", "lens", "q_ptr")]
+
+
+class attn_weights(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in ("in_", "out")] + \
+               [(f, ctypes.c_int64) for f in ("in_stride_b", "in_stride_h", "out_stride_b", "out_stride_h")] + \
+               [("decay", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class attn_eviction(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_int32) for f in ("budget", "first", "recent", "reserved")] + \
+               [(f, ctypes.c_void_p) for f in ("weight", "pos", "kept", "seen", "weight_out", "pos_out", "new_lens")] + \
+               [(f, ctypes.c_int64) for f in ("stride_b", "stride_h", "out_stride_b", "out_stride_h")]
 
 
 class AttnError(RuntimeError):
@@ -103,6 +116,17 @@ def lib():
         L.attn_cache_write.restype = L.attn_cache_read.restype = L.attn_paged_fwd.restype = ctypes.c_int
         L.attn_cache_write.argtypes = L.attn_cache_read.argtypes = [pp, cp, vp, vp, vp]
         L.attn_paged_fwd.argtypes = [pp, cp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        i32, i64, size = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+        L.attn_tree_workspace_bytes.restype = L.attn_evict_workspace_bytes.restype = size
+        L.attn_tree_workspace_bytes.argtypes = [pp]
+        L.attn_evict_workspace_bytes.argtypes = [pp, i32]
+        for fn in (L.attn_tree_mask, L.attn_tree_fwd, L.attn_tree_commit, L.attn_cache_weigh, L.attn_cache_evict):
+            fn.restype = ctypes.c_int
+        L.attn_tree_mask.argtypes = [i32, i32, i32, vp, vp, vp, i64, vp]
+        L.attn_tree_fwd.argtypes = [pp, cp, vp, i64, vp, vp, vp, vp, size, vp]
+        L.attn_tree_commit.argtypes = [pp, cp, vp, i64, vp, vp, vp]
+        L.attn_cache_weigh.argtypes = [pp, cp, vp, vp, vp, vp]
+        L.attn_cache_evict.argtypes = [pp, cp, vp, vp, size, vp]
         L.attn_status_str.restype = ctypes.c_char_p
         L.attn_status_str.argtypes = [ctypes.c_int]
         _lib = L
@@ -332,6 +356,8 @@ def attn_mfma_ceiling(iters, operands=0, stream=None):
 _WIN_DESC = struct.Struct("@5if4i6q")
 _PAGED_DESC = struct.Struct("@10if5i8q")
 _CACHE = struct.Struct("@7P")
+_WEIGHTS = struct.Struct("@2P4qfi")
+_EVICTION = struct.Struct("@4i7P4q")
 
 
 def _dtype(dtype):
@@ -477,18 +503,27 @@ def attn_cache_pages(num_pages, kv_heads, page_size, d, dtype, device="cuda"):
 
 def _paged(name, x, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp, kv_rows, scale=1.0, window=0, sinks=0):
     """The descriptor and the cache structure of a call whose rows are x: [total, heads, d]; kv_rows: x has the pages' heads."""
-    import torch
-    if x.dim() != 3 or K_pages.dim() != 4 or table.dim() != 2:
+    if x.dim() != 3 or K_pages.dim() != 4:
         raise ValueError("%s: expected rows [total, heads, d], pages [num_pages, kv_heads, page_size, d] and a table [batch, pages]" % name)
-    (total, h, dx), (sn, sh, sd), dtype, device = x.shape, x.stride(), x.dtype, x.device
+    (total, h, dx), (sn, sh, sd) = x.shape, x.stride()
+    if sd != 1:
+        raise ValueError("%s: expected unit stride along d" % name)
+    if dx != K_pages.shape[3] or (kv_rows and h != K_pages.shape[1]):
+        raise ValueError("%s: rows and pages must agree in d and in their heads" % name)
+    return _on_pages(name, total, h, sn, sh, x.dtype, x.device, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp, scale, window, sinks)
+
+
+def _on_pages(name, total, h, sn, sh, dtype, device, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp, scale=1.0, window=0, sinks=0):
+    """The same for rows [total, h, d] with strides sn, sh, or for none (total 0 or strides of the pages' width)."""
+    import torch
+    if K_pages.dim() != 4 or table.dim() != 2:
+        raise ValueError("%s: expected pages [num_pages, kv_heads, page_size, d] and a table [batch, pages]" % name)
     shape, strides, kind = K_pages.shape, K_pages.stride(), K_pages.dtype
     (num, kvh, page, d), (psp, psh, psn, psd) = shape, strides
-    if sd != 1 or psd != 1:
+    if psd != 1:
         raise ValueError("%s: expected unit stride along d" % name)
     if V_pages.shape != shape or V_pages.stride() != strides or V_pages.dtype != kind or V_pages.device != device or K_pages.device != device:
         raise ValueError("%s: K_pages and V_pages must share shape, strides, dtype and the rows' device" % name)
-    if dx != d or (kv_rows and h != kvh):
-        raise ValueError("%s: rows and pages must agree in d and in their heads" % name)
     fp8 = kind is torch.float8_e4m3fn
     if fp8:
         for e in (K_exp, V_exp):
@@ -506,7 +541,7 @@ def _paged(name, x, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp,
         if batch and total % batch:
             raise ValueError("%s: without q_ptr every sequence has the same number of rows" % name)
         max_q = total // batch if batch else 0
-    _on_gpu(x)
+    _on_gpu(K_pages)
     desc = _PAGED_DESC.pack(batch, h, kvh, d, total, max_q, width * page if max_len is None else max_len, page, num, width, scale, window, sinks,
                             _dtype(dtype), ATTN_CACHE_FP8 if fp8 else ATTN_CACHE_PLAIN, 0, sn, sh, sn, sh, psp, psh, psn, ts)
     cache = _CACHE.pack(K_pages.data_ptr(), V_pages.data_ptr(), K_exp.data_ptr() if fp8 else 0, V_exp.data_ptr() if fp8 else 0,
@@ -574,3 +609,191 @@ def attn_paged_fwd(Q, K_pages, V_pages, table, lens, scale, q_ptr=None, max_q=No
     if st != ATTN_OK:
         raise AttnError(st, "attn_paged_fwd")
     return O, LSE
+
+
+# ------------------------------------------------------------------------- what stays in the cache: trees, eviction
+def _on_current(device):
+    """Streams and launches are the current device's (a kernel given addresses of another one would fault)."""
+    import torch
+    if device.type != "cuda":
+        raise ValueError("expected tensors on a GPU, got %s" % device)
+    if device.index != torch.cuda.current_device():
+        raise ValueError("expected tensors on the current GPU (%d), got %s" % (torch.cuda.current_device(), device))
+
+
+def _cache_only(name, total, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp):
+    """The descriptor and the cache structure of a call on the pages alone."""
+    import torch
+    if K_pages.dim() != 4:
+        raise ValueError("%s: expected pages [num_pages, kv_heads, page_size, d] and a table [batch, pages]" % name)
+    kvh, d = K_pages.shape[1], K_pages.shape[3]
+    dtype = torch.bfloat16 if K_pages.dtype is torch.float8_e4m3fn else K_pages.dtype
+    out = _on_pages(name, total, kvh, kvh * d, d, dtype, K_pages.device, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp)
+    _on_current(K_pages.device)
+    return out
+
+
+def _check_mask(name, mask, total, max_q, device):
+    import torch
+    if (mask.dtype is not torch.int32 or mask.dim() != 2 or mask.shape[0] != total or mask.shape[1] * 32 < max_q or mask.device != device or
+            (mask.numel() and mask.stride(1) != 1)):
+        raise ValueError("%s: the mask must be an int32 tensor [total, words] on the rows' device, 32 new tokens to a word, with unit stride along them" % name)
+    return mask.data_ptr(), mask.stride(0)
+
+
+def _max_q(name, total, batch, q_ptr, max_q):
+    if max_q is not None:
+        return max_q
+    if q_ptr is not None:
+        raise ValueError("%s: q_ptr needs max_q, the largest number of new tokens of a sequence" % name)
+    if batch and total % batch:
+        raise ValueError("%s: without q_ptr every sequence has the same number of rows" % name)
+    return total // batch if batch else 0
+
+
+def attn_tree_mask(parents, max_q, q_ptr=None, stream=None, out=None):
+    """int32 words [total, (max_q + 31) // 32]: bit u % 32 of word u // 32 of a row says that it is drafted token u of its sequence, or follows it.
+    parents (int32 [total]): the number, among the drafted tokens of its sequence, of the one that a row follows; -1: it follows the context.  Rows
+    q_ptr[b] .. q_ptr[b + 1] - 1 belong to sequence b (None: max_q rows each).  Rows of no sequence come back as zeros (in `out`: as they were)."""
+    import torch
+    if parents.dim() != 1 or max_q < 0 or (q_ptr is not None and (q_ptr.dim() != 1 or q_ptr.shape[0] < 1)):
+        raise ValueError("attn_tree_mask: expected parents [total], q_ptr [batch + 1] and max_q, the largest number of drafted tokens of a sequence")
+    total, device, words = parents.shape[0], parents.device, -(-max_q // 32)
+    if q_ptr is None and (total % max_q if max_q else total):
+        raise ValueError("attn_tree_mask: without q_ptr every sequence has max_q rows")
+    batch = q_ptr.shape[0] - 1 if q_ptr is not None else total // max_q if max_q else 0
+    _on_current(device)
+    parents_at, q_ptr_at = _int32("parents", parents, total, device), _int32("q_ptr", q_ptr, batch + 1, device)
+    if out is None:
+        out = _made_on(stream, lambda: (torch.empty if q_ptr is None else torch.zeros)((total, words), dtype=torch.int32, device=device))
+    st = lib().attn_tree_mask(batch, total, max_q, q_ptr_at, parents_at, *_check_mask("attn_tree_mask", out, total, max_q, device), _stream(stream))
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_tree_mask")
+    return out
+
+
+def attn_tree_workspace_bytes(desc):
+    return lib().attn_tree_workspace_bytes(_as_argument(desc))
+
+
+def attn_tree_fwd(Q, mask, K_pages, V_pages, table, lens, scale, q_ptr=None, max_q=None, max_len=None, window=0, sinks=0, K_exp=None,
+                  V_exp=None, stream=None, out=None, workspace=None):
+    """attn_paged_fwd for new tokens that are a tree of drafted ones: each sees the context and the new tokens of its row of the mask
+    (attn_tree_mask's, or any bits).  O [total, heads, d], LSE [total, heads]."""
+    desc, cache = _paged("attn_tree_fwd", Q, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp, False, scale, window, sinks)
+    _on_current(Q.device)
+    bits = _check_mask("attn_tree_fwd", mask, Q.shape[0], _max_q("attn_tree_fwd", Q.shape[0], table.shape[0], q_ptr, max_q), Q.device)
+    if out is None:
+        import torch
+        O, LSE = _made_on(stream, lambda: (_empty_as(Q), torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device)))
+    else:
+        O, LSE = out
+        _same_layout(Q, O)
+        _check_lse(LSE, Q)
+    where = size = 0
+    if workspace is None:
+        size = attn_tree_workspace_bytes(desc)
+        if size > 256:  # (256: nothing is kept there)
+            workspace = _scratch(size, Q.device, stream)
+    else:
+        _check_workspace(workspace, Q.device)
+    if workspace is not None:
+        where, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    st = lib().attn_tree_fwd(desc, cache, *bits, Q.data_ptr(), O.data_ptr(), LSE.data_ptr(), where, size, _stream(stream))
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_tree_fwd")
+    return O, LSE
+
+
+def attn_tree_commit(mask, leaf, K_pages, V_pages, table, lens, q_ptr=None, max_q=None, K_exp=None, V_exp=None, stream=None, out=None):
+    """Of the drafted tokens (the last of every sequence in the cache) those that row leaf[b] of the mask sees stay, moved up behind the context in
+    their order.  leaf (int32 [batch]): a drafted token's number in its sequence, anything else: none stays.  Returns the lengths that are left."""
+    import torch
+    total, device, batch = mask.shape[0], K_pages.device, table.shape[0]
+    desc, cache = _cache_only("attn_tree_commit", total, K_pages, V_pages, table, lens, q_ptr, max_q, None, K_exp, V_exp)
+    bits = _check_mask("attn_tree_commit", mask, total, _max_q("attn_tree_commit", total, batch, q_ptr, max_q), device)
+    leaf_at = _int32("leaf", leaf, batch, device)
+    if leaf_at is None:
+        raise ValueError("attn_tree_commit: expected leaf, int32 [batch]")
+    nothing = total == 0 or max_q == 0 or K_pages.shape[1] == 0  # nothing is launched: no drafted token, all of the context stays
+    if out is None:
+        out = _made_on(stream, lambda: lens.clone() if nothing else torch.empty_like(lens))
+    elif nothing:
+        _made_on(stream, lambda: out.copy_(lens))
+    st = lib().attn_tree_commit(desc, cache, *bits, leaf_at, _int32("out", out, batch, device), _stream(stream))
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_tree_commit")
+    return out
+
+
+def _slots(name, what, x, dtype, batch, kv_heads, slots, device):
+    """Address and strides of an array [batch, kv_heads, at least `slots`]."""
+    if x.dtype is not dtype or x.dim() != 3 or x.shape[:2] != (batch, kv_heads) or x.shape[2] < slots or x.device != device or (x.numel() and x.stride(2) != 1):
+        raise ValueError("%s: %s must be a %s tensor [batch, kv_heads, at least %d] on the pages' device with unit stride along the slots"
+                         % (name, what, str(dtype).split(".")[-1], slots))
+    return x.data_ptr(), x.stride(0), x.stride(1)
+
+
+def attn_cache_weigh(Q, LSE, K_pages, V_pages, table, lens, scale, weight=None, decay=1.0, q_ptr=None, max_q=None, max_len=None, window=0, sinks=0,
+                     K_exp=None, V_exp=None, stream=None, out=None):
+    """Attention that the new tokens pay to every token of the cache: out[b, h, j] = decay * weight[b, h, j] + the sum of exp(scale q.k - LSE) over the
+    new tokens that see slot j and the query heads of key head h; Q, LSE and the rest as attn_paged_fwd had or gave them.  New tokens start at zero,
+    weight=None: all do.  weight, out: float32 [batch, kv_heads, at least max_len]; slots from a sequence's length on are left as they are.  out=None:
+    `weight` itself is updated, or without one a new array is made, with zeros in those slots."""
+    import torch
+    desc, cache = _paged("attn_cache_weigh", Q, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp, False, scale, window, sinks)
+    device, batch, kvh = Q.device, table.shape[0], K_pages.shape[1]
+    _on_current(device)
+    _check_lse(LSE, Q)
+    slots = table.shape[1] * K_pages.shape[2] if max_len is None else max_len
+    if out is None:
+        out = weight if weight is not None else _made_on(stream, lambda: torch.zeros((batch, kvh, slots), dtype=torch.float32, device=device))
+    to, to_b, to_h = _slots("attn_cache_weigh", "out", out, torch.float32, batch, kvh, slots, device)
+    at, at_b, at_h = (0, 0, 0) if weight is None else _slots("attn_cache_weigh", "weight", weight, torch.float32, batch, kvh, slots, device)
+    st = lib().attn_cache_weigh(desc, cache, Q.data_ptr(), LSE.data_ptr(), _WEIGHTS.pack(at, to, at_b, at_h, to_b, to_h, decay, 0), _stream(stream))
+    if st != ATTN_OK:
+        raise AttnError(st, "attn_cache_weigh")
+    return out
+
+
+def attn_evict_workspace_bytes(desc, budget):
+    return lib().attn_evict_workspace_bytes(_as_argument(desc), budget)
+
+
+def attn_cache_evict(weight, K_pages, V_pages, table, lens, budget, first=0, recent=0, pos=None, kept=None, seen=None, max_len=None, K_exp=None,
+                     V_exp=None, stream=None, out=None, workspace=None):
+    """Every key head of a sequence of more than `budget` tokens keeps `budget` of them: those at positions below `first`, the `recent` latest, and those
+    with the largest weights.  Kept tokens in slots from `budget` on move into the free ones below.  weight: float32 [batch, kv_heads, at least max_len];
+    pos: the same in int32, positions of the tokens in slots below kept[b] (int32 [batch], the lengths of the last eviction); later slots hold the latest
+    tokens of seen[b] (int32 [batch]; None: lens).  Returns weight, pos, the new lengths; out: where to put them (None: weight and pos
+    themselves).  Without pos, slots are positions, as they are until the first eviction, and pos comes back as None unless `out` has one."""
+    import torch
+    name, device, batch, kvh = "attn_cache_evict", K_pages.device, table.shape[0], K_pages.shape[1]
+    desc, cache = _cache_only(name, 0, K_pages, V_pages, table, lens, None, 0, max_len, K_exp, V_exp)
+    slots = table.shape[1] * K_pages.shape[2] if max_len is None else max_len
+    if out is None:
+        nothing = kvh == 0 or slots == 0  # nothing is launched
+        out = weight, pos, _made_on(stream, lambda: lens.clamp(0, min(budget, slots)) if nothing else torch.empty_like(lens))
+    weight_out, pos_out, new_lens = out
+    at, at_b, at_h = _slots(name, "weight", weight, torch.float32, batch, kvh, slots, device)
+    to, to_b, to_h = _slots(name, "weight's out", weight_out, torch.float32, batch, kvh, min(slots, budget), device)
+    pos_at = pos_to = 0
+    if pos is not None:
+        pos_at, *strides = _slots(name, "pos", pos, torch.int32, batch, kvh, slots, device)
+        if strides != [at_b, at_h] or pos_out is None:
+            raise ValueError("%s: pos must have weight's strides, and a place to go to" % name)
+    if pos_out is not None:
+        pos_to, *strides = _slots(name, "pos' out", pos_out, torch.int32, batch, kvh, min(slots, budget), device)
+        if strides != [to_b, to_h]:
+            raise ValueError("%s: what weight and pos come out in must share strides" % name)
+    lens_to = _int32("the new lengths", new_lens, batch, device)
+    if workspace is None:
+        workspace = _scratch(max(attn_evict_workspace_bytes(desc, budget), 256), device, stream)
+    else:
+        _check_workspace(workspace, device)
+    args = _EVICTION.pack(budget, first, recent, 0, at, pos_at, _int32("kept", kept, batch, device) or 0, _int32("seen", seen, batch, device) or 0,
+                          to, pos_to, lens_to, at_b, at_h, to_b, to_h)
+    st = lib().attn_cache_evict(desc, cache, args, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream))
+    if st != ATTN_OK:
+        raise AttnError(st, name)
+    return out

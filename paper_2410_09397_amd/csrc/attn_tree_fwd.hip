@@ -1,0 +1,51 @@
+// Attention of a tree of drafted tokens over the paged cache, bf16: the kernels of attn_win_fwd.hpp with the tiles and masks of a tree (Sight<BC, true>).
+//
+// The last tokens of a sequence are alternatives for what comes next: each sees the context and those in front of it on its own branch, so that
+// one pass answers all branches.  The context is read as for any new tokens, once for a block of rows (tokens times heads of a group).  Behind it
+// the drafted tokens are tiles of their own that start with the first of them: a tile of the context needs one comparison of positions for all of a
+// wave's rows, and in a tile of drafted tokens 32 bits of a row's mask are 32 keys, read where the tile is (a tree has one or two such tiles).
+#include "attn_win_fwd.hpp"
+
+namespace attn {
+namespace {
+
+template <int D, int SRC, int SPLIT, bool PAD>
+__global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) tree_out_kernel(WinParams p) {
+    win_out<D, SRC, SPLIT, PAD, true>(p, p.row_blocks);
+}
+template <int D, int SRC, bool PAD>
+__global__ void __launch_bounds__((64 * kFewWaves<D, SRC>), (D == 256 ? 1 : 2)) tree_few_kernel(WinParams p) {
+    win_few<D, SRC, PAD, true>(p);
+}
+template <int D, int SRC, bool PAD>
+__global__ void __launch_bounds__(kThreads, (kOnePerCu<D, SRC>)) tree_one_kernel(WinParams p) {
+    win_one<D, SRC, PAD, true>(p);
+}
+
+template <int D, int SRC, bool PAD>
+hipError_t launch_from(int rows, const WinParams& p, hipStream_t stream) {
+    const dim3 grid((unsigned)((long)p.blocks * p.kv_heads), (unsigned)p.splits);
+    auto run = [&](auto kernel, int lds, int threads) {
+        const hipError_t e = allow_lds(kernel, lds);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, stream, p);
+        return hipGetLastError();
+    };
+    if (rows == 16) return run(tree_one_kernel<D, SRC, PAD>, kOneLds<D, SRC>, kThreads);
+    if (rows == 32) return run(tree_few_kernel<D, SRC, PAD>, kFewLds<D, SRC>, 64 * kFewWaves<D, SRC>);
+    return rows == 64 ? run(tree_out_kernel<D, SRC, 2, PAD>, 4 * 64 * D * 2, kThreads) : run(tree_out_kernel<D, SRC, 1, PAD>, 4 * 64 * D * 2, kThreads);
+}
+template <int D>
+hipError_t launch(bool fp8, int rows, const WinParams& p, hipStream_t stream) {
+    if (fp8) return launch_from<D, kCodes, false>(rows, p, stream);
+    return p.d < D ? launch_from<D, kPages, true>(rows, p, stream) : launch_from<D, kPages, false>(rows, p, stream);
+}
+
+}  // namespace
+
+hipError_t launch_tree_fwd(bool fp8, int rows, const WinParams& p, hipStream_t stream) {
+    if (!p.table || !p.tree || (fp8 && p.d != 64 && p.d != 128 && p.d != 256)) return hipErrorInvalidValue;
+    return p.d <= 64 ? launch<64>(fp8, rows, p, stream) : p.d <= 128 ? launch<128>(fp8, rows, p, stream) : launch<256>(fp8, rows, p, stream);
+}
+
+}  // namespace attn

@@ -141,7 +141,7 @@ attn_status check_cache(const attn_paged_desc* d, const attn_cache* c) {
 
 int paged_rows(const attn_paged_desc* d) { return attn::paged_rows(is_wide(d), d->batch, d->heads, d->kv_heads, d->total_q, d->max_q); }
 
-WinParams paged_params(const attn_paged_desc* d, const attn_cache* c) {
+WinParams paged_params(const attn_paged_desc* d, const attn_cache* c, bool tree = false) {
     WinParams p;
     std::memset(&p, 0, sizeof(p));
     p.q_h = d->q_stride_h;
@@ -170,7 +170,7 @@ WinParams paged_params(const attn_paged_desc* d, const attn_cache* c) {
     p.scale = d->scale;
     set_window(p, d->window, d->sinks, d->max_len);
     p.parts = p.rest_parts = 1;
-    const attn::PagedSplits splits = attn::paged_splits(is_wide(d), d->batch, d->heads, d->kv_heads, d->d, d->total_q, d->max_q, d->max_len, p.window, p.sinks);
+    const attn::PagedSplits splits = attn::paged_splits(is_wide(d), d->batch, d->heads, d->kv_heads, d->d, d->total_q, d->max_q, d->max_len, p.window, p.sinks, tree);
     p.row_blocks = splits.row_blocks;
     p.blocks = splits.blocks;
     p.splits = splits.splits;
@@ -183,6 +183,41 @@ size_t part_ml_bytes(const attn_paged_desc* d, const WinParams& p) {
 }
 size_t part_o_bytes(const attn_paged_desc* d, const WinParams& p) {
     return p.splits > 1 ? (size_t)d->total_q * d->heads * p.splits * d->d * sizeof(float) : 0;
+}
+
+// Calls on the cache that have no new tokens' rows.
+bool no_cache(const attn_paged_desc* d) { return d->batch == 0 || d->heads == 0 || d->max_len == 0; }
+
+bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + b_bytes && y < x + a_bytes;
+}
+
+// Pages' rows move in units of 16, 8 or 4 bytes, whatever all of them are a multiple of and aligned to.
+int value_bytes(const attn_paged_desc* d) { return d->kind == ATTN_CACHE_FP8 ? 1 : d->dtype == ATTN_BF16 ? 2 : 4; }
+int page_unit(const attn_paged_desc* d, const attn_cache* c) {
+    const uint64_t es = value_bytes(d);
+    const uint64_t all = (es * d->d) | (es * d->page_stride_p) | (es * d->page_stride_h) | (es * d->page_stride_n) |
+                         reinterpret_cast<uintptr_t>(c->K) | reinterpret_cast<uintptr_t>(c->V);
+    return all % 16 == 0 ? 16 : all % 8 == 0 ? 8 : 4;
+}
+
+// Arrays [batch][kv_heads][slots]
+bool good_slots(const attn_paged_desc* d, int64_t stride_b, int64_t stride_h, int64_t slots) {
+    return stride_b >= 0 && stride_h >= 0 && (d->kv_heads <= 1 || stride_h >= slots) && (d->batch <= 1 || stride_b >= slots);
+}
+
+attn_status check_tree(const attn_paged_desc* d, const uint32_t* mask, int64_t mask_stride) {
+    if (!mask || mask_stride < 0 || (d->total_q > 1 && mask_stride < ((int64_t)d->max_q + 31) / 32)) return ATTN_ERR_INVALID_ARG;
+    return d->max_q > attn::kMostDrafted ? ATTN_ERR_UNSUPPORTED : ATTN_OK;
+}
+
+int evict_cap(const attn_paged_desc* d, int32_t budget) { return std::max(0, std::min(budget, d->max_len - budget)); }
+attn_status check_evict(const attn_paged_desc* d, int32_t budget) {
+    const attn_status st = check_paged(d);
+    if (st != ATTN_OK) return st;
+    if (budget < 1) return ATTN_ERR_INVALID_ARG;
+    return no_cache(d) || (int64_t)d->batch * d->kv_heads <= attn::kMostGroups ? ATTN_OK : ATTN_ERR_UNSUPPORTED;
 }
 
 attn_status status_of(hipError_t e) { return e == hipSuccess ? ATTN_OK : ATTN_ERR_DEVICE; }
@@ -304,6 +339,163 @@ attn_status attn_paged_fwd(const attn_paged_desc* desc, const attn_cache* cache,
     hipError_t e = is_wide(desc) ? attn::launch_win_fwd(fp8, paged_rows(desc), p, s) : attn::launch_win_plain_fwd(bf16, fp8, p, s);
     if (e == hipSuccess && p.splits > 1) e = attn::launch_win_join(bf16, p, s);
     return status_of(e);
+}
+
+attn_status attn_tree_mask(int32_t batch, int32_t total_q, int32_t max_q, const int32_t* q_ptr, const int32_t* parents, uint32_t* mask,
+                           int64_t mask_stride, void* stream) {
+    if (batch < 0 || total_q < 0 || max_q < 0 || mask_stride < 0) return ATTN_ERR_INVALID_ARG;
+    if (batch == 0 || total_q == 0 || max_q == 0) return ATTN_OK;
+    if (!parents || !mask || (total_q > 1 && mask_stride < ((int64_t)max_q + 31) / 32) || (!q_ptr && (int64_t)batch * max_q > total_q))
+        return ATTN_ERR_INVALID_ARG;
+    if (batch > 65535 || max_q > attn::kMostDrafted || total_q > kMostTokens) return ATTN_ERR_UNSUPPORTED;
+    WinParams p;
+    std::memset(&p, 0, sizeof(p));
+    p.batch = batch;
+    p.total_q = total_q;
+    p.n = max_q;
+    p.q_ptr = q_ptr;
+    p.tree_stride = mask_stride;
+    return status_of(attn::launch_tree_mask(p, parents, mask, static_cast<hipStream_t>(stream)));
+}
+
+size_t attn_tree_workspace_bytes(const attn_paged_desc* desc) {
+    if (check_paged(desc) != ATTN_OK || desc->max_q > attn::kMostDrafted) return 0;
+    if (is_empty(desc)) return 256;
+    const WinParams p = paged_params(desc, nullptr, true);
+    return std::max<size_t>(256, part_ml_bytes(desc, p) + part_o_bytes(desc, p));
+}
+
+attn_status attn_tree_fwd(const attn_paged_desc* desc, const attn_cache* cache, const uint32_t* mask, int64_t mask_stride, const void* Q, void* O,
+                          float* LSE, void* workspace, size_t workspace_bytes, void* stream) {
+    attn_status st = check_paged(desc);
+    if (st != ATTN_OK) return st;
+    if (is_empty(desc)) return ATTN_OK;
+    st = check_cache(desc, cache);
+    if (st == ATTN_OK) st = check_tree(desc, mask, mask_stride);
+    if (st != ATTN_OK) return st;
+    const bool bf16 = desc->dtype == ATTN_BF16, fp8 = desc->kind == ATTN_CACHE_FP8;
+    if (!Q || !O || !LSE || (bf16 && !(aligned16(Q) && aligned16(O)))) return ATTN_ERR_INVALID_ARG;
+    WinParams p = paged_params(desc, cache, true);
+    if (p.splits > 1 && (!workspace || workspace_bytes < part_ml_bytes(desc, p) + part_o_bytes(desc, p) || !aligned16(workspace)))
+        return ATTN_ERR_WORKSPACE;
+    p.tree = mask;
+    p.tree_stride = mask_stride;
+    p.Q = Q;
+    p.O = O;
+    p.LSE = LSE;
+    p.part_ml = static_cast<float*>(workspace);
+    p.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + part_ml_bytes(desc, p));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t e = is_wide(desc) ? attn::launch_tree_fwd(fp8, paged_rows(desc), p, s) : attn::launch_tree_plain_fwd(bf16, fp8, p, s);
+    if (e == hipSuccess && p.splits > 1) e = attn::launch_win_join(bf16, p, s);
+    return status_of(e);
+}
+
+attn_status attn_tree_commit(const attn_paged_desc* desc, const attn_cache* cache, const uint32_t* mask, int64_t mask_stride, const int32_t* leaf,
+                             int32_t* new_lens, void* stream) {
+    attn_status st = check_paged(desc);
+    if (st != ATTN_OK) return st;
+    if (is_empty(desc)) return ATTN_OK;
+    st = check_cache(desc, cache);
+    if (st == ATTN_OK) st = check_tree(desc, mask, mask_stride);
+    if (st != ATTN_OK) return st;
+    const size_t lens_bytes = sizeof(int32_t) * (size_t)desc->batch;
+    if (!leaf || !new_lens || overlap(new_lens, lens_bytes, cache->lens, lens_bytes) || overlap(new_lens, lens_bytes, leaf, lens_bytes))
+        return ATTN_ERR_INVALID_ARG;
+    if ((int64_t)desc->kv_heads * 2 > attn::kMostGroups / desc->batch) return ATTN_ERR_UNSUPPORTED;
+    WinParams p = paged_params(desc, cache);
+    p.tree = mask;
+    p.tree_stride = mask_stride;
+    return status_of(attn::launch_tree_commit(value_bytes(desc) * desc->d, page_unit(desc, cache), p, leaf, new_lens, static_cast<hipStream_t>(stream)));
+}
+
+attn_status attn_cache_weigh(const attn_paged_desc* desc, const attn_cache* cache, const void* Q, const float* LSE, const attn_weights* weights,
+                             void* stream) {
+    attn_status st = check_paged(desc);
+    if (st != ATTN_OK) return st;
+    if (!weights || weights->reserved != 0 || !std::isfinite(weights->decay)) return ATTN_ERR_INVALID_ARG;
+    if (no_cache(desc)) return ATTN_OK;
+    st = check_cache(desc, cache);
+    if (st != ATTN_OK) return st;
+    const bool bf16 = desc->dtype == ATTN_BF16, fp8 = desc->kind == ATTN_CACHE_FP8;
+    if (desc->total_q > 0 && desc->max_q > 0 && (!Q || !LSE)) return ATTN_ERR_INVALID_ARG;
+    if (!weights->out || (bf16 && !aligned16(Q))) return ATTN_ERR_INVALID_ARG;
+    if (!good_slots(desc, weights->out_stride_b, weights->out_stride_h, desc->max_len)) return ATTN_ERR_INVALID_ARG;
+    if (weights->in && (!good_slots(desc, weights->in_stride_b, weights->in_stride_h, desc->max_len) ||
+                        (weights->in == weights->out && (weights->in_stride_b != weights->out_stride_b || weights->in_stride_h != weights->out_stride_h))))
+        return ATTN_ERR_INVALID_ARG;
+    const int64_t bk = (int64_t)desc->batch * desc->kv_heads;
+    if (bk > kMostGroups || ((int64_t)desc->max_len + 127) / 128 * bk > kMostGroups) return ATTN_ERR_UNSUPPORTED;
+    attn::WeighParams w;
+    std::memset(&w, 0, sizeof(w));
+    w.p = paged_params(desc, cache);
+    w.p.Q = Q;
+    w.p.LSE_in = LSE;
+    w.in = weights->in;
+    w.out = weights->out;
+    w.in_b = weights->in_stride_b;
+    w.in_h = weights->in_stride_h;
+    w.out_b = weights->out_stride_b;
+    w.out_h = weights->out_stride_h;
+    w.decay = weights->decay;
+    w.chunk = 128;
+    w.blocks = (desc->max_len + w.chunk - 1) / w.chunk;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return status_of(is_wide(desc) ? attn::launch_weigh(fp8, w, s) : attn::launch_weigh_plain(bf16, fp8, w, s));
+}
+
+size_t attn_evict_workspace_bytes(const attn_paged_desc* desc, int32_t budget) {
+    if (check_evict(desc, budget) != ATTN_OK) return 0;
+    if (no_cache(desc)) return 256;
+    const size_t bk = (size_t)desc->batch * desc->kv_heads;
+    return std::max<size_t>(256, sizeof(int32_t) * bk * (1 + 2 * (size_t)evict_cap(desc, budget)));
+}
+
+attn_status attn_cache_evict(const attn_paged_desc* desc, const attn_cache* cache, const attn_eviction* eviction, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+    if (!eviction) return desc ? ATTN_ERR_INVALID_ARG : check_paged(desc);
+    const attn_eviction& v = *eviction;
+    attn_status st = check_evict(desc, v.budget);
+    if (st != ATTN_OK) return st;
+    if (v.first < 0 || v.recent < 0 || (int64_t)v.first + v.recent > v.budget || v.reserved != 0) return ATTN_ERR_INVALID_ARG;
+    if (no_cache(desc)) return ATTN_OK;
+    if (!cache || !cache->K || !cache->V) return ATTN_ERR_INVALID_ARG;
+    attn_paged_desc rest = *desc;  // (there are no rows to check)
+    rest.max_q = 0;
+    st = check_cache(&rest, cache);
+    if (st != ATTN_OK) return st;
+    if (!v.weight || !v.weight_out || !v.new_lens || (v.pos && !v.pos_out)) return ATTN_ERR_INVALID_ARG;
+    if (!good_slots(desc, v.stride_b, v.stride_h, desc->max_len) || !good_slots(desc, v.out_stride_b, v.out_stride_h, std::min(desc->max_len, v.budget)))
+        return ATTN_ERR_INVALID_ARG;
+    const bool same = v.stride_b == v.out_stride_b && v.stride_h == v.out_stride_h;
+    if (!same && (v.weight == v.weight_out || (v.pos && v.pos == v.pos_out))) return ATTN_ERR_INVALID_ARG;
+    const size_t lens_bytes = sizeof(int32_t) * (size_t)desc->batch;
+    for (const int32_t* in : {cache->lens, v.kept, v.seen})
+        if (in && overlap(v.new_lens, lens_bytes, in, lens_bytes)) return ATTN_ERR_INVALID_ARG;
+    if (!workspace || workspace_bytes < attn_evict_workspace_bytes(desc, v.budget) || !aligned16(workspace)) return ATTN_ERR_WORKSPACE;
+    attn::EvictParams e;
+    std::memset(&e, 0, sizeof(e));
+    e.p = paged_params(&rest, cache);
+    e.budget = v.budget;
+    e.first = v.first;
+    e.recent = v.recent;
+    e.cap = evict_cap(desc, v.budget);
+    e.weight = v.weight;
+    e.pos = v.pos;
+    e.kept = v.kept;
+    e.seen = v.seen;
+    e.weight_out = v.weight_out;
+    e.pos_out = v.pos_out;
+    e.new_lens = v.new_lens;
+    e.in_b = v.stride_b;
+    e.in_h = v.stride_h;
+    e.out_b = v.out_stride_b;
+    e.out_h = v.out_stride_h;
+    const size_t bk = (size_t)desc->batch * desc->kv_heads;
+    e.count = static_cast<int32_t*>(workspace);
+    e.from = e.count + bk;
+    e.to = e.from + bk * e.cap;
+    return status_of(attn::launch_evict(value_bytes(desc) * desc->d, page_unit(desc, cache), e, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

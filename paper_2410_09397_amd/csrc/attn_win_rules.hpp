@@ -84,14 +84,16 @@ inline int paged_rows(bool wide, int batch, int heads, int kv_heads, int total_q
 struct PagedSplits {
     int row_blocks, blocks, splits, chunk;
 };
-inline PagedSplits paged_splits(bool wide, int batch, int heads, int kv_heads, int d, int total_q, int max_q, int max_len, int window, int sinks) {
+inline PagedSplits paged_splits(bool wide, int batch, int heads, int kv_heads, int d, int total_q, int max_q, int max_len, int window, int sinks,
+                                bool tree = false) {
     const int64_t group = heads / kv_heads, rows = paged_rows(wide, batch, heads, kv_heads, total_q, max_q), tile = rows >= 64 ? 64 : 32;
     const bool few = rows < 64;
     PagedSplits p = {(int)((max_q * group + rows - 1) / rows), 0, 1, 0x7fffffff};
     p.blocks = (int)std::min((int64_t)p.row_blocks * batch, total_q * group / rows + batch);
     const int64_t blocks = (int64_t)p.blocks * kv_heads;
-    // (the windows of a block reach over window + its tokens - 1 keys, which lie in one tile more than they fill, as the sinks do)
-    const int64_t keys = std::min<int64_t>(max_len, (int64_t)window + max_q) + sinks, tiles = keys / tile + 3;
+    // (the windows of a block reach over window + its tokens - 1 keys, which lie in one tile more than they fill, as the sinks do; drafted tokens
+    // have tiles of their own)
+    const int64_t keys = std::min<int64_t>(max_len, (int64_t)window + max_q) + sinks, tiles = keys / tile + (tree ? 4 : 3);
     // How many: as many as there are places (some more for few rows, whose lengths differ), but not in pieces so small that the launch that
     // joins them costs more than they save.  us, split -> not: one token of b sequences of L keys, d = 128, quantised: b1 L600 11.0 -> 10.4,
     // b1 L1000 11.2 -> 13.6, b64 L1000 33 -> 24; d = 256: b1 L300 12.9 -> 11.4, b1 L600 13.0 -> 14.9
@@ -103,6 +105,12 @@ inline PagedSplits paged_splits(bool wide, int batch, int heads, int kv_heads, i
         p.splits = (int)((tiles + p.chunk - 1) / p.chunk);
     }
     return p;
+}
+
+constexpr int kMostDrafted = 1024;  // drafted tokens of a sequence: their masks are 32 words
+// Workgroups that move a (sequence, key head)'s kept tokens, `rows` at a time, of which there are at most `cap`.
+inline int evict_blocks(int64_t bk, int64_t cap, int64_t rows) {
+    return (int)std::max<int64_t>(1, std::min((cap + rows - 1) / rows, std::min<int64_t>(1024, kMostGroups / std::max<int64_t>(1, bk))));
 }
 
 // Threads that share a row of the cache, 8 values each.

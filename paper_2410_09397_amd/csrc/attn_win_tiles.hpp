@@ -1,6 +1,7 @@
 // Windowed attention on bf16-MFMA, d in {64, 128, 256}: how rows of a tile come from tensors or pages into the swizzled LDS tiles of
 // attn_common.hpp.  HIP device code only.
 #pragma once
+#include "attn_win_rules.hpp"
 #include "attn_window.hpp"
 
 namespace attn {
@@ -76,6 +77,120 @@ struct LaneBounds {
     __device__ __forceinline__ void init(const WinParams& p, int i, int len) {
         hi = i < len ? i : -1;
         lo = i - p.window + 1;
+    }
+};
+
+// The tiles of BC keys that a block of rows goes through, and which of a tile's keys the query of a lane sees.
+//   init        t: the lane's token; t_lo .. t_hi: those of its wave; b_lo .. b_hi: those of its workgroup
+//   all, none   every row of the wave sees all of the keys j0 .. j0 + last of tile `it`, or none of them
+//   keys        seen(T, c): the lane's query sees key j0 + 32 T + shift + c (of NT accumulators of 32 keys)
+template <int BC, bool TREE>
+struct Sight {
+    WinTiles<BC> tiles;
+    LaneBounds see;
+    int t_lo, t_hi, len;
+    __device__ __forceinline__ void init(const WinParams& p, const WinSeq& s, int t, int wave_lo, int wave_hi, int b_lo, int b_hi) {
+        see.init(p, s.first + t, s.len);
+        t_lo = s.first + wave_lo;
+        t_hi = s.first + wave_hi;
+        len = s.len;
+        tiles.init(p, s.len, s.first + b_lo, s.first + b_hi);
+    }
+    __device__ __forceinline__ bool all(const WinParams& p, int, int j0, int last) const {
+        return j0 + last <= t_lo && t_hi < len && (t_hi - j0 < p.window || j0 + last < p.sinks);
+    }
+    __device__ __forceinline__ bool none(const WinParams& p, int, int j0, int last) const {
+        return j0 > t_hi || (j0 + last < t_lo - p.window + 1 && j0 >= p.sinks);
+    }
+    struct Keys {
+        int hi, lo, sink;
+        __device__ __forceinline__ bool operator()(int T, int c) const {
+            c += 32 * T;
+            return c <= hi && (c >= lo || c < sink);
+        }
+    };
+    template <int NT>
+    __device__ __forceinline__ Keys keys(const WinParams& p, int, int j0, int shift) const {
+        const int j = j0 + shift;
+        return {see.hi - j, see.lo - j, p.sinks - j};
+    }
+};
+
+// A tree of drafted tokens behind a context: tiles of the context first (those of the sinks, then those of the windows), then tiles of the drafted
+// tokens, which start with the first of them, so that a tile's keys are all told by position or all by mask.
+template <int BC>
+struct Sight<BC, true> {
+    struct Tiles {
+        int context, lo, end;  // slots 0 .. context - 1 and context .. end - 1; of the context lo .. and 0 .. sinks - 1 are seen by some query
+        int ns, first, of_context, count;
+        __device__ __forceinline__ void init(const WinParams& p, const WinSeq& s) {
+            context = max(0, s.first);
+            end = max(context, min(s.len, s.first + s.nq));
+            lo = max(0, context - p.window);  // (of a query that sees no drafted token)
+            ns = (min(p.sinks, context) + BC - 1) / BC;
+            first = max(lo / BC, ns);
+            of_context = ns + max(0, (context + BC - 1) / BC - first);
+            count = of_context + (end - context + BC - 1) / BC;
+        }
+        __device__ __forceinline__ int start(int it) const {
+            return it < of_context ? (it < ns ? it : it - ns + first) * BC : context + (it - of_context) * BC;
+        }
+        __device__ __forceinline__ int row(const WinParams& p, int j) const {  // (as WinTiles)
+            j = min(j, end - 1);
+            return j < lo && j >= p.sinks ? ((j & -BC) < p.sinks ? p.sinks - 1 : lo) : j;
+        }
+        __device__ __forceinline__ bool whole(const WinParams&, int) const { return false; }
+    } tiles;
+    const uint32_t* mask;  // of the lane's query
+    int seen, lo;          // under a window: drafted tokens that it sees, and the first key of the context in its window
+    int first, nq;
+    static __device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
+    // bits u .. u + 31 of the mask; tokens in front of slot 0 and behind the last one are none
+    __device__ __forceinline__ uint32_t drafted(const WinParams& p, int u) const {
+        const int w = u >> 5, words = (p.n + 31) >> 5;
+        const uint32_t a = w < words ? mask[w] : 0u, b = (u & 31) && w + 1 < words ? mask[w + 1] : 0u;
+        return (uint32_t)((((uint64_t)b << 32) | a) >> (u & 31)) & below(nq - u) & ~below(-first - u);
+    }
+    __device__ __forceinline__ void init(const WinParams& p, const WinSeq& s, int t, int, int, int, int) {
+        tiles.init(p, s);
+        first = s.first;
+        nq = s.nq;
+        mask = p.tree + (s.row0 + t) * p.tree_stride;
+        seen = 0;
+        if (p.window < kNoWindow) {
+            for (int u = 0; u < nq; u += 32) seen += __popc(drafted(p, u));
+        }
+        lo = tiles.context + seen - p.window;  // the query is at position context + seen - 1
+    }
+    __device__ __forceinline__ bool all(const WinParams& p, int it, int j0, int last) const {
+        return it < tiles.of_context && j0 + last < tiles.context && (tiles.context + nq - 1 - j0 < p.window || j0 + last < p.sinks);
+    }
+    __device__ __forceinline__ bool none(const WinParams&, int it, int j0, int) const { return j0 >= (it < tiles.of_context ? tiles.context : tiles.end); }
+    // keys j .. j + 31 of a tile
+    __device__ __forceinline__ uint32_t bits(const WinParams& p, int it, int j) const {
+        if (it < tiles.of_context) return below(tiles.context - j) & (~below(lo - j) | below(p.sinks - j));
+        uint32_t v = drafted(p, j - first);
+        if (p.window < kNoWindow) {  // the r-th drafted token that the query sees is at position context + r
+            int r = 0;
+            for (int u = 0; u < j - first; u += 32) r += __popc(drafted(p, u) & below(j - first - u));
+            uint32_t in = 0;
+            for (uint32_t left = v; left; left &= left - 1, ++r)
+                if (seen - 1 - r < p.window || tiles.context + r < p.sinks) in |= left & -left;
+            v = in;
+        }
+        return v;
+    }
+    template <int NT>
+    struct Keys {
+        uint32_t v[NT];
+        __device__ __forceinline__ bool operator()(int T, int c) const { return (v[T] >> c) & 1u; }
+    };
+    template <int NT>
+    __device__ __forceinline__ Keys<NT> keys(const WinParams& p, int it, int j0, int shift) const {
+        Keys<NT> k;
+#pragma unroll
+        for (int T = 0; T < NT; ++T) k.v[T] = bits(p, it, j0 + 32 * T) >> shift;
+        return k;
     }
 };
 

@@ -35,6 +35,8 @@ struct WinParams {
     // share of the tokens; where there are several, their sums meet in win_keys_kernel
     int sink_tiles, parts, rest_parts;
     int slots;  // workgroups of a (sequence, key head) whose sums are parts
+    const uint32_t* tree;  // drafted tokens: which of them each sees, [row][(n + 31) / 32 words], rows tree_stride words apart
+    long tree_stride;
     float* part_kv;  // [batch * kv_heads][slot][dK, dV][keys of a tile][d]
 };
 
@@ -51,6 +53,7 @@ __device__ __forceinline__ int win_token(const WinParams& p, int r) {
 struct WinSeq {
     int len, nq, first;  // keys 0 .. len - 1; queries t = 0 .. nq - 1 at positions first + t
     long q_base, lse_base, lse_h, lse_t;
+    long row0;  // paged: its first row of Q
 };
 __device__ __forceinline__ WinSeq win_sequence(const WinParams& p, int b) {
     WinSeq s;
@@ -61,6 +64,7 @@ __device__ __forceinline__ WinSeq win_sequence(const WinParams& p, int b) {
         s.first = s.len - rows;
         s.nq = min(rows, p.n);
         s.q_base = (long)row0 * p.q_n;
+        s.row0 = row0;
         s.lse_base = (long)row0 * p.heads;
         s.lse_h = 1;
         s.lse_t = p.heads;
@@ -69,6 +73,7 @@ __device__ __forceinline__ WinSeq win_sequence(const WinParams& p, int b) {
         s.first = 0;
         s.nq = p.n;
         s.q_base = (long)b * p.q_b;
+        s.row0 = 0;
         s.lse_base = (long)b * p.heads * p.n;
         s.lse_h = p.n;
         s.lse_t = 1;
@@ -197,11 +202,42 @@ struct WinKeys {
 hipError_t launch_win_plain_fwd(bool is_bf16, bool fp8, const WinParams& p, hipStream_t stream);
 // bf16; quantised pages: d in {64, 128, 256}; rows of a workgroup: 16, 32 (pages), 64, 128
 hipError_t launch_win_fwd(bool fp8, int rows, const WinParams& p, hipStream_t stream);
+hipError_t launch_tree_fwd(bool fp8, int rows, const WinParams& p, hipStream_t stream);  // the same for p.tree: 16, 32, 64, 128
 hipError_t launch_win_bwd(int rows, const WinParams& p, hipStream_t stream);                                // rows: 64, 128; forms delta itself
+hipError_t launch_tree_plain_fwd(bool is_bf16, bool fp8, const WinParams& p, hipStream_t stream);
 hipError_t launch_win_plain_bwd(const WinParams& p, hipStream_t stream);  // fp32
 hipError_t launch_win_join(bool is_bf16, const WinParams& p, hipStream_t stream);
 hipError_t launch_win_keys(bool is_bf16, int tile, const WinParams& p, hipStream_t stream);
 hipError_t launch_win_rows(const WinParams& p, hipStream_t stream);       // fp32: delta
+// Which tokens each drafted one sees, from those that they follow: mask rows of (max_q + 31) / 32 words.
+hipError_t launch_tree_mask(const WinParams& p, const int32_t* parents, uint32_t* mask, hipStream_t stream);
+// Drafted tokens that row `leaf` of p.tree sees stay; unit: bytes (4, 8 or 16) that every row of the pages is a multiple of and aligned to.
+hipError_t launch_tree_commit(int row_bytes, int unit, const WinParams& p, const int32_t* leaf, int32_t* new_lens, hipStream_t stream);
+
+// attn_cache_weigh: weights of the tokens of a (sequence, key head)
+struct WeighParams {
+    WinParams p;
+    const float* in;  // nullptr: zeros
+    float* out;
+    long in_b, in_h, out_b, out_h;
+    float decay;
+    int blocks, chunk;  // workgroups of a (sequence, key head), and keys of each
+};
+hipError_t launch_weigh(bool fp8, const WeighParams& w, hipStream_t stream);                     // bf16; quantised pages: d in {64, 128, 256}
+hipError_t launch_weigh_plain(bool is_bf16, bool fp8, const WeighParams& w, hipStream_t stream);
+
+// attn_cache_evict: of longer sequences `budget` tokens stay
+struct EvictParams {
+    WinParams p;
+    int budget, first, recent, cap;  // cap: most tokens that move
+    const float* weight;
+    const int32_t *pos, *kept, *seen;
+    float* weight_out;
+    int32_t *pos_out, *new_lens;
+    long in_b, in_h, out_b, out_h;
+    int32_t *count, *from, *to;  // of every (sequence, key head): tokens that move, [cap] slots each
+};
+hipError_t launch_evict(int row_bytes, int unit, const EvictParams& e, hipStream_t stream);
 hipError_t launch_cache_write(bool is_bf16, bool fp8, const WinParams& p, const void* K, const void* V, long s_n, long s_h, hipStream_t stream);
 hipError_t launch_cache_read(bool is_bf16, bool fp8, const WinParams& p, void* K, void* V, long s_n, long s_h, hipStream_t stream);
 
