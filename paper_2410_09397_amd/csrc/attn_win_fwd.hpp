@@ -514,6 +514,7 @@ __device__ __forceinline__ void win_few(const WinParams& p) {
         for (int i = 0; i < 16; ++i) st[0][i] = 0.f;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) st[0] = mfma32(fo.frag(lds, 0, 0, ks), qf[ks], st[0]);
+        settle_products(st[0]);
         acc.weights(st, cs, !see.all(p, it, j0, 31), [&] { return see.template keys<1>(p, it, j0, 4 * h); });
 #pragma unroll
         for (int x = 0; x < 2; ++x) {

@@ -37,6 +37,11 @@ __device__ __forceinline__ unsigned lds_address(const void* at) {
     return __builtin_amdgcn_readfirstlane((unsigned)(size_t)(ATTN_LDS const char*)at);
 }
 
+// Behind the last product of a sum whose next reader is on the other side of a branch.  A product of 8 passes is in its registers 11 states later; the
+// compiler puts the states in between within a block, but on the way around a branch that is taken it has been seen to leave out all but three of them: at d = 256
+// the last register, read first, then lacked the last products (one key of 32 with a wrong score).
+__device__ __forceinline__ void settle_products(f32x16& sum) { asm volatile("s_nop 10" : "+v"(sum)); }
+
 // The pages of up to 64 consecutive entries of a sequence's table, one per lane: a wave asks for the page of a key by a shuffle, and reads the
 // table once per 64 entries (1024 keys in pages of 16), not once per tile: the wait for it drains the copies in flight.
 struct PageWindow {
