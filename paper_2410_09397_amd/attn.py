@@ -654,7 +654,7 @@ def _max_q(name, total, batch, q_ptr, max_q):
 def attn_tree_mask(parents, max_q, q_ptr=None, stream=None, out=None):
     """int32 words [total, (max_q + 31) // 32]: bit u % 32 of word u // 32 of a row says that it is drafted token u of its sequence, or follows it.
     parents (int32 [total]): the number, among the drafted tokens of its sequence, of the one that a row follows; -1: it follows the context.  Rows
-    q_ptr[b] .. q_ptr[b + 1] - 1 belong to sequence b (None: max_q rows each).  Rows of no sequence come back as zeros (in `out`: as they were)."""
+    q_ptr[b] .. q_ptr[b + 1] - 1 belong to sequence b (None: max_q rows each).  Rows of no sequence are not written."""
     import torch
     if parents.dim() != 1 or max_q < 0 or (q_ptr is not None and (q_ptr.dim() != 1 or q_ptr.shape[0] < 1)):
         raise ValueError("attn_tree_mask: expected parents [total], q_ptr [batch + 1] and max_q, the largest number of drafted tokens of a sequence")
@@ -665,7 +665,7 @@ def attn_tree_mask(parents, max_q, q_ptr=None, stream=None, out=None):
     _on_current(device)
     parents_at, q_ptr_at = _int32("parents", parents, total, device), _int32("q_ptr", q_ptr, batch + 1, device)
     if out is None:
-        out = _made_on(stream, lambda: (torch.empty if q_ptr is None else torch.zeros)((total, words), dtype=torch.int32, device=device))
+        out = _made_on(stream, lambda: torch.empty((total, words), dtype=torch.int32, device=device))
     st = lib().attn_tree_mask(batch, total, max_q, q_ptr_at, parents_at, *_check_mask("attn_tree_mask", out, total, max_q, device), _stream(stream))
     if st != ATTN_OK:
         raise AttnError(st, "attn_tree_mask")

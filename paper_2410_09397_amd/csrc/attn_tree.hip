@@ -10,6 +10,71 @@ __global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) tree_plain_out_ker
     win_plain_out<T, E, DP, true, true>(p, p.row_blocks);
 }
 
+// The sums of a row's parts, as win_join_kernel, for the parts of TreeItems.  A workgroup takes kJoinRows rows of a row block, so that its sequence, its parts and their
+// places are looked up once for all of them; 16 to 64 lanes have a row.  Row blocks of one part are written where they are worked on.
+constexpr int kJoinRows = 8;
+template <typename T, int BR, int LANES>
+__global__ void __launch_bounds__(kThreads) tree_join_kernel(WinParams p) {
+    constexpr int BC = BR >= 64 ? 64 : 32, kPer = 64 / LANES, kTurns = BR / kJoinRows;
+    const int lane = threadIdx.x & 63, in_row = threadIdx.x & (LANES - 1), idx = blockIdx.x / (p.kv_heads * kTurns);
+    const int kvh = blockIdx.x / kTurns % p.kv_heads, row0 = blockIdx.x % kTurns * kJoinRows;
+    TreeItems<BR, BC> items;
+    items.init(p, lane);
+    int start, blocks = 1, parts = 0, blk = 0;
+    const int b = items.find_block(p, idx, lane, start, blocks, parts, blk);
+    if (b < 0 || parts <= 1) return;
+    const WinSeq s = win_sequence(p, b);
+    const int rows = s.nq * p.group;
+    const long step = (long)blocks * p.kv_heads * BR, first = ((long)(start + blk) * p.kv_heads + kvh) * BR;  // row x, part k: first + x + k * step
+    for (int x = row0 + (int)threadIdx.x / LANES; x < row0 + kJoinRows; x += kThreads / LANES) {
+        const int r = blk * BR + x;
+        if (r >= rows) break;
+        float m_k[kPer], l_k[kPer], m = -__builtin_inff(), l = 0.f;
+#pragma unroll
+        for (int y = 0; y < kPer; ++y) {
+            const int k = y * LANES + in_row;
+            const float* ml = p.part_ml + (first + x + (long)min(k, parts - 1) * step) * 2;
+            m_k[y] = k < parts ? ml[0] : -__builtin_inff();
+            l_k[y] = k < parts ? ml[1] : 0.f;
+            m = __builtin_elementwise_maximum(m, m_k[y]);
+        }
+#pragma unroll
+        for (int y = 1; y < LANES; y <<= 1) m = __builtin_elementwise_maximum(m, __shfl_xor(m, y, 64));
+        const float m_use = m == -__builtin_inff() ? 0.f : m;
+#pragma unroll
+        for (int y = 0; y < kPer; ++y) {
+            m_k[y] = l_k[y] != 0.f ? __builtin_amdgcn_exp2f(m_k[y] - m_use) : 0.f;  // (NaN: not 0)
+            l += m_k[y] * l_k[y];
+        }
+#pragma unroll
+        for (int y = 1; y < LANES; y <<= 1) l += __shfl_xor(l, y, 64);
+        const bool none = l == 0.f;
+        const float inv = none ? 0.f : 1.f / l;
+        const int c = 4 * in_row, at = lane & ~(LANES - 1);
+        const float* src = p.part_o + (first + x) * p.d;
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        constexpr int kAhead = 8;
+#pragma unroll
+        for (int y = 0; y < kPer; ++y)
+            for (int k0 = 0; k0 < LANES && y * LANES + k0 < parts; k0 += kAhead) {
+                f32x4 part[kAhead];
+                float weight[kAhead];
+#pragma unroll
+                for (int a = 0; a < kAhead; ++a) {
+                    const int k = min(y * LANES + k0 + a, parts - 1);
+                    weight[a] = __shfl(m_k[y], at + k0 + a, 64);  // (0 behind the last part)
+                    part[a] = load4(src + (long)k * step * p.d, c, p.d);
+                }
+#pragma unroll
+                for (int a = 0; a < kAhead; ++a)
+                    if (weight[a] != 0.f) sum += part[a] * weight[a];
+            }
+        const int t = win_token(p, r), head = kvh * p.group + r - t * p.group;
+        if (c < p.d) store4(static_cast<T*>(p.O) + s.q_base + (long)head * p.q_h + (long)t * p.q_n, c, p.d, sum * inv);
+        if (in_row == 0) p.LSE[(s.row0 + t) * p.heads + head] = none ? -__builtin_inff() : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    }
+}
+
 // One workgroup per sequence.  A token's row of words is written from the last word down, as the way up its branch passes the tokens of each: the steps are
 // reads of LDS that wait for one another, as many as the branch is long, and every word is written once, without a word of LDS for it.  A
 // token that does not follow an earlier one of its sequence follows the context, so the way up always ends.
@@ -38,21 +103,32 @@ __global__ void __launch_bounds__(kThreads) tree_mask_kernel(WinParams p, const 
 }
 
 template <typename T, typename E>
-hipError_t fwd(const WinParams& p, hipStream_t stream) {
+hipError_t fwd(long grid, const WinParams& p, hipStream_t stream) {
     return with_width(p.d, [&](auto width) {
         constexpr int DP = decltype(width)::value;
-        hipLaunchKernelGGL((tree_plain_out_kernel<T, E, DP>), dim3((unsigned)((long)p.blocks * p.kv_heads), (unsigned)p.splits), dim3(kThreads), DP * 128 + 1024,
-                           stream, p);
+        hipLaunchKernelGGL((tree_plain_out_kernel<T, E, DP>), dim3((unsigned)grid), dim3(kThreads), DP * 128 + 1024, stream, p);
         return hipGetLastError();
     });
 }
 
 }  // namespace
 
-hipError_t launch_tree_plain_fwd(bool is_bf16, bool fp8, const WinParams& p, hipStream_t stream) {
+hipError_t launch_tree_plain_fwd(bool is_bf16, bool fp8, long grid, const WinParams& p, hipStream_t stream) {
     if (!p.table || !p.tree) return hipErrorInvalidValue;
-    if (fp8) return is_bf16 ? fwd<__bf16, uint8_t>(p, stream) : fwd<float, uint8_t>(p, stream);
-    return fwd<float, float>(p, stream);
+    if (fp8) return is_bf16 ? fwd<__bf16, uint8_t>(grid, p, stream) : fwd<float, uint8_t>(grid, p, stream);
+    return fwd<float, float>(grid, p, stream);
+}
+hipError_t launch_tree_join(bool is_bf16, int rows, const WinParams& p, hipStream_t stream) {
+    auto with = [&](auto lanes) {
+        constexpr int L = decltype(lanes)::value;
+        auto fn = !is_bf16 ? tree_join_kernel<float, 32, L> : rows == 16 ? tree_join_kernel<__bf16, 16, L> : rows == 32 ? tree_join_kernel<__bf16, 32, L>
+                  : rows == 64 ? tree_join_kernel<__bf16, 64, L> : tree_join_kernel<__bf16, 128, L>;
+        hipLaunchKernelGGL(fn, dim3((unsigned)((long)p.blocks * p.kv_heads * (rows / kJoinRows))), dim3(kThreads), 0, stream, p);
+    };
+    if (p.d <= 64) with(std::integral_constant<int, 16>{});
+    else if (p.d <= 128) with(std::integral_constant<int, 32>{});
+    else with(std::integral_constant<int, 64>{});
+    return hipGetLastError();
 }
 hipError_t launch_tree_mask(const WinParams& p, const int32_t* parents, uint32_t* mask, hipStream_t stream) {
     if (p.n > kMostDrafted) return hipErrorInvalidValue;

@@ -23,8 +23,8 @@ __global__ void __launch_bounds__(kThreads, (kOnePerCu<D, SRC>)) tree_one_kernel
 }
 
 template <int D, int SRC, bool PAD>
-hipError_t launch_from(int rows, const WinParams& p, hipStream_t stream) {
-    const dim3 grid((unsigned)((long)p.blocks * p.kv_heads), (unsigned)p.splits);
+hipError_t launch_from(int rows, long groups, const WinParams& p, hipStream_t stream) {
+    const dim3 grid((unsigned)groups);
     auto run = [&](auto kernel, int lds, int threads) {
         const hipError_t e = allow_lds(kernel, lds);
         if (e != hipSuccess) return e;
@@ -36,16 +36,16 @@ hipError_t launch_from(int rows, const WinParams& p, hipStream_t stream) {
     return rows == 64 ? run(tree_out_kernel<D, SRC, 2, PAD>, 4 * 64 * D * 2, kThreads) : run(tree_out_kernel<D, SRC, 1, PAD>, 4 * 64 * D * 2, kThreads);
 }
 template <int D>
-hipError_t launch(bool fp8, int rows, const WinParams& p, hipStream_t stream) {
-    if (fp8) return launch_from<D, kCodes, false>(rows, p, stream);
-    return p.d < D ? launch_from<D, kPages, true>(rows, p, stream) : launch_from<D, kPages, false>(rows, p, stream);
+hipError_t launch(bool fp8, int rows, long grid, const WinParams& p, hipStream_t stream) {
+    if (fp8) return launch_from<D, kCodes, false>(rows, grid, p, stream);
+    return p.d < D ? launch_from<D, kPages, true>(rows, grid, p, stream) : launch_from<D, kPages, false>(rows, grid, p, stream);
 }
 
 }  // namespace
 
-hipError_t launch_tree_fwd(bool fp8, int rows, const WinParams& p, hipStream_t stream) {
+hipError_t launch_tree_fwd(bool fp8, int rows, long grid, const WinParams& p, hipStream_t stream) {
     if (!p.table || !p.tree || (fp8 && p.d != 64 && p.d != 128 && p.d != 256)) return hipErrorInvalidValue;
-    return p.d <= 64 ? launch<64>(fp8, rows, p, stream) : p.d <= 128 ? launch<128>(fp8, rows, p, stream) : launch<256>(fp8, rows, p, stream);
+    return p.d <= 64 ? launch<64>(fp8, rows, grid, p, stream) : p.d <= 128 ? launch<128>(fp8, rows, grid, p, stream) : launch<256>(fp8, rows, grid, p, stream);
 }
 
 }  // namespace attn

@@ -141,7 +141,7 @@ attn_status check_cache(const attn_paged_desc* d, const attn_cache* c) {
 
 int paged_rows(const attn_paged_desc* d) { return attn::paged_rows(is_wide(d), d->batch, d->heads, d->kv_heads, d->total_q, d->max_q); }
 
-WinParams paged_params(const attn_paged_desc* d, const attn_cache* c, bool tree = false) {
+WinParams paged_params(const attn_paged_desc* d, const attn_cache* c) {
     WinParams p;
     std::memset(&p, 0, sizeof(p));
     p.q_h = d->q_stride_h;
@@ -170,7 +170,7 @@ WinParams paged_params(const attn_paged_desc* d, const attn_cache* c, bool tree 
     p.scale = d->scale;
     set_window(p, d->window, d->sinks, d->max_len);
     p.parts = p.rest_parts = 1;
-    const attn::PagedSplits splits = attn::paged_splits(is_wide(d), d->batch, d->heads, d->kv_heads, d->d, d->total_q, d->max_q, d->max_len, p.window, p.sinks, tree);
+    const attn::PagedSplits splits = attn::paged_splits(is_wide(d), d->batch, d->heads, d->kv_heads, d->d, d->total_q, d->max_q, d->max_len, p.window, p.sinks);
     p.row_blocks = splits.row_blocks;
     p.blocks = splits.blocks;
     p.splits = splits.splits;
@@ -210,6 +210,27 @@ bool good_slots(const attn_paged_desc* d, int64_t stride_b, int64_t stride_h, in
 attn_status check_tree(const attn_paged_desc* d, const uint32_t* mask, int64_t mask_stride) {
     if (!mask || mask_stride < 0 || (d->total_q > 1 && mask_stride < ((int64_t)d->max_q + 31) / 32)) return ATTN_ERR_INVALID_ARG;
     return d->max_q > attn::kMostDrafted ? ATTN_ERR_UNSUPPORTED : ATTN_OK;
+}
+
+int tree_rows(const attn_paged_desc* d) { return attn::tree_rows(is_wide(d), d->batch, d->heads, d->kv_heads, d->total_q, d->max_q); }
+// The parameters of a call on trees, and the workgroups of its launch.
+WinParams tree_params(const attn_paged_desc* d, const attn_cache* c, int64_t* grid) {
+    WinParams p = paged_params(d, c);
+    const attn::TreeShares shares = attn::tree_shares(is_wide(d), d->batch, d->heads, d->kv_heads, d->d, d->total_q, d->max_q, d->max_len, p.window, p.sinks);
+    p.row_blocks = shares.row_blocks;
+    p.blocks = shares.blocks;
+    p.places = shares.places;
+    p.least = shares.least;
+    p.splits = 1;
+    p.chunk = 0x7fffffff;
+    *grid = shares.grid;
+    return p;
+}
+size_t tree_ml_bytes(const attn_paged_desc* d, const WinParams& p, int64_t grid) {
+    return p.places > 0 ? round_up((size_t)grid * tree_rows(d) * 2 * sizeof(float), 256) : 0;
+}
+size_t tree_o_bytes(const attn_paged_desc* d, const WinParams& p, int64_t grid) {
+    return p.places > 0 ? (size_t)grid * tree_rows(d) * d->d * sizeof(float) : 0;
 }
 
 int evict_cap(const attn_paged_desc* d, int32_t budget) { return std::max(0, std::min(budget, d->max_len - budget)); }
@@ -361,8 +382,9 @@ attn_status attn_tree_mask(int32_t batch, int32_t total_q, int32_t max_q, const 
 size_t attn_tree_workspace_bytes(const attn_paged_desc* desc) {
     if (check_paged(desc) != ATTN_OK || desc->max_q > attn::kMostDrafted) return 0;
     if (is_empty(desc)) return 256;
-    const WinParams p = paged_params(desc, nullptr, true);
-    return std::max<size_t>(256, part_ml_bytes(desc, p) + part_o_bytes(desc, p));
+    int64_t grid;
+    const WinParams p = tree_params(desc, nullptr, &grid);
+    return std::max<size_t>(256, tree_ml_bytes(desc, p, grid) + tree_o_bytes(desc, p, grid));
 }
 
 attn_status attn_tree_fwd(const attn_paged_desc* desc, const attn_cache* cache, const uint32_t* mask, int64_t mask_stride, const void* Q, void* O,
@@ -375,8 +397,10 @@ attn_status attn_tree_fwd(const attn_paged_desc* desc, const attn_cache* cache, 
     if (st != ATTN_OK) return st;
     const bool bf16 = desc->dtype == ATTN_BF16, fp8 = desc->kind == ATTN_CACHE_FP8;
     if (!Q || !O || !LSE || (bf16 && !(aligned16(Q) && aligned16(O)))) return ATTN_ERR_INVALID_ARG;
-    WinParams p = paged_params(desc, cache, true);
-    if (p.splits > 1 && (!workspace || workspace_bytes < part_ml_bytes(desc, p) + part_o_bytes(desc, p) || !aligned16(workspace)))
+    int64_t grid;
+    WinParams p = tree_params(desc, cache, &grid);
+    const bool joins = p.places > 0;
+    if (joins && (!workspace || workspace_bytes < tree_ml_bytes(desc, p, grid) + tree_o_bytes(desc, p, grid) || !aligned16(workspace)))
         return ATTN_ERR_WORKSPACE;
     p.tree = mask;
     p.tree_stride = mask_stride;
@@ -384,10 +408,11 @@ attn_status attn_tree_fwd(const attn_paged_desc* desc, const attn_cache* cache, 
     p.O = O;
     p.LSE = LSE;
     p.part_ml = static_cast<float*>(workspace);
-    p.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + part_ml_bytes(desc, p));
+    p.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + tree_ml_bytes(desc, p, grid));
     hipStream_t s = static_cast<hipStream_t>(stream);
-    hipError_t e = is_wide(desc) ? attn::launch_tree_fwd(fp8, paged_rows(desc), p, s) : attn::launch_tree_plain_fwd(bf16, fp8, p, s);
-    if (e == hipSuccess && p.splits > 1) e = attn::launch_win_join(bf16, p, s);
+    const int rows = tree_rows(desc);
+    hipError_t e = is_wide(desc) ? attn::launch_tree_fwd(fp8, rows, grid, p, s) : attn::launch_tree_plain_fwd(bf16, fp8, grid, p, s);
+    if (e == hipSuccess && joins) e = attn::launch_tree_join(bf16, rows, p, s);
     return status_of(e);
 }
 

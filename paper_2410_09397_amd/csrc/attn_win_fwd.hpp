@@ -103,9 +103,31 @@ struct TileFeed {
     TileLoader<D, 64> loader;               // tensors
     PageWindow pages;
     CodeChunk kc[SRC == kCodes ? kChunks : 1], vc[SRC == kCodes ? kChunks : 1];
+    // Tiles of pages that start on a multiple of their size and are all there: the rows that one instruction of a wave fetches lie in one page, whose address is
+    // then scalar arithmetic, and what a lane adds to it is the same for every tile.
+    static constexpr int kWaveRows = SRC == kCodes ? 1024 / D : CopyLane<D>::kRows, kOffs = SRC == kPages && D == 256 ? 2 : 1;
+    static constexpr bool kEven = !PAD && !(SRC == kCodes && D == 64);  // (codes at d = 64: the registers of the second form cost a workgroup of four per CU)
+    unsigned off[kOffs];
+    bool even;
     __device__ __forceinline__ void init(const WinParams& p, int tid) {
-        if constexpr (SRC == kTensors) loader.init(tid, p.k_n);
-        else pages.init();
+        if constexpr (SRC == kTensors) {
+            loader.init(tid, p.k_n);
+        } else {
+            pages.init();
+            const int lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+            even = kEven && (1 << p.page_shift) >= kWaveRows && p.k_n < (1l << 26);
+            if constexpr (SRC == kPages) {
+#pragma unroll
+                for (int x = 0; x < kOffs; ++x)  // (the swizzle of a row repeats after 16)
+                    off[x] = (unsigned)(lane / (D / 8)) * (unsigned)p.k_n * 2u + 16u * ((lane % (D / 8)) ^ swz<D>(CopyLane<D>::row_of(x * 4 + w, lane)));
+            } else {
+                off[0] = (unsigned)(lane / (D / 16)) * (unsigned)p.k_n + 16u * (lane % (D / 16));
+            }
+        }
+    }
+    // key j, the same for all lanes, among the pages that cover() has read: element offset of its row and place of its exponent
+    __device__ __forceinline__ PageRow scalar_row(const WinParams& p, int kvh, int j) const {
+        return win_page_row(p, __builtin_amdgcn_readlane(pages.ids, (j >> p.page_shift) - pages.first), kvh, j);
     }
     // requests a tile; bf16: straight into the LDS stage (K at `stage`, V at stage + 2 kBytes); codes: into registers
     template <typename Tiles>
@@ -129,7 +151,26 @@ struct TileFeed {
             }
         } else {
             pages.cover(p, b, tiles.row(p, j0), tiles.row(p, j0 + 63), tiles.end, lane);
-            if constexpr (SRC == kPages) {
+            if (kEven && even && (j0 & 63) == 0 && tiles.whole(p, j0)) {
+                if constexpr (SRC == kPages) {
+                    const unsigned t0 = lds_address(stage) + w * 1024u;
+#pragma unroll
+                    for (int u = 0; u < kInst; ++u) {
+                        const long at = scalar_row(p, kvh, j0 + (u * 4 + w) * kWaveRows).at * 2;
+                        copy_to_lds<16, true>(t0, u * 4096, off[u % kOffs], static_cast<const char*>(p.K) + at);
+                        copy_to_lds<16, true>(t0, u * 4096 + 2 * kBytes, off[u % kOffs], static_cast<const char*>(p.V) + at);
+                    }
+                } else {
+#pragma unroll
+                    for (int x = 0; x < kChunks; ++x) {
+                        const PageRow r = scalar_row(p, kvh, j0 + (x * 4 + w) * kWaveRows);
+                        kc[x].codes = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(p.K) + r.at + off[0]);
+                        vc[x].codes = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(p.V) + r.at + off[0]);
+                        kc[x].scale = exp_value(p.K_exp[r.exp + lane / (D / 16)]);
+                        vc[x].scale = exp_value(p.V_exp[r.exp + lane / (D / 16)]);
+                    }
+                }
+            } else if constexpr (SRC == kPages) {
 #pragma unroll
                 for (int u = 0; u < kInst; ++u) {
                     const int inst = u * 4 + w, row = CopyLane<D>::row_of(inst, lane), j = tiles.row(p, j0 + row);
@@ -174,6 +215,7 @@ __device__ __forceinline__ void win_out(const WinParams& p, int row_blocks) {
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wq = SPLIT == 1 ? w : w & 1, wk = SPLIT == 1 ? 0 : w >> 1;
     int b, kvh, blk;
+    Share<BR, 64, TREE> at;
     if constexpr (SRC == kTensors) {
         int bk;
         decode_block(blockIdx.x, row_blocks, p.batch * p.kv_heads, bk, blk);
@@ -181,8 +223,7 @@ __device__ __forceinline__ void win_out(const WinParams& p, int row_blocks) {
         kvh = bk % p.kv_heads;
         blk = row_blocks - 1 - blk;  // the last rows see most keys
     } else {  // (a key head's blocks on as few XCDs as its number allows)
-        WinBlock at;
-        at.init(p, p.blocks - 1 - (int)(blockIdx.x / p.kv_heads), BR, lane);
+        at.init(p, TREE ? (int)(blockIdx.x / p.kv_heads) : p.blocks - 1 - (int)(blockIdx.x / p.kv_heads), lane);
         if (!at.any) return;
         b = at.b;
         kvh = blockIdx.x % p.kv_heads;
@@ -197,7 +238,7 @@ __device__ __forceinline__ void win_out(const WinParams& p, int row_blocks) {
     Sight<64, TREE> see;
     see.init(p, s, t, win_token(p, w0), win_token(p, w1), win_token(p, r0), win_token(p, min(r0 + BR - 1, rows - 1)));
     const auto& tiles = see.tiles;
-    const int it0 = blockIdx.y * p.chunk, it1 = (int)min((long)tiles.count, (long)it0 + p.chunk);
+    const int it0 = at.first(p), it1 = at.last(p, tiles.count);
 
     TileFeed<D, SRC, PAD> feed;
     feed.init(p, tid);
@@ -320,17 +361,17 @@ __device__ __forceinline__ void win_out(const WinParams& p, int row_blocks) {
         }
     }
     const bool ok = r0 + 32 * wq + l32 < rows, some = l != 0.f;  // (NaN: some)
-    if (p.splits > 1) {
-        const long row = s.lse_base + (long)t * p.heads + head;
+    if (!at.whole(p, tiles.count)) {  // (its sums meet those of the other parts in a launch of their own)
+        const long row = at.sums(p, s.lse_base + (long)t * p.heads + head, 32 * wq + l32);
         if (!ok) return;
-        float* ml = p.part_ml + (row * p.splits + blockIdx.y) * 2;
+        float* ml = p.part_ml + row * 2;
         if (h == 0) {
             ml[0] = acc.m;
             ml[1] = l;
         }
         if (some) {
             const int d = PAD ? p.d : D;
-            float* dst = p.part_o + (row * p.splits + blockIdx.y) * d + 4 * h;
+            float* dst = p.part_o + row * d + 4 * h;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -366,8 +407,8 @@ __device__ __forceinline__ void win_out(const WinParams& p, int row_blocks) {
 }
 
 // Rows r0 .. r1 of a workgroup from its waves' sums in LDS ([wave][ROWS][D + 4] fp32 and [wave][ROWS][m, l]): to O and LSE, or to the parts.
-template <int D, int NW, int ROWS, bool PAD>
-__device__ __forceinline__ void few_store(const WinParams& p, const WinSeq& s, const char* smem, const float* ml, int kvh, int r0, int r1) {
+template <int D, int NW, int ROWS, bool PAD, typename S>
+__device__ __forceinline__ void few_store(const WinParams& p, const WinSeq& s, const char* smem, const float* ml, int kvh, int r0, int r1, const S& share, int tiles) {
     constexpr int kPitch = D * 4 + 16;
     const int tid = threadIdx.x, d = PAD ? p.d : D;
     constexpr int kLanes = D / 4;  // threads per row
@@ -390,12 +431,13 @@ __device__ __forceinline__ void few_store(const WinParams& p, const WinSeq& s, c
         win_place(p, kvh, r, rt, rh);
         const long at = s.lse_base + (long)rt * p.heads + rh;
         const bool some = sum_l != 0.f;
-        if (p.splits > 1) {
+        if (!share.whole(p, tiles)) {
+            const long part = share.sums(p, at, row);
             if (c == 0) {
-                p.part_ml[(at * p.splits + blockIdx.y) * 2] = m;
-                p.part_ml[(at * p.splits + blockIdx.y) * 2 + 1] = sum_l;
+                p.part_ml[part * 2] = m;
+                p.part_ml[part * 2 + 1] = sum_l;
             }
-            if (some) *reinterpret_cast<f32x4*>(p.part_o + (at * p.splits + blockIdx.y) * d + c) = sum;
+            if (some) *reinterpret_cast<f32x4*>(p.part_o + part * d + c) = sum;
         } else {
             const float inv = some ? 1.f / sum_l : 0.f;
             if (c == 0) p.LSE[at] = some ? (m + __builtin_amdgcn_logf(sum_l)) * kLn2 : -__builtin_inff();
@@ -423,8 +465,8 @@ __device__ __forceinline__ void win_few(const WinParams& p) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, l32 = lane & 31;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    WinBlock at;
-    at.init(p, (int)(blockIdx.x / p.kv_heads), 32, lane);
+    Share<32, 32, TREE> at;
+    at.init(p, (int)(blockIdx.x / p.kv_heads), lane);
     if (!at.any) return;
     const int b = at.b, kvh = blockIdx.x % p.kv_heads;
     const WinSeq s = win_sequence(p, b);
@@ -437,7 +479,7 @@ __device__ __forceinline__ void win_few(const WinParams& p) {
     Sight<32, TREE> see;
     see.init(p, s, t, t_lo, t_hi, t_lo, t_hi);
     const auto& tiles = see.tiles;
-    const int it0 = blockIdx.y * p.chunk, it1 = (int)min((long)tiles.count, (long)it0 + p.chunk);
+    const int it0 = at.first(p), it1 = at.last(p, tiles.count);
 
     bf16x8 qf[KS];
     const char* q = reinterpret_cast<const char*>(static_cast<const __bf16*>(p.Q) + s.q_base + (long)head * p.q_h + (long)t * p.q_n);
@@ -541,7 +583,7 @@ __device__ __forceinline__ void win_few(const WinParams& p) {
             *reinterpret_cast<f32x4*>(smem + (w * 32 + l32) * kPitch + (32 * mt + 8 * g + 4 * h) * 4) =
                 f32x4{acc.o[mt][4 * g], acc.o[mt][4 * g + 1], acc.o[mt][4 * g + 2], acc.o[mt][4 * g + 3]};
     __syncthreads();
-    few_store<D, NW, 32, PAD>(p, s, smem, ml, kvh, r0, r1);
+    few_store<D, NW, 32, PAD>(p, s, smem, ml, kvh, r0, r1, at, tiles.count);
 }
 
 // ---------------------------------------------------------------------------------------------------------- a row tile
@@ -563,8 +605,8 @@ __device__ __forceinline__ void win_one(const WinParams& p) {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, l16 = lane & 15;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    WinBlock at;
-    at.init(p, (int)(blockIdx.x / p.kv_heads), 16, lane);
+    Share<16, 32, TREE> at;
+    at.init(p, (int)(blockIdx.x / p.kv_heads), lane);
     if (!at.any) return;
     const int b = at.b, kvh = blockIdx.x % p.kv_heads;
     const WinSeq s = win_sequence(p, b);
@@ -577,7 +619,7 @@ __device__ __forceinline__ void win_one(const WinParams& p) {
     Sight<32, TREE> see;
     see.init(p, s, t, t_lo, t_hi, t_lo, t_hi);
     const auto& tiles = see.tiles;
-    const int it0 = blockIdx.y * p.chunk, it1 = (int)min((long)tiles.count, (long)it0 + p.chunk);
+    const int it0 = at.first(p), it1 = at.last(p, tiles.count);
 
     PageWindow pages;
     pages.init();
@@ -716,7 +758,7 @@ __device__ __forceinline__ void win_one(const WinParams& p) {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) *reinterpret_cast<f32x4*>(smem + (w * 16 + l16) * kPitch + (16 * mt + 4 * q) * 4) = o[mt];
     __syncthreads();
-    few_store<D, NW, 16, PAD>(p, s, smem, ml, kvh, r0, r1);
+    few_store<D, NW, 16, PAD>(p, s, smem, ml, kvh, r0, r1, at, tiles.count);
 }
 
 }  // namespace

@@ -259,13 +259,13 @@ __device__ __forceinline__ void win_plain_out(const WinParams& p, int row_blocks
     constexpr int MT = DP / 32;
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int b, kvh, blk;
+    Share<32, 32, TREE> share;
     if constexpr (PAGED) {
-        WinBlock block;
-        block.init(p, (int)(blockIdx.x / p.kv_heads), 32, lane);
-        if (!block.any) return;
-        b = block.b;
+        share.init(p, (int)(blockIdx.x / p.kv_heads), lane);
+        if (!share.any) return;
+        b = share.b;
         kvh = blockIdx.x % p.kv_heads;
-        blk = block.blk;
+        blk = share.blk;
     } else {
         const int bk = blockIdx.x / row_blocks;
         b = bk / p.kv_heads;
@@ -281,7 +281,7 @@ __device__ __forceinline__ void win_plain_out(const WinParams& p, int row_blocks
     Sight<32, TREE> see;
     see.init(p, s, at.t, t_lo, t_hi, t_lo, t_hi);
     const auto& tiles = see.tiles;
-    const int it0 = blockIdx.y * p.chunk, it1 = (int)min((long)tiles.count, (long)it0 + p.chunk);
+    const int it0 = share.first(p), it1 = share.last(p, tiles.count);
 
     RowOperand<T, DP> q;
     q.init(static_cast<const T*>(p.Q) + s.q_base + (long)at.head * p.q_h + (long)at.t * p.q_n, p.d, h);
@@ -353,15 +353,15 @@ __device__ __forceinline__ void win_plain_out(const WinParams& p, int row_blocks
         for (int e = 0; e < 16; ++e) o[m][e] *= mine;
     meet_waves<MT>(o, meet, w, lane);
     if (w != 0 || r0 + l32 >= rows) return;
-    if (p.splits > 1) {
-        const long row = s.lse_base + (long)at.t * p.heads + at.head;
-        float* ml = p.part_ml + (row * p.splits + blockIdx.y) * 2;
+    if (!share.whole(p, tiles.count)) {
+        const long row = share.sums(p, s.lse_base + (long)at.t * p.heads + at.head, l32);
+        float* ml = p.part_ml + row * 2;
         if (h == 0) {
             ml[0] = m_run;
             ml[1] = l;
         }
         if (l > 0.f || l != l) {
-            float* dst = p.part_o + (row * p.splits + blockIdx.y) * p.d;
+            float* dst = p.part_o + row * p.d;
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll

@@ -84,16 +84,14 @@ inline int paged_rows(bool wide, int batch, int heads, int kv_heads, int total_q
 struct PagedSplits {
     int row_blocks, blocks, splits, chunk;
 };
-inline PagedSplits paged_splits(bool wide, int batch, int heads, int kv_heads, int d, int total_q, int max_q, int max_len, int window, int sinks,
-                                bool tree = false) {
+inline PagedSplits paged_splits(bool wide, int batch, int heads, int kv_heads, int d, int total_q, int max_q, int max_len, int window, int sinks) {
     const int64_t group = heads / kv_heads, rows = paged_rows(wide, batch, heads, kv_heads, total_q, max_q), tile = rows >= 64 ? 64 : 32;
     const bool few = rows < 64;
     PagedSplits p = {(int)((max_q * group + rows - 1) / rows), 0, 1, 0x7fffffff};
     p.blocks = (int)std::min((int64_t)p.row_blocks * batch, total_q * group / rows + batch);
     const int64_t blocks = (int64_t)p.blocks * kv_heads;
-    // (the windows of a block reach over window + its tokens - 1 keys, which lie in one tile more than they fill, as the sinks do; drafted tokens
-    // have tiles of their own)
-    const int64_t keys = std::min<int64_t>(max_len, (int64_t)window + max_q) + sinks, tiles = keys / tile + (tree ? 4 : 3);
+    // (the windows of a block reach over window + its tokens - 1 keys, which lie in one tile more than they fill, as the sinks do)
+    const int64_t keys = std::min<int64_t>(max_len, (int64_t)window + max_q) + sinks, tiles = keys / tile + 3;
     // How many: as many as there are places (some more for few rows, whose lengths differ), but not in pieces so small that the launch that
     // joins them costs more than they save.  us, split -> not: one token of b sequences of L keys, d = 128, quantised: b1 L600 11.0 -> 10.4,
     // b1 L1000 11.2 -> 13.6, b64 L1000 33 -> 24; d = 256: b1 L300 12.9 -> 11.4, b1 L600 13.0 -> 14.9
@@ -107,7 +105,41 @@ inline PagedSplits paged_splits(bool wide, int batch, int heads, int kv_heads, i
     return p;
 }
 
+// Trees of drafted tokens: rows of a workgroup.  Unlike the new tokens of a batch in their order, whose blocks are as many as their tokens make them, a tree has one or two
+// blocks, and what fills the chip are the parts of the context: more than 64 rows take blocks of 128, which convert and read a tile half as often.  us of a call
+// with 128 / 64 rows, h32 k8 d = 128, 64 drafted tokens: 16 sequences of 100 to 8192 tokens 84 / 144 (quantised), 74 / 119; one of 65536 102 / 124; one of 1000 (where
+// the chip is not full) 25.7 / 23.5; d = 256 h16 k4, 4 sequences 64 / 75.
 constexpr int kMostDrafted = 1024;  // drafted tokens of a sequence: their masks are 32 words
+inline int tree_rows(bool wide, int batch, int heads, int kv_heads, int total_q, int max_q) {
+    const int64_t group = heads / kv_heads, rows = max_q * group;
+    if (!wide || rows <= 64) return paged_rows(wide, batch, heads, kv_heads, total_q, max_q);
+    return 128;
+}
+// How a call on trees is shared out (see TreeItems): a part is `least` tiles, or as many as make `places` of all (0: nothing is shared out, and there are no sums to
+// join).  grid: workgroups, each of which has a block of sums if there are any to join.
+// Where row blocks alone are more than the chip's places, parts come in two rounds, so that the last ones are short.  us: parts of at least 4 tiles of 64 keys / of 8, one sequence of
+// 1000 tokens with 64 drafted 25.8 / 30.6, 8 sequences of 500 to 4000 with 30 38.5 / 40.8; at least 16 tiles of 32 keys, of four waves / 32, 16 sequences with 8 drafted 44.8 /
+// 47.2; two rounds / one / four, 64 sequences of 100 to 2000 tokens with 40 drafted 135 / 140 / 139.
+constexpr int64_t kTreeLeast = 4, kTreeLeastFew = 16, kTreeRounds = 2;
+struct TreeShares {
+    int row_blocks, blocks, places, least;
+    int64_t grid;
+};
+inline TreeShares tree_shares(bool wide, int batch, int heads, int kv_heads, int d, int total_q, int max_q, int max_len, int window, int sinks) {
+    const int64_t group = heads / kv_heads, rows = tree_rows(wide, batch, heads, kv_heads, total_q, max_q), tile = rows >= 64 ? 64 : 32;
+    TreeShares p = {(int)((max_q * group + rows - 1) / rows), 0, 0, 0x7fffffff, 0};
+    p.blocks = (int)std::min((int64_t)p.row_blocks * batch, total_q * group / rows + batch);
+    p.grid = (int64_t)p.blocks * kv_heads;
+    const int64_t chip = rows == 16 && d <= 128 ? 1024 : d > 128 ? 256 : 512, of_head = std::max<int64_t>(1, chip / kv_heads);
+    // (the windows reach over window keys, the sinks and the drafted tokens have tiles of their own, and each kind may fill one more than its keys)
+    const int64_t keys = std::min<int64_t>(max_len, (int64_t)window + max_q) + sinks, tiles = keys / tile + 4, least = rows >= 64 ? kTreeLeast : kTreeLeastFew;
+    if (tiles < 2 * least || p.grid > 8 * chip || (int64_t)total_q * heads > kMostGroups) return p;
+    p.places = (int)(p.blocks <= of_head ? of_head - p.blocks / 2 : kTreeRounds * of_head);
+    p.least = (int)std::max(least, (tiles + 63) / 64);  // (64 parts at most: the joining launch has a lane for each)
+    p.grid += (p.places + 1) * (int64_t)kv_heads;  // (one more: the device divides in 32-bit floating point)
+    return p;
+}
+
 // Workgroups that move a (sequence, key head)'s kept tokens, `rows` at a time, of which there are at most `cap`.
 inline int evict_blocks(int64_t bk, int64_t cap, int64_t rows) {
     return (int)std::max<int64_t>(1, std::min((cap + rows - 1) / rows, std::min<int64_t>(1024, kMostGroups / std::max<int64_t>(1, bk))));

@@ -144,7 +144,7 @@ struct Sight<BC, true> {
             j = min(j, end - 1);
             return j < lo && j >= p.sinks ? ((j & -BC) < p.sinks ? p.sinks - 1 : lo) : j;
         }
-        __device__ __forceinline__ bool whole(const WinParams&, int) const { return false; }
+        __device__ __forceinline__ bool whole(const WinParams& p, int j0) const { return j0 + BC <= end && (j0 >= lo || j0 + BC <= p.sinks); }
     } tiles;
     const uint32_t* mask;  // of the lane's query
     int seen, lo;          // under a window: drafted tokens that it sees, and the first key of the context in its window
@@ -197,6 +197,126 @@ struct Sight<BC, true> {
         for (int T = 0; T < NT; ++T) k.v[T] = bits(p, it, j0 + 32 * T) >> shift;
         return k;
     }
+};
+
+// How a call on trees is shared out.  An item is a row block of a sequence and a part of its tiles; the items of a key head are counted through the sequences, in
+// a sequence part by part (so that the row blocks that read the same keys run together), and are as many workgroups.  The sequences' lengths differ
+// more than anything else in such a call, and the host does not know them: a part is p.least tiles, or as many as a workgroup
+// gets if all tiles are shared out over p.places of them (so that these and one for each row block are enough).  A wave looks at 64 sequences at a time.
+template <int BR, int BC>
+struct TreeItems {
+    int chunk;
+    struct Sequence {
+        int blocks, tiles;
+    };
+    static __device__ __forceinline__ Sequence sequence(const WinParams& p, int b) {
+        if (b >= p.batch) return {0, 0};
+        const WinSeq s = win_sequence(p, b);
+        typename Sight<BC, true>::Tiles tiles;
+        tiles.init(p, s);
+        return {(s.nq * p.group + BR - 1) / BR, tiles.count};
+    }
+    __device__ __forceinline__ int parts(int tiles) const { return max(1, (int)(((long)tiles + chunk - 1) / chunk)); }
+    __device__ __forceinline__ void init(const WinParams& p, int lane) {
+        chunk = 0x7fffffff;
+        if (p.places == 0) return;  // no work is shared out
+        unsigned long sum = 0;
+        for (int base = 0; base < p.batch; base += 64) {
+            const Sequence s = sequence(p, base + lane);
+            unsigned long own = (unsigned long)s.blocks * (unsigned)s.tiles;
+            for (int x = 1; x < min(64, p.batch - base); x <<= 1) own += __shfl_xor(own, x, 64);
+            sum += (unsigned long)(unsigned)__builtin_amdgcn_readlane((int)(own >> 32), 0) << 32 | (unsigned)__builtin_amdgcn_readlane((int)own, 0);
+        }
+        chunk = max(p.least, (int)fminf(ceilf((float)sum / (float)p.places), 1e9f));
+    }
+    // the sequence that item idx belongs to (-1: there is none) and the number of its first item
+    __device__ __forceinline__ int find(const WinParams& p, int idx, int lane, int& start, int& blocks) const {
+        start = 0;
+        for (int base = 0; base < p.batch; base += 64) {
+            const Sequence s = sequence(p, base + lane);
+            const int own = s.blocks * parts(s.tiles);
+            int upto = own;
+            for (int x = 1; x < min(64, p.batch - base); x <<= 1) {
+                const int before = __shfl_up(upto, x, 64);
+                upto += lane >= x ? before : 0;
+            }
+            const unsigned long who = __builtin_amdgcn_ballot_w64(base + lane < p.batch && start + upto > idx);
+            if (who) {
+                const int first = __builtin_ctzl(who);
+                blocks = __builtin_amdgcn_readlane(s.blocks, first);
+                start += __builtin_amdgcn_readlane(upto - own, first);
+                return base + first;
+            }
+            start += __builtin_amdgcn_readlane(upto, min(64, p.batch - base) - 1);
+        }
+        return -1;
+    }
+    // row block idx of all sequences: its sequence (-1: there is none), that one's first item, row blocks and parts, and which of them it is
+    __device__ __forceinline__ int find_block(const WinParams& p, int idx, int lane, int& start, int& blocks, int& of_parts, int& blk) const {
+        start = 0;
+        for (int base = 0; base < p.batch; base += 64) {
+            const Sequence s = sequence(p, base + lane);
+            const int own = s.blocks * parts(s.tiles);
+            int upto = own, rows = s.blocks;
+            for (int x = 1; x < min(64, p.batch - base); x <<= 1) {
+                const int before = __shfl_up(upto, x, 64), rows_before = __shfl_up(rows, x, 64);
+                upto += lane >= x ? before : 0;
+                rows += lane >= x ? rows_before : 0;
+            }
+            const unsigned long who = __builtin_amdgcn_ballot_w64(base + lane < p.batch && rows > idx);
+            if (who) {
+                const int first = __builtin_ctzl(who);
+                start += __builtin_amdgcn_readlane(upto - own, first);
+                blocks = __builtin_amdgcn_readlane(s.blocks, first);
+                of_parts = __builtin_amdgcn_readlane(parts(s.tiles), first);
+                blk = idx - __builtin_amdgcn_readlane(rows - s.blocks, first);
+                return base + first;
+            }
+            const int last = min(64, p.batch - base) - 1;
+            start += __builtin_amdgcn_readlane(upto, last);
+            idx -= __builtin_amdgcn_readlane(rows, last);
+        }
+        return -1;
+    }
+};
+
+// The work of a workgroup: a row block of a sequence and its part of the tiles.
+template <int BR, int BC, bool TREE>
+struct Share {
+    int b, blk;
+    bool any;
+    __device__ __forceinline__ void init(const WinParams& p, int idx, int lane) {
+        WinBlock at;
+        at.init(p, idx, BR, lane);
+        b = at.b;
+        blk = at.blk;
+        any = at.any;
+    }
+    __device__ __forceinline__ int first(const WinParams& p) const { return blockIdx.y * p.chunk; }
+    __device__ __forceinline__ int last(const WinParams& p, int tiles) const { return (int)min((long)tiles, (long)first(p) + p.chunk); }
+    __device__ __forceinline__ bool whole(const WinParams& p, int) const { return p.splits <= 1; }
+    // where its sums lie among the parts: token_row = row of Q times heads + head, row = row of the block
+    __device__ __forceinline__ long sums(const WinParams& p, long token_row, int) const { return token_row * p.splits + blockIdx.y; }
+};
+template <int BR, int BC>
+struct Share<BR, BC, true> {
+    int b, blk, part, chunk;
+    bool any;
+    __device__ __forceinline__ void init(const WinParams& p, int idx, int lane) {
+        TreeItems<BR, BC> items;
+        items.init(p, lane);
+        int start, blocks = 1;
+        b = items.find(p, idx, lane, start, blocks);
+        any = b >= 0;
+        b = max(b, 0);
+        part = any ? (idx - start) / blocks : 0;
+        blk = any ? idx - start - part * blocks : 0;
+        chunk = items.chunk;
+    }
+    __device__ __forceinline__ int first(const WinParams&) const { return (int)min((long)part * chunk, 0x7fffffffl); }
+    __device__ __forceinline__ int last(const WinParams& p, int tiles) const { return (int)min((long)tiles, (long)first(p) + chunk); }
+    __device__ __forceinline__ bool whole(const WinParams&, int tiles) const { return tiles <= chunk; }
+    __device__ __forceinline__ long sums(const WinParams&, long, int row) const { return (long)blockIdx.x * BR + row; }
 };
 
 }  // namespace attn

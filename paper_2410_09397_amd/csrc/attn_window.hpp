@@ -30,7 +30,8 @@ struct WinParams {
     int row_blocks, blocks;  // paged: row blocks of the longest sequence, and at most of all of them
     // forward: work of a row block shared out over `splits` workgroups of `chunk` tiles each; their sums meet in win_join_kernel
     int splits, chunk;
-    float *part_o, *part_ml;  // [row][split][d], [row][split][2], row = token row * heads + head
+    float *part_o, *part_ml;  // [row][split][d], [row][split][2], row = token row * heads + head; trees: by workgroups, see TreeItems
+    int places, least;        // trees: workgroups of a key head that the work is shared out over (0: it is not), tiles that a part has at least
     // backward: the first `sink_tiles` key tiles are each worked on by `parts` workgroups, the others by `rest_parts`, each of which takes a
     // share of the tokens; where there are several, their sums meet in win_keys_kernel
     int sink_tiles, parts, rest_parts;
@@ -202,9 +203,10 @@ struct WinKeys {
 hipError_t launch_win_plain_fwd(bool is_bf16, bool fp8, const WinParams& p, hipStream_t stream);
 // bf16; quantised pages: d in {64, 128, 256}; rows of a workgroup: 16, 32 (pages), 64, 128
 hipError_t launch_win_fwd(bool fp8, int rows, const WinParams& p, hipStream_t stream);
-hipError_t launch_tree_fwd(bool fp8, int rows, const WinParams& p, hipStream_t stream);  // the same for p.tree: 16, 32, 64, 128
+hipError_t launch_tree_fwd(bool fp8, int rows, long grid, const WinParams& p, hipStream_t stream);  // the same for p.tree: 16, 32, 64, 128
 hipError_t launch_win_bwd(int rows, const WinParams& p, hipStream_t stream);                                // rows: 64, 128; forms delta itself
-hipError_t launch_tree_plain_fwd(bool is_bf16, bool fp8, const WinParams& p, hipStream_t stream);
+hipError_t launch_tree_plain_fwd(bool is_bf16, bool fp8, long grid, const WinParams& p, hipStream_t stream);
+hipError_t launch_tree_join(bool is_bf16, int rows, const WinParams& p, hipStream_t stream);
 hipError_t launch_win_plain_bwd(const WinParams& p, hipStream_t stream);  // fp32
 hipError_t launch_win_join(bool is_bf16, const WinParams& p, hipStream_t stream);
 hipError_t launch_win_keys(bool is_bf16, int tile, const WinParams& p, hipStream_t stream);
