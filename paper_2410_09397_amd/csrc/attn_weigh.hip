@@ -41,66 +41,135 @@ __device__ __forceinline__ void weigh_store(const WeighParams& w, const WinSeq& 
     w.out[(long)b * w.out_b + (long)kvh * w.out_h + j] = v;
 }
 
-// 16x16x32 products: 32 keys on a wave, straight from memory into operands (lane l: key l % 16, 16 bytes of it), rows 16 at a time.
-template <int D, int SRC, bool PAD>
-__global__ void __launch_bounds__(kThreads) weigh_kernel(WeighParams w) {
+// Which keys a workgroup takes: chunk `part` of a sequence.  The chunks of all sequences are counted 64 sequences at a time, so that those of short ones leave no workgroups idle
+// among those of long ones; what the host has launched too many lies at the end.
+struct WeighShare {
+    int b, part;
+    bool any;
+    __device__ __forceinline__ void init(const WinParams& p, int idx, int chunk, int lane) {
+        any = true;
+        for (int base = 0; base < p.batch; base += 64) {
+            const int mine = base + lane, n = min(64, p.batch - base);
+            const int own = mine < p.batch ? (min(max(p.lens[mine], 0), p.max_len) + chunk - 1) / chunk : 0;
+            int upto = own;
+            for (int x = 1; x < n; x <<= 1) {
+                const int before = __shfl_up(upto, x, 64);
+                upto += lane >= x ? before : 0;
+            }
+            const unsigned long who = __builtin_amdgcn_ballot_w64(mine < p.batch && upto > idx);
+            if (who) {
+                const int first = __builtin_ctzl(who);
+                b = base + first;
+                part = idx - __builtin_amdgcn_readlane(upto - own, first);
+                return;
+            }
+            idx -= __builtin_amdgcn_readlane(upto, n - 1);
+        }
+        any = false;
+        b = part = 0;
+    }
+};
+
+// 16 codes as two chunks of 8 bf16, exactly
+__device__ __forceinline__ bf16x8 code_half(u32x4 v, int half, float scale) {
+    u32x4 a;
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+        const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 * half + y], scale, false);
+        const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 * half + y], scale, true);
+        a[2 * y] = __builtin_bit_cast(uint32_t, lo);
+        a[2 * y + 1] = __builtin_bit_cast(uint32_t, hi);
+    }
+    return __builtin_bit_cast(bf16x8, a);
+}
+
+// Keys of GROUP columns of a product (16: 16x16x32, 32: 32x32x16), straight from memory into operands: lane l has key l % GROUP, and of it 16 bytes of every 64 / GROUP.  The
+// order of d inside a product is free as long as Q has the same: operand x of codes that lie together (a lane's 16 bytes are 8 columns twice).
+template <int D, int SRC, int GROUP, bool PAD>
+struct KeyOperand {
+    static constexpr int kProducts = D * GROUP / 512, kLoads = SRC == kCodes ? kProducts / 2 : kProducts, kQuarters = 64 / GROUP;
+    u32x4 raw[kLoads];
+    uint8_t exp;
+    // key j (clamped by the caller) in page `page`
+    __device__ __forceinline__ void request(const WinParams& p, int page, int kvh, int j, int lane) {
+        const PageRow r = win_page_row(p, page, kvh, j);
+        const char* src = static_cast<const char*>(p.K) + r.at * (SRC == kCodes ? 1 : 2);
+#pragma unroll
+        for (int x = 0; x < kLoads; ++x) raw[x] = load_chunk<PAD>(src, kQuarters * x + lane / GROUP, p.d);
+        if constexpr (SRC == kCodes) exp = p.K_exp[r.exp];
+    }
+    __device__ __forceinline__ bf16x8 operand(int x, float scale) const {
+        if constexpr (SRC == kCodes) return code_half(raw[x / 2], x % 2, scale);
+        else return __builtin_bit_cast(bf16x8, raw[x]);
+    }
+    // the 8 columns of a row of Q that go with operand x: their number in units of 8
+    static __device__ __forceinline__ int chunk_of(int x, int lane) {
+        return SRC == kCodes ? 2 * (kQuarters * (x / 2) + lane / GROUP) + x % 2 : kQuarters * x + lane / GROUP;
+    }
+};
+
+// At most 16 rows (ONE), on 16x16x32 products with Q in registers, or any number, 16 at a time from memory (rows that the other kernels' tiles do not hold).  32 keys to a wave, the
+// next ones on their way.
+template <int D, int SRC, bool PAD, bool ONE>
+__global__ void __launch_bounds__(kThreads) weigh_one_kernel(WeighParams w) {
     const WinParams& p = w.p;
-    constexpr int KS = D / 32;
+    typedef KeyOperand<D, SRC, 16, PAD> Keys;
+    constexpr int KS = Keys::kProducts;
     const int lane = threadIdx.x & 63, q = lane >> 4, l16 = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int blk = blockIdx.x % w.blocks, bk = blockIdx.x / w.blocks, b = bk / p.kv_heads, kvh = bk % p.kv_heads;
+    const int kvh = blockIdx.x % p.kv_heads;
+    WeighShare share;
+    share.init(p, blockIdx.x / p.kv_heads, w.chunk, lane);
+    if (!share.any) return;
+    const int b = share.b;
     const WinSeq s = win_sequence(p, b);
-    const int rows = s.nq * p.group, end = min(s.len, (blk + 1) * w.chunk);
+    const int rows = s.nq * p.group, end = min(s.len, (share.part + 1) * w.chunk);
     const float cs = p.scale * kLog2e;
-    for (int j0 = blk * w.chunk + 32 * wave; j0 < end; j0 += 128) {
-        bf16x8 kf[2][KS];
+    int j0 = share.part * w.chunk + 32 * wave;
+    PageWindow pages;
+    pages.init();
+    Keys keys[2];
+    auto request = [&] {
+        pages.cover(p, b, j0, min(j0 + 31, s.len - 1), s.len, lane);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             const int j = min(j0 + 16 * g + l16, s.len - 1);
-            const PageRow r = win_page_row(p, win_page(p, b, j), kvh, j);
-            if constexpr (SRC == kCodes) {
-                const char* src = static_cast<const char*>(p.K) + r.at;
-                const float scale = exp_value(p.K_exp[r.exp]);
-#pragma unroll
-                for (int x = 0; x < KS / 2; ++x) {
-                    const u32x4 v = load_chunk<PAD>(src, 4 * x + q, p.d);
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        u32x4 a;
-#pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 * half + y], scale, false);
-                            const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[2 * half + y], scale, true);
-                            a[2 * y] = __builtin_bit_cast(uint32_t, lo);
-                            a[2 * y + 1] = __builtin_bit_cast(uint32_t, hi);
-                        }
-                        kf[g][2 * x + half] = __builtin_bit_cast(bf16x8, a);
-                    }
-                }
-            } else {
-                const char* src = static_cast<const char*>(p.K) + r.at * 2;
-#pragma unroll
-                for (int x = 0; x < KS; ++x) kf[g][x] = __builtin_bit_cast(bf16x8, load_chunk<PAD>(src, 4 * x + q, p.d));
-            }
+            keys[g].request(p, pages.page(p, j), kvh, j, lane);
         }
+    };
+    if (j0 < end) request();
+    bf16x8 qf[KS];
+    WeighRow at[4];
+    auto load_rows = [&](int r0) {
+        const int x = min(r0 + l16, rows - 1), t = win_token(p, x), head = kvh * p.group + x - t * p.group;
+        const char* row = reinterpret_cast<const char*>(static_cast<const __bf16*>(p.Q) + s.q_base + (long)head * p.q_h + (long)t * p.q_n);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qf[ks] = __builtin_bit_cast(bf16x8, load_chunk<PAD>(row, Keys::chunk_of(ks, lane), p.d));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) at[i].init(p, s, kvh, r0 + 4 * q + i, rows);
+    };
+    if (ONE && rows > 0) load_rows(0);
+    while (j0 < end) {
+        const int here = j0;
+        bf16x8 kf[2][KS];
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const float scale = SRC == kCodes ? exp_value(keys[g].exp) : 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) kf[g][ks] = keys[g].operand(ks, scale);
+        }
+        j0 += 128;
+        if (j0 < end) request();
         float sum[2] = {0.f, 0.f};
         WeighRows<16> range;
-        range.init(p, s, j0, min(j0 + 31, s.len - 1));
+        range.init(p, s, here, min(here + 31, s.len - 1));
         for (int r0 = range.r0; r0 < range.r1; r0 += 16) {
-            const int x = min(r0 + l16, rows - 1), t = win_token(p, x), head = kvh * p.group + x - t * p.group;
-            const char* row = reinterpret_cast<const char*>(static_cast<const __bf16*>(p.Q) + s.q_base + (long)head * p.q_h + (long)t * p.q_n);
-            bf16x8 qf[KS];
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-                qf[ks] = __builtin_bit_cast(bf16x8, load_chunk<PAD>(row, SRC == kCodes ? 8 * (ks >> 1) + 2 * q + (ks & 1) : 4 * ks + q, p.d));
-            WeighRow at[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) at[i].init(p, s, kvh, r0 + 4 * q + i, rows);
+            if (!ONE) load_rows(r0);
 #pragma unroll
             for (int g = 0; g < 2; ++g) {
                 f32x4 st = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(qf[ks], kf[g][ks], st, 0, 0, 0);
-                const int j = j0 + 16 * g + l16;
+                const int j = here + 16 * g + l16;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) sum[g] += weigh_sees(p, at[i].i, j) ? __builtin_amdgcn_exp2f(fmaf(st[i], cs, -at[i].lse2)) : 0.f;
             }
@@ -111,8 +180,250 @@ __global__ void __launch_bounds__(kThreads) weigh_kernel(WeighParams w) {
             sum[g] += __shfl_xor(sum[g], 32, 64);
         }
         const float v = q & 1 ? sum[1] : sum[0];
-        if (q < 2) weigh_store(w, s, b, kvh, j0 + 16 * q + l16, v);
+        if (q < 2) weigh_store(w, s, b, kvh, here + 16 * q + l16, v);
     }
+}
+
+// ----------------------------------------------------------------------------------------------------- rows in tiles
+// More rows lie in LDS as tiles of 128: TT tokens with their heads, TT = 128 / group, so that a tile's rows are at the same distances from its first as every other tile's.
+// Beside each row: its position (-1: none, or nothing that it adds) and what its exponents are relative to.
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+constexpr int kWeighTile = 128;
+template <int D>
+struct WeighStage {
+    __bf16 rows[kWeighTile * D];  // swizzled as the tiles of attn_common.hpp
+    float lse2[kWeighTile];
+    int pos[kWeighTile];
+};
+
+// 32 rows of a stage times 32 NG keys: the weights that these rows give the lane's keys.  masked: not every row sees every key.
+template <int D, int SRC, int NG, bool PAD>
+__device__ __forceinline__ void weigh_rows(const WinParams& p, const WeighStage<D>& stage, int row0, const bf16x8 (&kf)[NG][D / 16], int j, float cs, bool masked, int lane,
+                                           float (&sum)[NG]) {
+    typedef KeyOperand<D, SRC, 32, PAD> Keys;
+    const int h = lane >> 5, row = row0 + (lane & 31);
+    const char* lds = reinterpret_cast<const char*>(stage.rows) + row * (2 * D);
+    f32x16 st[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st[g][i] = 0.f;
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x) {
+        const bf16x8 q = *reinterpret_cast<const bf16x8*>(lds + ((Keys::chunk_of(x, lane) ^ swz<D>(row)) << 4));
+#pragma unroll
+        for (int g = 0; g < NG; ++g) st[g] = mfma32(q, kf[g][x], st[g]);
+    }
+#pragma unroll
+    for (int g = 0; g < NG; ++g) settle_products(st[g]);
+    f32x4 lse[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) lse[x] = *reinterpret_cast<const f32x4*>(stage.lse2 + row0 + 8 * x + 4 * h);
+    if (masked) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            const i32x4 pos = *reinterpret_cast<const i32x4*>(stage.pos + row0 + 8 * x + 4 * h);
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    sum[g] += weigh_sees(p, pos[i], j + 32 * g) ? __builtin_amdgcn_exp2f(fmaf(st[g][4 * x + i], cs, -lse[x][i])) : 0.f;
+        }
+        return;
+    }
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+        float a = 0.f, c = 0.f;  // (two chains: an addition waits for the one before)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; i += 2) {
+                a += __builtin_amdgcn_exp2f(fmaf(st[g][4 * x + i], cs, -lse[x][i]));
+                c += __builtin_amdgcn_exp2f(fmaf(st[g][4 * x + i + 1], cs, -lse[x][i + 1]));
+            }
+        sum[g] += a + c;
+    }
+}
+
+// Brings tiles of rows into stages.  Tile `it` has tokens TT it .. of the sequence.
+template <int D, bool PAD>
+struct WeighFeed {
+    static constexpr int kInst = kWeighTile / (4 * CopyLane<D>::kRows);
+    unsigned off[kInst];  // of the lane's 16 bytes from the tile's first row, bytes
+    int tt, token, g;     // tokens of a tile; of threads 0 .. 127: token and head of row `tid`
+    float lse;
+    int pos;
+    __device__ __forceinline__ void init(const WinParams& p, int tid) {
+        const int lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+        tt = kWeighTile / p.group;
+#pragma unroll
+        for (int u = 0; u < kInst; ++u) {
+            const int row = CopyLane<D>::row_of(u * 4 + w, lane), t = min(win_token(p, row), tt - 1), g = min(row - t * p.group, p.group - 1);
+            off[u] = ((unsigned)t * (unsigned)p.q_n + (unsigned)g * (unsigned)p.q_h) * 2u + 16u * ((lane % (D / 8)) ^ swz<D>(row));
+        }
+        token = win_token(p, tid & (kWeighTile - 1));
+        g = (tid & (kWeighTile - 1)) - token * p.group;
+    }
+    __device__ __forceinline__ void request(const WinParams& p, const WinSeq& s, int kvh, int it, WeighStage<D>* stage, int tid) {
+        const int lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), t0 = it * tt;
+        if (tid < kWeighTile) {
+            const bool is = token < tt && t0 + token < s.nq;
+            lse = is ? p.LSE_in[(s.row0 + t0 + token) * p.heads + kvh * p.group + g] : -__builtin_inff();
+            pos = is && lse != -__builtin_inff() && s.first + t0 + token < s.len ? s.first + t0 + token : -1;
+        }
+        const char* first = reinterpret_cast<const char*>(static_cast<const __bf16*>(p.Q) + s.q_base + (long)(kvh * p.group) * p.q_h + (long)t0 * p.q_n);
+        const unsigned to = lds_address(stage->rows);
+        if (!PAD && t0 + tt <= s.nq) {
+#pragma unroll
+            for (int u = 0; u < kInst; ++u) copy_to_lds<16, true>(to + w * 1024u, u * 4096, off[u], TileLoader<D, 64>::uniform(reinterpret_cast<const __bf16*>(first)));
+        } else {
+#pragma unroll
+            for (int u = 0; u < kInst; ++u) {
+                const int row = CopyLane<D>::row_of(u * 4 + w, lane), t = min(min(win_token(p, row), tt - 1), s.nq - 1 - t0), g = min(row - win_token(p, row) * p.group, p.group - 1);
+                copy_row(CopyLane<D>::template at<PAD>(first + ((long)t * p.q_n + (long)g * p.q_h) * 2, row, lane, p.d), to + (u * 4 + w) * 1024u);
+            }
+        }
+    }
+    // the requested tile is in its stage once this and a barrier are past
+    __device__ __forceinline__ void arrive(WeighStage<D>* stage, int tid) const {
+        wait_direct_loads();
+        if (tid < kWeighTile) {
+            stage->lse2[tid] = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
+            stage->pos[tid] = pos;
+        }
+    }
+};
+
+// Whether every row of a stage sees all of the keys j0 .. j1: t0 .. t1 - 1 are its tokens; none of its rows is without a position.
+__device__ __forceinline__ bool weigh_whole(const WinParams& p, const WinSeq& s, int t0, int t1, int j0, int j1) {
+    const int i0 = s.first + t0, i1 = s.first + t1 - 1;
+    return j1 <= i0 && i1 < s.len && (i1 - j0 < p.window || j1 < p.sinks);
+}
+
+// Rows of one tile (a few new tokens): they stay in LDS, and the keys stream past, 32 to a wave, the next ones on their way.
+template <int D, int SRC, bool PAD>
+__global__ void __launch_bounds__(kThreads, 2) weigh_few_kernel(WeighParams w) {
+    const WinParams& p = w.p;
+    typedef KeyOperand<D, SRC, 32, PAD> Keys;
+    constexpr int KS = Keys::kProducts;
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    WeighStage<D>* stage = reinterpret_cast<WeighStage<D>*>(smem);
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int kvh = blockIdx.x % p.kv_heads;
+    WeighShare share;
+    share.init(p, blockIdx.x / p.kv_heads, w.chunk, lane);
+    if (!share.any) return;
+    const int b = share.b;
+    const WinSeq s = win_sequence(p, b);
+    const int rows = s.nq * p.group, end = min(s.len, (share.part + 1) * w.chunk);
+    const float cs = p.scale * kLog2e;
+    int j0 = share.part * w.chunk + 32 * wave;
+    PageWindow pages;
+    pages.init();
+    Keys key;
+    auto request = [&] {
+        pages.cover(p, b, j0, min(j0 + 31, s.len - 1), s.len, lane);
+        const int j = min(j0 + l32, s.len - 1);
+        key.request(p, pages.page(p, j), kvh, j, lane);
+    };
+    if (rows > 0) {
+        WeighFeed<D, PAD> feed;
+        feed.init(p, tid);
+        feed.request(p, s, kvh, 0, stage, tid);
+        if (j0 < end) request();
+        feed.arrive(stage, tid);
+        // rows without a position (behind the last, or of queries that saw nothing) are told in every tile
+        const bool has = tid >= kWeighTile || tid >= rows || feed.pos >= 0;
+        const int all = __builtin_amdgcn_ballot_w64(has) == ~0ul;
+        if (lane == 0) reinterpret_cast<int*>(smem + sizeof(WeighStage<D>))[wave] = all;
+    } else if (j0 < end) {
+        request();
+    }
+    __syncthreads();
+    const int* seen = reinterpret_cast<const int*>(smem + sizeof(WeighStage<D>));
+    const bool all = rows > 0 && seen[0] && seen[1];
+    while (j0 < end) {
+        const int here = j0;
+        bf16x8 kf[1][KS];
+        const float scale = SRC == kCodes ? exp_value(key.exp) : 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kf[0][ks] = key.operand(ks, scale);
+        j0 += 128;
+        if (j0 < end) request();
+        float sum[1] = {0.f};
+        WeighRows<32> range;
+        range.init(p, s, here, min(here + 31, s.len - 1));
+        const bool whole = all && weigh_whole(p, s, 0, s.nq, here, min(here + 31, s.len - 1));
+        for (int r0 = range.r0; r0 < range.r1; r0 += 32) weigh_rows<D, SRC, 1, PAD>(p, *stage, r0, kf, here + l32, cs, !whole || r0 + 32 > rows, lane, sum);
+        sum[0] += __shfl_xor(sum[0], 32, 64);
+        if (lane < 32) weigh_store(w, s, b, kvh, here + l32, sum[0]);
+    }
+}
+
+// Many rows: 64 keys of a workgroup are operands in all four waves, and tiles of rows stream past, 32 rows of each to a wave; the waves' sums meet at the end.
+template <int D, int SRC, bool PAD>
+__global__ void __launch_bounds__(kThreads, (D == 256 ? 1 : 2)) weigh_many_kernel(WeighParams w) {
+    const WinParams& p = w.p;
+    typedef KeyOperand<D, SRC, 32, PAD> Keys;
+    constexpr int KS = Keys::kProducts;
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    WeighStage<D>* stages = reinterpret_cast<WeighStage<D>*>(smem);
+    const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // the first keys of a sequence are seen by most rows: first keys first, and where all workgroups are on the chip at once the later half back from the last
+    const int bk_total = p.batch * p.kv_heads, bk = blockIdx.x % bk_total, b = bk / p.kv_heads, kvh = bk % p.kv_heads;
+    int blk = blockIdx.x / bk_total;
+    if (w.blocks * bk_total <= 512 && blk >= (w.blocks + 1) / 2) blk = w.blocks - 1 - (blk - (w.blocks + 1) / 2);
+    const WinSeq s = win_sequence(p, b);
+    const int j0 = 64 * blk, j1 = min(j0 + 63, s.len - 1);
+    if (j0 >= s.len) return;
+    const float cs = p.scale * kLog2e;
+    WeighFeed<D, PAD> feed;
+    feed.init(p, tid);
+    // tiles of tokens that see some of the keys
+    const int t_lo = max(0, j0 - s.first), t_hi = j0 < p.sinks ? s.nq : (int)min((long)s.nq, max(0l, (long)j1 + p.window - s.first));
+    const int it0 = t_lo / feed.tt, it1 = t_hi > t_lo ? (t_hi + feed.tt - 1) / feed.tt : it0;
+    float sum[2] = {0.f, 0.f};
+    if (it0 < it1) {
+        feed.request(p, s, kvh, it0, stages, tid);
+        bf16x8 kf[2][KS];
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const int j = min(j0 + 32 * g + l32, s.len - 1);
+            Keys key;
+            key.request(p, win_page(p, b, j), kvh, j, lane);
+            const float scale = SRC == kCodes ? exp_value(key.exp) : 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) kf[g][ks] = key.operand(ks, scale);
+        }
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) settle(kf[g][ks]);
+        feed.arrive(stages, tid);
+        __syncthreads();
+        for (int it = it0; it < it1; ++it) {
+            WeighStage<D>* stage = stages + ((it - it0) & 1);
+            WeighStage<D>* next = stages + ((it - it0 + 1) & 1);
+            if (it + 1 < it1) feed.request(p, s, kvh, it + 1, next, tid);
+            const int t0 = it * feed.tt, t1 = min(t0 + feed.tt, s.nq), rows = (t1 - t0) * p.group;
+            if (32 * wave < rows) {
+                // (a query that saw nothing has no position: looked up in the tile, two rows to a lane of 32)
+                const int mine = stage->pos[32 * wave + l32];
+                const bool has = 32 * wave + l32 >= rows || mine >= 0;
+                const bool whole = 32 * wave + 32 <= rows && __builtin_amdgcn_ballot_w64(has) == ~0ul &&
+                                   weigh_whole(p, s, t0 + win_token(p, 32 * wave), t0 + win_token(p, min(32 * wave + 31, rows - 1)) + 1, j0, j0 + 63);
+                weigh_rows<D, SRC, 2, PAD>(p, *stage, 32 * wave, kf, j0 + l32, cs, !whole, lane, sum);
+            }
+            if (it + 1 < it1) feed.arrive(next, tid);
+            __syncthreads();
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < 2; ++g) sum[g] += __shfl_xor(sum[g], 32, 64);
+    float* meet = reinterpret_cast<float*>(smem);  // (the stages are free: every wave is past the last barrier, or there was no tile)
+    meet[wave * 64 + lane] = lane < 32 ? sum[0] : sum[1];
+    __syncthreads();
+    if (tid < 64) weigh_store(w, s, b, kvh, j0 + tid, (meet[tid] + meet[64 + tid]) + (meet[128 + tid] + meet[192 + tid]));
 }
 
 // 32-bit arithmetic: 32x32x2 products of 32 keys on a wave, rows 32 at a time, both straight from memory.
@@ -157,11 +468,23 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_plain_kernel(WeighParams w)
 
 dim3 grid_of(const WeighParams& w) { return dim3((unsigned)((long)w.blocks * w.p.batch * w.p.kv_heads)); }
 
+template <int D, int SRC, bool PAD>
+hipError_t launch_from(WeighRowsKind kind, const WeighParams& w, hipStream_t stream) {
+    auto run = [&](auto kernel, int lds) {
+        const hipError_t e = lds ? allow_lds(kernel, lds) : hipSuccess;
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(kernel, grid_of(w), dim3(kThreads), lds, stream, w);
+        return hipGetLastError();
+    };
+    if (kind == kWeighOne) return run(weigh_one_kernel<D, SRC, PAD, true>, 0);
+    if (kind == kWeighAny) return run(weigh_one_kernel<D, SRC, PAD, false>, 0);
+    if (kind == kWeighFew) return run(weigh_few_kernel<D, SRC, PAD>, (int)sizeof(WeighStage<D>) + 16);
+    return run(weigh_many_kernel<D, SRC, PAD>, 2 * (int)sizeof(WeighStage<D>));
+}
 template <int D>
-hipError_t launch(bool fp8, const WeighParams& w, hipStream_t stream) {
-    auto fn = fp8 ? weigh_kernel<D, kCodes, false> : w.p.d < D ? weigh_kernel<D, kPages, true> : weigh_kernel<D, kPages, false>;
-    hipLaunchKernelGGL(fn, grid_of(w), dim3(kThreads), 0, stream, w);
-    return hipGetLastError();
+hipError_t launch(bool fp8, WeighRowsKind kind, const WeighParams& w, hipStream_t stream) {
+    if (fp8) return launch_from<D, kCodes, false>(kind, w, stream);
+    return w.p.d < D ? launch_from<D, kPages, true>(kind, w, stream) : launch_from<D, kPages, false>(kind, w, stream);
 }
 template <typename T, typename E>
 hipError_t plain(const WeighParams& w, hipStream_t stream) {
@@ -173,9 +496,9 @@ hipError_t plain(const WeighParams& w, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_weigh(bool fp8, const WeighParams& w, hipStream_t stream) {
+hipError_t launch_weigh(bool fp8, WeighRowsKind kind, const WeighParams& w, hipStream_t stream) {
     if (fp8 && w.p.d != 64 && w.p.d != 128 && w.p.d != 256) return hipErrorInvalidValue;
-    return w.p.d <= 64 ? launch<64>(fp8, w, stream) : w.p.d <= 128 ? launch<128>(fp8, w, stream) : launch<256>(fp8, w, stream);
+    return w.p.d <= 64 ? launch<64>(fp8, kind, w, stream) : w.p.d <= 128 ? launch<128>(fp8, kind, w, stream) : launch<256>(fp8, kind, w, stream);
 }
 hipError_t launch_weigh_plain(bool is_bf16, bool fp8, const WeighParams& w, hipStream_t stream) {
     if (fp8) return is_bf16 ? plain<__bf16, uint8_t>(w, stream) : plain<float, uint8_t>(w, stream);

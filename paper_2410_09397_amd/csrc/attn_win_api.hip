@@ -450,7 +450,7 @@ attn_status attn_cache_weigh(const attn_paged_desc* desc, const attn_cache* cach
                         (weights->in == weights->out && (weights->in_stride_b != weights->out_stride_b || weights->in_stride_h != weights->out_stride_h))))
         return ATTN_ERR_INVALID_ARG;
     const int64_t bk = (int64_t)desc->batch * desc->kv_heads;
-    if (bk > kMostGroups || ((int64_t)desc->max_len + 127) / 128 * bk > kMostGroups) return ATTN_ERR_UNSUPPORTED;
+    if (bk > kMostGroups || ((int64_t)desc->max_len + 63) / 64 * bk > kMostGroups) return ATTN_ERR_UNSUPPORTED;
     attn::WeighParams w;
     std::memset(&w, 0, sizeof(w));
     w.p = paged_params(desc, cache);
@@ -463,10 +463,12 @@ attn_status attn_cache_weigh(const attn_paged_desc* desc, const attn_cache* cach
     w.out_b = weights->out_stride_b;
     w.out_h = weights->out_stride_h;
     w.decay = weights->decay;
-    w.chunk = 128;
+    const bool wide = is_wide(desc);
+    const attn::WeighPlan plan = attn::weigh_plan(desc->batch, desc->heads, desc->kv_heads, desc->max_q, desc->max_len, desc->q_stride_n, desc->q_stride_h);
+    w.chunk = wide ? plan.chunk : 128;
     w.blocks = (desc->max_len + w.chunk - 1) / w.chunk;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return status_of(is_wide(desc) ? attn::launch_weigh(fp8, w, s) : attn::launch_weigh_plain(bf16, fp8, w, s));
+    return status_of(wide ? attn::launch_weigh(fp8, plan.kind, w, s) : attn::launch_weigh_plain(bf16, fp8, w, s));
 }
 
 size_t attn_evict_workspace_bytes(const attn_paged_desc* desc, int32_t budget) {

@@ -140,6 +140,23 @@ inline TreeShares tree_shares(bool wide, int batch, int heads, int kv_heads, int
     return p;
 }
 
+// Kernels of attn_cache_weigh by the rows of a (sequence, key head): at most 16, one tile of 128, more of them; any: groups or strides that a tile does not hold.
+enum WeighRowsKind { kWeighOne, kWeighFew, kWeighMany, kWeighAny };
+constexpr int64_t kWeighGroups = 2048;
+struct WeighPlan {
+    WeighRowsKind kind;
+    int blocks, chunk;  // workgroups of a (sequence, key head), and keys of each
+};
+inline WeighPlan weigh_plan(int batch, int heads, int kv_heads, int max_q, int max_len, int64_t q_stride_n, int64_t q_stride_h) {
+    const int64_t group = heads / kv_heads, rows = max_q * group, bk = (int64_t)batch * kv_heads;
+    const bool tiles = group <= 128 && q_stride_n < (1 << 22) && q_stride_h < (1 << 22);
+    WeighPlan p = {rows <= 16 ? kWeighOne : !tiles ? kWeighAny : rows <= 128 ? kWeighFew : kWeighMany, 0, 128};
+    if (p.kind == kWeighMany) p.chunk = 64;
+    else while (p.chunk < 1024 && (max_len + p.chunk * 2 - 1) / (p.chunk * 2) * bk >= kWeighGroups) p.chunk *= 2;
+    p.blocks = (max_len + p.chunk - 1) / p.chunk;
+    return p;
+}
+
 // Workgroups that move a (sequence, key head)'s kept tokens, `rows` at a time, of which there are at most `cap`.
 inline int evict_blocks(int64_t bk, int64_t cap, int64_t rows) {
     return (int)std::max<int64_t>(1, std::min((cap + rows - 1) / rows, std::min<int64_t>(1024, kMostGroups / std::max<int64_t>(1, bk))));

@@ -9,6 +9,7 @@
 #include <stdint.h>
 
 #include "attn_common.hpp"
+#include "attn_win_rules.hpp"
 
 namespace attn {
 
@@ -225,7 +226,7 @@ struct WeighParams {
     float decay;
     int blocks, chunk;  // workgroups of a (sequence, key head), and keys of each
 };
-hipError_t launch_weigh(bool fp8, const WeighParams& w, hipStream_t stream);                     // bf16; quantised pages: d in {64, 128, 256}
+hipError_t launch_weigh(bool fp8, WeighRowsKind kind, const WeighParams& w, hipStream_t stream);  // bf16; quantised pages: d in {64, 128, 256}
 hipError_t launch_weigh_plain(bool is_bf16, bool fp8, const WeighParams& w, hipStream_t stream);
 
 // attn_cache_evict: of longer sequences `budget` tokens stay

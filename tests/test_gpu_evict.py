@@ -72,6 +72,9 @@ WEIGH = [
     ("bf16", "fp8", [1500, 64, 900, 3], [700, 64, 1, 3], 6, 2, 128, 64, 130, 65),
     ("bf16", "fp8", [300, 200], [100, 200], 4, 2, 256, 256, 50, 3),
     ("bf16", "plain", [300, 1111], [100, 200], 8, 2, 256, 16, 0, 0),
+    ("bf16", "plain", [90, 40], [5, 2], 260, 2, 64, 16, 0, 0),                         # groups of more heads than a tile has rows
+    ("bf16", "fp8", [300, 40], [33, 40], 34, 2, 128, 16, 20, 2),                       # tiles of 7 tokens of 17 heads
+    ("bf16", "plain", [700, 128, 129], [32, 32, 16], 8, 2, 256, 16, 0, 0),             # a tile that is full
     ("bf16", "plain", [400], [90], 15, 3, 96, 16, 60, 3),
     ("bf16", "plain", [400, 90], [1, 70], 6, 3, 200, 16, 0, 0),
     ("bf16", "fp8", [2000, 50], [1, 7], 4, 2, 72, 16, 0, 0),
