@@ -363,8 +363,10 @@ typedef struct { /* DEVICE memory; strides in elements, the slots' is 1 and thos
     float decay;      /* finite */
     int32_t reserved; /* 0 */
 } attn_weights;
+/* Device scratch of attn_cache_weigh: sums of the parts that many new tokens are shared out in.  0 if desc is invalid. */
+size_t attn_weigh_workspace_bytes(const attn_paged_desc *desc);
 attn_status attn_cache_weigh(const attn_paged_desc *desc, const attn_cache *cache, const void *Q, const float *LSE, const attn_weights *weights,
-                             void *stream);
+                             void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * attn_cache_evict: of every sequence of more than `budget` tokens each key head keeps `budget`, for itself: those at positions in front of `first`, the

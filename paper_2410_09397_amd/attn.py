@@ -24,7 +24,7 @@ EXPORTS = ("attn_workspace_bytes", "attn_fwd", "attn_bwd", "attn_bwd_noalloc", "
            "attn_wgrad_workspace_bytes", "attn_bwd_wgrad", "attn_blockmask_validate", "attn_mfma_ceiling",
            "attn_win_workspace_bytes", "attn_win_fwd", "attn_win_bwd", "attn_cache_write", "attn_cache_read",
            "attn_paged_workspace_bytes", "attn_paged_fwd", "attn_tree_mask", "attn_tree_workspace_bytes", "attn_tree_fwd", "attn_tree_commit",
-           "attn_cache_weigh", "attn_evict_workspace_bytes", "attn_cache_evict", "attn_status_str")
+           "attn_weigh_workspace_bytes", "attn_cache_weigh", "attn_evict_workspace_bytes", "attn_cache_evict", "attn_status_str")
 
 
 class attn_desc(ctypes.Structure):
@@ -117,15 +117,15 @@ def lib():
         L.attn_cache_write.argtypes = L.attn_cache_read.argtypes = [pp, cp, vp, vp, vp]
         L.attn_paged_fwd.argtypes = [pp, cp, vp, vp, vp, vp, ctypes.c_size_t, vp]
         i32, i64, size = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
-        L.attn_tree_workspace_bytes.restype = L.attn_evict_workspace_bytes.restype = size
-        L.attn_tree_workspace_bytes.argtypes = [pp]
+        L.attn_tree_workspace_bytes.restype = L.attn_weigh_workspace_bytes.restype = L.attn_evict_workspace_bytes.restype = size
+        L.attn_tree_workspace_bytes.argtypes = L.attn_weigh_workspace_bytes.argtypes = [pp]
         L.attn_evict_workspace_bytes.argtypes = [pp, i32]
         for fn in (L.attn_tree_mask, L.attn_tree_fwd, L.attn_tree_commit, L.attn_cache_weigh, L.attn_cache_evict):
             fn.restype = ctypes.c_int
         L.attn_tree_mask.argtypes = [i32, i32, i32, vp, vp, vp, i64, vp]
         L.attn_tree_fwd.argtypes = [pp, cp, vp, i64, vp, vp, vp, vp, size, vp]
         L.attn_tree_commit.argtypes = [pp, cp, vp, i64, vp, vp, vp]
-        L.attn_cache_weigh.argtypes = [pp, cp, vp, vp, vp, vp]
+        L.attn_cache_weigh.argtypes = [pp, cp, vp, vp, vp, vp, size, vp]
         L.attn_cache_evict.argtypes = [pp, cp, vp, vp, size, vp]
         L.attn_status_str.restype = ctypes.c_char_p
         L.attn_status_str.argtypes = [ctypes.c_int]
@@ -735,7 +735,7 @@ def _slots(name, what, x, dtype, batch, kv_heads, slots, device):
 
 
 def attn_cache_weigh(Q, LSE, K_pages, V_pages, table, lens, scale, weight=None, decay=1.0, q_ptr=None, max_q=None, max_len=None, window=0, sinks=0,
-                     K_exp=None, V_exp=None, stream=None, out=None):
+                     K_exp=None, V_exp=None, stream=None, out=None, workspace=None):
     """Attention that the new tokens pay to every token of the cache: out[b, h, j] = decay * weight[b, h, j] + the sum of exp(scale q.k - LSE) over the
     new tokens that see slot j and the query heads of key head h; Q, LSE and the rest as attn_paged_fwd had or gave them.  New tokens start at zero,
     weight=None: all do.  weight, out: float32 [batch, kv_heads, at least max_len]; slots from a sequence's length on are left as they are.  out=None:
@@ -750,10 +750,24 @@ def attn_cache_weigh(Q, LSE, K_pages, V_pages, table, lens, scale, weight=None, 
         out = weight if weight is not None else _made_on(stream, lambda: torch.zeros((batch, kvh, slots), dtype=torch.float32, device=device))
     to, to_b, to_h = _slots("attn_cache_weigh", "out", out, torch.float32, batch, kvh, slots, device)
     at, at_b, at_h = (0, 0, 0) if weight is None else _slots("attn_cache_weigh", "weight", weight, torch.float32, batch, kvh, slots, device)
-    st = lib().attn_cache_weigh(desc, cache, Q.data_ptr(), LSE.data_ptr(), _WEIGHTS.pack(at, to, at_b, at_h, to_b, to_h, decay, 0), _stream(stream))
+    where = size = 0
+    if workspace is None:
+        size = attn_weigh_workspace_bytes(desc)
+        if size > 256:  # (256: nothing is kept there)
+            workspace = _scratch(size, device, stream)
+    else:
+        _check_workspace(workspace, device)
+    if workspace is not None:
+        where, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    st = lib().attn_cache_weigh(desc, cache, Q.data_ptr(), LSE.data_ptr(), _WEIGHTS.pack(at, to, at_b, at_h, to_b, to_h, decay, 0), where, size,
+                                _stream(stream))
     if st != ATTN_OK:
         raise AttnError(st, "attn_cache_weigh")
     return out
+
+
+def attn_weigh_workspace_bytes(desc):
+    return lib().attn_weigh_workspace_bytes(_as_argument(desc))
 
 
 def attn_evict_workspace_bytes(desc, budget):

@@ -194,6 +194,7 @@ struct WeighStage {
     __bf16 rows[kWeighTile * D];  // swizzled as the tiles of attn_common.hpp
     float lse2[kWeighTile];
     int pos[kWeighTile];
+    int whole[4];  // of 32 rows each: every one has a position
 };
 
 // 32 rows of a stage times 32 NG keys: the weights that these rows give the lane's keys.  masked: not every row sees every key.
@@ -245,6 +246,61 @@ __device__ __forceinline__ void weigh_rows(const WinParams& p, const WeighStage<
     }
 }
 
+// A whole stage of rows that all see all of 64 keys: the products of 32 rows and 32 keys are issued between the exponentials of the 32 keys before (the vector arithmetic takes
+// longer than the matrix pipe: an exponential is four instructions' time).
+template <int D, int SRC, bool PAD>
+__device__ __forceinline__ void weigh_stage(const WeighStage<D>& stage, const bf16x8 (&kf)[2][D / 16], float cs, int lane, float (&sum)[2]) {
+    typedef KeyOperand<D, SRC, 32, PAD> Keys;
+    constexpr int KS = D / 16;
+    const int h = lane >> 5, l32 = lane & 31;
+    const char* lds = reinterpret_cast<const char*>(stage.rows) + l32 * (2 * D);
+    bf16x8 q[2][KS];
+    f32x16 st[2];
+    f32x4 lse[4];
+    auto fetch = [&](int x) {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) q[x & 1][ks] = *reinterpret_cast<const bf16x8*>(lds + x * (64 * D) + ((Keys::chunk_of(ks, lane) ^ swz<D>(l32)) << 4));
+    };
+    auto products = [&](int x, int g) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st[g][i] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) st[g] = mfma32(q[x & 1][ks], kf[g][ks], st[g]);
+    };
+    auto weights = [&](int g) {
+        float a = 0.f, c = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+            a += __builtin_amdgcn_exp2f(fmaf(st[g][i], cs, -lse[i >> 2][i & 3]));
+            c += __builtin_amdgcn_exp2f(fmaf(st[g][i + 1], cs, -lse[i >> 2][(i & 3) + 1]));
+        }
+        sum[g] += a + c;
+    };
+    auto mix = [&] {
+#pragma unroll
+        for (int y = 0; y < KS; ++y) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);        // one product
+            __builtin_amdgcn_sched_group_barrier(0x2, 48 / KS, 0);  // and its share of the vector arithmetic
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    fetch(0);
+    products(0, 0);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+#pragma unroll
+        for (int y = 0; y < 4; ++y) lse[y] = *reinterpret_cast<const f32x4*>(stage.lse2 + 32 * x + 8 * y + 4 * h);
+        if (x < 3) fetch(x + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        products(x, 1);
+        weights(0);
+        mix();
+        if (x < 3) products(x + 1, 0);
+        weights(1);
+        mix();
+    }
+}
+
 // Brings tiles of rows into stages.  Tile `it` has tokens TT it .. of the sequence.
 template <int D, bool PAD>
 struct WeighFeed {
@@ -290,6 +346,8 @@ struct WeighFeed {
         if (tid < kWeighTile) {
             stage->lse2[tid] = lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
             stage->pos[tid] = pos;
+            const unsigned long has = __builtin_amdgcn_ballot_w64(pos >= 0);
+            if ((tid & 31) == 0) stage->whole[tid >> 5] = (unsigned)(has >> (tid & 32)) == ~0u;
         }
     }
 };
@@ -332,16 +390,10 @@ __global__ void __launch_bounds__(kThreads, 2) weigh_few_kernel(WeighParams w) {
         feed.request(p, s, kvh, 0, stage, tid);
         if (j0 < end) request();
         feed.arrive(stage, tid);
-        // rows without a position (behind the last, or of queries that saw nothing) are told in every tile
-        const bool has = tid >= kWeighTile || tid >= rows || feed.pos >= 0;
-        const int all = __builtin_amdgcn_ballot_w64(has) == ~0ul;
-        if (lane == 0) reinterpret_cast<int*>(smem + sizeof(WeighStage<D>))[wave] = all;
     } else if (j0 < end) {
         request();
     }
     __syncthreads();
-    const int* seen = reinterpret_cast<const int*>(smem + sizeof(WeighStage<D>));
-    const bool all = rows > 0 && seen[0] && seen[1];
     while (j0 < end) {
         const int here = j0;
         bf16x8 kf[1][KS];
@@ -353,14 +405,17 @@ __global__ void __launch_bounds__(kThreads, 2) weigh_few_kernel(WeighParams w) {
         float sum[1] = {0.f};
         WeighRows<32> range;
         range.init(p, s, here, min(here + 31, s.len - 1));
-        const bool whole = all && weigh_whole(p, s, 0, s.nq, here, min(here + 31, s.len - 1));
-        for (int r0 = range.r0; r0 < range.r1; r0 += 32) weigh_rows<D, SRC, 1, PAD>(p, *stage, r0, kf, here + l32, cs, !whole || r0 + 32 > rows, lane, sum);
+        const bool whole = weigh_whole(p, s, 0, s.nq, here, here + 31);
+        for (int r0 = range.r0; r0 < range.r1; r0 += 32)
+            weigh_rows<D, SRC, 1, PAD>(p, *stage, r0, kf, here + l32, cs, !whole || !__builtin_amdgcn_readfirstlane(stage->whole[r0 >> 5]), lane, sum);
         sum[0] += __shfl_xor(sum[0], 32, 64);
         if (lane < 32) weigh_store(w, s, b, kvh, here + l32, sum[0]);
     }
 }
 
-// Many rows: 64 keys of a workgroup are operands in all four waves, and tiles of rows stream past, 32 rows of each to a wave; the waves' sums meet at the end.
+// Many rows: a workgroup has 256 keys, 64 in the operands of each wave, and tiles of rows stream past all of them.  Few keys, or those of a prompt that most rows see, are
+// shared out: a workgroup takes one of w.parts shares of the tiles, and weigh_join_kernel adds up the sums, in their order.
+constexpr int kWeighKeys = 256;
 template <int D, int SRC, bool PAD>
 __global__ void __launch_bounds__(kThreads, (D == 256 ? 1 : 2)) weigh_many_kernel(WeighParams w) {
     const WinParams& p = w.p;
@@ -369,19 +424,27 @@ __global__ void __launch_bounds__(kThreads, (D == 256 ? 1 : 2)) weigh_many_kerne
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     WeighStage<D>* stages = reinterpret_cast<WeighStage<D>*>(smem);
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // the first keys of a sequence are seen by most rows: first keys first, and where all workgroups are on the chip at once the later half back from the last
-    const int bk_total = p.batch * p.kv_heads, bk = blockIdx.x % bk_total, b = bk / p.kv_heads, kvh = bk % p.kv_heads;
-    int blk = blockIdx.x / bk_total;
-    if (w.blocks * bk_total <= 512 && blk >= (w.blocks + 1) / 2) blk = w.blocks - 1 - (blk - (w.blocks + 1) / 2);
+    // most rows see the first keys of a sequence: these workgroups come first, and where all are on the chip at once the later half comes back from the last
+    const int bk_total = p.batch * p.kv_heads, bk = blockIdx.x % bk_total, b = bk / p.kv_heads, kvh = bk % p.kv_heads, all = w.blocks * w.parts;
+    int idx = blockIdx.x / bk_total;
+    if ((long)all * bk_total <= 512 && idx >= (all + 1) / 2) idx = all - 1 - (idx - (all + 1) / 2);
+    const int blk = idx / w.parts, part = idx - blk * w.parts;
     const WinSeq s = win_sequence(p, b);
-    const int j0 = 64 * blk, j1 = min(j0 + 63, s.len - 1);
-    if (j0 >= s.len) return;
+    const int b0 = kWeighKeys * blk, b1 = min(b0 + kWeighKeys - 1, s.len - 1), j0 = b0 + 64 * wave, j1 = j0 + 63;
+    if (b0 >= s.len) return;
     const float cs = p.scale * kLog2e;
     WeighFeed<D, PAD> feed;
     feed.init(p, tid);
-    // tiles of tokens that see some of the keys
-    const int t_lo = max(0, j0 - s.first), t_hi = j0 < p.sinks ? s.nq : (int)min((long)s.nq, max(0l, (long)j1 + p.window - s.first));
-    const int it0 = t_lo / feed.tt, it1 = t_hi > t_lo ? (t_hi + feed.tt - 1) / feed.tt : it0;
+    // tiles of tokens that see some of the keys, and this workgroup's share of them
+    const int t_lo = max(0, b0 - s.first), t_hi = b0 < p.sinks ? s.nq : (int)min((long)s.nq, max(0l, (long)b1 + p.window - s.first));
+    const int first = t_lo / feed.tt, tiles = t_hi > t_lo ? (t_hi + feed.tt - 1) / feed.tt - first : 0;
+    const int it0 = first + (int)((long)tiles * part / w.parts), it1 = first + (int)((long)tiles * (part + 1) / w.parts);
+    int tok0[4], tok1[4];  // first and last token of 32 rows of a tile
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        tok0[x] = __builtin_amdgcn_readfirstlane(win_token(p, 32 * x));
+        tok1[x] = __builtin_amdgcn_readfirstlane(win_token(p, 32 * x + 31));
+    }
     float sum[2] = {0.f, 0.f};
     if (it0 < it1) {
         feed.request(p, s, kvh, it0, stages, tid);
@@ -402,17 +465,22 @@ __global__ void __launch_bounds__(kThreads, (D == 256 ? 1 : 2)) weigh_many_kerne
         feed.arrive(stages, tid);
         __syncthreads();
         for (int it = it0; it < it1; ++it) {
-            WeighStage<D>* stage = stages + ((it - it0) & 1);
+            const WeighStage<D>& stage = stages[(it - it0) & 1];
             WeighStage<D>* next = stages + ((it - it0 + 1) & 1);
             if (it + 1 < it1) feed.request(p, s, kvh, it + 1, next, tid);
-            const int t0 = it * feed.tt, t1 = min(t0 + feed.tt, s.nq), rows = (t1 - t0) * p.group;
-            if (32 * wave < rows) {
-                // (a query that saw nothing has no position: looked up in the tile, two rows to a lane of 32)
-                const int mine = stage->pos[32 * wave + l32];
-                const bool has = 32 * wave + l32 >= rows || mine >= 0;
-                const bool whole = 32 * wave + 32 <= rows && __builtin_amdgcn_ballot_w64(has) == ~0ul &&
-                                   weigh_whole(p, s, t0 + win_token(p, 32 * wave), t0 + win_token(p, min(32 * wave + 31, rows - 1)) + 1, j0, j0 + 63);
-                weigh_rows<D, SRC, 2, PAD>(p, *stage, 32 * wave, kf, j0 + l32, cs, !whole, lane, sum);
+            const int t0 = it * feed.tt, i0 = s.first + t0, i_end = s.first + s.nq - 1;
+            const int i1 = min(i0 + tok1[3], i_end);
+            const bool full = D <= 128 && j1 <= i0 && (i1 - j0 < p.window || j1 < p.sinks) &&
+                              __builtin_amdgcn_readfirstlane(stage.whole[0] & stage.whole[1] & stage.whole[2] & stage.whole[3]);
+            if (full) {
+                if constexpr (D <= 128) weigh_stage<D, SRC, PAD>(stage, kf, cs, lane, sum);
+            } else
+#pragma unroll 1
+            for (int x = 0; x < 4; ++x) {
+                const int lo = i0 + tok0[x], hi = min(i0 + tok1[x], i_end);
+                if (lo > i_end || hi < j0 || (lo - j1 >= p.window && j0 >= p.sinks)) continue;  // none of the rows sees any of the keys
+                const bool whole = __builtin_amdgcn_readfirstlane(stage.whole[x]) && j1 <= lo && (hi - j0 < p.window || j1 < p.sinks);
+                weigh_rows<D, SRC, 2, PAD>(p, stage, 32 * x, kf, j0 + l32, cs, !whole, lane, sum);
             }
             if (it + 1 < it1) feed.arrive(next, tid);
             __syncthreads();
@@ -420,10 +488,19 @@ __global__ void __launch_bounds__(kThreads, (D == 256 ? 1 : 2)) weigh_many_kerne
     }
 #pragma unroll
     for (int g = 0; g < 2; ++g) sum[g] += __shfl_xor(sum[g], 32, 64);
-    float* meet = reinterpret_cast<float*>(smem);  // (the stages are free: every wave is past the last barrier, or there was no tile)
-    meet[wave * 64 + lane] = lane < 32 ? sum[0] : sum[1];
-    __syncthreads();
-    if (tid < 64) weigh_store(w, s, b, kvh, j0 + tid, (meet[tid] + meet[64 + tid]) + (meet[128 + tid] + meet[192 + tid]));
+    const float v = lane < 32 ? sum[0] : sum[1];
+    const int j = j0 + lane;
+    if (w.parts == 1) weigh_store(w, s, b, kvh, j, v);
+    else if (j < s.len) w.sums[((long)part * bk_total + bk) * p.max_len + j] = v;
+}
+__global__ void __launch_bounds__(kThreads) weigh_join_kernel(WeighParams w, int blocks) {
+    const WinParams& p = w.p;
+    const int bk = blockIdx.x / blocks, b = bk / p.kv_heads, kvh = bk % p.kv_heads, j = blockIdx.x % blocks * kThreads + threadIdx.x;
+    const WinSeq s = win_sequence(p, b);
+    if (j >= s.len) return;
+    float sum = 0.f;
+    for (int x = 0; x < w.parts; ++x) sum += w.sums[((long)x * p.batch * p.kv_heads + bk) * p.max_len + j];
+    weigh_store(w, s, b, kvh, j, sum);
 }
 
 // 32-bit arithmetic: 32x32x2 products of 32 keys on a wave, rows 32 at a time, both straight from memory.
@@ -466,7 +543,7 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_plain_kernel(WeighParams w)
     }
 }
 
-dim3 grid_of(const WeighParams& w) { return dim3((unsigned)((long)w.blocks * w.p.batch * w.p.kv_heads)); }
+dim3 grid_of(const WeighParams& w) { return dim3((unsigned)((long)w.blocks * w.parts * w.p.batch * w.p.kv_heads)); }
 
 template <int D, int SRC, bool PAD>
 hipError_t launch_from(WeighRowsKind kind, const WeighParams& w, hipStream_t stream) {
@@ -478,8 +555,12 @@ hipError_t launch_from(WeighRowsKind kind, const WeighParams& w, hipStream_t str
     };
     if (kind == kWeighOne) return run(weigh_one_kernel<D, SRC, PAD, true>, 0);
     if (kind == kWeighAny) return run(weigh_one_kernel<D, SRC, PAD, false>, 0);
-    if (kind == kWeighFew) return run(weigh_few_kernel<D, SRC, PAD>, (int)sizeof(WeighStage<D>) + 16);
-    return run(weigh_many_kernel<D, SRC, PAD>, 2 * (int)sizeof(WeighStage<D>));
+    if (kind == kWeighFew) return run(weigh_few_kernel<D, SRC, PAD>, (int)sizeof(WeighStage<D>));
+    const hipError_t e = run(weigh_many_kernel<D, SRC, PAD>, 2 * (int)sizeof(WeighStage<D>));
+    if (e != hipSuccess || w.parts == 1) return e;
+    const int blocks = (w.p.max_len + kThreads - 1) / kThreads;
+    hipLaunchKernelGGL(weigh_join_kernel, dim3((unsigned)((long)blocks * w.p.batch * w.p.kv_heads)), dim3(kThreads), 0, stream, w, blocks);
+    return hipGetLastError();
 }
 template <int D>
 hipError_t launch(bool fp8, WeighRowsKind kind, const WeighParams& w, hipStream_t stream) {

@@ -233,6 +233,19 @@ size_t tree_o_bytes(const attn_paged_desc* d, const WinParams& p, int64_t grid) 
     return p.places > 0 ? (size_t)grid * tree_rows(d) * d->d * sizeof(float) : 0;
 }
 
+attn_status check_weigh(const attn_paged_desc* d) {
+    const attn_status st = check_paged(d);
+    if (st != ATTN_OK || no_cache(d)) return st;
+    const int64_t bk = (int64_t)d->batch * d->kv_heads;
+    return bk > kMostGroups || ((int64_t)d->max_len + 63) / 64 * bk > kMostGroups ? ATTN_ERR_UNSUPPORTED : ATTN_OK;
+}
+attn::WeighPlan weigh_plan(const attn_paged_desc* d) {
+    return attn::weigh_plan(is_wide(d), d->batch, d->heads, d->kv_heads, d->max_q, d->max_len, d->q_stride_n, d->q_stride_h);
+}
+size_t weigh_bytes(const attn_paged_desc* d, const attn::WeighPlan& plan) {
+    return plan.parts > 1 ? sizeof(float) * plan.parts * d->batch * d->kv_heads * d->max_len : 0;
+}
+
 int evict_cap(const attn_paged_desc* d, int32_t budget) { return std::max(0, std::min(budget, d->max_len - budget)); }
 attn_status check_evict(const attn_paged_desc* d, int32_t budget) {
     const attn_status st = check_paged(d);
@@ -434,9 +447,14 @@ attn_status attn_tree_commit(const attn_paged_desc* desc, const attn_cache* cach
     return status_of(attn::launch_tree_commit(value_bytes(desc) * desc->d, page_unit(desc, cache), p, leaf, new_lens, static_cast<hipStream_t>(stream)));
 }
 
+size_t attn_weigh_workspace_bytes(const attn_paged_desc* desc) {
+    if (check_weigh(desc) != ATTN_OK) return 0;
+    return no_cache(desc) ? 256 : std::max<size_t>(256, weigh_bytes(desc, weigh_plan(desc)));
+}
+
 attn_status attn_cache_weigh(const attn_paged_desc* desc, const attn_cache* cache, const void* Q, const float* LSE, const attn_weights* weights,
-                             void* stream) {
-    attn_status st = check_paged(desc);
+                             void* workspace, size_t workspace_bytes, void* stream) {
+    attn_status st = check_weigh(desc);
     if (st != ATTN_OK) return st;
     if (!weights || weights->reserved != 0 || !std::isfinite(weights->decay)) return ATTN_ERR_INVALID_ARG;
     if (no_cache(desc)) return ATTN_OK;
@@ -449,8 +467,6 @@ attn_status attn_cache_weigh(const attn_paged_desc* desc, const attn_cache* cach
     if (weights->in && (!good_slots(desc, weights->in_stride_b, weights->in_stride_h, desc->max_len) ||
                         (weights->in == weights->out && (weights->in_stride_b != weights->out_stride_b || weights->in_stride_h != weights->out_stride_h))))
         return ATTN_ERR_INVALID_ARG;
-    const int64_t bk = (int64_t)desc->batch * desc->kv_heads;
-    if (bk > kMostGroups || ((int64_t)desc->max_len + 63) / 64 * bk > kMostGroups) return ATTN_ERR_UNSUPPORTED;
     attn::WeighParams w;
     std::memset(&w, 0, sizeof(w));
     w.p = paged_params(desc, cache);
@@ -463,12 +479,14 @@ attn_status attn_cache_weigh(const attn_paged_desc* desc, const attn_cache* cach
     w.out_b = weights->out_stride_b;
     w.out_h = weights->out_stride_h;
     w.decay = weights->decay;
-    const bool wide = is_wide(desc);
-    const attn::WeighPlan plan = attn::weigh_plan(desc->batch, desc->heads, desc->kv_heads, desc->max_q, desc->max_len, desc->q_stride_n, desc->q_stride_h);
-    w.chunk = wide ? plan.chunk : 128;
-    w.blocks = (desc->max_len + w.chunk - 1) / w.chunk;
+    const attn::WeighPlan plan = weigh_plan(desc);
+    if (plan.parts > 1 && (!workspace || workspace_bytes < weigh_bytes(desc, plan) || !aligned16(workspace))) return ATTN_ERR_WORKSPACE;
+    w.chunk = plan.chunk;
+    w.blocks = plan.blocks;
+    w.parts = plan.parts;
+    w.sums = static_cast<float*>(workspace);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    return status_of(wide ? attn::launch_weigh(fp8, plan.kind, w, s) : attn::launch_weigh_plain(bf16, fp8, w, s));
+    return status_of(is_wide(desc) ? attn::launch_weigh(fp8, plan.kind, w, s) : attn::launch_weigh_plain(bf16, fp8, w, s));
 }
 
 size_t attn_evict_workspace_bytes(const attn_paged_desc* desc, int32_t budget) {

@@ -140,20 +140,31 @@ inline TreeShares tree_shares(bool wide, int batch, int heads, int kv_heads, int
     return p;
 }
 
-// Kernels of attn_cache_weigh by the rows of a (sequence, key head): at most 16, one tile of 128, more of them; any: groups or strides that a tile does not hold.
+// Kernels of attn_cache_weigh by the rows of a (sequence, key head): at most 16, one tile of 128, more of them; any: groups or strides that a tile does not hold (and the
+// kernel of 32-bit arithmetic).  us of a call: one kernel for all, 16 rows at a time -> these, h32 k8 d = 128: newest token of 64 sequences (quantised) 72 -> 31, last 32
+// tokens of 8 prompts 52 -> 18, a prompt of 4096 tokens 1101 -> 101.
+// One tile or less: keys of a workgroup, as many as leave 2048 workgroups (512 / 1024 / 4096: last 32 tokens of 8 prompts 24.9 / 19.9 / 21.1 for 18.1).
+// Many rows: the keys of a workgroup are 256, and the tiles of rows are shared out until there are some 768 workgroups, a round and a half, with two tiles each at least.  us of
+// 512 / 768 / 1024 workgroups: a prompt of 4096 tokens 114 / 101 / 105, 4 prompts of 500 to 2000 107 / 93 / 91, the last 512 of 16384 tokens 90 / 90 / 98; one / two / four tiles:
+// a prompt of 300 tokens 16 / 21 / 32, d = 256, 64 of 4000 tokens 47 / 39 / 39.
 enum WeighRowsKind { kWeighOne, kWeighFew, kWeighMany, kWeighAny };
 constexpr int64_t kWeighGroups = 2048;
+constexpr int64_t kWeighParts = 768, kWeighLeast = 2;
 struct WeighPlan {
     WeighRowsKind kind;
-    int blocks, chunk;  // workgroups of a (sequence, key head), and keys of each
+    int blocks, chunk, parts;  // workgroups of a (sequence, key head): blocks of `chunk` keys, times parts of the rows
 };
-inline WeighPlan weigh_plan(int batch, int heads, int kv_heads, int max_q, int max_len, int64_t q_stride_n, int64_t q_stride_h) {
+inline WeighPlan weigh_plan(bool wide, int batch, int heads, int kv_heads, int max_q, int max_len, int64_t q_stride_n, int64_t q_stride_h) {
     const int64_t group = heads / kv_heads, rows = max_q * group, bk = (int64_t)batch * kv_heads;
     const bool tiles = group <= 128 && q_stride_n < (1 << 22) && q_stride_h < (1 << 22);
-    WeighPlan p = {rows <= 16 ? kWeighOne : !tiles ? kWeighAny : rows <= 128 ? kWeighFew : kWeighMany, 0, 128};
-    if (p.kind == kWeighMany) p.chunk = 64;
-    else while (p.chunk < 1024 && (max_len + p.chunk * 2 - 1) / (p.chunk * 2) * bk >= kWeighGroups) p.chunk *= 2;
+    WeighPlan p = {rows <= 16 ? kWeighOne : !tiles || !wide ? kWeighAny : rows <= 128 ? kWeighFew : kWeighMany, 0, 128, 1};
+    if (p.kind == kWeighMany) p.chunk = 256;
+    else while (wide && p.chunk < 1024 && (max_len + p.chunk * 2 - 1) / (p.chunk * 2) * bk >= kWeighGroups) p.chunk *= 2;
     p.blocks = (max_len + p.chunk - 1) / p.chunk;
+    if (p.kind == kWeighMany) {
+        const int64_t of_rows = (max_q + 128 / group - 1) / (128 / group);  // tiles
+        p.parts = (int)std::max<int64_t>(1, std::min(std::min<int64_t>(64, kWeighParts / std::max<int64_t>(1, p.blocks * bk)), of_rows / kWeighLeast));
+    }
     return p;
 }
 

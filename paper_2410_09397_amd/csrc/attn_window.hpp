@@ -224,7 +224,8 @@ struct WeighParams {
     float* out;
     long in_b, in_h, out_b, out_h;
     float decay;
-    int blocks, chunk;  // workgroups of a (sequence, key head), and keys of each
+    int blocks, chunk, parts;  // workgroups of a (sequence, key head): blocks of `chunk` keys, times parts of the rows
+    float* sums;               // of the parts, if there are several: [part][batch * kv_heads][max_len]
 };
 hipError_t launch_weigh(bool fp8, WeighRowsKind kind, const WeighParams& w, hipStream_t stream);  // bf16; quantised pages: d in {64, 128, 256}
 hipError_t launch_weigh_plain(bool is_bf16, bool fp8, const WeighParams& w, hipStream_t stream);

@@ -75,7 +75,7 @@ int main() {
         const size_t tree = attn_tree_workspace_bytes(&p), scratch = attn_evict_workspace_bytes(&p, budget);
         tree ? ++taken : ++refused;
         scratch ? ++taken : ++refused;
-        EXPECT(tree < (1ull << 50) && scratch < (1ull << 56));
+        EXPECT(tree < (1ull << 50) && scratch < (1ull << 56) && attn_weigh_workspace_bytes(&p) < (1ull << 50));
         // of every sequence and key head: what moves, from and to
         const int64_t cap = std::fmax(0, std::fmin(budget, (double)p.max_len - budget));
         if (scratch && p.batch > 0 && p.heads > 0 && p.max_len > 0) EXPECT(scratch >= 8ull * p.batch * p.kv_heads * cap);
@@ -95,7 +95,7 @@ int main() {
         const bool none = p.batch == 0 || p.heads == 0, no_rows = none || p.total_q == 0 || p.max_q == 0;
         EXPECT(attn_tree_fwd(&p, &c, M, any_stride(20), P, P, W, nullptr, 0, nullptr) != ATTN_OK || no_rows);
         EXPECT(attn_tree_commit(&p, &c, M, any_stride(20), I, I + 70000, nullptr) != ATTN_OK || no_rows);
-        EXPECT(attn_cache_weigh(&p, &c, P, W, &w, nullptr) != ATTN_OK || none || p.max_len == 0);
+        EXPECT(attn_cache_weigh(&p, &c, P, W, &w, P, ~(size_t)0, nullptr) != ATTN_OK || none || p.max_len == 0);
         EXPECT(attn_cache_evict(&p, &c, &e, P, ~(size_t)0, nullptr) != ATTN_OK || none || p.max_len == 0);
         // with them and without a workspace, or without a place for the lengths
         c.K = c.V = P;
@@ -105,7 +105,7 @@ int main() {
         e.new_lens = I + 70000;
         EXPECT(attn_cache_evict(&p, &c, &e, nullptr, 0, nullptr) != ATTN_OK || none || p.max_len == 0);
         w.out = nullptr;
-        EXPECT(attn_cache_weigh(&p, &c, P, W, &w, nullptr) != ATTN_OK || none || p.max_len == 0);
+        EXPECT(attn_cache_weigh(&p, &c, P, W, &w, P, ~(size_t)0, nullptr) != ATTN_OK || none || p.max_len == 0);
         const int32_t batch = any_int(70), total = any_int(5000), most = any_int(500);
         EXPECT(attn_tree_mask(batch, total, most, I, nullptr, nullptr, any_stride(16), nullptr) != ATTN_OK || batch == 0 || total == 0 || most == 0);
     }

@@ -28,8 +28,8 @@ def weights(**kw):
     return attn.attn_weights(**base)
 
 
-def weigh(d, c="cache", q=P, lse=P, w="weights"):
-    return attn.lib().attn_cache_weigh(ref(d), ref(cache() if c == "cache" else c), q, lse, ref(weights() if w == "weights" else w), None)
+def weigh(d, c="cache", q=P, lse=P, w="weights", ws=P, size=1 << 40):
+    return attn.lib().attn_cache_weigh(ref(d), ref(cache() if c == "cache" else c), q, lse, ref(weights() if w == "weights" else w), ws, size, None)
 
 
 def eviction(**kw):
@@ -58,7 +58,7 @@ def test_bad_cache_descriptors(kw, status):
     assert [call(d) for call in CALLS] == [status] * 4
     if "num_pages" not in kw or kw["num_pages"] < 0:
         assert attn.lib().attn_tree_workspace_bytes(ctypes.byref(d)) == 0
-        assert attn.lib().attn_evict_workspace_bytes(ctypes.byref(d), 50) == 0
+        assert attn.lib().attn_evict_workspace_bytes(ctypes.byref(d), 50) == attn.lib().attn_weigh_workspace_bytes(ctypes.byref(d)) == 0
 
 
 @pytest.mark.parametrize("kw", [dict(K=None), dict(V=None), dict(table=None), dict(lens=None), dict(K_exp=None), dict(V_exp=None), dict(K=P + 8),
@@ -118,6 +118,12 @@ def test_weigh_pointers_and_sizes():
     assert weigh(paged(total_q=5), cache(q_ptr=None)) == BAD
     for kw in (dict(batch=0), dict(heads=0, kv_heads=0), dict(max_len=0)):
         assert weigh(paged(**kw), None, None, None) == OK
+    prompt = paged(total_q=4000, max_q=2000, max_len=2000, max_pages=200, table_stride=200)  # many rows for few keys: they are shared out
+    need = attn.lib().attn_weigh_workspace_bytes(ctypes.byref(prompt))
+    assert need > 256
+    slots = weights(in_stride_b=4000, in_stride_h=2000, out_stride_b=4000, out_stride_h=2000)
+    for ws, size in ((None, need), (P, need - 1), (P + 8, need)):
+        assert weigh(prompt, w=slots, ws=ws, size=size) == WORKSPACE
     big = dict(max_len=1 << 28, max_pages=1 << 24, table_stride=1 << 24)
     huge = dict(in_stride_b=1 << 40, in_stride_h=1 << 30, out_stride_b=1 << 40, out_stride_h=1 << 30)
     assert weigh(paged(batch=64, **big), w=weights(**huge)) == UNSUPPORTED
