@@ -2,6 +2,8 @@
 //
 // Rows move whole, codes with their exponents, and no value is computed.  All of it is bound by memory or, at the size of a decoding step, by the chain of
 // reads that depend on one another (length, choice, page, row).
+#include <type_traits>
+
 #include "attn_internal.hpp"
 #include "attn_win_rules.hpp"
 #include "attn_window.hpp"
@@ -24,6 +26,18 @@ __device__ __forceinline__ Place place_of(const WinParams& p, int b, int kvh, in
     return r;
 }
 
+// Sums of a wave's values up to and including each lane's, by moves between lanes that are part of the additions (an exchange through LDS takes some 100 cycles, and the next of
+// the six waits for it: a scan of the bins in evict_select_kernel took 0.8 us).
+__device__ __forceinline__ int wave_sums(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);  // from the lane before in a row of 16
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);  // two before
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // the last lane of a row to the next row, rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // lane 31 to rows 2 and 3
+    return v;
+}
+
 // ---------------------------------------------------------------------------------------------------- accepted tokens
 // A workgroup takes K or V of a (sequence, key head).  The x-th of the tokens that stay, drafted token u_x, moves to place x behind the context.
 // u_x ascends, so a row is overwritten only by a row that is read with it or later: a chunk of rows is in registers before any of it is written, and
@@ -44,13 +58,7 @@ __global__ void __launch_bounds__(kThreads) tree_commit_kernel(WinParams p, cons
             for (int x = 0; x < 32; ++x)
                 if (32 * tid + x >= s.nq || s.first + 32 * tid + x < 0) v &= ~(1u << x);
         }
-        int upto = __popc(v);
-        const int own = upto;
-#pragma unroll
-        for (int x = 1; x < 64; x <<= 1) {
-            const int before = __shfl_up(upto, x, 64);
-            upto += tid >= x ? before : 0;
-        }
+        const int own = __popc(v), upto = wave_sums(own);
         int at = upto - own;
         for (; v; v &= v - 1) stay[at++] = 32 * tid + __builtin_ctz(v);
         if (tid == 63) total = upto;
@@ -100,173 +108,239 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
-
-// Places of set flags of all threads, in the order of the threads; `total`: how many there are.
-__device__ __forceinline__ int block_rank(bool flag, int* waves, int& total) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const unsigned long set = __builtin_amdgcn_ballot_w64(flag);
-    __syncthreads();
-    if (lane == 0) waves[w] = __builtin_popcountl(set);
-    __syncthreads();
-    int before = 0;
-    total = 0;
-#pragma unroll
-    for (int x = 0; x < kSelectWaves; ++x) {
-        before += x < w ? waves[x] : 0;
-        total += waves[x];
+constexpr uint32_t kStays = 0xfffffffeu;  // above the key of every weight, and below ~0
+// The tokens of a (sequence, key head).
+struct EvictSequence {
+    int len, n, kept;  // n stay; slots below `kept` have their positions in an array
+    long seen;
+    const float* weight;
+    const int32_t* pos;
+    float* weight_out;
+    int32_t* pos_out;
+    __device__ __forceinline__ void init(const EvictParams& e, int b, int h) {
+        len = min(max(e.p.lens[b], 0), e.p.max_len);
+        n = min(len, e.budget);
+        seen = e.seen ? e.seen[b] : len;
+        kept = e.pos ? (e.kept ? min(max(e.kept[b], 0), len) : 0) : 0;
+        weight = e.weight + (long)b * e.in_b + (long)h * e.in_h;
+        pos = e.pos ? e.pos + (long)b * e.in_b + (long)h * e.in_h : nullptr;
+        weight_out = e.weight_out + (long)b * e.out_b + (long)h * e.out_h;
+        pos_out = e.pos_out ? e.pos_out + (long)b * e.out_b + (long)h * e.out_h : nullptr;
     }
-    return before + __builtin_popcountl(set & ((1ul << lane) - 1ul));
-}
+    __device__ __forceinline__ long position(int slot) const { return slot < kept ? (long)pos[slot] : seen - len + slot; }
+    __device__ __forceinline__ uint32_t key(const EvictParams& e, float w, long at) const { return at < e.first || at >= seen - e.recent ? kStays : weight_key(w); }
+};
 
-// One workgroup per (sequence, key head): of its len tokens, len - n leave, n = min(len, budget).  The key of the last one that leaves is found 8 bits at
-// a time from the top: a histogram of the keys that agree in the bits found so far says in which of 256 bins it lies.  Of tokens with this very key
-// those in the highest slots leave.  Free slots below n and tokens that stay above it are as many as one another; both are listed in ascending order.
-__global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(EvictParams e) {
-    const WinParams& p = e.p;
-    __shared__ int bins[256], waves[kSelectWaves], found[2];
-    const int bk = blockIdx.x, b = bk / p.kv_heads, h = bk % p.kv_heads, tid = threadIdx.x;
-    const int len = min(max(p.lens[b], 0), p.max_len), n = min(len, e.budget), leave = len - n;
-    const long seen = e.seen ? e.seen[b] : len;
-    const int kept = e.pos ? (e.kept ? min(max(e.kept[b], 0), len) : 0) : 0;
-    const float* weight = e.weight + (long)b * e.in_b + (long)h * e.in_h;
-    const int32_t* pos = e.pos ? e.pos + (long)b * e.in_b + (long)h * e.in_h : nullptr;
-    float* weight_out = e.weight_out + (long)b * e.out_b + (long)h * e.out_h;
-    int32_t* pos_out = e.pos_out ? e.pos_out + (long)b * e.out_b + (long)h * e.out_h : nullptr;
-    auto position = [&](int slot) -> long { return slot < kept ? (long)pos[slot] : seen - len + slot; };
-    auto key_of = [&](int slot) -> uint32_t {
-        const long at = position(slot);
-        return at < e.first || at >= seen - e.recent ? 0xffffffffu : weight_key(weight[slot]);
-    };
-    if (h == 0 && tid == 0) e.new_lens[b] = n;
-
-    uint32_t last = 0;  // the key of the last token that leaves
-    int equal = 0;      // how many with this key leave
-    if (leave > 0) {
-        int rank = leave - 1;  // among the keys that agree with `last` in the bits found
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int x = tid; x < 256; x += kSelectThreads) bins[x] = 0;
-            __syncthreads();
-            for (int slot = tid; slot < len; slot += kSelectThreads) {
-                const uint32_t k = key_of(slot);
-                if (shift == 24 || (k >> (shift + 8)) == (last >> (shift + 8))) atomicAdd(&bins[(k >> shift) & 255u], 1);
-            }
-            __syncthreads();
-            if (tid < 64) {  // four bins to a lane
-                int c[4], sum = 0;
-#pragma unroll
-                for (int x = 0; x < 4; ++x) sum += c[x] = bins[4 * tid + x];
-                int upto = sum;
-#pragma unroll
-                for (int x = 1; x < 64; x <<= 1) {
-                    const int before = __shfl_up(upto, x, 64);
-                    upto += tid >= x ? before : 0;
-                }
-                int below = upto - sum;
-                if (rank >= below && rank < upto) {
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        if (rank >= below && rank < below + c[x]) {
-                            found[0] = 4 * tid + x;
-                            found[1] = rank - below;
-                        }
-                        below += c[x];
-                    }
-                }
-            }
-            __syncthreads();
-            last |= (uint32_t)found[0] << shift;
-            rank = found[1];
-        }
-        equal = rank + 1;
-    }
-    // of the tokens with the last key, those behind the first `stay_equal` leave
-    int stay_equal = 0;
-    if (leave > 0) {
-        int all_equal = 0;
-        for (int s0 = 0; s0 < len; s0 += kSelectThreads) {
-            int here;
-            block_rank(s0 + tid < len && key_of(s0 + tid) == last, waves, here);
-            all_equal += here;
-        }
-        stay_equal = all_equal - equal;
-    }
-    int equals = 0, free = 0, come = 0;
-    for (int s0 = 0; s0 < len; s0 += kSelectThreads) {
-        const int slot = s0 + tid;
-        const bool inside = slot < len;
-        const uint32_t k = inside ? key_of(slot) : 0xffffffffu;
-        int here;
-        const int rank = leave > 0 ? block_rank(inside && k == last, waves, here) : 0;
-        const bool goes = leave > 0 && inside && (k < last || (k == last && equals + rank >= stay_equal));
-        if (leave > 0) equals += here;
-        if (inside && slot < n && !goes) {
-            weight_out[slot] = weight[slot];
-            if (pos_out) pos_out[slot] = (int32_t)position(slot);
-        }
-        if (leave > 0) {
-            const int f = block_rank(inside && slot < n && goes, waves, here);
-            if (inside && slot < n && goes && free + f < e.cap) e.to[(long)bk * e.cap + free + f] = slot;
-            free += here;
-            const int c = block_rank(inside && slot >= n && !goes, waves, here);
-            if (inside && slot >= n && !goes && come + c < e.cap) e.from[(long)bk * e.cap + come + c] = slot;
-            come += here;
-        }
-    }
-    if (tid == 0) e.count[bk] = min(min(free, come), e.cap);
-}
-
-// Rows, weights and positions of the tokens that move.  What is read lies at slots of at least n, what is written below.
+// Rows, weights and positions of the tokens that move, by kThreads-sized steps: lists of `count` slots, this workgroup's first row and the distance to its next ones.  What is read
+// lies in slots of at least n, what is written below.
 constexpr int kMoveRows = 4;  // rows of K and V of a thread on the way
 template <typename U>
-__global__ void __launch_bounds__(kThreads) evict_move_kernel(EvictParams e, int blocks, int units, int lanes, int value_bytes) {
+__device__ __forceinline__ void evict_rows(const EvictParams& e, const EvictSequence& q, int b, int h, const int* from, const int* to, int count, int row0, int step, int threads,
+                                           int units, int lanes, int value_bytes) {
     const WinParams& p = e.p;
-    const int bk = blockIdx.x / blocks, b = bk / p.kv_heads, h = bk % p.kv_heads, tid = threadIdx.x;
-    const int count = e.count[bk], per = kThreads / lanes, c = tid & (lanes - 1);
+    const int tid = threadIdx.x, per = threads / lanes, c = tid & (lanes - 1);
     char *K = static_cast<char*>(const_cast<void*>(p.K)), *V = static_cast<char*>(const_cast<void*>(p.V));
     uint8_t *K_exp = const_cast<uint8_t*>(p.K_exp), *V_exp = const_cast<uint8_t*>(p.V_exp);
-    const int len = min(max(p.lens[b], 0), p.max_len);
-    const long seen = e.seen ? e.seen[b] : len;
-    const int kept = e.pos ? (e.kept ? min(max(e.kept[b], 0), len) : 0) : 0;
-    for (int x0 = (blockIdx.x % blocks) * per * kMoveRows; x0 < count; x0 += blocks * per * kMoveRows) {
+    for (int x0 = row0; x0 < count; x0 += step) {
         U k[kMoveRows], v[kMoveRows];
         uint8_t ke[kMoveRows], ve[kMoveRows];
-        Place to[kMoveRows];
+        Place place[kMoveRows];
 #pragma unroll
         for (int r = 0; r < kMoveRows; ++r) {
             const int x = x0 + r * per + tid / lanes;
-            to[r].there = false;
+            place[r].there = false;
             if (x >= count || c >= units) continue;
-            const int source = e.from[(long)bk * e.cap + x], target = e.to[(long)bk * e.cap + x];
-            const Place from = place_of(p, b, h, source, value_bytes);
-            to[r] = place_of(p, b, h, target, value_bytes);
-            to[r].there = to[r].there && from.there;
-            if (to[r].there) {
-                k[r] = *reinterpret_cast<const U*>(K + from.at + (long)c * sizeof(U));
-                v[r] = *reinterpret_cast<const U*>(V + from.at + (long)c * sizeof(U));
+            const int source = from[x], target = to[x];
+            const Place at = place_of(p, b, h, source, value_bytes);
+            place[r] = place_of(p, b, h, target, value_bytes);
+            place[r].there = place[r].there && at.there;
+            if (place[r].there) {
+                k[r] = *reinterpret_cast<const U*>(K + at.at + (long)c * sizeof(U));
+                v[r] = *reinterpret_cast<const U*>(V + at.at + (long)c * sizeof(U));
                 if (K_exp && c == 0) {
-                    ke[r] = K_exp[from.exp];
-                    ve[r] = V_exp[from.exp];
+                    ke[r] = K_exp[at.exp];
+                    ve[r] = V_exp[at.exp];
                 }
             }
             if (c == 0) {
-                e.weight_out[(long)b * e.out_b + (long)h * e.out_h + target] = e.weight[(long)b * e.in_b + (long)h * e.in_h + source];
-                if (e.pos_out)
-                    e.pos_out[(long)b * e.out_b + (long)h * e.out_h + target] =
-                        source < kept ? e.pos[(long)b * e.in_b + (long)h * e.in_h + source] : (int32_t)(seen - len + source);
+                q.weight_out[target] = q.weight[source];
+                if (q.pos_out) q.pos_out[target] = (int32_t)q.position(source);
             }
         }
 #pragma unroll
         for (int r = 0; r < kMoveRows; ++r) {
-            if (!to[r].there) continue;
-            *reinterpret_cast<U*>(K + to[r].at + (long)c * sizeof(U)) = k[r];
-            *reinterpret_cast<U*>(V + to[r].at + (long)c * sizeof(U)) = v[r];
+            if (!place[r].there) continue;
+            *reinterpret_cast<U*>(K + place[r].at + (long)c * sizeof(U)) = k[r];
+            *reinterpret_cast<U*>(V + place[r].at + (long)c * sizeof(U)) = v[r];
             if (K_exp && c == 0) {
-                K_exp[to[r].exp] = ke[r];
-                V_exp[to[r].exp] = ve[r];
+                K_exp[place[r].exp] = ke[r];
+                V_exp[place[r].exp] = ve[r];
             }
         }
     }
+}
+
+// One workgroup per (sequence, key head): of its len tokens, len - n leave.  The key of the last one that leaves is found 11, 11 and 10 bits at a time from the top: a histogram of
+// the keys that agree in the bits found so far says in which bin it lies, and every wave reads it for itself (11 bits are the exponent and two more: with 8, most weights of a
+// wave fall into a few bins, and their additions wait for one another).  Of tokens with this very key those in the highest slots leave.
+// Free slots below n and tokens that stay above it are as many as one another; both are listed in ascending order, at places that come from a table of how many
+// each 64 slots have.  Keys are in LDS, 16 to a thread (longer sequences are gone through again for every step).  What bounds it at the size of a decoding step is how many
+// instructions are fetched for the first time: with the keys in registers, and every loop over them written out, 1040 tokens took 19 us.
+// Few moves (e.here) are made by the same workgroup.
+constexpr int kSelectItems = 16, kSelectPasses = 3, kSelectBins = 2048;
+__device__ __forceinline__ int select_bin(uint32_t digit) { return (int)(digit + (digit >> 5)); }
+template <int THREADS>
+struct SelectLds {
+    uint32_t key[kSelectItems * THREADS];
+    int bins[kSelectPasses][kSelectBins + kSelectBins / 32];  // (a lane reads 32 in a row: a word of padding behind them keeps the lanes on different banks)
+    int table[kSelectItems * THREADS / 64 + 1];  // places, and behind them how many there are
+    int from[kEvictHere], to[kEvictHere];
+};
+template <typename U, int THREADS>
+__global__ void __launch_bounds__(THREADS) evict_select_kernel(EvictParams e, int units, int lanes, int value_bytes) {
+    constexpr int W = THREADS / 64, kEntries = kSelectItems * W, kChunk = kSelectItems * THREADS;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    SelectLds<THREADS>& lds = *reinterpret_cast<SelectLds<THREADS>*>(smem);
+    const int bk = blockIdx.x, b = bk / e.p.kv_heads, h = bk % e.p.kv_heads, tid = threadIdx.x, lane = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    EvictSequence q;
+    q.init(e, b, h);
+    const int leave = q.len - q.n;
+    if (h == 0 && tid == 0) e.new_lens[b] = q.n;
+    // weights and positions of slots s0 .. end - 1, four of a thread on the way together (so none behind a condition): use(slot, weight, position)
+    auto each = [&](int s0, int end, auto use) {
+#pragma unroll 1
+        for (int s = s0 + tid; s < end; s += 4 * THREADS) {
+            float weight[4];
+            int32_t pos[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int y = 0; y < 4; ++y) weight[y] = q.weight[min(s + y * THREADS, end - 1)];
+            if (q.kept > 0) {
+#pragma unroll
+                for (int y = 0; y < 4; ++y) pos[y] = q.pos[min(s + y * THREADS, q.kept - 1)];
+            }
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const int slot = s + y * THREADS;
+                if (slot < end) use(slot, weight[y], slot < q.kept ? (long)pos[y] : q.seen - q.len + slot);
+            }
+        }
+    };
+    auto load = [&](int s0, int end) { each(s0, end, [&](int slot, float weight, long at) { lds.key[slot - s0] = q.key(e, weight, at); }); };
+    // places of flags of slots s0 .. end - 1 (up to 16 bits each of two kinds): count(slot) says which of them a slot has
+    auto places = [&](int s0, int end, auto count) {
+        __syncthreads();  // (the table may still be read)
+        for (int x = 0; s0 + x * THREADS < end; ++x) {
+            const int slot = s0 + x * THREADS + tid, c = slot < end ? count(slot) : 0;
+            const int own = __builtin_popcountl(__builtin_amdgcn_ballot_w64(c & 1)) | __builtin_popcountl(__builtin_amdgcn_ballot_w64(c & 0x10000)) << 16;
+            if (lane == 0) lds.table[x * W + w] = own;
+        }
+        __syncthreads();
+        if (w == 0) {
+            const int entries = (end - s0 + THREADS - 1) / THREADS * W;
+            int before = 0;
+            for (int x = lane; x - lane < entries; x += 64) {
+                const int own = x < entries ? lds.table[x] : 0;
+                const int upto = wave_sums(own);
+                if (x < entries) lds.table[x] = before + upto - own;
+                before += __builtin_amdgcn_readlane(upto, 63);
+            }
+            if (lane == 0) lds.table[kEntries] = before;
+        }
+        __syncthreads();
+    };
+    const unsigned long lower = (1ul << lane) - 1ul;
+
+    uint32_t last = 0;                // the key of the last token that leaves
+    int rank = leave - 1, equal = 0;  // its place among the keys that agree in the bits found; how many tokens have this key
+    if (leave > 0) {
+        for (int x = tid; x < (int)(sizeof(lds.bins) / sizeof(int)); x += THREADS) lds.bins[0][x] = 0;
+        if (q.len <= kChunk) load(0, q.len);
+        __syncthreads();
+#pragma unroll 1
+        for (int pass = 0; pass < kSelectPasses; ++pass) {
+            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+            const uint32_t found = pass == 0 ? 0u : pass == 1 ? ~0u << 21 : ~0u << 10, digits = pass == 2 ? 1023u : 2047u;
+            int* bins = lds.bins[pass];
+            for (int s0 = 0; s0 < q.len; s0 += kChunk) {
+                const int end = min(q.len, s0 + kChunk);
+                if (q.len > kChunk) load(s0, end);  // (every thread reads back its own)
+                for (int slot = s0 + tid; slot < end; slot += THREADS) {
+                    const uint32_t k = lds.key[slot - s0];
+                    if (((k ^ last) & found) == 0) atomicAdd(&bins[select_bin((k >> shift) & digits)], 1);
+                }
+            }
+            __syncthreads();
+            int sum = 0;
+#pragma unroll 8
+            for (int x = 0; x < 32; ++x) sum += bins[33 * lane + x];
+            const int upto = wave_sums(sum), who = __builtin_ctzl(__builtin_amdgcn_ballot_w64(upto > rank));  // (all keys together are more than `rank`)
+            rank -= __builtin_amdgcn_readlane(upto - sum, who);
+            // the 32 bins of that lane, one to a lane
+            const int own = lane < 32 ? bins[33 * who + lane] : 0, within = wave_sums(own);
+            const int at = __builtin_ctzl(__builtin_amdgcn_ballot_w64(within > rank));
+            last |= (uint32_t)(32 * who + at) << shift;
+            rank -= __builtin_amdgcn_readlane(within - own, at);
+            equal = __builtin_amdgcn_readlane(own, at);
+        }
+    }
+    const int stay_equal = leave > 0 ? equal - (rank + 1) : 0;  // of the tokens with the last key so many stay, in the lowest slots
+    // what stays where it is, is written out; in place, positions of the tokens that had none
+    const bool in_place = q.weight_out == q.weight && q.pos_out == q.pos;
+    const int copied = !in_place ? 0 : q.pos_out ? q.kept : q.n;
+    int equals = 0, free = 0, come = 0;
+    for (int s0 = 0; s0 < q.len; s0 += kChunk) {
+        const int end = min(q.len, s0 + kChunk);
+        if (leave > 0) {
+            if (q.len > kChunk) load(s0, end);
+            if (stay_equal > 0) {  // tokens with the last key that stay get one above all others
+                places(s0, end, [&](int slot) { return lds.key[slot - s0] == last ? 1 : 0; });
+                for (int x = 0; s0 + x * THREADS < end; ++x) {
+                    const int slot = s0 + x * THREADS + tid;
+                    const bool is = slot < end && lds.key[slot - s0] == last;
+                    const int at = equals + lds.table[x * W + w] + __builtin_popcountl(__builtin_amdgcn_ballot_w64(is) & lower);
+                    if (is && at < stay_equal) lds.key[slot - s0] = ~0u;
+                }
+                equals += lds.table[kEntries];
+            }
+            auto goes = [&](int slot) { return lds.key[slot - s0] <= last; };
+            places(s0, end, [&](int slot) { return slot < q.n ? (goes(slot) ? 1 : 0) : goes(slot) ? 0 : 0x10000; });
+            for (int x = 0; s0 + x * THREADS < end; ++x) {
+                const int slot = s0 + x * THREADS + tid;
+                const bool g = slot < end && goes(slot), f = g && slot < q.n, m = slot < end && slot >= q.n && !g;
+                const int at = lds.table[x * W + w];
+                const int fi = free + (at & 0xffff) + __builtin_popcountl(__builtin_amdgcn_ballot_w64(f) & lower);
+                const int mi = come + (at >> 16) + __builtin_popcountl(__builtin_amdgcn_ballot_w64(m) & lower);
+                if (f && fi < e.cap) (e.here ? lds.to : e.to + (long)bk * e.cap)[fi] = slot;
+                if (m && mi < e.cap) (e.here ? lds.from : e.from + (long)bk * e.cap)[mi] = slot;
+            }
+            const int all = lds.table[kEntries];
+            free += all & 0xffff;
+            come += all >> 16;
+        }
+        if (max(s0, copied) < min(end, q.n))
+            each(max(s0, copied), min(end, q.n), [&](int slot, float weight, long at) {
+                if (leave > 0 && lds.key[slot - s0] <= last) return;
+                q.weight_out[slot] = weight;
+                if (q.pos_out) q.pos_out[slot] = (int32_t)at;
+            });
+        if (q.len > kChunk) __syncthreads();  // (the keys of the next slots come)
+    }
+    const int count = min(min(free, come), e.cap);
+    if (e.here) {
+        __syncthreads();
+        evict_rows<U>(e, q, b, h, lds.from, lds.to, count, 0, THREADS / lanes * kMoveRows, THREADS, units, lanes, value_bytes);
+    } else if (tid == 0) {
+        e.count[bk] = count;
+    }
+}
+
+template <typename U>
+__global__ void __launch_bounds__(kThreads) evict_move_kernel(EvictParams e, int blocks, int units, int lanes, int value_bytes) {
+    const int bk = blockIdx.x / blocks, b = bk / e.p.kv_heads, h = bk % e.p.kv_heads, count = e.count[bk], rows = kThreads / lanes * kMoveRows;
+    EvictSequence q;
+    q.init(e, b, h);
+    evict_rows<U>(e, q, b, h, e.from + (long)bk * e.cap, e.to + (long)bk * e.cap, count, blockIdx.x % blocks * rows, blocks * rows, kThreads, units, lanes, value_bytes);
 }
 
 // f(a value of the unit's type)
@@ -296,14 +370,24 @@ hipError_t launch_tree_commit(int row_bytes, int unit, const WinParams& p, const
 hipError_t launch_evict(int row_bytes, int unit, const EvictParams& e, hipStream_t stream) {
     const int units = row_bytes / unit, lanes = lanes_of(units), bk = e.p.batch * e.p.kv_heads;
     if (row_bytes % unit || lanes > kThreads) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)bk), dim3(kSelectThreads), 0, stream, e);
-    if (e.cap > 0) {
-        const int blocks = evict_blocks(bk, e.cap, kThreads / lanes * kMoveRows);
-        with_unit(unit, [&](auto u) {
-            hipLaunchKernelGGL(evict_move_kernel<decltype(u)>, dim3((unsigned)(bk * blocks)), dim3(kThreads), 0, stream, e, blocks, units, lanes, row_bytes / e.p.d);
-        });
-    }
-    return hipGetLastError();
+    hipError_t error = hipSuccess;
+    with_unit(unit, [&](auto u) {
+        typedef decltype(u) U;
+        auto select = [&](auto threads) {
+            constexpr int T = decltype(threads)::value;
+            error = allow_lds(evict_select_kernel<U, T>, sizeof(SelectLds<T>));
+            if (error == hipSuccess)
+                hipLaunchKernelGGL((evict_select_kernel<U, T>), dim3((unsigned)bk), dim3(T), sizeof(SelectLds<T>), stream, e, units, lanes, row_bytes / e.p.d);
+        };
+        if (e.p.max_len <= kSelectItems * 256) select(std::integral_constant<int, 256>{});
+        else select(std::integral_constant<int, 1024>{});
+        if (error != hipSuccess) return;
+        if (e.cap > 0 && !e.here) {
+            const int blocks = evict_blocks(bk, e.cap, kThreads / lanes * kMoveRows);
+            hipLaunchKernelGGL(evict_move_kernel<U>, dim3((unsigned)(bk * blocks)), dim3(kThreads), 0, stream, e, blocks, units, lanes, row_bytes / e.p.d);
+        }
+    });
+    return error != hipSuccess ? error : hipGetLastError();
 }
 
 }  // namespace attn

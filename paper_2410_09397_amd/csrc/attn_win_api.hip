@@ -525,6 +525,7 @@ attn_status attn_cache_evict(const attn_paged_desc* desc, const attn_cache* cach
     e.first = v.first;
     e.recent = v.recent;
     e.cap = evict_cap(desc, v.budget);
+    e.here = e.cap <= attn::kEvictHere;
     e.weight = v.weight;
     e.pos = v.pos;
     e.kept = v.kept;

@@ -168,6 +168,7 @@ inline WeighPlan weigh_plan(bool wide, int batch, int heads, int kv_heads, int m
     return p;
 }
 
+constexpr int kEvictHere = 64;  // moves that the workgroup that chooses them makes itself
 // Workgroups that move a (sequence, key head)'s kept tokens, `rows` at a time, of which there are at most `cap`.
 inline int evict_blocks(int64_t bk, int64_t cap, int64_t rows) {
     return (int)std::max<int64_t>(1, std::min((cap + rows - 1) / rows, std::min<int64_t>(1024, kMostGroups / std::max<int64_t>(1, bk))));

@@ -234,6 +234,7 @@ hipError_t launch_weigh_plain(bool is_bf16, bool fp8, const WeighParams& w, hipS
 struct EvictParams {
     WinParams p;
     int budget, first, recent, cap;  // cap: most tokens that move
+    int here;                        // they are few enough for the workgroup that chooses them to move them
     const float* weight;
     const int32_t *pos, *kept, *seen;
     float* weight_out;
