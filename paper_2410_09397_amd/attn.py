@@ -801,13 +801,18 @@ def attn_cache_evict(weight, K_pages, V_pages, table, lens, budget, first=0, rec
         if strides != [to_b, to_h]:
             raise ValueError("%s: what weight and pos come out in must share strides" % name)
     lens_to = _int32("the new lengths", new_lens, batch, device)
+    where = size = 0
     if workspace is None:
-        workspace = _scratch(max(attn_evict_workspace_bytes(desc, budget), 256), device, stream)
+        size = attn_evict_workspace_bytes(desc, budget)
+        if size > 256:  # (256: nothing is kept there)
+            workspace = _scratch(size, device, stream)
     else:
         _check_workspace(workspace, device)
+    if workspace is not None:
+        where, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     args = _EVICTION.pack(budget, first, recent, 0, at, pos_at, _int32("kept", kept, batch, device) or 0, _int32("seen", seen, batch, device) or 0,
                           to, pos_to, lens_to, at_b, at_h, to_b, to_h)
-    st = lib().attn_cache_evict(desc, cache, args, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream))
+    st = lib().attn_cache_evict(desc, cache, args, where, size, _stream(stream))
     if st != ATTN_OK:
         raise AttnError(st, name)
     return out

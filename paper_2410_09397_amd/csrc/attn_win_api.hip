@@ -493,7 +493,8 @@ size_t attn_evict_workspace_bytes(const attn_paged_desc* desc, int32_t budget) {
     if (check_evict(desc, budget) != ATTN_OK) return 0;
     if (no_cache(desc)) return 256;
     const size_t bk = (size_t)desc->batch * desc->kv_heads;
-    return std::max<size_t>(256, sizeof(int32_t) * bk * (1 + 2 * (size_t)evict_cap(desc, budget)));
+    const size_t cap = (size_t)evict_cap(desc, budget);
+    return cap <= attn::kEvictHere ? 256 : sizeof(int32_t) * bk * (1 + 2 * cap);
 }
 
 attn_status attn_cache_evict(const attn_paged_desc* desc, const attn_cache* cache, const attn_eviction* eviction, void* workspace,
@@ -517,7 +518,8 @@ attn_status attn_cache_evict(const attn_paged_desc* desc, const attn_cache* cach
     const size_t lens_bytes = sizeof(int32_t) * (size_t)desc->batch;
     for (const int32_t* in : {cache->lens, v.kept, v.seen})
         if (in && overlap(v.new_lens, lens_bytes, in, lens_bytes)) return ATTN_ERR_INVALID_ARG;
-    if (!workspace || workspace_bytes < attn_evict_workspace_bytes(desc, v.budget) || !aligned16(workspace)) return ATTN_ERR_WORKSPACE;
+    const bool here = evict_cap(desc, v.budget) <= attn::kEvictHere;
+    if (!here && (!workspace || workspace_bytes < attn_evict_workspace_bytes(desc, v.budget) || !aligned16(workspace))) return ATTN_ERR_WORKSPACE;
     attn::EvictParams e;
     std::memset(&e, 0, sizeof(e));
     e.p = paged_params(&rest, cache);
@@ -525,7 +527,7 @@ attn_status attn_cache_evict(const attn_paged_desc* desc, const attn_cache* cach
     e.first = v.first;
     e.recent = v.recent;
     e.cap = evict_cap(desc, v.budget);
-    e.here = e.cap <= attn::kEvictHere;
+    e.here = here;
     e.weight = v.weight;
     e.pos = v.pos;
     e.kept = v.kept;

@@ -238,7 +238,7 @@ __device__ __forceinline__ void win_out(const WinParams& p, int row_blocks) {
     Sight<64, TREE> see;
     see.init(p, s, t, win_token(p, w0), win_token(p, w1), win_token(p, r0), win_token(p, min(r0 + BR - 1, rows - 1)));
     const auto& tiles = see.tiles;
-    const int it0 = at.first(p), it1 = at.last(p, tiles.count);
+    const int it0 = at.first(p, tiles.count), it1 = at.last(p, tiles.count);
 
     TileFeed<D, SRC, PAD> feed;
     feed.init(p, tid);
@@ -479,7 +479,7 @@ __device__ __forceinline__ void win_few(const WinParams& p) {
     Sight<32, TREE> see;
     see.init(p, s, t, t_lo, t_hi, t_lo, t_hi);
     const auto& tiles = see.tiles;
-    const int it0 = at.first(p), it1 = at.last(p, tiles.count);
+    const int it0 = at.first(p, tiles.count), it1 = at.last(p, tiles.count);
 
     bf16x8 qf[KS];
     const char* q = reinterpret_cast<const char*>(static_cast<const __bf16*>(p.Q) + s.q_base + (long)head * p.q_h + (long)t * p.q_n);
@@ -619,7 +619,7 @@ __device__ __forceinline__ void win_one(const WinParams& p) {
     Sight<32, TREE> see;
     see.init(p, s, t, t_lo, t_hi, t_lo, t_hi);
     const auto& tiles = see.tiles;
-    const int it0 = at.first(p), it1 = at.last(p, tiles.count);
+    const int it0 = at.first(p, tiles.count), it1 = at.last(p, tiles.count);
 
     PageWindow pages;
     pages.init();

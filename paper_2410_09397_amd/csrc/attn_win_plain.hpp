@@ -281,7 +281,7 @@ __device__ __forceinline__ void win_plain_out(const WinParams& p, int row_blocks
     Sight<32, TREE> see;
     see.init(p, s, at.t, t_lo, t_hi, t_lo, t_hi);
     const auto& tiles = see.tiles;
-    const int it0 = share.first(p), it1 = share.last(p, tiles.count);
+    const int it0 = share.first(p, tiles.count), it1 = share.last(p, tiles.count);
 
     RowOperand<T, DP> q;
     q.init(static_cast<const T*>(p.Q) + s.q_base + (long)at.head * p.q_h + (long)at.t * p.q_n, p.d, h);

@@ -117,7 +117,8 @@ inline int tree_rows(bool wide, int batch, int heads, int kv_heads, int total_q,
 }
 // How a call on trees is shared out (see TreeItems): a part is `least` tiles, or as many as make `places` of all (0: nothing is shared out, and there are no sums to
 // join).  grid: workgroups, each of which has a block of sums if there are any to join.
-// Where row blocks alone are more than the chip's places, parts come in two rounds, so that the last ones are short.  us: parts of at least 4 tiles of 64 keys / of 8, one sequence of
+// Where the row blocks leave places free, parts are sized to fill them once (a round and a half, two, three: 16 sequences with 64 drafted 81 -> 89, 87, 96 us, one of 65536 tokens
+// 106 -> 128, 124, 121). Where row blocks alone are more than the chip's places, parts come in two rounds, so that the last ones are short.  us: parts of at least 4 tiles of 64 keys / of 8, one sequence of
 // 1000 tokens with 64 drafted 25.8 / 30.6, 8 sequences of 500 to 4000 with 30 38.5 / 40.8; at least 16 tiles of 32 keys, of four waves / 32, 16 sequences with 8 drafted 44.8 /
 // 47.2; two rounds / one / four, 64 sequences of 100 to 2000 tokens with 40 drafted 135 / 140 / 139.
 constexpr int64_t kTreeLeast = 4, kTreeLeastFew = 16, kTreeRounds = 2;

@@ -229,9 +229,10 @@ struct TreeItems {
         }
         chunk = max(p.least, (int)fminf(ceilf((float)sum / (float)p.places), 1e9f));
     }
-    // the sequence that item idx belongs to (-1: there is none) and the number of its first item
-    __device__ __forceinline__ int find(const WinParams& p, int idx, int lane, int& start, int& blocks) const {
+    // the sequence that item idx belongs to (-1: there is none), the number of its first item, its row blocks and parts
+    __device__ __forceinline__ int find(const WinParams& p, int idx, int lane, int& start, int& blocks, int& of_parts) const {
         start = 0;
+        of_parts = 1;
         for (int base = 0; base < p.batch; base += 64) {
             const Sequence s = sequence(p, base + lane);
             const int own = s.blocks * parts(s.tiles);
@@ -244,6 +245,7 @@ struct TreeItems {
             if (who) {
                 const int first = __builtin_ctzl(who);
                 blocks = __builtin_amdgcn_readlane(s.blocks, first);
+                of_parts = __builtin_amdgcn_readlane(parts(s.tiles), first);
                 start += __builtin_amdgcn_readlane(upto - own, first);
                 return base + first;
             }
@@ -292,30 +294,30 @@ struct Share {
         blk = at.blk;
         any = at.any;
     }
-    __device__ __forceinline__ int first(const WinParams& p) const { return blockIdx.y * p.chunk; }
-    __device__ __forceinline__ int last(const WinParams& p, int tiles) const { return (int)min((long)tiles, (long)first(p) + p.chunk); }
+    __device__ __forceinline__ int first(const WinParams& p, int) const { return blockIdx.y * p.chunk; }
+    __device__ __forceinline__ int last(const WinParams& p, int tiles) const { return (int)min((long)tiles, (long)first(p, tiles) + p.chunk); }
     __device__ __forceinline__ bool whole(const WinParams& p, int) const { return p.splits <= 1; }
     // where its sums lie among the parts: token_row = row of Q times heads + head, row = row of the block
     __device__ __forceinline__ long sums(const WinParams& p, long token_row, int) const { return token_row * p.splits + blockIdx.y; }
 };
 template <int BR, int BC>
 struct Share<BR, BC, true> {
-    int b, blk, part, chunk;
+    int b, blk, part, parts;
     bool any;
     __device__ __forceinline__ void init(const WinParams& p, int idx, int lane) {
         TreeItems<BR, BC> items;
         items.init(p, lane);
         int start, blocks = 1;
-        b = items.find(p, idx, lane, start, blocks);
+        b = items.find(p, idx, lane, start, blocks, parts);
         any = b >= 0;
         b = max(b, 0);
         part = any ? (idx - start) / blocks : 0;
         blk = any ? idx - start - part * blocks : 0;
-        chunk = items.chunk;
     }
-    __device__ __forceinline__ int first(const WinParams&) const { return (int)min((long)part * chunk, 0x7fffffffl); }
-    __device__ __forceinline__ int last(const WinParams& p, int tiles) const { return (int)min((long)tiles, (long)first(p) + chunk); }
-    __device__ __forceinline__ bool whole(const WinParams&, int tiles) const { return tiles <= chunk; }
+    // (the parts of a sequence are as long as one another)
+    __device__ __forceinline__ int first(const WinParams&, int tiles) const { return (int)((unsigned long)tiles * (unsigned)part / (unsigned)parts); }
+    __device__ __forceinline__ int last(const WinParams&, int tiles) const { return (int)((unsigned long)tiles * (unsigned)(part + 1) / (unsigned)parts); }
+    __device__ __forceinline__ bool whole(const WinParams&, int) const { return parts <= 1; }
     __device__ __forceinline__ long sums(const WinParams&, long, int row) const { return (long)blockIdx.x * BR + row; }
 };
 

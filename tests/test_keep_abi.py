@@ -140,10 +140,13 @@ def test_bad_evictions(kw):
 
 def test_evict_workspace():
     L, d = attn.lib(), paged()
-    need = L.attn_evict_workspace_bytes(ctypes.byref(d), 50)
-    assert need >= 2 * 2 * 2 * 50 * 4  # 50 of 100 tokens may move, from and to, for two key heads of two sequences
+    assert L.attn_evict_workspace_bytes(ctypes.byref(d), 50) == 256  # 50 tokens move without one
+    long = paged(max_len=400, max_pages=30, table_stride=30)
+    need = L.attn_evict_workspace_bytes(ctypes.byref(long), 200)
+    assert need >= 2 * 2 * 2 * 200 * 4  # 200 of 400 tokens may move, from and to, for two key heads of two sequences
+    slots = eviction(budget=200, stride_b=1000, stride_h=400, out_stride_b=1000, out_stride_h=400)
     for ws, size in ((None, need), (P, need - 1), (P + 4, need)):
-        assert evict(d, ws=ws, size=size) == WORKSPACE
+        assert evict(long, e=slots, ws=ws, size=size) == WORKSPACE
     assert L.attn_evict_workspace_bytes(ctypes.byref(d), 0) == 0 and L.attn_evict_workspace_bytes(None, 5) == 0
     assert L.attn_evict_workspace_bytes(ctypes.byref(d), 100) == 256 and L.attn_evict_workspace_bytes(ctypes.byref(d), 2 ** 31 - 1) == 256
     for kw in (dict(batch=0), dict(heads=0, kv_heads=0), dict(max_len=0)):
