@@ -41,29 +41,30 @@ __device__ __forceinline__ void weigh_store(const WeighParams& w, const WinSeq& 
     w.out[(long)b * w.out_b + (long)kvh * w.out_h + j] = v;
 }
 
-// Which keys a workgroup takes: chunk `part` of a sequence.  The chunks of all sequences are counted 64 sequences at a time, so that those of short ones leave no workgroups idle
-// among those of long ones; what the host has launched too many lies at the end.
+// Which keys a workgroup takes: chunk `part` of a sequence.  The chunks of all sequences are counted, so that those of short ones leave no workgroups idle
+// among those of long ones; what the host has launched too many lies at the end.  (More than 64 sequences fill the chip whatever their lengths are, and each has w.blocks.)
 struct WeighShare {
     int b, part;
     bool any;
-    __device__ __forceinline__ void init(const WinParams& p, int idx, int chunk, int lane) {
+    __device__ __forceinline__ void init(const WinParams& p, int idx, int chunk, int blocks, int lane) {
+        if (p.batch > 64) {
+            b = idx / blocks;
+            part = idx - b * blocks;
+            any = part * (long)chunk < min(max(p.lens[b], 0), p.max_len);
+            return;
+        }
         any = true;
-        for (int base = 0; base < p.batch; base += 64) {
-            const int mine = base + lane, n = min(64, p.batch - base);
-            const int own = mine < p.batch ? (min(max(p.lens[mine], 0), p.max_len) + chunk - 1) / chunk : 0;
-            int upto = own;
-            for (int x = 1; x < n; x <<= 1) {
-                const int before = __shfl_up(upto, x, 64);
-                upto += lane >= x ? before : 0;
-            }
-            const unsigned long who = __builtin_amdgcn_ballot_w64(mine < p.batch && upto > idx);
-            if (who) {
-                const int first = __builtin_ctzl(who);
-                b = base + first;
-                part = idx - __builtin_amdgcn_readlane(upto - own, first);
-                return;
-            }
-            idx -= __builtin_amdgcn_readlane(upto, n - 1);
+        const int own = lane < p.batch ? (min(max(p.lens[lane], 0), p.max_len) + chunk - 1) / chunk : 0;
+        int upto = own;
+        for (int x = 1; x < p.batch; x <<= 1) {
+            const int before = __shfl_up(upto, x, 64);
+            upto += lane >= x ? before : 0;
+        }
+        const unsigned long who = __builtin_amdgcn_ballot_w64(lane < p.batch && upto > idx);
+        if (who) {
+            b = __builtin_ctzl(who);
+            part = idx - __builtin_amdgcn_readlane(upto - own, b);
+            return;
         }
         any = false;
         b = part = 0;
@@ -118,7 +119,7 @@ __global__ void __launch_bounds__(kThreads) weigh_one_kernel(WeighParams w) {
     const int lane = threadIdx.x & 63, q = lane >> 4, l16 = lane & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kvh = blockIdx.x % p.kv_heads;
     WeighShare share;
-    share.init(p, blockIdx.x / p.kv_heads, w.chunk, lane);
+    share.init(p, blockIdx.x / p.kv_heads, w.chunk, w.blocks, lane);
     if (!share.any) return;
     const int b = share.b;
     const WinSeq s = win_sequence(p, b);
@@ -369,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, 2) weigh_few_kernel(WeighParams w) {
     const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int kvh = blockIdx.x % p.kv_heads;
     WeighShare share;
-    share.init(p, blockIdx.x / p.kv_heads, w.chunk, lane);
+    share.init(p, blockIdx.x / p.kv_heads, w.chunk, w.blocks, lane);
     if (!share.any) return;
     const int b = share.b;
     const WinSeq s = win_sequence(p, b);

@@ -233,6 +233,11 @@ struct TreeItems {
     __device__ __forceinline__ int find(const WinParams& p, int idx, int lane, int& start, int& blocks, int& of_parts) const {
         start = 0;
         of_parts = 1;
+        if (p.places == 0 && (!p.q_ptr || p.row_blocks == 1)) {  // (every sequence has as many workgroups: batches of thousands are not searched)
+            blocks = p.row_blocks;
+            start = idx / blocks * blocks;
+            return idx < p.batch * blocks ? idx / blocks : -1;
+        }
         for (int base = 0; base < p.batch; base += 64) {
             const Sequence s = sequence(p, base + lane);
             const int own = s.blocks * parts(s.tiles);

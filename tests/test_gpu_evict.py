@@ -110,6 +110,15 @@ def test_weights_of_random_sizes(seed):
         _weigh_case(*case, seed=seed, layout=rng.choice(["phnd", "pnhd"]), old=rng.random() < 0.5, scale=rng.choice([None, None, -0.1, 0.0]))
 
 
+@pytest.mark.parametrize("kind,d", [("fp8", 128), ("plain", 40)])
+def test_weights_of_more_than_64_sequences(kind, d):
+    print("case weigh many sequences", kind, d, flush=True)
+    lens = [(37 * i) % 700 for i in range(90)]
+    _weigh_case("bf16", kind, lens, [min(l, 1) for l in lens], 4, 2, d, 16)
+    _weigh_case("bf16", kind, lens, [min(l, (0, 20, 3)[i % 3]) for i, l in enumerate(lens)], 4, 2, d, 16)
+    _weigh_case("bf16", kind, lens, [min(l, (0, 200, 3)[i % 3]) for i, l in enumerate(lens)], 4, 2, d, 16)
+
+
 def test_a_tight_bound_on_the_lengths_and_a_cut_number_of_new_tokens():
     print("case weigh bounds", flush=True)
     _weigh_case("bf16", "plain", [300, 77, 1000], [30, 7, 100], 4, 2, 128, 16, max_len=1000)

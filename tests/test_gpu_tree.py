@@ -148,6 +148,18 @@ def test_token_major_pages_and_a_tight_bound_on_the_lengths(kind):
         _case("bf16", kind, [300, 77, 1000], [3, 20, 40], 4, 2, d, 16, layout="pnhd", max_len=1000)
 
 
+def test_batches_of_more_than_64_sequences():
+    """Sequences are counted 64 at a time; some have no drafted token, and where there are many the work is not shared out."""
+    print("case tree many sequences", flush=True)
+    lens = [1 + (37 * i) % 300 for i in range(150)]
+    new = [min(l, (0, 1, 0, 3, 40, 1)[i % 6]) for i, l in enumerate(lens)]
+    _case("bf16", "fp8", lens, new, 4, 1, 64, 16)
+    _case("bf16", "plain", [l + 2000 for l in lens], new, 4, 1, 64, 16, window=50, sinks=3)
+    _case("bf16", "plain", [l + 1500 for l in lens], [2] * 150, 4, 1, 128, 16)
+    _case("bf16", "plain", [40 + (37 * i) % 100 for i in range(1100)], [(0, 2, 20)[i % 3] for i in range(1100)], 8, 4, 64, 16)
+    _case("f32", "plain", [40 + (37 * i) % 100 for i in range(1100)], [(0, 2)[i % 2] for i in range(1100)], 8, 4, 24, 16)
+
+
 def test_a_chain_sees_what_new_tokens_in_order_see():
     """attn_tree_fwd with the mask of a chain against attn_paged_fwd: both within their bounds of the same values."""
     import torch
