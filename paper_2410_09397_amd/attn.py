@@ -612,13 +612,19 @@ def attn_paged_fwd(Q, K_pages, V_pages, table, lens, scale, q_ptr=None, max_q=No
 
 
 # ------------------------------------------------------------------------- what stays in the cache: trees, eviction
-def _on_current(device):
-    """Streams and launches are the current device's (a kernel given addresses of another one would fault)."""
+def _stream_on(device, stream):
+    """The handle of the stream to launch on: the current one of the tensors' device, which has to be the current device (launches and allocations are
+    that one's), or the one that is given, of the same device."""
     import torch
     if device.type != "cuda":
         raise ValueError("expected tensors on a GPU, got %s" % device)
-    if device.index != torch.cuda.current_device():
-        raise ValueError("expected tensors on the current GPU (%d), got %s" % (torch.cuda.current_device(), device))
+    here = torch.cuda.current_device()
+    if device.index != here or (stream is not None and stream.device_index != here):
+        raise ValueError("expected tensors, and a stream, of the current GPU (%d), got tensors on %s" % (here, device))
+    if stream is not None:
+        return stream.cuda_stream
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # (as _stream)
+    return raw(here) if raw is not None else torch.cuda.current_stream().cuda_stream
 
 
 def _cache_only(name, total, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp):
@@ -628,9 +634,7 @@ def _cache_only(name, total, K_pages, V_pages, table, lens, q_ptr, max_q, max_le
         raise ValueError("%s: expected pages [num_pages, kv_heads, page_size, d] and a table [batch, pages]" % name)
     kvh, d = K_pages.shape[1], K_pages.shape[3]
     dtype = torch.bfloat16 if K_pages.dtype is torch.float8_e4m3fn else K_pages.dtype
-    out = _on_pages(name, total, kvh, kvh * d, d, dtype, K_pages.device, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp)
-    _on_current(K_pages.device)
-    return out
+    return _on_pages(name, total, kvh, kvh * d, d, dtype, K_pages.device, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp)
 
 
 def _check_mask(name, mask, total, max_q, device):
@@ -662,11 +666,11 @@ def attn_tree_mask(parents, max_q, q_ptr=None, stream=None, out=None):
     if q_ptr is None and (total % max_q if max_q else total):
         raise ValueError("attn_tree_mask: without q_ptr every sequence has max_q rows")
     batch = q_ptr.shape[0] - 1 if q_ptr is not None else total // max_q if max_q else 0
-    _on_current(device)
+    on = _stream_on(device, stream)
     parents_at, q_ptr_at = _int32("parents", parents, total, device), _int32("q_ptr", q_ptr, batch + 1, device)
     if out is None:
         out = _made_on(stream, lambda: torch.empty((total, words), dtype=torch.int32, device=device))
-    st = lib().attn_tree_mask(batch, total, max_q, q_ptr_at, parents_at, *_check_mask("attn_tree_mask", out, total, max_q, device), _stream(stream))
+    st = lib().attn_tree_mask(batch, total, max_q, q_ptr_at, parents_at, *_check_mask("attn_tree_mask", out, total, max_q, device), on)
     if st != ATTN_OK:
         raise AttnError(st, "attn_tree_mask")
     return out
@@ -681,7 +685,7 @@ def attn_tree_fwd(Q, mask, K_pages, V_pages, table, lens, scale, q_ptr=None, max
     """attn_paged_fwd for new tokens that are a tree of drafted ones: each sees the context and the new tokens of its row of the mask
     (attn_tree_mask's, or any bits).  O [total, heads, d], LSE [total, heads]."""
     desc, cache = _paged("attn_tree_fwd", Q, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp, False, scale, window, sinks)
-    _on_current(Q.device)
+    on = _stream_on(Q.device, stream)
     bits = _check_mask("attn_tree_fwd", mask, Q.shape[0], _max_q("attn_tree_fwd", Q.shape[0], table.shape[0], q_ptr, max_q), Q.device)
     if out is None:
         import torch
@@ -699,7 +703,7 @@ def attn_tree_fwd(Q, mask, K_pages, V_pages, table, lens, scale, q_ptr=None, max
         _check_workspace(workspace, Q.device)
     if workspace is not None:
         where, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    st = lib().attn_tree_fwd(desc, cache, *bits, Q.data_ptr(), O.data_ptr(), LSE.data_ptr(), where, size, _stream(stream))
+    st = lib().attn_tree_fwd(desc, cache, *bits, Q.data_ptr(), O.data_ptr(), LSE.data_ptr(), where, size, on)
     if st != ATTN_OK:
         raise AttnError(st, "attn_tree_fwd")
     return O, LSE
@@ -711,6 +715,7 @@ def attn_tree_commit(mask, leaf, K_pages, V_pages, table, lens, q_ptr=None, max_
     import torch
     total, device, batch = mask.shape[0], K_pages.device, table.shape[0]
     desc, cache = _cache_only("attn_tree_commit", total, K_pages, V_pages, table, lens, q_ptr, max_q, None, K_exp, V_exp)
+    on = _stream_on(device, stream)
     bits = _check_mask("attn_tree_commit", mask, total, _max_q("attn_tree_commit", total, batch, q_ptr, max_q), device)
     leaf_at = _int32("leaf", leaf, batch, device)
     if leaf_at is None:
@@ -720,7 +725,7 @@ def attn_tree_commit(mask, leaf, K_pages, V_pages, table, lens, q_ptr=None, max_
         out = _made_on(stream, lambda: lens.clone() if nothing else torch.empty_like(lens))
     elif nothing:
         _made_on(stream, lambda: out.copy_(lens))
-    st = lib().attn_tree_commit(desc, cache, *bits, leaf_at, _int32("out", out, batch, device), _stream(stream))
+    st = lib().attn_tree_commit(desc, cache, *bits, leaf_at, _int32("out", out, batch, device), on)
     if st != ATTN_OK:
         raise AttnError(st, "attn_tree_commit")
     return out
@@ -743,7 +748,7 @@ def attn_cache_weigh(Q, LSE, K_pages, V_pages, table, lens, scale, weight=None, 
     import torch
     desc, cache = _paged("attn_cache_weigh", Q, K_pages, V_pages, table, lens, q_ptr, max_q, max_len, K_exp, V_exp, False, scale, window, sinks)
     device, batch, kvh = Q.device, table.shape[0], K_pages.shape[1]
-    _on_current(device)
+    on = _stream_on(device, stream)
     _check_lse(LSE, Q)
     slots = table.shape[1] * K_pages.shape[2] if max_len is None else max_len
     if out is None:
@@ -759,8 +764,7 @@ def attn_cache_weigh(Q, LSE, K_pages, V_pages, table, lens, scale, weight=None, 
         _check_workspace(workspace, device)
     if workspace is not None:
         where, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    st = lib().attn_cache_weigh(desc, cache, Q.data_ptr(), LSE.data_ptr(), _WEIGHTS.pack(at, to, at_b, at_h, to_b, to_h, decay, 0), where, size,
-                                _stream(stream))
+    st = lib().attn_cache_weigh(desc, cache, Q.data_ptr(), LSE.data_ptr(), _WEIGHTS.pack(at, to, at_b, at_h, to_b, to_h, decay, 0), where, size, on)
     if st != ATTN_OK:
         raise AttnError(st, "attn_cache_weigh")
     return out
@@ -784,6 +788,7 @@ def attn_cache_evict(weight, K_pages, V_pages, table, lens, budget, first=0, rec
     import torch
     name, device, batch, kvh = "attn_cache_evict", K_pages.device, table.shape[0], K_pages.shape[1]
     desc, cache = _cache_only(name, 0, K_pages, V_pages, table, lens, None, 0, max_len, K_exp, V_exp)
+    on = _stream_on(device, stream)
     slots = table.shape[1] * K_pages.shape[2] if max_len is None else max_len
     if out is None:
         nothing = kvh == 0 or slots == 0  # nothing is launched
@@ -801,6 +806,8 @@ def attn_cache_evict(weight, K_pages, V_pages, table, lens, budget, first=0, rec
         if strides != [to_b, to_h]:
             raise ValueError("%s: what weight and pos come out in must share strides" % name)
     lens_to = _int32("the new lengths", new_lens, batch, device)
+    if lens_to is None:
+        raise ValueError("%s: out must have a place for the new lengths" % name)
     where = size = 0
     if workspace is None:
         size = attn_evict_workspace_bytes(desc, budget)
@@ -812,7 +819,7 @@ def attn_cache_evict(weight, K_pages, V_pages, table, lens, budget, first=0, rec
         where, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     args = _EVICTION.pack(budget, first, recent, 0, at, pos_at, _int32("kept", kept, batch, device) or 0, _int32("seen", seen, batch, device) or 0,
                           to, pos_to, lens_to, at_b, at_h, to_b, to_h)
-    st = lib().attn_cache_evict(desc, cache, args, where, size, _stream(stream))
+    st = lib().attn_cache_evict(desc, cache, args, where, size, on)
     if st != ATTN_OK:
         raise AttnError(st, name)
     return out

@@ -17,8 +17,9 @@ template <int D, int SRC, bool PAD>
 __global__ void __launch_bounds__((64 * kFewWaves<D, SRC>), (D == 256 ? 1 : 2)) tree_few_kernel(WinParams p) {
     win_few<D, SRC, PAD, true>(p);
 }
+// (padded rows of 65 to 127 columns: the masks' registers do not fit beside the tile's with three workgroups on a CU)
 template <int D, int SRC, bool PAD>
-__global__ void __launch_bounds__(kThreads, (kOnePerCu<D, SRC>)) tree_one_kernel(WinParams p) {
+__global__ void __launch_bounds__(kThreads, (D == 128 && PAD ? 2 : kOnePerCu<D, SRC>)) tree_one_kernel(WinParams p) {
     win_one<D, SRC, PAD, true>(p);
 }
 

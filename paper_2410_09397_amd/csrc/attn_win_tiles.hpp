@@ -146,13 +146,18 @@ struct Sight<BC, true> {
         }
         __device__ __forceinline__ bool whole(const WinParams& p, int j0) const { return j0 + BC <= end && (j0 >= lo || j0 + BC <= p.sinks); }
     } tiles;
-    const uint32_t* mask;  // of the lane's query
-    int seen, lo;          // under a window: drafted tokens that it sees, and the first key of the context in its window
+    int row, lo;  // of the lane's query: its row of the mask, and under a window the first key of the context that is in it
     int first, nq;
+    // x, in a way that what is made of it is made where it stands: kept over the loop, it costs registers that the kernels of single tokens do not have
+    static __device__ __forceinline__ int here(int x) {
+        asm volatile("" : "+v"(x));
+        return x;
+    }
     static __device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; }
     // bits u .. u + 31 of the mask; tokens in front of slot 0 and behind the last one are none
     __device__ __forceinline__ uint32_t drafted(const WinParams& p, int u) const {
         const int w = u >> 5, words = (p.n + 31) >> 5;
+        const uint32_t* mask = p.tree + (long)here(row) * p.tree_stride;
         const uint32_t a = w < words ? mask[w] : 0u, b = (u & 31) && w + 1 < words ? mask[w + 1] : 0u;
         return (uint32_t)((((uint64_t)b << 32) | a) >> (u & 31)) & below(nq - u) & ~below(-first - u);
     }
@@ -160,8 +165,8 @@ struct Sight<BC, true> {
         tiles.init(p, s);
         first = s.first;
         nq = s.nq;
-        mask = p.tree + (s.row0 + t) * p.tree_stride;
-        seen = 0;
+        row = (int)s.row0 + t;
+        int seen = 0;  // drafted tokens
         if (p.window < kNoWindow) {
             for (int u = 0; u < nq; u += 32) seen += __popc(drafted(p, u));
         }
@@ -176,6 +181,7 @@ struct Sight<BC, true> {
         if (it < tiles.of_context) return below(tiles.context - j) & (~below(lo - j) | below(p.sinks - j));
         uint32_t v = drafted(p, j - first);
         if (p.window < kNoWindow) {  // the r-th drafted token that the query sees is at position context + r
+            const int seen = here(lo) + p.window - tiles.context;
             int r = 0;
             for (int u = 0; u < j - first; u += 32) r += __popc(drafted(p, u) & below(j - first - u));
             uint32_t in = 0;
@@ -316,12 +322,13 @@ struct Share<BR, BC, true> {
         b = items.find(p, idx, lane, start, blocks, parts);
         any = b >= 0;
         b = max(b, 0);
-        part = any ? (idx - start) / blocks : 0;
+        part = any ? __builtin_amdgcn_readfirstlane((idx - start) / blocks) : 0;  // (divisions are vector arithmetic)
         blk = any ? idx - start - part * blocks : 0;
     }
     // (the parts of a sequence are as long as one another)
-    __device__ __forceinline__ int first(const WinParams&, int tiles) const { return (int)((unsigned long)tiles * (unsigned)part / (unsigned)parts); }
-    __device__ __forceinline__ int last(const WinParams&, int tiles) const { return (int)((unsigned long)tiles * (unsigned)(part + 1) / (unsigned)parts); }
+    __device__ __forceinline__ int share(int tiles, int x) const { return __builtin_amdgcn_readfirstlane((int)((unsigned long)tiles * (unsigned)x / (unsigned)parts)); }
+    __device__ __forceinline__ int first(const WinParams&, int tiles) const { return share(tiles, part); }
+    __device__ __forceinline__ int last(const WinParams&, int tiles) const { return share(tiles, part + 1); }
     __device__ __forceinline__ bool whole(const WinParams&, int) const { return parts <= 1; }
     __device__ __forceinline__ long sums(const WinParams&, long, int row) const { return (long)blockIdx.x * BR + row; }
 };
