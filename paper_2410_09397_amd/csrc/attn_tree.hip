@@ -10,14 +10,13 @@ __global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) tree_plain_out_ker
     win_plain_out<T, E, DP, true, true>(p, p.row_blocks);
 }
 
-// The sums of a row's parts, as win_join_kernel, for the parts of TreeItems.  A workgroup takes kJoinRows rows of a row block, so that its sequence, its parts and their
+// The sums of a row's parts, as win_join_kernel, for the parts of TreeItems.  A workgroup takes `many` rows of a row block, so that its sequence, its parts and their
 // places are looked up once for all of them; 16 to 64 lanes have a row.  Row blocks of one part are written where they are worked on.
-constexpr int kJoinRows = 8;
 template <typename T, int BR, int LANES>
-__global__ void __launch_bounds__(kThreads) tree_join_kernel(WinParams p) {
-    constexpr int BC = BR >= 64 ? 64 : 32, kPer = 64 / LANES, kTurns = BR / kJoinRows;
-    const int lane = threadIdx.x & 63, in_row = threadIdx.x & (LANES - 1), idx = blockIdx.x / (p.kv_heads * kTurns);
-    const int kvh = blockIdx.x / kTurns % p.kv_heads, row0 = blockIdx.x % kTurns * kJoinRows;
+__global__ void __launch_bounds__(kThreads) tree_join_kernel(WinParams p, int many) {
+    constexpr int BC = BR >= 64 ? 64 : 32, kPer = 64 / LANES;
+    const int turns = BR / many, lane = threadIdx.x & 63, in_row = threadIdx.x & (LANES - 1), idx = blockIdx.x / (p.kv_heads * turns);
+    const int kvh = blockIdx.x / turns % p.kv_heads, row0 = blockIdx.x % turns * many;
     TreeItems<BR, BC> items;
     items.init(p, lane);
     int start, blocks = 1, parts = 0, blk = 0;
@@ -26,7 +25,7 @@ __global__ void __launch_bounds__(kThreads) tree_join_kernel(WinParams p) {
     const WinSeq s = win_sequence(p, b);
     const int rows = s.nq * p.group;
     const long step = (long)blocks * p.kv_heads * BR, first = ((long)(start + blk) * p.kv_heads + kvh) * BR;  // row x, part k: first + x + k * step
-    for (int x = row0 + (int)threadIdx.x / LANES; x < row0 + kJoinRows; x += kThreads / LANES) {
+    for (int x = row0 + (int)threadIdx.x / LANES; x < row0 + many; x += kThreads / LANES) {
         const int r = blk * BR + x;
         if (r >= rows) break;
         float m_k[kPer], l_k[kPer], m = -__builtin_inff(), l = 0.f;
@@ -119,11 +118,12 @@ hipError_t launch_tree_plain_fwd(bool is_bf16, bool fp8, long grid, const WinPar
     return fwd<float, float>(grid, p, stream);
 }
 hipError_t launch_tree_join(bool is_bf16, int rows, const WinParams& p, hipStream_t stream) {
+    const int many = join_rows((int64_t)p.blocks * p.kv_heads, rows);
     auto with = [&](auto lanes) {
         constexpr int L = decltype(lanes)::value;
         auto fn = !is_bf16 ? tree_join_kernel<float, 32, L> : rows == 16 ? tree_join_kernel<__bf16, 16, L> : rows == 32 ? tree_join_kernel<__bf16, 32, L>
                   : rows == 64 ? tree_join_kernel<__bf16, 64, L> : tree_join_kernel<__bf16, 128, L>;
-        hipLaunchKernelGGL(fn, dim3((unsigned)((long)p.blocks * p.kv_heads * (rows / kJoinRows))), dim3(kThreads), 0, stream, p);
+        hipLaunchKernelGGL(fn, dim3((unsigned)((long)p.blocks * p.kv_heads * (rows / many))), dim3(kThreads), 0, stream, p, many);
     };
     if (p.d <= 64) with(std::integral_constant<int, 16>{});
     else if (p.d <= 128) with(std::integral_constant<int, 32>{});

@@ -141,6 +141,15 @@ inline TreeShares tree_shares(bool wide, int batch, int heads, int kv_heads, int
     return p;
 }
 
+// Rows of a workgroup of the joining launch, out of blocks of `rows`: 8, or as many as leave 2048 workgroups (each looks its sequence up first).  us of a call with
+// 512 / 1024 / 2048 / 4096 / any number of them: 64 sequences with 40 drafted tokens 129 / 130 / 121 / 119 / 139, 16 with 64 84 / 78 / 76 / 80 / 79.
+constexpr int64_t kJoinGroups = 2048;
+inline int join_rows(int64_t blocks, int rows) {
+    int many = 8;
+    while (many < rows && blocks * (rows / many) > kJoinGroups) many *= 2;
+    return many;
+}
+
 // Kernels of attn_cache_weigh by the rows of a (sequence, key head): at most 16, one tile of 128, more of them; any: groups or strides that a tile does not hold (and the
 // kernel of 32-bit arithmetic).  us of a call: one kernel for all, 16 rows at a time -> these, h32 k8 d = 128: newest token of 64 sequences (quantised) 72 -> 31, last 32
 // tokens of 8 prompts 52 -> 18, a prompt of 4096 tokens 1101 -> 101.
