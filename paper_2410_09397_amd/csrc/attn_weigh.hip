@@ -504,44 +504,52 @@ __global__ void __launch_bounds__(kThreads) weigh_join_kernel(WeighParams w, int
     weigh_store(w, s, b, kvh, j, sum);
 }
 
-// 32-bit arithmetic: 32x32x2 products of 32 keys on a wave, rows 32 at a time, both straight from memory.
-template <typename T, typename E, int DP>
+// 32-bit arithmetic: 32x32x2 products of 32 keys and 32 rows, both straight from memory.  At most 32 rows: every wave has keys of its own.  More (SHARED): the four waves have the
+// same keys and take the rows in turn, and their sums meet in LDS (a tile of rows is 64 cycles for every two columns, and a small model has few keys to fill the chip with: 50 new
+// tokens of 3 sequences, h6 k2 d = 80, 16.6 us with keys to each wave, 9.0 so).
+template <typename T, typename E, int DP, bool SHARED>
 __global__ void __launch_bounds__(kThreads, 1) weigh_plain_kernel(WeighParams w) {
     const WinParams& p = w.p;
+    __shared__ float meet[4][32];
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int blk = blockIdx.x % w.blocks, bk = blockIdx.x / w.blocks, b = bk / p.kv_heads, kvh = bk % p.kv_heads;
     const WinSeq s = win_sequence(p, b);
-    const int rows = s.nq * p.group, end = min(s.len, (blk + 1) * w.chunk);
-    for (int j0 = blk * w.chunk + 32 * wave; j0 < end; j0 += 128) {
-        const int j = j0 + l32, at_j = min(j, s.len - 1);
-        const PageRow place = win_page_row(p, win_page(p, b, at_j), kvh, at_j);
-        RowOperand<E, DP> key;
-        key.init(static_cast<const E*>(p.K) + place.at, p.d, h);
-        float cs = p.scale * kLog2e;
-        if constexpr (std::is_same_v<E, uint8_t>) cs *= exp_value(p.K_exp[place.exp]);
-        float sum = 0.f;
-        WeighRows<32> range;
-        range.init(p, s, j0, min(j0 + 31, s.len - 1));
-        for (int r0 = range.r0; r0 < range.r1; r0 += 32) {
-            const int x = min(r0 + l32, rows - 1), t = win_token(p, x), head = kvh * p.group + x - t * p.group;
-            TileRow<T, DP> row;
-            row.init(static_cast<const T*>(p.Q) + s.q_base + (long)head * p.q_h + (long)t * p.q_n, p.d, h);
-            WeighRow mine;
-            mine.init(p, s, kvh, r0 + l32, rows);
-            f32x16 st;
+    const int rows = s.nq * p.group, j0 = blk * w.chunk + (SHARED ? 0 : 32 * wave);
+    if (j0 >= s.len) return;  // (SHARED: all waves)
+    const int j = j0 + l32, at_j = min(j, s.len - 1);
+    const PageRow place = win_page_row(p, win_page(p, b, at_j), kvh, at_j);
+    RowOperand<E, DP> key;
+    key.init(static_cast<const E*>(p.K) + place.at, p.d, h);
+    float cs = p.scale * kLog2e;
+    if constexpr (std::is_same_v<E, uint8_t>) cs *= exp_value(p.K_exp[place.exp]);
+    float sum = 0.f;
+    WeighRows<32> range;
+    range.init(p, s, j0, min(j0 + 31, s.len - 1));
+    for (int r0 = range.r0 + (SHARED ? 32 * wave : 0); r0 < range.r1; r0 += SHARED ? 128 : 32) {
+        const int x = min(r0 + l32, rows - 1), t = win_token(p, x), head = kvh * p.group + x - t * p.group;
+        TileRow<T, DP> row;
+        row.init(static_cast<const T*>(p.Q) + s.q_base + (long)head * p.q_h + (long)t * p.q_n, p.d, h);
+        WeighRow mine;
+        mine.init(p, s, kvh, r0 + l32, rows);
+        f32x16 st;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) st[e] = 0.f;
-            scores(st, row, 1.f, key);
+        for (int e = 0; e < 16; ++e) st[e] = 0.f;
+        scores(st, row, 1.f, key);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int i = __shfl(mine.i, acc_row(e, h), 64);
-                const float lse2 = __shfl(mine.lse2, acc_row(e, h), 64);
-                sum += weigh_sees(p, i, j) ? __builtin_amdgcn_exp2f(fmaf(st[e], cs, -lse2)) : 0.f;
-            }
+        for (int e = 0; e < 16; ++e) {
+            const int i = __shfl(mine.i, acc_row(e, h), 64);
+            const float lse2 = __shfl(mine.lse2, acc_row(e, h), 64);
+            sum += weigh_sees(p, i, j) ? __builtin_amdgcn_exp2f(fmaf(st[e], cs, -lse2)) : 0.f;
         }
-        sum += __shfl_xor(sum, 32, 64);
-        if (h == 0) weigh_store(w, s, b, kvh, j, sum);
     }
+    sum += __shfl_xor(sum, 32, 64);
+    if constexpr (SHARED) {
+        if (h == 0) meet[wave][l32] = sum;
+        __syncthreads();
+        if (wave != 0) return;
+        sum = (meet[0][l32] + meet[1][l32]) + (meet[2][l32] + meet[3][l32]);
+    }
+    if (h == 0) weigh_store(w, s, b, kvh, j, sum);
 }
 
 dim3 grid_of(const WeighParams& w) { return dim3((unsigned)((long)w.blocks * w.parts * w.p.batch * w.p.kv_heads)); }
@@ -571,7 +579,9 @@ hipError_t launch(bool fp8, WeighRowsKind kind, const WeighParams& w, hipStream_
 template <typename T, typename E>
 hipError_t plain(const WeighParams& w, hipStream_t stream) {
     return with_width(w.p.d, [&](auto width) {
-        hipLaunchKernelGGL((weigh_plain_kernel<T, E, decltype(width)::value>), grid_of(w), dim3(kThreads), 0, stream, w);
+        constexpr int DP = decltype(width)::value;
+        auto fn = w.chunk == 32 ? weigh_plain_kernel<T, E, DP, true> : weigh_plain_kernel<T, E, DP, false>;
+        hipLaunchKernelGGL(fn, grid_of(w), dim3(kThreads), 0, stream, w);
         return hipGetLastError();
     });
 }

@@ -237,7 +237,7 @@ attn_status check_weigh(const attn_paged_desc* d) {
     const attn_status st = check_paged(d);
     if (st != ATTN_OK || no_cache(d)) return st;
     const int64_t bk = (int64_t)d->batch * d->kv_heads;
-    return bk > kMostGroups || ((int64_t)d->max_len + 63) / 64 * bk > kMostGroups ? ATTN_ERR_UNSUPPORTED : ATTN_OK;
+    return bk > kMostGroups || ((int64_t)d->max_len + 31) / 32 * bk > kMostGroups ? ATTN_ERR_UNSUPPORTED : ATTN_OK;
 }
 attn::WeighPlan weigh_plan(const attn_paged_desc* d) {
     return attn::weigh_plan(is_wide(d), d->batch, d->heads, d->kv_heads, d->max_q, d->max_len, d->q_stride_n, d->q_stride_h);

@@ -168,6 +168,7 @@ inline WeighPlan weigh_plan(bool wide, int batch, int heads, int kv_heads, int m
     const int64_t group = heads / kv_heads, rows = max_q * group, bk = (int64_t)batch * kv_heads;
     const bool tiles = group <= 128 && q_stride_n < (1 << 22) && q_stride_h < (1 << 22);
     WeighPlan p = {rows <= 16 ? kWeighOne : !tiles || !wide ? kWeighAny : rows <= 128 ? kWeighFew : kWeighMany, 0, 128, 1};
+    if (!wide && rows > 32) p.chunk = 32;  // (32-bit arithmetic: see weigh_plain_kernel)
     if (p.kind == kWeighMany) p.chunk = 256;
     else while (wide && p.chunk < 1024 && (max_len + p.chunk * 2 - 1) / (p.chunk * 2) * bk >= kWeighGroups) p.chunk *= 2;
     p.blocks = (max_len + p.chunk - 1) / p.chunk;
