@@ -639,10 +639,11 @@ def _cache_only(name, total, K_pages, V_pages, table, lens, q_ptr, max_q, max_le
 
 def _check_mask(name, mask, total, max_q, device):
     import torch
-    if (mask.dtype is not torch.int32 or mask.dim() != 2 or mask.shape[0] != total or mask.shape[1] * 32 < max_q or mask.device != device or
-            (mask.numel() and mask.stride(1) != 1)):
-        raise ValueError("%s: the mask must be an int32 tensor [total, words] on the rows' device, 32 new tokens to a word, with unit stride along them" % name)
-    return mask.data_ptr(), mask.stride(0)
+    if mask.dtype is torch.int32 and mask.dim() == 2 and mask.device == device:
+        (rows, words), (stride, unit) = mask.shape, mask.stride()
+        if rows == total and words * 32 >= max_q and (unit == 1 or rows * words == 0):
+            return mask.data_ptr(), stride
+    raise ValueError("%s: the mask must be an int32 tensor [total, words] on the rows' device, 32 new tokens to a word, with unit stride along them" % name)
 
 
 def _max_q(name, total, batch, q_ptr, max_q):
@@ -733,10 +734,12 @@ def attn_tree_commit(mask, leaf, K_pages, V_pages, table, lens, q_ptr=None, max_
 
 def _slots(name, what, x, dtype, batch, kv_heads, slots, device):
     """Address and strides of an array [batch, kv_heads, at least `slots`]."""
-    if x.dtype is not dtype or x.dim() != 3 or x.shape[:2] != (batch, kv_heads) or x.shape[2] < slots or x.device != device or (x.numel() and x.stride(2) != 1):
-        raise ValueError("%s: %s must be a %s tensor [batch, kv_heads, at least %d] on the pages' device with unit stride along the slots"
-                         % (name, what, str(dtype).split(".")[-1], slots))
-    return x.data_ptr(), x.stride(0), x.stride(1)
+    if x.dtype is dtype and x.dim() == 3 and x.device == device:
+        (b, h, n), (stride_b, stride_h, unit) = x.shape, x.stride()
+        if b == batch and h == kv_heads and n >= slots and (unit == 1 or b * h * n == 0):
+            return x.data_ptr(), stride_b, stride_h
+    raise ValueError("%s: %s must be a %s tensor [batch, kv_heads, at least %d] on the pages' device with unit stride along the slots"
+                     % (name, what, str(dtype).split(".")[-1], slots))
 
 
 def attn_cache_weigh(Q, LSE, K_pages, V_pages, table, lens, scale, weight=None, decay=1.0, q_ptr=None, max_q=None, max_len=None, window=0, sinks=0,
@@ -798,12 +801,12 @@ def attn_cache_evict(weight, K_pages, V_pages, table, lens, budget, first=0, rec
     to, to_b, to_h = _slots(name, "weight's out", weight_out, torch.float32, batch, kvh, min(slots, budget), device)
     pos_at = pos_to = 0
     if pos is not None:
-        pos_at, *strides = _slots(name, "pos", pos, torch.int32, batch, kvh, slots, device)
-        if strides != [at_b, at_h] or pos_out is None:
+        pos_at, pos_b, pos_h = _slots(name, "pos", pos, torch.int32, batch, kvh, slots, device)
+        if pos_b != at_b or pos_h != at_h or pos_out is None:
             raise ValueError("%s: pos must have weight's strides, and a place to go to" % name)
     if pos_out is not None:
-        pos_to, *strides = _slots(name, "pos' out", pos_out, torch.int32, batch, kvh, min(slots, budget), device)
-        if strides != [to_b, to_h]:
+        pos_to, pos_b, pos_h = _slots(name, "pos' out", pos_out, torch.int32, batch, kvh, min(slots, budget), device)
+        if pos_b != to_b or pos_h != to_h:
             raise ValueError("%s: what weight and pos come out in must share strides" % name)
     lens_to = _int32("the new lengths", new_lens, batch, device)
     if lens_to is None:
