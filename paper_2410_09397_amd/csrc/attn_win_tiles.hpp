@@ -258,7 +258,7 @@ struct TreeItems {
                 blocks = __builtin_amdgcn_readlane(s.blocks, first);
                 of_parts = __builtin_amdgcn_readlane(parts(s.tiles), first);
                 start += __builtin_amdgcn_readlane(upto - own, first);
-                return base + first;
+                return (unsigned)(idx - start) < (unsigned)__builtin_amdgcn_readlane(own, first) ? base + first : -1;  // (no item: the numbers have passed 32 bits, by rows of several sequences)
             }
             start += __builtin_amdgcn_readlane(upto, min(64, p.batch - base) - 1);
         }
@@ -283,7 +283,9 @@ struct TreeItems {
                 blocks = __builtin_amdgcn_readlane(s.blocks, first);
                 of_parts = __builtin_amdgcn_readlane(parts(s.tiles), first);
                 blk = idx - __builtin_amdgcn_readlane(rows - s.blocks, first);
-                return base + first;
+                // (all of its parts are among the launch's: not so only where q_ptr gives rows to several sequences)
+                const long last_part = (long)start + blk + (long)(of_parts - 1) * blocks;
+                return start >= 0 && (unsigned)blk < (unsigned)blocks && last_part <= (long)p.blocks + p.places ? base + first : -1;
             }
             const int last = min(64, p.batch - base) - 1;
             start += __builtin_amdgcn_readlane(upto, last);

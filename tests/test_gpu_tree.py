@@ -217,6 +217,31 @@ def test_rows_of_no_sequence_are_left_alone():
         check("head %d" % h, O[3:7, h], o, bound)
 
 
+@pytest.mark.parametrize("kind,d", [("plain", 64), ("fp8", 128), ("fp8", 72)])
+def test_rows_of_several_sequences(kind, d):
+    """q_ptr has to ascend.  One that does not, and gives a row to several sequences, makes more parts than the workspace has places: what comes out is one
+    sequence's or the other's, or nothing of a row's, but nothing else is written and what is behind the workspace is not read."""
+    import torch
+    from paper_2410_09397_amd import attn
+    print("case tree rows of several sequences", kind, d, flush=True)
+    lens, rows, batch = [3000] * 6, 200, 6
+    c = Cache("bf16", kind, lens, 2, d, 64)
+    Q = torch.randn(rows, 4, d, device="cuda").to(torch.bfloat16)
+    ptr = torch.tensor([0, rows, 0, rows, 0, rows, 0], dtype=torch.int32, device="cuda")
+    mask = _mask([_bits("chain", rows, random.Random(0))], rows)
+    kw = dict(q_ptr=ptr, max_q=rows, **c.exps())
+    exps = c.exps()
+    desc, _ = attn._paged("attn_tree_fwd", Q, *c.args(), ptr, rows, None, exps.get("K_exp"), exps.get("V_exp"), False, 0.1, 0, 0)
+    size = attn.attn_tree_workspace_bytes(desc)
+    assert size > 256
+    workspace = torch.zeros(size + 4096, dtype=torch.uint8, device="cuda")
+    out = torch.full((rows + 2, 4, d), 7.0, device="cuda", dtype=torch.bfloat16), torch.full((rows + 2, 4), 7.0, device="cuda")
+    attn.attn_tree_fwd(Q, mask, *c.args(), 0.1, out=(out[0][1:-1], out[1][1:-1]), workspace=workspace[:size], **kw)
+    for x in out:
+        assert bool((x[0] == 7.0).all()) and bool((x[-1] == 7.0).all())
+    assert not bool(workspace[size:].any())
+
+
 @pytest.mark.parametrize("counts,max_q", [([1], 1), ([0, 5, 31, 32, 33], 33), ([64] * 70, 64), ([1024, 1000, 3], 1024), ([300], 512)])
 def test_masks_of_parents(counts, max_q):
     import torch
