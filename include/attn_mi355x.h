@@ -343,7 +343,8 @@ attn_status attn_tree_fwd(const attn_paged_desc *desc, const attn_cache *cache, 
 /* Of the new tokens those that row leaf[b] of a sequence sees stay, behind the context, in their order: their rows move there, and new_lens[b] (DEVICE
  * int32 [batch], overlaps no input) is the number of tokens that are left.  leaf[b] (DEVICE int32 [batch]) counts within the sequence's new tokens; any other
  * number, -1 say: none stays.  The slots behind the new length hold what they held.  A token whose page, or the page that it moves to, is outside the
- * cache does not move.  Of desc the sizes of Q, O, K and V, scale and window do not matter (heads may be kv_heads).  A call with batch, heads, total_q or
+ * cache does not move.  A page of new tokens belongs to one sequence (as attn_cache_write needs it); pages of the context may be shared.
+ * Of desc the sizes of Q, O, K and V, scale and window do not matter (heads may be kv_heads).  A call with batch, heads, total_q or
  * max_q 0 has nothing to do and writes nothing, not new_lens either. */
 attn_status attn_tree_commit(const attn_paged_desc *desc, const attn_cache *cache, const uint32_t *mask, int64_t mask_stride, const int32_t *leaf,
                              int32_t *new_lens, void *stream);
@@ -379,6 +380,7 @@ attn_status attn_cache_weigh(const attn_paged_desc *desc, const attn_cache *cach
  * without pos.  weight_out and pos_out (may be NULL without pos) get the values of the tokens that stay, in slots 0 .. new_lens[b] - 1; they may be weight
  * and pos themselves, with the same strides.  new_lens[b] = min(lens[b], budget), in memory of its own.  A token whose page, or the page that it moves to, is
  * outside the cache does not move.
+ * A page of a sequence that is cut down belongs to it alone: of a page that two tables name, or one table twice, copies are made first.
  * A call with batch, kv_heads or max_len 0 writes nothing.  first + recent <= budget, budget >= 1.  Of desc batch, kv_heads, d, max_len, the pages' fields, dtype and kind matter.
  */
 typedef struct { /* DEVICE memory; strides in elements, that of the slots is 1 */
