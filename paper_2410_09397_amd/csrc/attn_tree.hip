@@ -122,7 +122,7 @@ hipError_t launch_tree_join(bool is_bf16, int rows, const WinParams& p, hipStrea
     auto with = [&](auto lanes) {
         constexpr int L = decltype(lanes)::value;
         auto fn = !is_bf16 ? tree_join_kernel<float, 32, L> : rows == 16 ? tree_join_kernel<__bf16, 16, L> : rows == 32 ? tree_join_kernel<__bf16, 32, L>
-                  : rows == 64 ? tree_join_kernel<__bf16, 64, L> : tree_join_kernel<__bf16, 128, L>;
+                  : tree_join_kernel<__bf16, 128, L>;
         hipLaunchKernelGGL(fn, dim3((unsigned)((long)p.blocks * p.kv_heads * (rows / many))), dim3(kThreads), 0, stream, p, many);
     };
     if (p.d <= 64) with(std::integral_constant<int, 16>{});

@@ -9,9 +9,9 @@
 namespace attn {
 namespace {
 
-template <int D, int SRC, int SPLIT, bool PAD>
+template <int D, int SRC, bool PAD>
 __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) tree_out_kernel(WinParams p) {
-    win_out<D, SRC, SPLIT, PAD, true>(p, p.row_blocks);
+    win_out<D, SRC, 1, PAD, true>(p, p.row_blocks);
 }
 template <int D, int SRC, bool PAD>
 __global__ void __launch_bounds__((64 * kFewWaves<D, SRC>), (D == 256 ? 1 : 2)) tree_few_kernel(WinParams p) {
@@ -34,7 +34,7 @@ hipError_t launch_from(int rows, long groups, const WinParams& p, hipStream_t st
     };
     if (rows == 16) return run(tree_one_kernel<D, SRC, PAD>, kOneLds<D, SRC>, kThreads);
     if (rows == 32) return run(tree_few_kernel<D, SRC, PAD>, kFewLds<D, SRC>, 64 * kFewWaves<D, SRC>);
-    return rows == 64 ? run(tree_out_kernel<D, SRC, 2, PAD>, 4 * 64 * D * 2, kThreads) : run(tree_out_kernel<D, SRC, 1, PAD>, 4 * 64 * D * 2, kThreads);
+    return run(tree_out_kernel<D, SRC, PAD>, 4 * 64 * D * 2, kThreads);
 }
 template <int D>
 hipError_t launch(bool fp8, int rows, long grid, const WinParams& p, hipStream_t stream) {

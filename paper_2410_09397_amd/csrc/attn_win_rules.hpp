@@ -106,7 +106,7 @@ inline PagedSplits paged_splits(bool wide, int batch, int heads, int kv_heads, i
 }
 
 // Trees of drafted tokens: rows of a workgroup.  Unlike the new tokens of a batch in their order, whose blocks are as many as their tokens make them, a tree has one or two
-// blocks, and what fills the chip are the parts of the context: more than 64 rows take blocks of 128, which convert and read a tile half as often.  us of a call
+// blocks, and what fills the chip are the parts of the context: more than 64 rows always take blocks of 128, which convert and read a tile half as often.  us of a call
 // with 128 / 64 rows, h32 k8 d = 128, 64 drafted tokens: 16 sequences of 100 to 8192 tokens 84 / 144 (quantised), 74 / 119; one of 65536 102 / 124; one of 1000 (where
 // the chip is not full) 25.7 / 23.5; d = 256 h16 k4, 4 sequences 64 / 75.
 constexpr int kMostDrafted = 1024;  // drafted tokens of a sequence: their masks are 32 words

@@ -77,12 +77,15 @@ CASES = [
     ("bf16", "fp8", [5, 1, 0, 40], [3, 1, 0, 40], 4, 2, 128, 16, 0, 0, "tree"),             # no context; nothing at all
     ("bf16", "plain", [17, 600, 64, 333], [4, 4, 4, 3], 8, 2, 64, 16, 0, 0, "star"),         # 16 rows
     ("bf16", "fp8", [17, 600, 64, 333], [4, 2, 1, 3], 16, 4, 128, 32, 0, 0, "tree"),
+    ("bf16", "fp8", [5000, 300, 2000], [4, 2, 3], 8, 2, 128, 16, 0, 0, "tree"),              # the same, shared out over workgroups
+    ("bf16", "plain", [2500, 40], [3, 4], 8, 2, 64, 16, 0, 0, "bits"),
+    ("bf16", "plain", [3000, 1700], [5, 1], 3, 1, 256, 16, 200, 3, "tree"),
     ("bf16", "plain", [130, 900], [9, 13], 8, 2, 128, 64, 0, 0, "tree"),                     # 32 rows
     ("bf16", "fp8", [5000], [15], 4, 1, 128, 16, 0, 0, "bits"),                              # shared out over workgroups
     ("bf16", "plain", [3000, 30], [31, 30], 10, 5, 256, 128, 0, 0, "tree"),
-    ("bf16", "fp8", [700, 431], [64, 33], 8, 2, 128, 16, 0, 0, "tree"),                      # 64 and 128 rows
+    ("bf16", "fp8", [700, 431], [64, 33], 8, 2, 128, 16, 0, 0, "tree"),                      # 128 rows
     ("bf16", "plain", [2100, 100], [64, 64], 16, 1, 64, 16, 0, 0, "bits"),
-    ("bf16", "fp8", [400] * 24, [64] * 24, 32, 8, 64, 16, 0, 0, "tree"),                     # more blocks of 128 rows than the line between 64 and 128
+    ("bf16", "fp8", [400] * 24, [64] * 24, 32, 8, 64, 16, 0, 0, "tree"),                     # blocks for all places of the chip
     ("bf16", "plain", [300, 299], [65, 100], 4, 2, 256, 16, 0, 0, "bits"),
     ("bf16", "fp8", [300, 200], [100, 200], 4, 2, 256, 256, 0, 0, "chain"),
     ("bf16", "plain", [400], [90], 15, 3, 96, 16, 0, 0, "tree"),                             # padded widths
