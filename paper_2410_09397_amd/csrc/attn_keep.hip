@@ -41,7 +41,7 @@ __device__ __forceinline__ int wave_sums(int v) {
 // ---------------------------------------------------------------------------------------------------- accepted tokens
 // A workgroup takes K or V of a (sequence, key head).  The x-th of the tokens that stay, drafted token u_x, moves to place x behind the context.
 // u_x ascends, so a row is overwritten only by a row that is read with it or later: a chunk of rows is in registers before any of it is written, and
-// chunks ascend.
+// chunks ascend.  The chain of reads bounds it: 64 sequences with 64 drafted tokens each, k8 d = 128, quantised, 5.9 us, 15 tokens of 4 heads 4.6.
 constexpr int kChunkRows = 4;  // rows of a thread on the way
 
 template <typename U>
@@ -186,7 +186,8 @@ __device__ __forceinline__ void evict_rows(const EvictParams& e, const EvictSequ
 // Free slots below n and tokens that stay above it are as many as one another; both are listed in ascending order, at places that come from a table of how many
 // each 64 slots have.  Keys are in LDS, 16 to a thread (longer sequences are gone through again for every step).  What bounds it at the size of a decoding step is how many
 // instructions are fetched for the first time: with the keys in registers, and every loop over them written out, 1040 tokens took 19 us.
-// Few moves (e.here) are made by the same workgroup.
+// Few moves (e.here) are made by the same workgroup.  64 sequences of 1040 tokens, k8 d = 128, quantised, 16 leave: 13 us with the moves; 8 prompts of 500 to 16384 cut down to 2048: 25 us and 13 of
+// evict_move_kernel (3.9 TB/s).
 constexpr int kSelectItems = 16, kSelectPasses = 3, kSelectBins = 2048;
 __device__ __forceinline__ int select_bin(uint32_t digit) { return (int)(digit + (digit >> 5)); }
 template <int THREADS>
