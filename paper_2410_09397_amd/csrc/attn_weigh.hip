@@ -21,15 +21,16 @@ struct WeighRows {
     }
 };
 
-// Row r of a (sequence, key head): its position, or -1 where it sees nothing, and what its exponents are relative to (+inf: weights 0).
+// Row r of a (sequence, key head): its position, or -1 where it sees nothing or adds nothing (whatever its Q holds), and what its exponents are relative to (+inf: weights 0).
 struct WeighRow {
     int i;
     float lse2;
     __device__ __forceinline__ void init(const WinParams& p, const WinSeq& s, int kvh, int r, int rows) {
         const int x = min(r, rows - 1), t = win_token(p, x), head = kvh * p.group + x - t * p.group;
         const float lse = p.LSE_in[(s.row0 + t) * p.heads + head];
-        i = r < rows && s.first + t < s.len ? s.first + t : -1;
-        lse2 = r >= rows || lse == -__builtin_inff() ? __builtin_inff() : lse * kLog2e;
+        const bool adds = r < rows && s.first + t < s.len && lse != -__builtin_inff();
+        i = adds ? s.first + t : -1;
+        lse2 = adds ? lse * kLog2e : __builtin_inff();
     }
 };
 __device__ __forceinline__ bool weigh_sees(const WinParams& p, int i, int j) { return j <= i && (i - j < p.window || j < p.sinks); }

@@ -6,6 +6,7 @@ import random
 import pytest
 
 from tests import keep_ref
+from tests.helpers import LSE_TOL
 from tests.test_gpu_paged import DTYPES, Cache
 from tests.test_gpu_tree import _raw, _starts
 from tests.window_bounds import F, check
@@ -146,6 +147,26 @@ def test_weights_of_pages_behind_the_window(kind, d, new):
                     exps[gone] = 255
     again = attn.attn_cache_weigh(Q, LSE, *c.args(), d ** -0.5, out=torch.full_like(out, 9.0), **kw)
     assert torch.equal(again, out)
+
+
+@pytest.mark.parametrize("dtype,kind,d,new,h", [("bf16", "plain", 64, 3, 4), ("bf16", "fp8", 128, 20, 4), ("bf16", "plain", 128, 150, 4), ("bf16", "plain", 64, 3, 260),
+                                                ("f32", "plain", 40, 3, 4), ("f32", "plain", 64, 50, 4), ("bf16", "fp8", 72, 20, 4)])
+def test_queries_without_an_lse_add_nothing(dtype, kind, d, new, h):
+    """LSE = -inf: a query that adds nothing, also where its Q holds NaN; the others' weights are as without it."""
+    import torch
+    from paper_2410_09397_amd import attn
+    print("case weigh left out", dtype, kind, d, new, h, flush=True)
+    c = Cache(dtype, kind, [300], 2, d, 16)
+    Q = torch.randn(new, h, d, device="cuda").to(getattr(torch, DTYPES[dtype]))
+    kw = dict(max_q=new, **c.exps())
+    _, LSE = attn.attn_paged_fwd(Q, *c.args(), d ** -0.5, **kw)
+    LSE[::2] = -float("inf")
+    want = attn.attn_cache_weigh(Q, LSE, *c.args(), d ** -0.5, **kw)
+    Q[::2] = float("nan")
+    got = attn.attn_cache_weigh(Q, LSE, *c.args(), d ** -0.5, **kw)
+    assert bool(got.isfinite().all()) and torch.equal(got, want)
+    # (a row's weights add up to e^(error of its LSE); their own exponents are of sums of 40, rounded by 2^-24 each in two steps)
+    assert abs(float(got.double().sum()) - (new // 2) * h) <= (new // 2) * h * (1.01 * LSE_TOL[dtype] * max(1.0, float(LSE[1::2].abs().max())) + 1e-5)
 
 
 def test_weights_of_one_query_are_its_softmax():
