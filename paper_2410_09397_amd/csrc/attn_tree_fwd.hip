@@ -10,7 +10,7 @@ namespace attn {
 namespace {
 
 // More than 64 rows (tree_rows says why 128 of them).  As without a tree the softmax and the waits of a tile bound it, not memory: 64 drafted tokens, h32 k8 d = 128, of one sequence of
-// 65536 84 us (3.2 TB/s, 820 TFLOP/s), of 16 of 100 to 8192, quantised, 66 us (512 workgroups, the longest 22 tiles and the mean 16).
+// 65536 84 us (3.2 TB/s, 820 TFLOP/s), of 16 of 100 to 8192, quantised, 63 us (512 workgroups, the longest 22 tiles and the mean 16).
 template <int D, int SRC, bool PAD>
 __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) tree_out_kernel(WinParams p) {
     win_out<D, SRC, 1, PAD, true>(p, p.row_blocks);

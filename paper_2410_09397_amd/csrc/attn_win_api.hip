@@ -221,6 +221,7 @@ WinParams tree_params(const attn_paged_desc* d, const attn_cache* c, int64_t* gr
     p.blocks = shares.blocks;
     p.places = shares.places;
     p.least = shares.least;
+    p.fold = shares.fold;
     p.splits = 1;
     p.chunk = 0x7fffffff;
     *grid = shares.grid;

@@ -121,14 +121,16 @@ inline int tree_rows(bool wide, int batch, int heads, int kv_heads, int total_q,
 // 106 -> 128, 124, 121). Where row blocks alone are more than the chip's places, parts come in two rounds, so that the last ones are short.  us: parts of at least 4 tiles of 64 keys / of 8, one sequence of
 // 1000 tokens with 64 drafted 25.8 / 30.6, 8 sequences of 500 to 4000 with 30 38.5 / 40.8; at least 16 tiles of 32 keys, of four waves / 32, 16 sequences with 8 drafted 44.8 /
 // 47.2; two rounds / one / four, 64 sequences of 100 to 2000 tokens with 40 drafted 135 / 140 / 139.
+// fold: one round of 128 rows, two workgroups to a CU, of several sequences: long parts share a CU with short ones (see find_folded; 16 sequences with 64 drafted, quantised 82.3 -> 79.3, not 70.4 -> 67.6;
+// 8 sequences of 500 to 4000 with 30 38.4 -> 38.2).
 constexpr int64_t kTreeLeast = 4, kTreeLeastFew = 16, kTreeRounds = 2;
 struct TreeShares {
-    int row_blocks, blocks, places, least;
+    int row_blocks, blocks, places, least, fold;
     int64_t grid;
 };
 inline TreeShares tree_shares(bool wide, int batch, int heads, int kv_heads, int d, int total_q, int max_q, int max_len, int window, int sinks) {
     const int64_t group = heads / kv_heads, rows = tree_rows(wide, batch, heads, kv_heads, total_q, max_q), tile = rows >= 64 ? 64 : 32;
-    TreeShares p = {(int)((max_q * group + rows - 1) / rows), 0, 0, 0x7fffffff, 0};
+    TreeShares p = {(int)((max_q * group + rows - 1) / rows), 0, 0, 0x7fffffff, 0, 0};
     p.blocks = (int)std::min((int64_t)p.row_blocks * batch, total_q * group / rows + batch);
     p.grid = (int64_t)p.blocks * kv_heads;
     const int64_t chip = rows == 16 && d <= 128 ? 1024 : d > 128 ? 256 : 512, of_head = std::max<int64_t>(1, chip / kv_heads);
@@ -136,6 +138,7 @@ inline TreeShares tree_shares(bool wide, int batch, int heads, int kv_heads, int
     const int64_t keys = std::min<int64_t>(max_len, (int64_t)window + max_q) + sinks, tiles = keys / tile + 4, least = rows >= 64 ? kTreeLeast : kTreeLeastFew;
     if (tiles < 2 * least || p.grid > 8 * chip || (int64_t)total_q * heads > kMostGroups) return p;
     p.places = (int)(p.blocks <= of_head ? of_head - p.blocks / 2 : kTreeRounds * of_head);
+    if (rows == 128 && d <= 128 && p.blocks <= of_head && batch > 1 && batch <= 64) p.fold = (int)(256 / kv_heads);
     p.least = (int)std::max(least, (tiles + 63) / 64);  // (64 parts at most: the joining launch has a lane for each)
     p.grid += (p.places + 1) * (int64_t)kv_heads;  // (one more: the device divides in 32-bit floating point)
     return p;

@@ -264,6 +264,30 @@ struct TreeItems {
         }
         return -1;
     }
+    // Where all items are on the chip at once, two to a CU, the later half of them with the earlier one: those with most tiles come first, and of the later half those with fewest, so that
+    // long ones share a CU with short ones.  The sequence of the idx-th in this order (-1: there is none), its row blocks and parts, which item of the sequence it is, and the number of
+    // the sequence's first item in the order that the sums have.  Up to 64 sequences.
+    __device__ __forceinline__ int find_folded(const WinParams& p, int idx, int lane, int& start, int& blocks, int& of_parts, int& within) const {
+        const Sequence s = sequence(p, lane);
+        const int of = parts(s.tiles), own = s.blocks * of, size = (s.tiles + of - 1) / of;
+        int before = 0, all = 0, first = 0;
+        for (int x = 0; x < p.batch; ++x) {
+            const int items = __builtin_amdgcn_readlane(own, x), tiles = __builtin_amdgcn_readlane(size, x);
+            all += items;
+            before += x < lane ? items : 0;
+            first += tiles > size || (tiles == size && x < lane) ? items : 0;
+        }
+        if (idx >= all || all > p.blocks + p.places + 1) return -1;  // (more items than the launch has: as in find_block)
+        if (idx >= p.fold) idx = all - 1 - (idx - p.fold);
+        const unsigned long who = __builtin_amdgcn_ballot_w64(idx >= first && idx - first < own);
+        if (!who) return -1;
+        const int b = __builtin_ctzl(who);
+        blocks = __builtin_amdgcn_readlane(s.blocks, b);
+        of_parts = __builtin_amdgcn_readlane(of, b);
+        start = __builtin_amdgcn_readlane(before, b);
+        within = idx - __builtin_amdgcn_readlane(first, b);
+        return b;
+    }
     // row block idx of all sequences: its sequence (-1: there is none), that one's first item, row blocks and parts, and which of them it is
     __device__ __forceinline__ int find_block(const WinParams& p, int idx, int lane, int& start, int& blocks, int& of_parts, int& blk) const {
         start = 0;
@@ -315,24 +339,30 @@ struct Share {
 };
 template <int BR, int BC>
 struct Share<BR, BC, true> {
-    int b, blk, part, parts;
+    int b, blk, part, parts, item;
     bool any;
     __device__ __forceinline__ void init(const WinParams& p, int idx, int lane) {
         TreeItems<BR, BC> items;
         items.init(p, lane);
-        int start, blocks = 1;
-        b = items.find(p, idx, lane, start, blocks, parts);
+        int start = 0, blocks = 1, within;
+        if (BR == 128 && p.fold > 0) {
+            b = items.find_folded(p, idx, lane, start, blocks, parts, within);
+        } else {
+            b = items.find(p, idx, lane, start, blocks, parts);
+            within = idx - start;
+        }
         any = b >= 0;
         b = max(b, 0);
-        part = any ? __builtin_amdgcn_readfirstlane((idx - start) / blocks) : 0;  // (divisions are vector arithmetic)
-        blk = any ? idx - start - part * blocks : 0;
+        part = any ? __builtin_amdgcn_readfirstlane(within / blocks) : 0;  // (divisions are vector arithmetic)
+        blk = any ? within - part * blocks : 0;
+        item = start + within;
     }
     // (the parts of a sequence are as long as one another)
     __device__ __forceinline__ int share(int tiles, int x) const { return __builtin_amdgcn_readfirstlane((int)((unsigned long)tiles * (unsigned)x / (unsigned)parts)); }
     __device__ __forceinline__ int first(const WinParams&, int tiles) const { return share(tiles, part); }
     __device__ __forceinline__ int last(const WinParams&, int tiles) const { return share(tiles, part + 1); }
     __device__ __forceinline__ bool whole(const WinParams&, int) const { return parts <= 1; }
-    __device__ __forceinline__ long sums(const WinParams&, long, int row) const { return (long)blockIdx.x * BR + row; }
+    __device__ __forceinline__ long sums(const WinParams& p, long, int row) const { return ((long)item * p.kv_heads + blockIdx.x % p.kv_heads) * BR + row; }
 };
 
 }  // namespace attn

@@ -32,7 +32,7 @@ struct WinParams {
     // forward: work of a row block shared out over `splits` workgroups of `chunk` tiles each; their sums meet in win_join_kernel
     int splits, chunk;
     float *part_o, *part_ml;  // [row][split][d], [row][split][2], row = token row * heads + head; trees: by workgroups, see TreeItems
-    int places, least;        // trees: workgroups of a key head that the work is shared out over (0: it is not), tiles that a part has at least
+    int places, least, fold;  // trees: workgroups of a key head that the work is shared out over (0: it is not), tiles that a part has at least, and see find_folded
     // backward: the first `sink_tiles` key tiles are each worked on by `parts` workgroups, the others by `rest_parts`, each of which takes a
     // share of the tokens; where there are several, their sums meet in win_keys_kernel
     int sink_tiles, parts, rest_parts;

@@ -20,7 +20,7 @@ extern "C" void tree_of(int bf16, int fp8, int b, int h, int k, int d, int total
     const bool wide = win_is_wide(bf16 != 0, d, fp8 != 0);
     const TreeShares p = tree_shares(wide, b, h, k, d, total, max_q, max_len, r.window, r.sinks);
     const int rows = tree_rows(wide, b, h, k, total, max_q);
-    out[0] = rows, out[1] = p.row_blocks, out[2] = p.blocks, out[3] = p.places, out[4] = p.least, out[5] = p.grid, out[6] = join_rows((int64_t)p.blocks * k, rows);
+    out[0] = rows, out[1] = p.row_blocks, out[2] = p.blocks, out[3] = p.places, out[4] = p.least, out[5] = p.grid, out[6] = join_rows((int64_t)p.blocks * k, rows), out[7] = p.fold;
 }
 extern "C" void weigh_of(int bf16, int fp8, int b, int h, int k, int d, int max_q, int max_len, long long n, long long s, int* out) {
     const WeighPlan p = weigh_plan(win_is_wide(bf16 != 0, d, fp8 != 0), b, h, k, max_q, max_len, n, s);
@@ -43,7 +43,7 @@ def lib(tmp_path_factory):
 
 
 def _tree(lib, *args):
-    out = (ctypes.c_longlong * 7)()
+    out = (ctypes.c_longlong * 8)()
     lib.tree_of(*args, out)
     return tuple(out)
 
@@ -55,14 +55,16 @@ def _weigh(lib, *args):
 
 
 def test_the_shapes_of_the_gpu_tests_reach_every_kernel_of_trees(lib):
-    met, joined = set(), set()
+    met, joined, folded = set(), set(), set()
     for dtype, kind, lens, new, h, k, d, page, window, sinks, _ in CASES:
         width = max(-(-x // page) for x in lens) * page
-        rows, _, _, places, _, _, many = _tree(lib, int(dtype == "bf16"), int(kind == "fp8"), len(lens), h, k, d, sum(new), max([1] + new), width, window, sinks)
+        rows, _, _, places, _, _, many, fold = _tree(lib, int(dtype == "bf16"), int(kind == "fp8"), len(lens), h, k, d, sum(new), max([1] + new), width, window, sinks)
         met.add((rows, places > 0))
+        folded.add((rows, fold > 0)) if places > 0 else None
         joined.add((places > 0, many > 8))
     assert met == {(rows, shared) for rows in (16, 32, 128) for shared in (False, True)}
     assert joined >= {(True, False), (True, True)}, joined
+    assert folded >= {(128, False), (128, True), (32, False), (16, False)}, folded
 
 
 def test_every_part_of_a_tree_has_a_workgroup_and_a_lane(lib):
@@ -79,7 +81,7 @@ def test_every_part_of_a_tree_has_a_workgroup_and_a_lane(lib):
         window = rng.choice([0, 0, 100, 5000])
         sinks = rng.choice([0, 4, 70]) if window else 0
         total = sum(new)
-        rows, _, blocks, places, least, grid, many = _tree(lib, bf16, fp8, batch, k * group, k, d, total, max_q, max_len, window, sinks)
+        rows, _, blocks, places, least, grid, many, fold = _tree(lib, bf16, fp8, batch, k * group, k, d, total, max_q, max_len, window, sinks)
         assert rows % many == 0 and grid % k == 0 and 0 < grid < 1 << 31
         tile, items, tiles_of = 64 if rows >= 64 else 32, grid // k, []
         for length, q in zip(lens, new):
@@ -97,6 +99,11 @@ def test_every_part_of_a_tree_has_a_workgroup_and_a_lane(lib):
         parts = [max(1, -(-t // chunk)) for _, t in tiles_of]
         assert max(parts) <= 64
         assert sum(b * x for (b, _), x in zip(tiles_of, parts)) <= items
+        if fold:  # every item is some workgroup's: the order of find_folded
+            assert rows == 128 and 1 < batch <= 64 and blocks * k <= 512
+            order = sorted(range(batch), key=lambda x: (-(-(-tiles_of[x][1] // parts[x])), x))
+            runs, every = [tiles_of[x][0] * parts[x] for x in order], sum(b * x for (b, _), x in zip(tiles_of, parts))
+            assert sorted(x if x < fold else every - 1 - (x - fold) for x in range(every)) == list(range(every)) and sum(runs) == every
     assert shared > 500
 
 
