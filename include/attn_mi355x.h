@@ -364,7 +364,8 @@ typedef struct { /* DEVICE memory; strides in elements, the slots' is 1 and thos
     float decay;      /* finite */
     int32_t reserved; /* 0 */
 } attn_weights;
-/* Device scratch of attn_cache_weigh: sums of the parts that many new tokens are shared out in.  0 if desc is invalid. */
+/* Device scratch of attn_cache_weigh: sums of the parts that many new tokens are shared out in; 256: none, and `workspace` may be NULL (so it is with
+ * attn_tree_workspace_bytes and attn_evict_workspace_bytes).  0 if desc is invalid. */
 size_t attn_weigh_workspace_bytes(const attn_paged_desc *desc);
 attn_status attn_cache_weigh(const attn_paged_desc *desc, const attn_cache *cache, const void *Q, const float *LSE, const attn_weights *weights,
                              void *workspace, size_t workspace_bytes, void *stream);

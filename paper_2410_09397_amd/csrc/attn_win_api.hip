@@ -450,7 +450,9 @@ attn_status attn_tree_commit(const attn_paged_desc* desc, const attn_cache* cach
 
 size_t attn_weigh_workspace_bytes(const attn_paged_desc* desc) {
     if (check_weigh(desc) != ATTN_OK) return 0;
-    return no_cache(desc) ? 256 : std::max<size_t>(256, weigh_bytes(desc, weigh_plan(desc)));
+    if (no_cache(desc)) return 256;
+    const attn::WeighPlan plan = weigh_plan(desc);
+    return plan.parts > 1 ? std::max<size_t>(512, weigh_bytes(desc, plan)) : 256;  // (256: nothing is kept there, and there may be none)
 }
 
 attn_status attn_cache_weigh(const attn_paged_desc* desc, const attn_cache* cache, const void* Q, const float* LSE, const attn_weights* weights,
