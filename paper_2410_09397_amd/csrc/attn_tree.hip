@@ -8,7 +8,50 @@ namespace {
 // (three sequences of 50 to 777 tokens with 21 to 37 drafted, h6 k2 d = 80, window 128: 16 us, waits for operands as without a tree)
 template <typename T, typename E, int DP>
 __global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) tree_plain_out_kernel(WinParams p) {
-    win_plain_out<T, E, DP, true, true>(p, p.row_blocks);
+    constexpr int MT = DP / 32;
+    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Share<32, 32, true> share;
+    share.init(p, (int)(blockIdx.x / p.kv_heads), lane);
+    if (!share.any) return;
+    const int b = share.b, kvh = blockIdx.x % p.kv_heads;
+    const WinSeq s = win_sequence(p, b);
+    const int rows = s.nq * p.group, r0 = share.blk * 32;
+    if (r0 >= rows) return;
+    const RowPlace at = place(p, kvh, min(r0 + l32, rows - 1));
+    Sight<32, true> see;
+    see.init(p, s, at.t, 0, 0, 0, 0);
+    const auto& tiles = see.tiles;
+    const int it0 = share.first(p, tiles.count), it1 = share.last(p, tiles.count);
+
+    RowOperand<T, DP> q;
+    q.init(static_cast<const T*>(p.Q) + s.q_base + (long)at.head * p.q_h + (long)at.t * p.q_n, p.d, h);
+    f32x16 o[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[m][e] = 0.f;
+    float m_run = -__builtin_inff(), l_run = 0.f;  // of scale log2(e) s; this lane's half of the sum
+    const float cs = p.scale * kLog2e;
+    for (int it = it0 + w; it < it1; it += 4) {
+        const int j0 = tiles.start(it);
+        KeyTile<E, true> keys;
+        keys.init(p, tiles, b, kvh, j0, l32);
+        f32x16 st;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) st[e] = 0.f;
+        TileRow<E, DP> key;
+        key.init(keys.K + keys.at, p.d, h);
+        scores(st, key, keys.sk, q);
+        const auto seen = see.template keys<1>(p, it, j0, 4 * h);
+        float mx = -__builtin_inff();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            st[e] = seen(0, 8 * (e >> 2) + (e & 3)) ? st[e] * cs : -__builtin_inff();
+            mx = __builtin_elementwise_maximum(mx, st[e]);
+        }
+        plain_weights<E, DP, true>(p, keys, h, l32, st, mx, o, m_run, l_run);
+    }
+    plain_store<T, MT>(p, s, at, share, tiles.count, r0, rows, w, lane, o, m_run, l_run);
 }
 
 // The sums of a row's parts, as win_join_kernel, for the parts of TreeItems.  A workgroup takes `many` rows of a row block, so that its sequence, its parts and their

@@ -16,9 +16,92 @@
 namespace attn {
 namespace {
 
+// How the masks of a tile's keys are written decides where the compiler works them out, and with that how long the wave waits between its products and its softmax.  us as they
+// stood in one function with those of trees (above the products, in 32 scalar registers) -> written as here:
+//   tensors                   sees(e) behind the products                                 train n777 d80 w128 104 -> 100, full n777 d80 235 -> 227, n1500 d128 w300 380 -> 365
+//   codes                     the same, up to 64 columns relative to the tile's first key   a token of 8 sequences d72 36.1 -> 30.6, d40 25.7 -> 25.1; 200 tokens of 2 sequences d72 47 -> 43
+//   fp32 pages, 65 to 128     kEarly: above the products, nothing of theirs before        200 tokens of 2 sequences d80 37.4 -> 35.0, d128 58 -> 45
+//   fp32 pages, to 64         kPlain: compared where they are used                        200 tokens of 2 sequences d64 27.7 -> 28.5 (sees(e) 32.5)
 template <typename T, typename E, int DP, bool PAGED>
 __global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) win_plain_out_kernel(WinParams p, int row_blocks) {
-    win_plain_out<T, E, DP, PAGED, false>(p, row_blocks);
+    constexpr int MT = DP / 32;
+    constexpr bool kCodes = KeyTile<E, PAGED>::kCodes, kNear = kCodes && DP <= 64;
+    constexpr bool kEarly = PAGED && !kCodes && (DP == 96 || DP == 128), kPlain = PAGED && !kCodes && DP <= 64;
+    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int b, kvh, blk;
+    if constexpr (PAGED) {
+        WinBlock block;
+        block.init(p, (int)(blockIdx.x / p.kv_heads), 32, lane);
+        if (!block.any) return;
+        b = block.b;
+        kvh = blockIdx.x % p.kv_heads;
+        blk = block.blk;
+    } else {
+        const int bk = blockIdx.x / row_blocks;
+        b = bk / p.kv_heads;
+        kvh = bk % p.kv_heads;
+        blk = blockIdx.x % row_blocks;
+    }
+    const WinSeq s = win_sequence(p, b);
+    const int rows = s.nq * p.group, r0 = blk * 32;
+    if (r0 >= rows) return;
+    const int r = min(r0 + l32, rows - 1);
+    const RowPlace at = place(p, kvh, r);
+    const int i = s.first + at.t;
+    const int hi = i < s.len ? i : -1, lo = i - p.window + 1;  // this row sees lo .. hi, and the sinks up to hi
+    WinTiles<32> tiles;
+    tiles.init(p, s.len, s.first + place(p, kvh, r0).t, s.first + place(p, kvh, min(r0 + 31, rows - 1)).t);
+    const int it0 = blockIdx.y * p.chunk, it1 = min(tiles.count, it0 + p.chunk);
+
+    RowOperand<T, DP> q;
+    q.init(static_cast<const T*>(p.Q) + s.q_base + (long)at.head * p.q_h + (long)at.t * p.q_n, p.d, h);
+    f32x16 o[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[m][e] = 0.f;
+    float m_run = -__builtin_inff(), l_run = 0.f;  // of scale log2(e) s; this lane's half of the sum
+    const float cs = p.scale * kLog2e;
+    for (int it = it0 + w; it < it1; it += 4) {
+        const int j0 = tiles.start(it);
+        KeyTile<E, PAGED> keys;
+        keys.init(p, tiles, b, kvh, j0, l32);
+        f32x16 st;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) st[e] = 0.f;
+        TileRow<E, DP> key;
+        key.init(keys.K + keys.at, p.d, h);
+        auto sees = [&](int e) {
+            if constexpr (kNear) {
+                const int from = j0 + 4 * h, c = 8 * (e >> 2) + (e & 3);
+                return c <= hi - from && (c >= lo - from || c < p.sinks - from);
+            } else {
+                const int j = j0 + acc_row(e, h);
+                return j <= hi && (j >= lo || j < p.sinks);
+            }
+        };
+        bool seen[16];
+        if constexpr (kEarly) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) seen[e] = sees(e);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        scores(st, key, keys.sk, q);
+        float mx = -__builtin_inff();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            if constexpr (kPlain) {
+                const int j = j0 + acc_row(e, h);
+                st[e] = j <= hi && (j >= lo || j < p.sinks) ? st[e] * cs : -__builtin_inff();
+            } else {
+                if constexpr (!kEarly) seen[e] = sees(e);
+                st[e] = seen[e] ? st[e] * cs : -__builtin_inff();
+            }
+            mx = __builtin_elementwise_maximum(mx, st[e]);
+        }
+        plain_weights<E, DP, PAGED>(p, keys, h, l32, st, mx, o, m_run, l_run);
+    }
+    plain_store<T, MT>(p, s, at, Share<32, 32, false>(), tiles.count, r0, rows, w, lane, o, m_run, l_run);
 }
 
 // The sums of the parts of a row: O = sum_k 2^(m_k - m) O_k / l, l = sum_k 2^(m_k - m) l_k, always in the same order.  WAVES waves per row; every

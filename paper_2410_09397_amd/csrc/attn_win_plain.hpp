@@ -1,5 +1,5 @@
-// Windowed attention in 32-bit arithmetic (attn_win_plain.hip says how): how its operands are read, and the forward as a function, over tensors or
-// pages, and (TREE) over pages whose last tokens are a tree of drafted ones.  HIP device code only.
+// Windowed attention in 32-bit arithmetic (attn_win_plain.hip says how): how its operands are read, and what the forward kernels, over tensors, over
+// pages and over pages whose last tokens are a tree of drafted ones, have in common.  HIP device code only.
 #pragma once
 #include <type_traits>
 
@@ -254,82 +254,41 @@ __device__ __forceinline__ void meet_waves(f32x16 (&a)[MT], float* meet, int w, 
 }
 
 // --------------------------------------------------------------------------------------------------------- forward
-template <typename T, typename E, int DP, bool PAGED, bool TREE>
-__device__ __forceinline__ void win_plain_out(const WinParams& p, int row_blocks) {
-    constexpr int MT = DP / 32;
-    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int b, kvh, blk;
-    Share<32, 32, TREE> share;
-    if constexpr (PAGED) {
-        share.init(p, (int)(blockIdx.x / p.kv_heads), lane);
-        if (!share.any) return;
-        b = share.b;
-        kvh = blockIdx.x % p.kv_heads;
-        blk = share.blk;
-    } else {
-        const int bk = blockIdx.x / row_blocks;
-        b = bk / p.kv_heads;
-        kvh = bk % p.kv_heads;
-        blk = blockIdx.x % row_blocks;
-    }
-    const WinSeq s = win_sequence(p, b);
-    const int rows = s.nq * p.group, r0 = blk * 32;
-    if (r0 >= rows) return;
-    const int r = min(r0 + l32, rows - 1);
-    const RowPlace at = place(p, kvh, r);
-    const int t_lo = place(p, kvh, r0).t, t_hi = place(p, kvh, min(r0 + 31, rows - 1)).t;
-    Sight<32, TREE> see;
-    see.init(p, s, at.t, t_lo, t_hi, t_lo, t_hi);
-    const auto& tiles = see.tiles;
-    const int it0 = share.first(p, tiles.count), it1 = share.last(p, tiles.count);
+// What the forward kernels (attn_win_plain.hip, and over trees attn_tree.hip) have in common.  A tile's rows and which of its keys a row sees stand in the kernels themselves
+// (win_plain_out_kernel says why).
 
-    RowOperand<T, DP> q;
-    q.init(static_cast<const T*>(p.Q) + s.q_base + (long)at.head * p.q_h + (long)at.t * p.q_n, p.d, h);
-    f32x16 o[MT];
+// A tile's scores times scale log2(e) (-inf: not seen; mx: the lane's largest) become weights of the running reference, and their products with V are added to O.
+template <typename E, int DP, bool PAGED>
+__device__ __forceinline__ void plain_weights(const WinParams& p, const KeyTile<E, PAGED>& keys, int h, int l32, f32x16& st, float mx, f32x16 (&o)[DP / 32], float& m_run,
+                                              float& l_run) {
+    constexpr int MT = DP / 32;
+    mx = __builtin_elementwise_maximum(mx, __shfl_xor(mx, 32, 64));
+    const float m_new = __builtin_elementwise_maximum(m_run, mx), m_use = m_new == -__builtin_inff() ? 0.f : m_new;
+    const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
+    m_run = m_new;
+    l_run *= alpha;
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) o[m][e] = 0.f;
-    float m_run = -__builtin_inff(), l_run = 0.f;  // of scale log2(e) s; this lane's half of the sum
-    const float cs = p.scale * kLog2e;
-    for (int it = it0 + w; it < it1; it += 4) {
-        const int j0 = tiles.start(it);
-        KeyTile<E, PAGED> keys;
-        keys.init(p, tiles, b, kvh, j0, l32);
-        f32x16 st;
+        for (int e = 0; e < 16; ++e) o[m][e] *= alpha;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) st[e] = 0.f;
-        TileRow<E, DP> key;
-        key.init(keys.K + keys.at, p.d, h);
-        scores(st, key, keys.sk, q);
-        const auto seen = see.template keys<1>(p, it, j0, 4 * h);
-        float mx = -__builtin_inff();
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            st[e] = seen(0, 8 * (e >> 2) + (e & 3)) ? st[e] * cs : -__builtin_inff();
-            mx = __builtin_elementwise_maximum(mx, st[e]);
-        }
-        mx = __builtin_elementwise_maximum(mx, __shfl_xor(mx, 32, 64));
-        const float m_new = __builtin_elementwise_maximum(m_run, mx), m_use = m_new == -__builtin_inff() ? 0.f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
-        m_run = m_new;
-        l_run *= alpha;
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) o[m][e] *= alpha;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            st[e] = __builtin_amdgcn_exp2f(st[e] - m_use);
-            l_run += st[e];
-        }
-        if constexpr (KeyTile<E, PAGED>::kCodes) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) st[e] *= __shfl(keys.sv, acc_row(e, h), 64);
-        }
-        by_rows<MT, DP>([&](int e, int m) { return load1<DP>(keys.V + keys.row_of(acc_row(e, h)), m, l32, p.d); },
-                        [&](int e, int m, float v) { o[m] = mfma_f32(v, st[e], o[m]); });
+    for (int e = 0; e < 16; ++e) {
+        st[e] = __builtin_amdgcn_exp2f(st[e] - m_use);
+        l_run += st[e];
     }
+    if constexpr (KeyTile<E, PAGED>::kCodes) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) st[e] *= __shfl(keys.sv, acc_row(e, h), 64);
+    }
+    by_rows<MT, DP>([&](int e, int m) { return load1<DP>(keys.V + keys.row_of(acc_row(e, h)), m, l32, p.d); },
+                    [&](int e, int m, float v) { o[m] = mfma_f32(v, st[e], o[m]); });
+}
+
+// The waves' sums of 32 rows meet and are stored, as O and LSE or (share) as those of a part.  at: the lane's row, r0: the workgroup's first.
+template <typename T, int MT, typename S>
+__device__ __forceinline__ void plain_store(const WinParams& p, const WinSeq& s, const RowPlace& at, const S& share, int tiles, int r0, int rows, int w, int lane,
+                                            f32x16 (&o)[MT], float m_run, float l_run) {
+    const int h = lane >> 5, l32 = lane & 31;
     // every wave's m and l, then its O in units of the common reference
     float l = l_run + __shfl_xor(l_run, 32, 64);
     extern __shared__ __attribute__((aligned(16))) float meet[];  // [MT][4][64] x 16 bytes, [4][m, l][32]
@@ -353,7 +312,7 @@ __device__ __forceinline__ void win_plain_out(const WinParams& p, int row_blocks
         for (int e = 0; e < 16; ++e) o[m][e] *= mine;
     meet_waves<MT>(o, meet, w, lane);
     if (w != 0 || r0 + l32 >= rows) return;
-    if (!share.whole(p, tiles.count)) {
+    if (!share.whole(p, tiles)) {
         const long row = share.sums(p, s.lse_base + (long)at.t * p.heads + at.head, l32);
         float* ml = p.part_ml + row * 2;
         if (h == 0) {
