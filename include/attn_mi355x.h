@@ -355,7 +355,8 @@ attn_status attn_tree_commit(const attn_paged_desc *desc, const attn_cache *cach
  * by attn_cache_weigh, with the visibility and the LSE of attn_paged_fwd (a query with LSE = -inf adds nothing).  New tokens start at zero: `in` is read
  * for the tokens in front of them only, and may be NULL (zeros).  Slots below lens[b] are written, others not.  `out` may be `in` (with the same strides).
  * Every token of the cache is worked on, those of sequences without new tokens too: they keep decay times their weight.  Q and LSE (contiguous [total_q,
- * heads]) may be NULL if total_q or max_q is 0.  batch * kv_heads * ceil(max_len / 32) < 2^24.  Arithmetic as attn_paged_fwd, weights in fp32.
+ * heads]) may be NULL if heads, total_q or max_q is 0; a call with batch, kv_heads or max_len 0 writes nothing.  batch * kv_heads * ceil(max_len / 32) < 2^24.
+ * Arithmetic as attn_paged_fwd, weights in fp32.
  */
 typedef struct { /* DEVICE memory; strides in elements, the slots' is 1 and those of batches and heads at least max_len */
     const float *in;

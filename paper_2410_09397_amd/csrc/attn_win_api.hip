@@ -185,8 +185,8 @@ size_t part_o_bytes(const attn_paged_desc* d, const WinParams& p) {
     return p.splits > 1 ? (size_t)d->total_q * d->heads * p.splits * d->d * sizeof(float) : 0;
 }
 
-// Calls on the cache that have no new tokens' rows.
-bool no_cache(const attn_paged_desc* d) { return d->batch == 0 || d->heads == 0 || d->max_len == 0; }
+// Weights and eviction: no token in the cache.  (Without query heads there are no rows, but tokens all the same.)
+bool no_cache(const attn_paged_desc* d) { return d->batch == 0 || d->kv_heads == 0 || d->max_len == 0; }
 
 bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
@@ -464,7 +464,7 @@ attn_status attn_cache_weigh(const attn_paged_desc* desc, const attn_cache* cach
     st = check_cache(desc, cache);
     if (st != ATTN_OK) return st;
     const bool bf16 = desc->dtype == ATTN_BF16, fp8 = desc->kind == ATTN_CACHE_FP8;
-    if (desc->total_q > 0 && desc->max_q > 0 && (!Q || !LSE)) return ATTN_ERR_INVALID_ARG;
+    if (!is_empty(desc) && (!Q || !LSE)) return ATTN_ERR_INVALID_ARG;
     if (!weights->out || (bf16 && !aligned16(Q))) return ATTN_ERR_INVALID_ARG;
     if (!good_slots(desc, weights->out_stride_b, weights->out_stride_h, desc->max_len)) return ATTN_ERR_INVALID_ARG;
     if (weights->in && (!good_slots(desc, weights->in_stride_b, weights->in_stride_h, desc->max_len) ||
