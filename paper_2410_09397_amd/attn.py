@@ -795,8 +795,7 @@ def attn_cache_evict(weight, K_pages, V_pages, table, lens, budget, first=0, rec
     on = _stream_on(device, stream)
     slots = table.shape[1] * K_pages.shape[2] if max_len is None else max_len
     if out is None:
-        nothing = kvh == 0 or slots == 0  # nothing is launched
-        out = weight, pos, _made_on(stream, lambda: lens.clamp(0, min(budget, slots)) if nothing else torch.empty_like(lens))
+        out = weight, pos, _made_on(stream, lambda: torch.empty_like(lens))
     weight_out, pos_out, new_lens = out
     at, at_b, at_h = _slots(name, "weight", weight, torch.float32, batch, kvh, slots, device)
     to, to_b, to_h = _slots(name, "weight's out", weight_out, torch.float32, batch, kvh, min(slots, budget), device)
@@ -826,4 +825,6 @@ def attn_cache_evict(weight, K_pages, V_pages, table, lens, budget, first=0, rec
     st = lib().attn_cache_evict(desc, cache, args, where, size, on)
     if st != ATTN_OK:
         raise AttnError(st, name)
+    if kvh == 0 or slots == 0:  # nothing is launched
+        _made_on(stream, lambda: new_lens.copy_(lens.clamp(0, min(budget, slots))))
     return out

@@ -56,3 +56,24 @@ def test_evicting_without_query_heads(budget):
     assert attn.lib().attn_cache_evict(desc, cache, args, scratch.data_ptr(), scratch.numel(), torch.cuda.current_stream().cuda_stream) == OK
     assert torch.equal(lens_out, want[2]) and torch.equal(got, want[0])
     assert torch.equal(_raw(a.K), _raw(b.K)) and torch.equal(_raw(a.V), _raw(b.V))
+
+
+@pytest.mark.gpu
+def test_new_lengths_of_a_cache_without_tokens_are_written_where_they_are_wanted():
+    """No key heads, or max_len = 0: nothing moves, and the new lengths come back in `out` as they do without it."""
+    import torch
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    lens, table = ints([5, 9]), torch.zeros(2, 1, dtype=torch.int32, device="cuda")
+    for kvh, max_len, want in ((0, None, [5, 7]), (2, 0, [0, 0])):
+        pages = torch.zeros(2, kvh, 16, 64, dtype=torch.bfloat16, device="cuda")
+        w = torch.ones(2, kvh, 16, device="cuda")
+        side = torch.cuda.Stream()
+        for stream in (None, side):
+            out = w.clone(), None, ints([-1, -1])
+            torch.cuda.synchronize()
+            got = attn.attn_cache_evict(w, pages, pages.clone(), table, lens, 7, max_len=max_len, out=out, stream=stream)
+            torch.cuda.synchronize()
+            assert got is out and out[2].tolist() == want
+            made = attn.attn_cache_evict(w, pages, pages.clone(), table, lens, 7, max_len=max_len, stream=stream)
+            torch.cuda.synchronize()
+            assert made[2].tolist() == want
