@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) tree_plain_out_ker
 // places are looked up once for all of them; 16 to 64 lanes have a row.  Row blocks of one part are written where they are worked on.  34 MB of sums of one sequence of 65536 tokens: 8 us.
 template <typename T, int BR, int LANES>
 __global__ void __launch_bounds__(kThreads) tree_join_kernel(WinParams p, int many) {
-    constexpr int BC = BR >= 64 ? 64 : 32, kPer = 64 / LANES;
+    constexpr int BC = tree_tile(BR), kPer = 64 / LANES;
     const int turns = BR / many, lane = threadIdx.x & 63, in_row = threadIdx.x & (LANES - 1), idx = blockIdx.x / (p.kv_heads * turns);
     const int kvh = blockIdx.x / turns % p.kv_heads, row0 = blockIdx.x % turns * many;
     TreeItems<BR, BC> items;
@@ -163,6 +163,7 @@ hipError_t launch_tree_plain_fwd(bool is_bf16, bool fp8, long grid, const WinPar
     return fwd<float, float>(grid, p, stream);
 }
 hipError_t launch_tree_join(bool is_bf16, int rows, const WinParams& p, hipStream_t stream) {
+    if (!tree_rows_exist(is_bf16, rows)) return hipErrorInvalidValue;
     const int many = join_rows((int64_t)p.blocks * p.kv_heads, rows);
     auto with = [&](auto lanes) {
         constexpr int L = decltype(lanes)::value;

@@ -48,7 +48,7 @@ hipError_t launch(bool fp8, int rows, long grid, const WinParams& p, hipStream_t
 }  // namespace
 
 hipError_t launch_tree_fwd(bool fp8, int rows, long grid, const WinParams& p, hipStream_t stream) {
-    if (!p.table || !p.tree || (fp8 && p.d != 64 && p.d != 128 && p.d != 256)) return hipErrorInvalidValue;
+    if (!tree_rows_exist(true, rows) || !p.table || !p.tree || (fp8 && p.d != 64 && p.d != 128 && p.d != 256)) return hipErrorInvalidValue;
     return p.d <= 64 ? launch<64>(fp8, rows, grid, p, stream) : p.d <= 128 ? launch<128>(fp8, rows, grid, p, stream) : launch<256>(fp8, rows, grid, p, stream);
 }
 

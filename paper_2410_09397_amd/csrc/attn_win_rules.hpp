@@ -110,6 +110,9 @@ inline PagedSplits paged_splits(bool wide, int batch, int heads, int kv_heads, i
 // with 128 / 64 rows, h32 k8 d = 128, 64 drafted tokens: 16 sequences of 100 to 8192 tokens 84 / 144 (quantised), 74 / 119; one of 65536 102 / 124; one of 1000 (where
 // the chip is not full) 25.7 / 23.5; d = 256 h16 k4, 4 sequences 64 / 75.
 constexpr int kMostDrafted = 1024;  // drafted tokens of a sequence: their masks are 32 words
+// The kernels there are, and keys of their tiles.
+inline bool tree_rows_exist(bool bf16, int rows) { return rows == 32 || (bf16 && (rows == 16 || rows == 128)); }
+constexpr int tree_tile(int rows) { return rows == 128 ? 64 : 32; }
 inline int tree_rows(bool wide, int batch, int heads, int kv_heads, int total_q, int max_q) {
     const int64_t group = heads / kv_heads, rows = max_q * group;
     if (!wide || rows <= 64) return paged_rows(wide, batch, heads, kv_heads, total_q, max_q);
@@ -129,13 +132,13 @@ struct TreeShares {
     int64_t grid;
 };
 inline TreeShares tree_shares(bool wide, int batch, int heads, int kv_heads, int d, int total_q, int max_q, int max_len, int window, int sinks) {
-    const int64_t group = heads / kv_heads, rows = tree_rows(wide, batch, heads, kv_heads, total_q, max_q), tile = rows >= 64 ? 64 : 32;
+    const int64_t group = heads / kv_heads, rows = tree_rows(wide, batch, heads, kv_heads, total_q, max_q), tile = tree_tile((int)rows);
     TreeShares p = {(int)((max_q * group + rows - 1) / rows), 0, 0, 0x7fffffff, 0, 0};
     p.blocks = (int)std::min((int64_t)p.row_blocks * batch, total_q * group / rows + batch);
     p.grid = (int64_t)p.blocks * kv_heads;
     const int64_t chip = rows == 16 && d <= 128 ? 1024 : d > 128 ? 256 : 512, of_head = std::max<int64_t>(1, chip / kv_heads);
     // (the windows reach over window keys, the sinks and the drafted tokens have tiles of their own, and each kind may fill one more than its keys)
-    const int64_t keys = std::min<int64_t>(max_len, (int64_t)window + max_q) + sinks, tiles = keys / tile + 4, least = rows >= 64 ? kTreeLeast : kTreeLeastFew;
+    const int64_t keys = std::min<int64_t>(max_len, (int64_t)window + max_q) + sinks, tiles = keys / tile + 4, least = rows == 128 ? kTreeLeast : kTreeLeastFew;
     if (tiles < 2 * least || p.grid > 8 * chip || (int64_t)total_q * heads > kMostGroups) return p;
     p.places = (int)(p.blocks <= of_head ? of_head - p.blocks / 2 : kTreeRounds * of_head);
     if (rows == 128 && d <= 128 && p.blocks <= of_head && batch > 1 && batch <= 64) p.fold = (int)(256 / kv_heads);

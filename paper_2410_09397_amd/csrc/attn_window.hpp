@@ -204,10 +204,10 @@ struct WinKeys {
 hipError_t launch_win_plain_fwd(bool is_bf16, bool fp8, const WinParams& p, hipStream_t stream);
 // bf16; quantised pages: d in {64, 128, 256}; rows of a workgroup: 16, 32 (pages), 64, 128
 hipError_t launch_win_fwd(bool fp8, int rows, const WinParams& p, hipStream_t stream);
-hipError_t launch_tree_fwd(bool fp8, int rows, long grid, const WinParams& p, hipStream_t stream);  // the same for p.tree: 16, 32, 64, 128
+hipError_t launch_tree_fwd(bool fp8, int rows, long grid, const WinParams& p, hipStream_t stream);  // the same for p.tree: 16, 32, 128, and no others
 hipError_t launch_win_bwd(int rows, const WinParams& p, hipStream_t stream);                                // rows: 64, 128; forms delta itself
 hipError_t launch_tree_plain_fwd(bool is_bf16, bool fp8, long grid, const WinParams& p, hipStream_t stream);
-hipError_t launch_tree_join(bool is_bf16, int rows, const WinParams& p, hipStream_t stream);
+hipError_t launch_tree_join(bool is_bf16, int rows, const WinParams& p, hipStream_t stream);  // (fp32: 32)
 hipError_t launch_win_plain_bwd(const WinParams& p, hipStream_t stream);  // fp32
 hipError_t launch_win_join(bool is_bf16, const WinParams& p, hipStream_t stream);
 hipError_t launch_win_keys(bool is_bf16, int tile, const WinParams& p, hipStream_t stream);
