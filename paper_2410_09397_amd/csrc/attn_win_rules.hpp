@@ -147,6 +147,19 @@ inline TreeShares tree_shares(bool wide, int batch, int heads, int kv_heads, int
     return p;
 }
 
+// The folded order of the items of a key head (see find_folded): what the sequence `own`, with parts of `size` tiles, learns of the others, each counted once.
+struct TreeFold {
+    int all = 0, before = 0, first = 0;  // items of all sequences; in front of its own in the order of the sequences (that of the sums); and in that of the parts' sizes
+    constexpr void count(int own, int size, int other, int items, int tiles) {
+        all += items;
+        before += other < own ? items : 0;
+        first += tiles > size || (tiles == size && other < own) ? items : 0;
+    }
+    // which item workgroup idx has in the order of the sizes: the later half comes back from the last
+    static constexpr int place(int idx, int all, int fold) { return idx < fold ? idx : all - 1 - (idx - fold); }
+    constexpr bool has(int place, int items) const { return place >= first && place - first < items; }
+};
+
 // Rows of a workgroup of the joining launch, out of blocks of `rows`: 8, or as many as leave 2048 workgroups (each looks its sequence up first).  us of a call with
 // 512 / 1024 / 2048 / 4096 / any number of them: 64 sequences with 40 drafted tokens 129 / 130 / 121 / 119 / 139, 16 with 64 84 / 78 / 76 / 80 / 79.
 constexpr int64_t kJoinGroups = 2048;

@@ -270,22 +270,17 @@ struct TreeItems {
     __device__ __forceinline__ int find_folded(const WinParams& p, int idx, int lane, int& start, int& blocks, int& of_parts, int& within) const {
         const Sequence s = sequence(p, lane);
         const int of = parts(s.tiles), own = s.blocks * of, size = (s.tiles + of - 1) / of;
-        int before = 0, all = 0, first = 0;
-        for (int x = 0; x < p.batch; ++x) {
-            const int items = __builtin_amdgcn_readlane(own, x), tiles = __builtin_amdgcn_readlane(size, x);
-            all += items;
-            before += x < lane ? items : 0;
-            first += tiles > size || (tiles == size && x < lane) ? items : 0;
-        }
-        if (idx >= all || all > p.blocks + p.places + 1) return -1;  // (more items than the launch has: as in find_block)
-        if (idx >= p.fold) idx = all - 1 - (idx - p.fold);
-        const unsigned long who = __builtin_amdgcn_ballot_w64(idx >= first && idx - first < own);
+        TreeFold at;
+        for (int x = 0; x < p.batch; ++x) at.count(lane, size, x, __builtin_amdgcn_readlane(own, x), __builtin_amdgcn_readlane(size, x));
+        if (idx >= at.all || at.all > p.blocks + p.places + 1) return -1;  // (more items than the launch has: as in find_block)
+        idx = TreeFold::place(idx, at.all, p.fold);
+        const unsigned long who = __builtin_amdgcn_ballot_w64(at.has(idx, own));
         if (!who) return -1;
         const int b = __builtin_ctzl(who);
         blocks = __builtin_amdgcn_readlane(s.blocks, b);
         of_parts = __builtin_amdgcn_readlane(of, b);
-        start = __builtin_amdgcn_readlane(before, b);
-        within = idx - __builtin_amdgcn_readlane(first, b);
+        start = __builtin_amdgcn_readlane(at.before, b);
+        within = idx - __builtin_amdgcn_readlane(at.first, b);
         return b;
     }
     // row block idx of all sequences: its sequence (-1: there is none), that one's first item, row blocks and parts, and which of them it is
