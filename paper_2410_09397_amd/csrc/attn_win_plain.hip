@@ -9,24 +9,29 @@
 // (any layout of the rows will do) into accumulators of its own, which meet in LDS at the end: a short window is only a handful of tiles, and a tile
 // takes a wave 64 cycles for every 2 x 32 of its products.  What bounds them is the wait for those reads, not the products (four dependent trips to a tile: 49 to 63 % of the
 // wave cycles wait, the matrix pipe is 16 to 19 % busy; the kernels of attn_stream.hip, which stage whole rows in LDS, keep it 45 to 65 % busy).  us of a step, full causal
-// through those -> windowed through these, b2 h6: n777 d80 w128 81 -> 101 (two key heads) and 118 (six), w64 81 -> 81, n1500 d64 w128 159 -> 135,
-// n2048 d64 w128 278 -> 149; without a window b2 h16 n1000 d96 287 -> 840.
+// through those -> windowed through these, b2 h6: n777 d80 w128 81 -> 101 (two key heads) and 116 (six), w64 81 -> 82, n1500 d64 w128 159 -> 135,
+// n2048 d64 w128 278 -> 141; without a window b2 h16 n1000 d96 287 -> 827.
 #include "attn_win_plain.hpp"
 
 namespace attn {
 namespace {
 
-// How the masks of a tile's keys are written decides where the compiler works them out, and with that how long the wave waits between its products and its softmax.  us as they
-// stood in one function with those of trees (above the products, in 32 scalar registers) -> written as here:
-//   tensors                   sees(e) behind the products                                 train n777 d80 w128 104 -> 100, full n777 d80 235 -> 227, n1500 d128 w300 380 -> 365
-//   codes                     the same, up to 64 columns relative to the tile's first key   a token of 8 sequences d72 36.1 -> 30.6, d40 25.7 -> 25.1; 200 tokens of 2 sequences d72 47 -> 43
-//   fp32 pages, 65 to 128     kEarly: above the products, nothing of theirs before        200 tokens of 2 sequences d80 37.4 -> 35.0, d128 58 -> 45
-//   fp32 pages, to 64         kPlain: compared where they are used                        200 tokens of 2 sequences d64 27.7 -> 28.5 (sees(e) 32.5)
+// How the masks of a tile's 16 keys per lane are written decides where the compiler works them out and in which registers, and with that how long a wave waits between its products and
+// its softmax.  us where all of the kernel is one function with that of trees -> as written here (-> written in another of the three ways), b2 h6 k2 unless said otherwise:
+//   compared by a function, from the first key of the sequence; codes up to 64 columns from the first of the tile:
+//     tensors, 65 to 128      train n777 d80 w128 104.5 -> 100.5 (-> 102.5), n1500 d128 w100 246 -> 239 (-> 241), b2 h16 n1000 d96 869 -> 827 (-> 842)
+//     codes                   one token of 8 sequences d24 20.5 -> 20.5 (-> 23), d40 26.5 -> 25.7 (-> 29), d72 36 -> 31 (-> 32), d104 48 -> 37, d200 72 -> 72
+//     fp32 pages, 65 to 128   above the products, so that nothing of theirs is in front (kEarly): 200 tokens d80 40 -> 36 (-> 41), d128 59 -> 46 (-> 51)
+//   where they are used, from the first key of the sequence (kPlain):
+//     fp32 pages, up to 64    200 tokens d64 28.0 -> 28.8 (-> 31, 33), 1000 of 4000 220 -> 205 (-> 231, 242); tensors, up to 32: n777 d32 151 -> 151 (-> 153)
+//   where they are used, from the first key of the tile (kFromTile):
+//     tensors, 33 to 64       n1500 d64 w128 133 -> 134.5 (-> 139, 139), n777 d64 170 -> 173 (-> 171); tensors and fp32 pages from 129: n777 d192 w100 308 -> 302 (-> 305, 307)
 template <typename T, typename E, int DP, bool PAGED>
 __global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) win_plain_out_kernel(WinParams p, int row_blocks) {
     constexpr int MT = DP / 32;
-    constexpr bool kCodes = KeyTile<E, PAGED>::kCodes, kNear = kCodes && DP <= 64;
-    constexpr bool kEarly = PAGED && !kCodes && (DP == 96 || DP == 128), kPlain = PAGED && !kCodes && DP <= 64;
+    constexpr bool kCodes = KeyTile<E, PAGED>::kCodes;
+    constexpr bool kEarly = PAGED && !kCodes && (DP == 96 || DP == 128), kPlain = !kCodes && DP <= (PAGED ? 64 : 32);
+    constexpr bool kFromTile = !kCodes && (DP >= 192 || (DP == 64 && !PAGED));
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     int b, kvh, blk;
     if constexpr (PAGED) {
@@ -71,10 +76,11 @@ __global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) win_plain_out_kern
         for (int e = 0; e < 16; ++e) st[e] = 0.f;
         TileRow<E, DP> key;
         key.init(keys.K + keys.at, p.d, h);
+        const int from = j0 + 4 * h, hi_c = hi - from, lo_c = lo - from, sinks_c = p.sinks - from;  // (a lane's key of register e is from + 8 (e / 4) + e % 4)
         auto sees = [&](int e) {
-            if constexpr (kNear) {
-                const int from = j0 + 4 * h, c = 8 * (e >> 2) + (e & 3);
-                return c <= hi - from && (c >= lo - from || c < p.sinks - from);
+            if constexpr (kCodes && DP <= 64) {
+                const int c = 8 * (e >> 2) + (e & 3);
+                return c <= hi_c && (c >= lo_c || c < sinks_c);
             } else {
                 const int j = j0 + acc_row(e, h);
                 return j <= hi && (j >= lo || j < p.sinks);
@@ -93,6 +99,9 @@ __global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) win_plain_out_kern
             if constexpr (kPlain) {
                 const int j = j0 + acc_row(e, h);
                 st[e] = j <= hi && (j >= lo || j < p.sinks) ? st[e] * cs : -__builtin_inff();
+            } else if constexpr (kFromTile) {
+                const int c = 8 * (e >> 2) + (e & 3);
+                st[e] = c <= hi_c && (c >= lo_c || c < sinks_c) ? st[e] * cs : -__builtin_inff();
             } else {
                 if constexpr (!kEarly) seen[e] = sees(e);
                 st[e] = seen[e] ? st[e] * cs : -__builtin_inff();
