@@ -333,7 +333,8 @@ attn_status attn_paged_fwd(const attn_paged_desc *desc, const attn_cache *cache,
  * the last `window` tokens and the first `sinks` are read.  A query that sees nothing: O = 0, LSE = -inf.  max_q <= 1024.
  * attn_tree_mask takes batch, total_q, max_q and q_ptr as in attn_paged_desc and attn_cache; rows of no sequence, and rows from max_q on, are not written.
  * attn_tree_fwd is attn_paged_fwd with the mask in the place of the order of the new tokens: a mask whose row t has bits 0 .. t gives what that gives
- * (not the same bits: its key tiles differ).  Its workspace is attn_tree_workspace_bytes.
+ * (not the same bits: its key tiles differ).  Its workspace is attn_tree_workspace_bytes: sums in fp32 of every workgroup that there may be, 128 rows of d (16 or 32 with few
+ * rows), known from desc alone: 137 MB for 64 sequences with 64 drafted tokens, h32 k8 d = 128, 35 MB for one.  ATTN_BF16 rounds weights to bf16 as attn_paged_fwd does.
  */
 attn_status attn_tree_mask(int32_t batch, int32_t total_q, int32_t max_q, const int32_t *q_ptr, const int32_t *parents, uint32_t *mask,
                            int64_t mask_stride, void *stream);
@@ -352,7 +353,8 @@ attn_status attn_tree_commit(const attn_paged_desc *desc, const attn_cache *cach
 /*
  * Eviction from the paged cache by accumulated attention weight.  weight[b][h][j] is what the queries have paid to the token in slot j of key head h so far:
  *     out[b][h][j] = decay * in[b][h][j] + sum exp(scale <Q, K_j> - LSE)     over the new tokens that see j and the query heads of the group,
- * by attn_cache_weigh, with the visibility and the LSE of attn_paged_fwd (a query with LSE = -inf adds nothing).  New tokens start at zero: `in` is read
+ * by attn_cache_weigh, with the visibility and the LSE of attn_paged_fwd (a query with LSE = -inf adds nothing).  Behind a tree step its new tokens are the accepted ones: Q and LSE are
+ * the rows of those, which the caller brings together, with the lengths that attn_tree_commit left.  New tokens start at zero: `in` is read
  * for the tokens in front of them only, and may be NULL (zeros).  Slots below lens[b] are written, others not.  `out` may be `in` (with the same strides).
  * Every token of the cache is worked on, those of sequences without new tokens too: they keep decay times their weight.  Q and LSE (contiguous [total_q,
  * heads]) may be NULL if heads, total_q or max_q is 0; a call with batch, kv_heads or max_len 0 writes nothing.  batch * kv_heads * ceil(max_len / 32) < 2^24.
@@ -382,6 +384,9 @@ attn_status attn_cache_weigh(const attn_paged_desc *desc, const attn_cache *cach
  * without pos.  weight_out and pos_out (may be NULL without pos) get the values of the tokens that stay, in slots 0 .. new_lens[b] - 1; they may be weight
  * and pos themselves, with the same strides.  new_lens[b] = min(lens[b], budget), in memory of its own.  A token whose page, or the page that it moves to, is
  * outside the cache does not move.
+ * max_len - budget bounds how many tokens move, whatever the lengths are: up to 64 (a sequence that decodes, a page of tokens over its budget) a call is one launch without a workspace, beyond it
+ * is two, and beyond max_len = 4096 the first has larger workgroups.  So give a tight max_len where it is known: 64 sequences of 1040 tokens, budget 1024, 14 us with max_len 1040 or 1056, 23
+ * with 2048 or 4096, 30 with 8192 or more.
  * A page of a sequence that is cut down belongs to it alone: of a page that two tables name, or one table twice, copies are made first.
  * A call with batch, kv_heads or max_len 0 writes nothing.  first + recent <= budget, budget >= 1.  Of desc batch, kv_heads, d, max_len, the pages' fields, dtype and kind matter.
  */

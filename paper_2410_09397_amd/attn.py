@@ -785,7 +785,8 @@ def attn_cache_evict(weight, K_pages, V_pages, table, lens, budget, first=0, rec
                      V_exp=None, stream=None, out=None, workspace=None):
     """Every key head of a sequence of more than `budget` tokens keeps `budget` of them: those at positions below `first`, the `recent` latest, and those
     with the largest weights.  Kept tokens in slots from `budget` on move into the free ones below (so a
-    page of a sequence that is cut down belongs to it alone).  weight: float32 [batch, kv_heads, at least max_len];
+    page of a sequence that is cut down belongs to it alone).  max_len: a bound on the lengths (None: all of the table's pages); one at most 64
+    above the budget makes a call twice as fast, as few moves need one launch.  weight: float32 [batch, kv_heads, at least max_len];
     pos: the same in int32, positions of the tokens in slots below kept[b] (int32 [batch], the lengths of the last eviction); later slots hold the latest
     tokens of seen[b] (int32 [batch]; None: lens).  Returns weight, pos, the new lengths; out: where to put them (None: weight and pos
     themselves).  Without pos, slots are positions, as they are until the first eviction, and pos comes back as None unless `out` has one."""

@@ -186,6 +186,8 @@ __device__ __forceinline__ void evict_rows(const EvictParams& e, const EvictSequ
 // Free slots below n and tokens that stay above it are as many as one another; both are listed in ascending order, at places that come from a table of how many
 // each 64 slots have.  Keys are in LDS, 16 to a thread (longer sequences are gone through again for every step).  What bounds it at the size of a decoding step is how many
 // instructions are fetched for the first time: with the keys in registers, and every loop over them written out, 1040 tokens took 19 us.
+// Beyond 16384 tokens each of the five sweeps (three histograms, places, what stays) reads the weights from memory again, and one CU does it: one sequence of 65536 cut down to 8192, k8
+// d = 128, 122 us a call, of 131072 221 (what has to be read and written takes 12 and 14).
 // Few moves (e.here) are made by the same workgroup.  64 sequences of 1040 tokens, k8 d = 128, quantised, 16 leave: 13 us with the moves; 8 prompts of 500 to 16384 cut down to 2048: 25 us and 13 of
 // evict_move_kernel (3.9 TB/s).
 constexpr int kSelectItems = 16, kSelectPasses = 3, kSelectBins = 2048;

@@ -4,18 +4,23 @@
 // one pass answers all branches.  The context is read as for any new tokens, once for a block of rows (tokens times heads of a group).  Behind it
 // the drafted tokens are tiles of their own that start with the first of them: a tile of the context needs one comparison of positions for all of a
 // wave's rows, and in a tile of drafted tokens 32 bits of a row's mask are 32 keys, read where the tile is (a tree has one or two such tiles).
+//
+// As in attn_win_fwd.hip the weights are rounded to bf16 for the product with V, so that it runs on the bf16 matrix pipe straight from the accumulators of the first product; scores,
+// maxima, sums and O are 32 bits wide.  With the rounding of O itself that is 2.2e-3 to 2.4e-3 of the norm from 64 bits, of which O's own is 1.65e-3.
 #include "attn_win_fwd.hpp"
 
 namespace attn {
 namespace {
 
 // More than 64 rows (tree_rows says why 128 of them).  As without a tree the softmax and the waits of a tile bound it, not memory: 64 drafted tokens, h32 k8 d = 128, of one sequence of
-// 65536 84 us (3.2 TB/s, 820 TFLOP/s), of 16 of 100 to 8192, quantised, 63 us (512 workgroups, the longest 22 tiles and the mean 16).
+// 65536 85 us (3.2 TB/s, 810 TFLOP/s), of 16 of 100 to 8192, quantised, 64 us (512 workgroups, the longest 22 tiles and the mean 16; 72 us where the caches are cold).  A window of 1024
+// with 4 sinks leaves 11 of their 32 GFLOP: 49 us a call for 77.
 template <int D, int SRC, bool PAD>
 __global__ void __launch_bounds__(kThreads, D <= 128 ? 2 : 1) tree_out_kernel(WinParams p) {
     win_out<D, SRC, 1, PAD, true>(p, p.row_blocks);
 }
-// 17 to 64 rows.  The latency of a launch and of few tiles: 15 drafted tokens of 333, h16 k4 d = 64, 9 us.
+// 17 to 64 rows.  The latency of a launch and of few tiles: 15 drafted tokens of 333, h16 k4 d = 64, 9 us.  8 drafted tokens of 16 sequences of 100 to 8192, h32 k8 d = 128: a call
+// takes 34 us quantised (68 MB), 48 not (133 MB, 2.8 TB/s).
 template <int D, int SRC, bool PAD>
 __global__ void __launch_bounds__((64 * kFewWaves<D, SRC>), (D == 256 ? 1 : 2)) tree_few_kernel(WinParams p) {
     win_few<D, SRC, PAD, true>(p);

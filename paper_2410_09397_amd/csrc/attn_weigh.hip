@@ -248,7 +248,7 @@ __device__ __forceinline__ void weigh_rows(const WinParams& p, const WeighStage<
     }
 }
 
-// A whole stage of rows that all see all of 64 keys: the products of 32 rows and 32 keys are issued between the exponentials of the 32 keys before (the vector arithmetic takes
+// A whole stage of rows (128 / group has no remainder, d up to 128) that all see all of 64 keys: the products of 32 rows and 32 keys are issued between the exponentials of the 32 keys before (the vector arithmetic takes
 // longer than the matrix pipe: an exponential is four instructions' time).
 template <int D, int SRC, bool PAD>
 __device__ __forceinline__ void weigh_stage(const WeighStage<D>& stage, const bf16x8 (&kf)[2][D / 16], float cs, int lane, float (&sum)[2]) {

@@ -105,6 +105,9 @@ inline PagedSplits paged_splits(bool wide, int batch, int heads, int kv_heads, i
     return p;
 }
 
+// (The times below, of trees, weights and eviction, compare two or more forms of the code as it stood when a line was drawn.  Later steps have made the calls shorter, and the same call
+// stands with different times in different comments: what counts is the ratio within a comment.)
+//
 // Trees of drafted tokens: rows of a workgroup.  Unlike the new tokens of a batch in their order, whose blocks are as many as their tokens make them, a tree has one or two
 // blocks, and what fills the chip are the parts of the context: more than 64 rows always take blocks of 128, which convert and read a tile half as often.  us of a call
 // with 128 / 64 rows, h32 k8 d = 128, 64 drafted tokens: 16 sequences of 100 to 8192 tokens 84 / 144 (quantised), 74 / 119; one of 65536 102 / 124; one of 1000 (where
@@ -173,6 +176,8 @@ inline int join_rows(int64_t blocks, int rows) {
 // kernel of 32-bit arithmetic).  us of a call: one kernel for all, 16 rows at a time -> these, h32 k8 d = 128: newest token of 64 sequences (quantised) 72 -> 31, last 32
 // tokens of 8 prompts 52 -> 18, a prompt of 4096 tokens 1101 -> 101.
 // One tile or less: keys of a workgroup, as many as leave 2048 workgroups (512 / 1024 / 4096: last 32 tokens of 8 prompts 24.9 / 19.9 / 21.1 for 18.1).
+// Groups of heads that do not divide 128 leave rows of a tile empty, and those tiles, like all of d = 256, take the rows 32 at a time, without the products between the exponentials: a prompt of
+// 4096 tokens, d = 128, h32 k8 99 us (690 TFLOP/s), h24 k8 93 (560), h28 k4 120 (500); d = 256 h16 k4 149 (460).
 // Many rows: the keys of a workgroup are 256, and the tiles of rows are shared out until there are some 768 workgroups, a round and a half, with two tiles each at least.  us of
 // 512 / 768 / 1024 workgroups: a prompt of 4096 tokens 114 / 101 / 105, 4 prompts of 500 to 2000 107 / 93 / 91, the last 512 of 16384 tokens 90 / 90 / 98; one / two / four tiles:
 // a prompt of 300 tokens 16 / 21 / 32, d = 256, 64 of 4000 tokens 47 / 39 / 39.
